@@ -1,0 +1,632 @@
+"""Performance cases of the 8-bit paged cache and the operators around it.
+
+    listed()             the named cases
+    draw(rng)            one more case of the same ranges
+    prepare(case, seed)  what a serving program holds before the call
+    run(state)           one call and its outputs: plain torch, or with `own` the library's entry points
+    work(case)           bytes and operations no implementation of the call can do without
+    exact(case, seed)    the same outputs in float64
+
+A case names its operator in "op":
+    rotary      ee_rotary on the query and key rows of a call (direction "inverse": the gradient's)
+    append      ee_kv_quant_append of one position per sequence, or of chunks, and ee_kv_quant_read of every position
+                of the blocks it touched (tokens that were there change when a block's scale grows)
+    attention   ee_paged_attention_quant on one position per sequence, or on chunks of prompts
+    evict       ee_kv_quant_evict into other blocks, and ee_kv_quant_read of what it kept
+
+The cache: k bytes [num_blocks][kv heads][16][head_dim], v bytes [num_blocks][kv heads][head_dim][16], scales
+[num_blocks][kv heads][2] (k, v).  A byte stands for its own value (a signed integer, or an e4m3 number) times the scale,
+as a float32: where a block's scale changes, that float32 is what is rounded anew.
+Sizes are a case's own: lengths run evenly from ctx_min to ctx_max over the sequences, in an order the seed decides.
+"""
+import math
+
+import torch
+
+own = False
+DEVICE = "cuda"
+BLOCK = 16
+FLOOR = 2.0 ** -126   # the smallest scale
+
+
+# ----------------------------------------------------------------------------------------------------------------
+# the cases
+# ----------------------------------------------------------------------------------------------------------------
+def listed():
+    return [
+        # One token of one conversation on the 7B shape: nothing but latency.
+        dict(name="rotary_7b_b1", op="rotary", rows=1, heads=32, kv_heads=32, head_dim=128, rotary_dim=128, dtype="bf16",
+             layout="half", scaling="plain", factor=1.0, max_position=4096, direction="forward"),
+        # A long prompt pass with grouped K/V heads, frequencies stretched for a context beyond the trained one.
+        dict(name="rotary_prompt_4096", op="rotary", rows=4096, heads=32, kv_heads=8, head_dim=128, rotary_dim=128,
+             dtype="bf16", layout="half", scaling="turns", factor=8.0, max_position=131072, direction="forward"),
+        # The gradient's direction in float, interleaved pairs in a part of an odd head.
+        dict(name="rotary_gradient_partial", op="rotary", rows=1001, heads=20, kv_heads=5, head_dim=80, rotary_dim=48,
+             dtype="fp32", layout="interleaved", scaling="linear", factor=4.0, max_position=16000, direction="inverse"),
+        # A decode step of a large ragged batch writes one token per sequence.
+        dict(name="append_decode_b256", op="append", batch=256, rows=1, ctx_min=100, ctx_max=2000, kv_heads=8, head_dim=128,
+             dtype="bf16", format="int8"),
+        # Three prompts' chunks on the 7B shape, starting inside blocks.
+        dict(name="append_chunk_7b", op="append", batch=3, rows=701, ctx_min=5, ctx_max=1500, kv_heads=32, head_dim=128,
+             dtype="bf16", format="e4m3"),
+        # The first tokens of one conversation: the smallest attention.
+        dict(name="attention_b1_short", op="attention", batch=1, rows=1, ctx_min=100, ctx_max=100, heads=32, kv_heads=8,
+             head_dim=128, format="int8", weights=True),
+        # The headline decode batch of the 7B shape, every head with K/V of its own.
+        dict(name="attention_7b_b32", op="attention", batch=32, rows=1, ctx_min=512, ctx_max=640, heads=32, kv_heads=32,
+             head_dim=128, format="e4m3", weights=False),
+        # A large batch of long contexts over grouped heads that also sums its weights for a later eviction.
+        dict(name="attention_gqa_b64_ctx4k", op="attention", batch=64, rows=1, ctx_min=2000, ctx_max=6000, heads=32,
+             kv_heads=8, head_dim=128, format="int8", weights=True),
+        # One very long conversation.
+        dict(name="attention_b1_ctx128k", op="attention", batch=1, rows=1, ctx_min=131000, ctx_max=131000, heads=32, kv_heads=8,
+             head_dim=128, format="e4m3", weights=False),
+        # A prompt chunk as the scheduler cuts it: 512 rows of four prompts that are at different places.
+        dict(name="attention_prompt_512_rows", op="attention", batch=4, rows=128, ctx_min=0, ctx_max=3000, heads=32, kv_heads=8,
+             head_dim=128, format="int8", weights=False),
+        # A conversation that has just outgrown its budget.
+        dict(name="evict_b1", op="evict", batch=1, ctx_min=300, ctx_max=300, keep=256, recent=32, kv_heads=8, head_dim=128,
+             format="int8"),
+        # A batch cut down to a quarter, some of its sequences short of the budget.
+        dict(name="evict_b16_ctx4k", op="evict", batch=16, ctx_min=700, ctx_max=6000, keep=1000, recent=130, kv_heads=8,
+             head_dim=128, format="e4m3"),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi + 0.49)))))))
+
+
+def draw(rng):
+    op = rng.choice(["rotary", "append", "attention", "attention", "evict"])
+    kv, dh = rng.choice([1, 2, 4, 5, 8, 8, 16, 32]), rng.choice([64, 64, 80, 96, 128, 128, 128, 192, 256])
+    fmt = rng.choice(["int8", "e4m3"])
+    if op == "rotary":
+        heads = kv * rng.choice([1, 1, 2, 4]) if kv <= 16 else kv
+        part = 2 * rng.randint(1, dh // 2) if rng.random() < 0.4 else dh
+        return dict(op=op, rows=_log_int(rng, 1, 4096), heads=heads, kv_heads=kv, head_dim=dh, rotary_dim=part,
+                    dtype=rng.choice(["bf16", "fp32"]), layout=rng.choice(["half", "interleaved"]),
+                    scaling=rng.choice(["plain", "linear", "turns"]), factor=round(rng.uniform(1.5, 16.0), 2),
+                    max_position=_log_int(rng, 100, 131072), direction=rng.choice(["forward", "forward", "inverse"]))
+    if op == "append":
+        batch = _log_int(rng, 1, 256)
+        rows = 1 if rng.random() < 0.5 else _log_int(rng, 1, max(1, 2048 // batch))
+        return dict(op=op, batch=batch, rows=rows, ctx_min=rng.randint(0, 100), ctx_max=_log_int(rng, 100, 2000), kv_heads=kv,
+                    head_dim=dh, dtype=rng.choice(["bf16", "fp32"]), format=fmt)
+    token = 2 * kv * dh
+    if op == "attention":
+        batch = _log_int(rng, 1, 64)
+        rows = 1 if rng.random() < 0.7 else _log_int(rng, 2, max(2, 512 // batch))
+        group = rng.choice([1, 2, 3, 4, 7, 8]) if kv <= 8 else 1
+        # up to half of what the largest listed case reads, and no more products than its listed chunk has
+        room = min(2.6e8 / (token * batch), 2.5e9 / (batch * rows * kv * group * dh))
+        ctx_max = _log_int(rng, 16, max(16, int(min(130000 if rows == 1 else 3000, room))))
+        return dict(op=op, batch=batch, rows=rows, ctx_min=rng.choice([0, ctx_max // 4, ctx_max]), ctx_max=ctx_max,
+                    heads=kv * group, kv_heads=kv, head_dim=dh, format=fmt, weights=rows == 1 and rng.random() < 0.4)
+    batch = _log_int(rng, 1, 32)
+    ctx_max = _log_int(rng, 40, max(40, min(16000, int(6e7 / (token * batch)))))
+    keep = rng.randint(17, ctx_max)
+    return dict(op=op, batch=batch, ctx_min=ctx_max // rng.choice([1, 2, 8]), ctx_max=ctx_max, keep=keep,
+                recent=rng.randint(0, keep), kv_heads=kv, head_dim=dh, format=fmt)
+
+
+# ----------------------------------------------------------------------------------------------------------------
+# what a case says about sizes (the same for every seed)
+# ----------------------------------------------------------------------------------------------------------------
+def _lens(case):
+    """Positions cached before the call, per sequence."""
+    n, lo, hi = case["batch"], case["ctx_min"], max(case["ctx_min"], case["ctx_max"])
+    return [lo + (i * (hi - lo)) // max(1, n - 1) for i in range(n)]
+
+
+def _blocks(n):
+    return (n + BLOCK - 1) // BLOCK
+
+
+def work(case):
+    if case["op"] == "rotary":
+        size = 2 if case["dtype"] == "bf16" else 4
+        elems = case["rows"] * (case["heads"] + case["kv_heads"]) * case["head_dim"]
+        return {"bytes": 2 * elems * size + 4 * case["rows"] + 4 * case["rotary_dim"], "flops": 3 * elems * case["rotary_dim"] / case["head_dim"]}
+    kv, dh, lens = case["kv_heads"], case["head_dim"], _lens(case)
+    if case["op"] == "append":
+        size, rows = (2 if case["dtype"] == "bf16" else 4), case["rows"]
+        new = case["batch"] * rows
+        touched = sum(n + rows - n // BLOCK * BLOCK for n in lens)
+        blocks = sum(_blocks(n + rows) - n // BLOCK for n in lens)
+        return {"bytes": new * kv * 2 * dh * (size + 1) + blocks * kv * 8 * 3 + touched * kv * 2 * dh * 5, "flops": 2 * new * kv * 2 * dh}
+    if case["op"] == "attention":
+        h, rows = case["heads"], case["rows"]
+        seen = [n + rows for n in lens]
+        attended = sum(rows * n + rows * (rows + 1) // 2 for n in lens)
+        b = sum(seen) * kv * 2 * dh + sum(map(_blocks, seen)) * (kv * 8 + 4) + 2 * case["batch"] * rows * h * dh * 4
+        return {"bytes": b + (8 * kv * sum(seen) if case["weights"] else 0), "flops": 4 * h * dh * attended}
+    kept = sum(min(n, case["keep"]) for n in lens)
+    b = sum(lens) * kv * 4 + kept * kv * (4 * dh + 8) + 2 * _blocks(kept) * kv * 8 + kept * kv * 2 * dh * 5
+    return {"bytes": b, "flops": 4 * kept * kv * dh}
+
+
+# ----------------------------------------------------------------------------------------------------------------
+# inputs
+# ----------------------------------------------------------------------------------------------------------------
+def _generators(seed):
+    host, dev = torch.Generator(), torch.Generator(device=DEVICE)
+    host.manual_seed(int(seed))
+    dev.manual_seed(int(seed))
+    return host, dev
+
+
+def _int32(values):
+    return torch.tensor(values, dtype=torch.int32).to(DEVICE)
+
+
+def _cache(case, num_blocks, dev):
+    """Bytes whose values times their block's scale are about N(0, 1)."""
+    shape = (num_blocks, case["kv_heads"], BLOCK, case["head_dim"])
+    std = 40.0 if case["format"] == "int8" else 100.0
+
+    def filled(*dims):
+        x = torch.randn(dims, generator=dev, device=DEVICE, dtype=torch.float16 if case["format"] == "int8" else torch.float32).mul_(std)
+        return x.round_().clamp_(-127, 127).to(torch.int8) if case["format"] == "int8" else x.clamp_(-448, 448).to(torch.float8_e4m3fn)
+
+    k = filled(*shape)
+    v = filled(shape[0], shape[1], shape[3], shape[2])
+    s = torch.randn((num_blocks, case["kv_heads"], 2), generator=dev, device=DEVICE).mul_(0.3)
+    s = torch.exp(s) / std if case["format"] == "int8" else torch.exp2(torch.round(s) - 7)
+    return k, v, s
+
+
+def _tables(need, pool, host):
+    """Every sequence's blocks from a shuffled pool, -1 where the table goes on."""
+    order = torch.randperm(pool, generator=host, dtype=torch.int64).to(torch.int32)
+    wide = max(1, max(need))
+    table, used = torch.full((len(need), wide), -1, dtype=torch.int32), 0
+    for i, n in enumerate(need):
+        table[i, :n] = order[used:used + n]
+        used += n
+    return table.to(DEVICE), order[used:]
+
+
+def prepare(case, seed):
+    host, dev = _generators(seed)
+    s = dict(case=case)
+    if case["op"] == "rotary":
+        t = torch.bfloat16 if case["dtype"] == "bf16" else torch.float32
+        rows, dh = case["rows"], case["head_dim"]
+        s["q"] = torch.randn((rows, case["heads"], dh), generator=dev, device=DEVICE).to(t)
+        s["k"] = torch.randn((rows, case["kv_heads"], dh), generator=dev, device=DEVICE).to(t)
+        start = int(torch.randint(0, max(1, case["max_position"] - rows), (1,), generator=host))
+        s["positions"] = torch.arange(start, start + rows, dtype=torch.int32).to(DEVICE)
+        s["q_out"], s["k_out"] = torch.empty_like(s["q"]), torch.empty_like(s["k"])
+        s["theta"], s["original"], s["turns"], s["amplitude"] = 10000.0, 8192, (1.0, 4.0), 1.25
+        if own:
+            s["handle"] = _rotary_handle(s)
+        return s
+    lens = _lens(case)
+    lens = [lens[i] for i in torch.randperm(len(lens), generator=host).tolist()]
+    rows = case.get("rows", 0)
+    need = [_blocks(n + rows) for n in lens]
+    if case["op"] == "evict":
+        dst = [_blocks(min(n, case["keep"])) for n in lens]
+        pool = sum(need) + sum(dst) + 3
+        s["tables"], rest = _tables(need, pool, host)
+        wide = _blocks(case["keep"])
+        s["dst_tables"], used = torch.full((len(lens), wide), -1, dtype=torch.int32), 0
+        for i, n in enumerate(dst):
+            s["dst_tables"][i, :n] = rest[used:used + n]
+            used += n
+        s["dst_tables"] = s["dst_tables"].to(DEVICE)
+        s["max_context"] = max(lens)
+        s["lens"] = _int32(lens)
+        s["weights"] = torch.rand((len(lens), case["kv_heads"], max(lens)), generator=dev, device=DEVICE).pow_(4).mul_(8)
+        s["weights_out"] = torch.zeros((len(lens), case["kv_heads"], case["keep"]), device=DEVICE)
+        s["kept"] = torch.full((len(lens), case["kv_heads"], case["keep"]), -1, dtype=torch.int32, device=DEVICE)
+        s["out_lens"] = torch.zeros(len(lens), dtype=torch.int32, device=DEVICE)
+        # every position that is left, to read back
+        s["read_seq"] = _int32([i for i, n in enumerate(lens) for _ in range(min(n, case["keep"]))])
+        s["read_pos"] = _int32([p for n in lens for p in range(min(n, case["keep"]))])
+    else:
+        pool = sum(need) + 3
+        s["tables"], _ = _tables(need, pool, host)
+        s["max_context"] = max(lens) + rows
+        s["row_seq"] = _int32([i for i in range(len(lens)) for _ in range(rows)])
+        s["row_pos"] = _int32([n + r for n in lens for r in range(rows)])
+        total = len(lens) * rows
+        if case["op"] == "append":
+            t = torch.bfloat16 if case["dtype"] == "bf16" else torch.float32
+            for name in ("k_new", "v_new"):
+                s[name] = torch.randn((total, case["kv_heads"], case["head_dim"]), generator=dev, device=DEVICE).mul_(1.2).to(t)
+            touched = [(i, p) for i, n in enumerate(lens) for p in range(n // BLOCK * BLOCK, n + rows)]
+            s["read_seq"], s["read_pos"] = _int32([i for i, _ in touched]), _int32([p for _, p in touched])
+        else:
+            h, dh = case["heads"], case["head_dim"]
+            s["q"] = torch.randn((total, h, dh), generator=dev, device=DEVICE).mul_(1.5)
+            s["out"] = torch.empty_like(s["q"])
+            if case["weights"]:
+                s["weights"] = torch.rand((len(lens), case["kv_heads"], s["max_context"]), generator=dev, device=DEVICE)
+                s["weights_out"] = torch.zeros_like(s["weights"])
+    s["pool"] = pool
+    s["cache_k"], s["cache_v"], s["scales"] = _cache(case, pool, dev)
+    if "read_seq" in s:
+        shape = (len(s["read_seq"]), case["kv_heads"], case["head_dim"])
+        s["k_read"], s["v_read"] = torch.empty(shape, device=DEVICE), torch.empty(shape, device=DEVICE)
+    if own:
+        s["handle"] = _cache_handle(s)
+    return s
+
+
+# ----------------------------------------------------------------------------------------------------------------
+# the library's calls
+# ----------------------------------------------------------------------------------------------------------------
+def _rotary_handle(s):
+    """The plan a program makes once: the frequencies of its pairs."""
+    from paper_2407_20272_amd import binding as B
+    c = s["case"]
+    desc = B.make_rotary_desc(c["head_dim"], c["rotary_dim"], layout=c["layout"], theta=s["theta"], scaling=c["scaling"],
+                              factor=c["factor"], original_context=s["original"], turns=s["turns"], amplitude=s["amplitude"])
+    return dict(B=B, desc=desc, freqs=B.ee_rotary_frequencies(desc))
+
+
+def _cache_handle(s):
+    """The records a program keeps beside its cache, and the workspace of its largest call."""
+    from paper_2407_20272_amd import binding as B
+    c = s["case"]
+    h = dict(B=B, cache=B.QuantKV.of(s["cache_k"][None], s["cache_v"][None], s["scales"][None]))
+    if c["op"] == "evict":
+        h["batch"] = B.make_batch(None, s["lens"], s["tables"], s["max_context"])
+        h["ws"] = None
+    else:
+        h["batch"] = B.make_batch(None, s["row_pos"], s["tables"], s["max_context"], s["row_seq"] if c["rows"] > 1 else None)
+    if "read_seq" in s:
+        tables, most = (s["dst_tables"], c["keep"]) if c["op"] == "evict" else (s["tables"], s["max_context"])
+        h["read"] = B.make_batch(None, s["read_pos"], tables, most, s["read_seq"])
+    if c["op"] == "attention":
+        h["ws"] = B.QuantWorkspace(h["cache"], c["heads"], c["batch"] * c["rows"], s["max_context"], c["weights"])
+    return h
+
+
+def _run_own(s):
+    c, h = s["case"], s["handle"]
+    B = h["B"]
+    if c["op"] == "rotary":
+        B.ee_rotary(h["desc"], h["freqs"], s["positions"], s["q"], s["q_out"], s["k"], s["k_out"], transpose=c["direction"] == "inverse")
+        return {"q": s["q_out"], "k": s["k_out"]}
+    if c["op"] == "append":
+        B.ee_kv_quant_append(h["cache"], 1, s["k_new"], s["v_new"], h["batch"])
+        B.ee_kv_quant_read(h["cache"], 1, h["read"], s["k_read"], s["v_read"])
+        return {"k": s["k_read"], "v": s["v_read"], "scales": s["scales"]}
+    if c["op"] == "attention":
+        if not c["weights"]:
+            B.ee_paged_attention_quant(h["cache"], 1, s["q"], h["batch"], s["out"], h["ws"])
+            return {"out": s["out"]}
+        B.ee_paged_attention_quant(h["cache"], 1, s["q"], h["batch"], s["out"], h["ws"], s["weights"], s["weights_out"])
+        return {"out": s["out"], "weights": s["weights_out"]}
+    B.ee_kv_quant_evict(h["cache"], 1, h["batch"], s["weights"], s["weights_out"], c["keep"], c["recent"], s["kept"], s["out_lens"],
+                        h["ws"], dst_tables=s["dst_tables"])
+    B.ee_kv_quant_read(h["cache"], 1, h["read"], s["k_read"], s["v_read"])
+    return {"k": s["k_read"], "v": s["v_read"], "weights": s["weights_out"], "kept": s["kept"], "lens": s["out_lens"]}
+
+
+# ----------------------------------------------------------------------------------------------------------------
+# the plain form
+# ----------------------------------------------------------------------------------------------------------------
+def _frequencies(s):
+    c = s["case"]
+    r = c["rotary_dim"]
+    f = torch.pow(torch.tensor(s["theta"], dtype=torch.float64, device=DEVICE), -torch.arange(0, r, 2, device=DEVICE, dtype=torch.float64) / r)
+    if c["scaling"] == "linear":
+        f = f / c["factor"]
+    if c["scaling"] == "turns":
+        low, high = s["turns"]
+        keep = ((s["original"] * f / (2 * math.pi) - low) / (high - low)).clamp(0, 1)
+        f = f * (keep + (1 - keep) / c["factor"])
+    return f
+
+
+def _rotated(x, cos, sin, c):
+    r = c["rotary_dim"]
+    y = x.to(cos.dtype)
+    if c["layout"] == "half":
+        a, b = y[..., :r // 2], y[..., r // 2:r]
+        turned = torch.cat([a * cos - b * sin, b * cos + a * sin], -1)
+    else:
+        a, b = y[..., 0:r:2], y[..., 1:r:2]
+        turned = torch.stack([a * cos - b * sin, b * cos + a * sin], -1).flatten(-2)
+    return torch.cat([turned, y[..., r:]], -1)
+
+
+def _rotary(s):
+    c = s["case"]
+    angle = s["positions"].double()[:, None] * _frequencies(s)[None, :]
+    cos, sin = (s["amplitude"] * torch.cos(angle)).float()[:, None], (s["amplitude"] * torch.sin(angle)).float()[:, None]
+    sin = -sin if c["direction"] == "inverse" else sin
+    return {"q": _rotated(s["q"], cos, sin, c).to(s["q"].dtype), "k": _rotated(s["k"], cos, sin, c).to(s["k"].dtype)}
+
+
+def _scale_for(largest, fmt):
+    """The scale a block whose largest magnitude is `largest` takes."""
+    if fmt == "int8":
+        return (largest.double() / 127).float().clamp(min=FLOOR)
+    m, e = torch.frexp(largest)   # 448 = 0.875 * 2^9
+    return torch.exp2((e - 9 + (m > 0.875).int()).double().clamp(min=-126)).float()
+
+
+def _quantised(x, scale, fmt):
+    y = x.double() / scale.double()
+    return torch.round(y).clamp(-127, 127).to(torch.int8) if fmt == "int8" else y.float().to(torch.float8_e4m3fn)
+
+
+def _read(s, table):
+    """The values of the positions (read_seq, read_pos): float [rows][kv heads][head_dim], k and v."""
+    pos = s["read_pos"].long()
+    blk, off = table[s["read_seq"].long(), pos // BLOCK].long(), pos % BLOCK
+    k = s["cache_k"].view(torch.int8)[blk, :, off].view(s["cache_k"].dtype).float()
+    v = s["cache_v"].view(torch.int8)[blk, :, :, off].view(s["cache_v"].dtype).float()
+    return k * s["scales"][blk, :, 0, None], v * s["scales"][blk, :, 1, None]
+
+
+def _append(s):
+    c, fmt = s["case"], s["case"]["format"]
+    seq, pos = s["row_seq"].long(), s["row_pos"].long()
+    wide = s["tables"].shape[1]
+    # the blocks this call writes, and each row's place among them
+    logical, at = torch.unique(seq * wide + pos // BLOCK, return_inverse=True)
+    blk, off, n = s["tables"].flatten()[logical].long(), pos % BLOCK, len(logical)
+    first = torch.full((n,), BLOCK, device=DEVICE).scatter_reduce(0, at, off, "amin")
+    older = (torch.arange(BLOCK, device=DEVICE)[None, :] < first[:, None])          # [n][16]
+    for new, pool, which in ((s["k_new"], s["cache_k"], 0), (s["v_new"], s["cache_v"], 1)):
+        largest = torch.zeros((n, c["kv_heads"]), device=DEVICE)
+        largest = largest.scatter_reduce(0, at[:, None].expand(-1, c["kv_heads"]), new.float().abs().amax(-1), "amax")
+        was = s["scales"][blk, :, which]
+        scale = _scale_for(largest, fmt)
+        scale = torch.where((first > 0)[:, None], torch.maximum(scale, was), scale)
+        old = pool.view(torch.int8)[blk].view(pool.dtype)
+        keep = older[:, None, :, None] if which == 0 else older[:, None, None, :]
+        value = torch.where(keep, old.float() * was[:, :, None, None], 0.0)
+        pool.view(torch.int8)[blk] = torch.where(keep, _quantised(value, scale[:, :, None, None], fmt).view(torch.int8), old.view(torch.int8))
+        rows = _quantised(new.float(), scale[at][:, :, None], fmt).view(torch.int8)
+        if which == 0:
+            pool.view(torch.int8)[blk[at], :, off] = rows
+        else:
+            pool.view(torch.int8)[blk[at], :, :, off] = rows
+        s["scales"][blk, :, which] = scale
+    k, v = _read(s, s["tables"])
+    return {"k": k, "v": v, "scales": s["scales"]}
+
+
+def _attention(s):
+    c = s["case"]
+    n, rows, h, kv, dh = c["batch"], c["rows"], c["heads"], c["kv_heads"], c["head_dim"]
+    blk = s["tables"].clamp(min=0).long()
+    scale = s["scales"][blk]                                                              # [n][blocks][kv][2]
+    ctx = blk.shape[1] * BLOCK
+    pos = s["row_pos"].view(n, rows)
+    here = torch.arange(ctx, device=DEVICE)
+    live = (here[None, :] <= pos[:, -1:])[:, None, :, None]                               # what holds a position of the sequence
+    k = s["cache_k"].view(torch.int8)[blk].view(s["cache_k"].dtype).float() * scale[..., 0, None, None]
+    k = torch.where(live, k.transpose(1, 2).reshape(n, kv, ctx, dh), 0.0)
+    q = s["q"].view(n, rows, kv, h // kv, dh).permute(0, 2, 1, 3, 4).reshape(n, kv, -1, dh)
+    z = torch.matmul(q, k.transpose(-1, -2).contiguous()).div_(math.sqrt(dh)).view(n, kv, rows, h // kv, ctx)
+    del k
+    z = torch.where((here <= pos[:, :, None])[:, None, :, None, :], z, -math.inf)
+    e = torch.exp_(z - z.amax(-1, keepdim=True))
+    e = e / e.sum(-1, keepdim=True)
+    v = s["cache_v"].view(torch.int8)[blk].view(s["cache_v"].dtype).float() * scale[..., 1, None, None]
+    v = torch.where(live, v.permute(0, 2, 1, 4, 3).reshape(n, kv, ctx, dh), 0.0)
+    out = torch.matmul(e.view(n, kv, -1, ctx), v).view(n, kv, rows, h // kv, dh).permute(0, 2, 1, 3, 4).reshape(n * rows, h, dh)
+    if not c["weights"]:
+        return {"out": out}
+    wide = s["weights"].shape[2]
+    w = e[:, :, 0].sum(2)[..., :wide]
+    here = here[None, None, :wide]
+    at = pos[:, :1, None]
+    new = torch.where(here < at, s["weights"] + w, torch.where(here == at, w, s["weights_out"]))
+    return {"out": out, "weights": new}
+
+
+def _evict(s):
+    c, fmt = s["case"], s["case"]["format"]
+    n, kv, keep, recent = c["batch"], c["kv_heads"], c["keep"], c["recent"]
+    wide = s["weights"].shape[2]
+    lens = s["lens"].long()[:, None, None]
+    here = torch.arange(wide, device=DEVICE)[None, None, :]
+    # the newest first, then by weight (the sort is stable: of equal weights the lowest index), what holds no position last
+    rank = torch.where(here >= lens - recent, math.inf, s["weights"])
+    rank = torch.where(here >= lens, -math.inf, rank)
+    order = torch.sort(rank, dim=-1, descending=True, stable=True).indices[..., :keep]
+    order = torch.where(torch.arange(order.shape[-1], device=DEVICE) < lens, order, wide)
+    kept = torch.sort(order, -1).values
+    kept = torch.cat([kept, kept.new_full((n, kv, keep - kept.shape[-1]), wide)], -1)
+    there = kept < wide
+    at = torch.where(there, kept, 0)
+    blk = torch.gather(s["tables"].long()[:, None, :].expand(-1, kv, -1), 2, at // BLOCK).clamp(min=0)
+    head = torch.arange(kv, device=DEVICE)[None, :, None].expand_as(blk)
+    slots = (keep + BLOCK - 1) // BLOCK
+    dst = s["dst_tables"][:, :slots].long()
+    full = slots * BLOCK
+    used = torch.nn.functional.pad(there, (0, full - keep)).view(n, kv, slots, BLOCK)
+    for pool, which in ((s["cache_k"], 0), (s["cache_v"], 1)):
+        raw = pool.view(torch.int8)
+        q = (raw[blk, head, at % BLOCK] if which == 0 else raw[blk, head, :, at % BLOCK]).view(pool.dtype).float()   # [n][kv][keep][dh]
+        was = s["scales"][blk, head, which]
+        value = torch.where(there[..., None], q * was[..., None], 0.0)
+        most = q.abs().amax(-1)
+        # a token that fills its block's range stands for the block's scale as it is
+        need = _scale_for(most * was, fmt)
+        need = torch.where(most >= 127, was, need) if fmt == "int8" else need
+        need = torch.where(there, need, FLOOR)
+        need = torch.nn.functional.pad(need, (0, full - keep), value=FLOOR).view(n, kv, slots, BLOCK).amax(-1)
+        value = torch.nn.functional.pad(value, (0, 0, 0, full - keep)).view(n, kv, slots, BLOCK, -1)
+        image = _quantised(value, need[..., None, None], fmt).view(torch.int8)
+        owned = (dst >= 0) & used.any(-1).any(1)
+        image = image.permute(0, 2, 1, 3, 4)[owned]                    # [blocks][kv][16][dh]
+        raw[dst[owned]] = image if which == 0 else image.transpose(-1, -2).contiguous()
+        s["scales"][dst[owned], :, which] = need.transpose(1, 2)[owned]
+    k, v = _read(s, s["dst_tables"])
+    weights = torch.where(there, torch.gather(s["weights"], 2, at), s["weights_out"])
+    return {"k": k, "v": v, "weights": weights, "kept": torch.where(there, kept, -1).int(), "lens": s["lens"].clamp(max=keep)}
+
+
+def run(state):
+    if own:
+        return _run_own(state)
+    return {"rotary": _rotary, "append": _append, "attention": _attention, "evict": _evict}[state["case"]["op"]](state)
+
+
+# ----------------------------------------------------------------------------------------------------------------
+# float64, sequence by sequence from the definitions
+# ----------------------------------------------------------------------------------------------------------------
+def _exact_rotary(s):
+    c, r = s["case"], s["case"]["rotary_dim"]
+    pairs = torch.arange(r // 2, dtype=torch.float64, device=DEVICE)
+    freq = torch.exp(-2.0 * pairs / r * math.log(s["theta"]))
+    if c["scaling"] == "linear":
+        freq = freq / c["factor"]
+    elif c["scaling"] == "turns":
+        ramp = (s["original"] / (2 * math.pi / freq) - s["turns"][0]) / (s["turns"][1] - s["turns"][0])
+        ramp = torch.clamp(ramp, 0, 1)
+        freq = ramp * freq + (1 - ramp) * freq / c["factor"]
+    sign = -1.0 if c["direction"] == "inverse" else 1.0
+    turn = torch.polar(torch.full_like(freq, s["amplitude"])[None].expand(c["rows"], -1).contiguous(), sign * s["positions"].double()[:, None] * freq)
+    res = {}
+    for name in ("q", "k"):
+        x = s[name].double()
+        y = x.clone()
+        first = slice(0, r // 2) if c["layout"] == "half" else slice(0, r, 2)
+        second = slice(r // 2, r) if c["layout"] == "half" else slice(1, r, 2)
+        z = torch.complex(x[..., first].contiguous(), x[..., second].contiguous()) * turn[:, None, :]
+        y[..., first], y[..., second] = z.real, z.imag
+        res[name] = y
+    return res
+
+
+def _near(x, scale, fmt):
+    """x's nearest multiple of the format at this scale, ties to even, as a value."""
+    y = x / scale
+    if fmt == "int8":
+        return torch.round(y).clamp(-127, 127) * scale
+    step = torch.exp2(torch.clamp(torch.floor(torch.log2(y.abs().clamp(min=1e-30))), min=-6) - 3)
+    return (torch.round(y / step) * step).clamp(-448, 448) * scale
+
+
+def _fitting(largest, fmt):
+    if fmt == "int8":
+        return max(FLOOR, float(torch.tensor(largest / 127.0, dtype=torch.float64).float()))
+    e = math.ceil(math.log2(largest / 448.0)) if largest > 0 else -126
+    while e > -126 and largest <= 448.0 * 2.0 ** (e - 1):
+        e -= 1
+    while largest > 448.0 * 2.0 ** e:
+        e += 1
+    return 2.0 ** max(e, -126)
+
+
+def _values(s, which, blk, head=slice(None)):
+    """The values [kv][16][dh] (or of one head) of a block."""
+    pool = s["cache_v"] if which else s["cache_k"]
+    x = (pool[int(blk)].float()[head] * s["scales"][int(blk), :, which][head][..., None, None]).double()
+    return x.transpose(-1, -2) if which else x
+
+
+def _exact_append(s):
+    c, fmt = s["case"], s["case"]["format"]
+    if c["batch"] * _blocks(c["rows"] + BLOCK) * c["kv_heads"] > 20000:
+        return None
+    tables, pos = s["tables"].cpu(), s["row_pos"].cpu().view(c["batch"], -1)
+    reads, scales = [[], []], s["scales"].double()
+    for which, name in ((0, "k_new"), (1, "v_new")):
+        new = s[name].double().view(c["batch"], c["rows"], c["kv_heads"], -1)
+        for b in range(c["batch"]):
+            lo, hi = int(pos[b, 0]), int(pos[b, -1]) + 1
+            for lb in range(lo // BLOCK, (hi - 1) // BLOCK + 1):
+                blk = int(tables[b, lb])
+                a, z = max(lo, lb * BLOCK), min(hi, lb * BLOCK + BLOCK)
+                rows = new[b, a - lo:z - lo].transpose(0, 1)                            # [kv][tokens][dh]
+                older = _values(s, which, blk)[:, :a - lb * BLOCK]
+                need = [_fitting(x, fmt) for x in rows.abs().amax((1, 2)).tolist()]
+                if older.shape[1]:
+                    need = [max(x, y) for x, y in zip(need, s["scales"][blk, :, which].tolist())]
+                need = torch.tensor(need, dtype=torch.float64, device=DEVICE)
+                reads[which].append(_near(torch.cat([older, rows], 1), need[:, None, None], fmt).transpose(0, 1))
+                scales[blk, :, which] = need
+    return {"k": torch.cat(reads[0]), "v": torch.cat(reads[1]), "scales": scales}
+
+
+def _exact_attention(s):
+    c = s["case"]
+    n, rows, h, kv, dh = c["batch"], c["rows"], c["heads"], c["kv_heads"], c["head_dim"]
+    if n * (c["ctx_max"] + rows) * h * dh * rows > 4e12:
+        return None
+    out = torch.zeros((n, rows, h, dh), dtype=torch.float64, device=DEVICE)
+    weights = s["weights_out"].double() if c["weights"] else None
+    for b in range(n):
+        pos = s["row_pos"].view(n, rows)[b]
+        last = int(pos[-1])
+        blk = s["tables"][b, :last // BLOCK + 1].long()
+        for g in range(kv):
+            k = (s["cache_k"][:, g].view(torch.int8)[blk].view(s["cache_k"].dtype).double() * s["scales"][blk, g, 0].double()[:, None, None]).reshape(-1, dh)[:last + 1]
+            v = (s["cache_v"][:, g].view(torch.int8)[blk].view(s["cache_v"].dtype).double() * s["scales"][blk, g, 1].double()[:, None, None])
+            v = v.transpose(1, 2).reshape(-1, dh)[:last + 1]
+            q = s["q"].view(n, rows, h, dh)[b, :, g * (h // kv):(g + 1) * (h // kv)].double()
+            z = (q.reshape(-1, dh) @ k.t()).view(rows, h // kv, last + 1) / math.sqrt(dh)
+            z = z.masked_fill(torch.arange(last + 1, device=DEVICE)[None, None, :] > pos[:, None, None], -math.inf)
+            p = torch.softmax(z, -1)
+            out[b, :, g * (h // kv):(g + 1) * (h // kv)] = (p.reshape(-1, last + 1) @ v).view(rows, h // kv, dh)
+            if c["weights"]:
+                weights[b, g, :last] = s["weights"][b, g, :last].double() + p[0].sum(0)[:last]
+                weights[b, g, last] = p[0].sum(0)[last]
+    res = {"out": out.view(n * rows, h, dh)}
+    if c["weights"]:
+        res["weights"] = weights
+    return res
+
+
+def _exact_evict(s):
+    c, fmt = s["case"], s["case"]["format"]
+    kv, keep = c["kv_heads"], c["keep"]
+    lens = s["lens"].cpu().tolist()
+    if sum(min(n, keep) for n in lens) * kv > 400000:
+        return None
+    weights, kept = s["weights_out"].double(), torch.full((len(lens), kv, keep), -1, dtype=torch.int32)
+    reads = [[], []]
+    host = s["weights"].cpu().double().numpy()
+    for b, n in enumerate(lens):
+        m = min(n, keep)
+        chosen = []
+        for g in range(kv):
+            old = sorted(range(max(0, n - c["recent"])), key=lambda i: (-host[b, g, i], i))[:m - min(c["recent"], n)] if n > keep else list(range(n))
+            ids = sorted(set(old) | set(range(max(0, n - c["recent"]), n))) if n > keep else old
+            kept[b, g, :m] = torch.tensor(ids, dtype=torch.int32)
+            weights[b, g, :m] = s["weights"][b, g, torch.tensor(ids, device=DEVICE, dtype=torch.long)].double()
+            chosen.append(ids)
+        if not m:
+            continue
+        ids = torch.tensor(chosen, device=DEVICE)                                        # [kv][m]
+        blk, head = s["tables"][b].long()[ids // BLOCK], torch.arange(kv, device=DEVICE)[:, None].expand_as(ids)
+        for which, pool in ((0, s["cache_k"]), (1, s["cache_v"])):
+            q = pool.double()[blk, head, ids % BLOCK] if pool.numel() < 1 << 26 and not which else None
+            if q is None:
+                raw = pool.view(torch.int8)
+                q = (raw[blk, head, ids % BLOCK] if not which else raw[blk, head, :, ids % BLOCK]).view(pool.dtype).double()
+            was = s["scales"][blk, head, which].double()
+            most = q.abs().amax(-1)
+            wide = -(-m // BLOCK) * BLOCK
+            if fmt == "int8":
+                need = torch.where(most >= 127, was, ((most * was).float().double() / 127).float().double()).clamp(min=FLOOR)
+            else:
+                need = torch.exp2(torch.ceil(torch.log2((most * was).clamp(min=1e-37) / 448))).clamp(min=FLOOR)
+            need = torch.cat([need, need.new_full((kv, wide - m), FLOOR)], 1).view(kv, -1, BLOCK).amax(-1)
+            need = need.repeat_interleave(BLOCK, 1)[:, :m]
+            value = (q * was[..., None]).float().double()
+            reads[which].append(_near(value, need[..., None], fmt).transpose(0, 1))
+    return {"k": torch.cat(reads[0]), "v": torch.cat(reads[1]), "weights": weights, "kept": kept.to(DEVICE),
+            "lens": s["lens"].clamp(max=keep)}
+
+
+def exact(case, seed):
+    global own
+    was, own = own, False   # inputs only: no handle of the library's
+    try:
+        s = prepare(case, seed)
+    finally:
+        own = was
+    return {"rotary": _exact_rotary, "append": _exact_append, "attention": _exact_attention, "evict": _exact_evict}[case["op"]](s)
