@@ -348,7 +348,7 @@ def _scale_for(largest, fmt):
     if fmt == "int8":
         return (largest.double() / 127).float().clamp(min=FLOOR)
     m, e = torch.frexp(largest)   # 448 = 0.875 * 2^9
-    return torch.exp2((e - 9 + (m > 0.875).int()).double().clamp(min=-126)).float()
+    return torch.where(largest > 0, torch.exp2((e - 9 + (m > 0.875).int()).double().clamp(min=-126)).float(), FLOOR)
 
 
 def _quantised(x, scale, fmt):
