@@ -232,6 +232,134 @@ int ee_paged_attention_decode(const ee_model_desc* desc, const ee_kv_cache* cach
                               const ee_batch* batch, float* out, void* workspace, size_t workspace_bytes,
                               void* stream);
 
+/* ---- An 8-bit paged cache, and the steps around it ------------------------------------------------------------
+ * For programs that run a model's layers one call at a time: rotary positions, a cache of half (EE_BF16) or a quarter of
+ * the bytes, the attention that reads it, and an eviction that bounds its length.  Same conventions as above: nothing
+ * here allocates, synchronises or keeps anything between calls.
+ *
+ * Positions are counted twice.  `positions` of ee_rotary are the places in the text; context_lens of the other calls
+ * are slots of the cache.  The two differ once a sequence has been through ee_kv_quant_evict. */
+
+#define EE_ROTARY_HALF 0         /* pair j = channels j and j + rotary_dim/2                              */
+#define EE_ROTARY_INTERLEAVED 1  /* pair j = channels 2j and 2j + 1                                       */
+
+#define EE_ROTARY_PLAIN 0   /* f_j = theta^(-2j / rotary_dim)                                             */
+#define EE_ROTARY_LINEAR 1  /* f_j / factor: positions squeezed into the context the model was trained on */
+#define EE_ROTARY_TURNS 2   /* by how often pair j turns within original_context, t = original_context f_j / (2 pi):
+                               f_j (w + (1 - w) / factor), w = (t - turns_low) / (turns_high - turns_low) within 0..1:
+                               fast pairs keep their frequency, slow ones are squeezed                    */
+
+typedef struct ee_rotary_desc {
+  int32_t head_dim;    /* channels of a head, 2 .. 1024                                                   */
+  int32_t rotary_dim;  /* even, 2 .. head_dim: the first rotary_dim channels are rotated, the others copied */
+  int32_t layout;      /* EE_ROTARY_HALF | EE_ROTARY_INTERLEAVED                                          */
+  int32_t scaling;     /* EE_ROTARY_PLAIN | _LINEAR | _TURNS                                              */
+  int32_t original_context;     /* >= 1 (TURNS)                                                           */
+  double theta;        /* > 0                                                                             */
+  double factor;       /* > 0 (LINEAR, TURNS)                                                             */
+  double turns_low, turns_high; /* low < high (TURNS)                                                     */
+  double amplitude;    /* multiplies every rotated pair (1 = a rotation; finite as a float)               */
+} ee_rotary_desc;
+
+/* The rows of one tensor [rows][n_heads][head_dim]: heads and channels are consecutive, rows `stride` elements apart
+ * (>= n_heads * head_dim).  in == out with equal strides works in place; otherwise the two must not overlap. */
+typedef struct ee_rotary_rows {
+  const void* in;      /* dev                                                                             */
+  void* out;           /* dev                                                                             */
+  int64_t in_stride, out_stride;
+  int32_t n_heads;
+} ee_rotary_rows;
+
+/* Angular frequency per position of every pair, in double: freqs dev [rotary_dim/2].  A set-up step: the result serves
+ * every later call with the same desc.  A caller with a scaling of its own fills freqs itself. */
+int ee_rotary_frequencies(const ee_rotary_desc* desc, double* freqs, void* stream);
+
+/* Rotary embedding of query and key rows in one launch: for every row m, head and pair j with channels (a, b)
+ *   (a, b) -> amplitude * (a cos w - b sin w, a sin w + b cos w),   w = positions[m] * freqs[j],
+ * the angle formed in double, the rest in float, rounded once to `dtype` (EE_FP32 | EE_BF16: the type of all four
+ * tensors).  transpose = 1 multiplies by the transposed matrix instead (sin w -> -sin w): the gradient of `in` from
+ * the gradient of `out`.
+ *   positions dev [rows] int32 (any value).  q, k host; either may be NULL, not both. */
+int ee_rotary(const ee_rotary_desc* desc, const double* freqs, const int32_t* positions, int32_t rows, int32_t dtype,
+              const ee_rotary_rows* q, const ee_rotary_rows* k, int32_t transpose, void* stream);
+
+#define EE_QUANT_INT8 0  /* a byte is a signed integer -127..127; the scale is a float                    */
+#define EE_QUANT_E4M3 1  /* a byte is a float of 4 exponent and 3 mantissa bits (largest 448, no infinity); the scale
+                            is a power of two                                                            */
+
+/* Paged cache in 8 bits with one scale for each block of 16 positions and head, K and V apart.  A byte stands for the
+ * float (byte's value) * scale.  Block tables as in ee_kv_cache.  Pools start on 16 bytes.
+ * Slots that hold no position of a sequence may contain anything in bytes and scales.  The bytes of a cached position
+ * are finite (ee_kv_quant_append writes no others). */
+typedef struct ee_quant_cache {
+  void* k_pool;        /* dev [n_layers][num_blocks][n_kv_heads][16][head_dim]                            */
+  void* v_pool;        /* dev [n_layers][num_blocks][n_kv_heads][head_dim][16]                            */
+  float* scales;       /* dev [n_layers][num_blocks][n_kv_heads][2]: of K, of V                           */
+  int32_t n_layers, num_blocks, block_size; /* block_size must be 16                                      */
+  int32_t n_kv_heads, head_dim;             /* head_dim: a multiple of 16, 16 .. 256                      */
+  int32_t format;      /* EE_QUANT_INT8 | EE_QUANT_E4M3                                                   */
+} ee_quant_cache;
+
+/* Caches K and V of the batch's rows: row m goes to position context_lens[m] of its sequence.  With row_table several rows
+ * may share a sequence; those that fall into one block stand next to each other in the batch, at consecutive ascending
+ * positions.  A row with context_lens[m] < 0 is skipped (padding).
+ * A block's scale is the smallest with which the largest magnitude ever appended to it fits,
+ *   INT8: float(largest / 127), at least 2^-126;   E4M3: the smallest power of two with largest <= 448 * scale, at least
+ *   2^-126,
+ * and the first position of a block starts anew, whatever the block held.  Where a call makes a block's scale grow, the
+ * positions in front of the call's are rounded again, from the floats their bytes stood for.  Every rounding is to the
+ * nearest, ties to even, of the exact quotient.  An infinity or NaN makes the block's scale NaN (every result that
+ * depends on the block is then NaN, until the block starts anew).
+ *   k, v dev, rows [n_kv_heads][head_dim] of `dtype` (EE_FP32 | EE_BF16), k_stride / v_stride elements apart (even, >=
+ *   n_kv_heads * head_dim), starting on 8 (EE_FP32) or 4 bytes.  batch->tokens is not read. */
+int ee_kv_quant_append(const ee_quant_cache* cache, int32_t layer, const void* k, int64_t k_stride, const void* v,
+                       int64_t v_stride, int32_t dtype, const ee_batch* batch, void* stream);
+
+/* The floats that the cache holds: row m reads position context_lens[m] of its sequence (row_table as above; any
+ * order).  k, v dev [rows][n_kv_heads][head_dim] of `dtype`, starting on 8 (EE_FP32) or 4 bytes; zeros for
+ * context_lens[m] < 0. */
+int ee_kv_quant_read(const ee_quant_cache* cache, int32_t layer, const ee_batch* batch, void* k, void* v, int32_t dtype,
+                     void* stream);
+
+/* Attention of single queries over the 8-bit cache:
+ *   out[m][h] = softmax_j(q[m][h] . K[j][h / g] / sqrt(head_dim)) . V[j][h / g],  j = 0..context_lens[m] INCLUSIVE,
+ * with g = n_heads / n_kv_heads query heads to a K/V head.  Rows that share a sequence (row_table) are a causal chunk of a
+ * prompt, and quickest when they stand next to each other.  A row with context_lens[m] < 0 attends nothing: its
+ * result is 0.  q and out dev [rows][n_heads][head_dim] float, 16-byte aligned.
+ * weights_out (dev [rows][n_kv_heads][weights_pitch] float, or NULL) receives the attention each cached position got, added
+ * over the g heads that share it, for j <= p = context_lens[m]:
+ *   weights_out[m][k][j] = weights_in[m][k][j] + sum_g probability   (j < p),   = sum_g probability   (j = p);
+ * what lies behind is left as it was.  weights_in (same pitch) may be weights_out, or NULL for zeros.  Not with
+ * row_table (EE_ERR_UNSUPPORTED).  weights_pitch >= max_context.
+ * workspace: ee_paged_attention_quant_bytes for the call's sizes or larger ones (256-byte aligned; NULL where that is 0);
+ * it needs no initialisation. */
+size_t ee_paged_attention_quant_bytes(const ee_quant_cache* cache, int32_t n_heads, int32_t max_batch, int32_t max_context,
+                                      int32_t with_weights);
+int ee_paged_attention_quant(const ee_quant_cache* cache, int32_t layer, int32_t n_heads, const float* q,
+                             const ee_batch* batch, float* out, const float* weights_in, float* weights_out,
+                             int32_t weights_pitch, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Shortens the cache of every sequence of the batch to `keep` positions, for each K/V head by itself: the latest `recent`
+ * (0 .. keep) positions stay, and of the others those with the largest weights_in (of equal ones the lowest position; NaN
+ * counts as largest).  What stays moves together in its old order.  Here context_lens[b] is the NUMBER of cached
+ * positions, at most max_context; row_table must be NULL; a sequence of `keep` positions or fewer keeps them all.
+ * out_lens[b] = min(context_lens[b], keep) is the new number: the caller passes it on when every layer is done.
+ *   dst_tables   dev [B][dst_max_blocks] or NULL.  NULL: the sequence's first blocks are written over (what lies behind
+ *                out_lens[b] is free afterwards).  Else the result goes to these blocks, which must not be among the
+ *                blocks the batch's sequences are read from (for blocks that are shared, which must stay as they are).
+ *   weights_in   dev [B][n_kv_heads][weights_pitch] float, weights_pitch >= max_context.
+ *   weights_out  dev [B][n_kv_heads][weights_out_pitch] float or NULL, weights_out_pitch >= keep: the weights of what
+ *                stays; may be weights_in (equal pitches).  Entries from out_lens[b] on are left as they were.
+ *   kept         dev [B][n_kv_heads][keep] int32: the positions that stay, ascending, then -1.
+ * A block that is written is built from its positions: its scale is the smallest that fits, and a position rounds
+ * again (from the float its byte stood for) only where that scale differs from its old one.
+ * workspace: ee_kv_quant_evict_bytes bytes, 256-byte aligned, without dst_tables; else unused. */
+size_t ee_kv_quant_evict_bytes(const ee_quant_cache* cache, int32_t max_batch, int32_t keep);
+int ee_kv_quant_evict(const ee_quant_cache* cache, int32_t layer, const ee_batch* batch, const int32_t* dst_tables,
+                      int32_t dst_max_blocks, const float* weights_in, int32_t weights_pitch, float* weights_out,
+                      int32_t weights_out_pitch, int32_t keep, int32_t recent, int32_t* kept, int32_t* out_lens,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- Measurement helpers (not part of the decode path) ------------------------------------------------------
  * While enabled, every later ee_* call brackets the kernels it enqueues with pairs of HIP events on the call's
  * stream (the events add a few microseconds per kernel, so throughput is timed with profiling off).

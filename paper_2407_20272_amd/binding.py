@@ -21,7 +21,12 @@ EE_PACK_PLAIN, EE_PACK_QKV, EE_PACK_GATE_UP = 0, 1, 2
 EXPORTS = ["ee_last_error", "ee_packed_weight_bytes", "ee_pack_weight", "ee_workspace_bytes", "ee_decode_iteration",
            "ee_exit_check", "ee_kv_fill", "ee_paged_attention_decode", "ee_profile_enable", "ee_profile_read", "ee_calibration_copy",
            "ee_noalloc_init", "ee_exit_check_noalloc_bytes", "ee_exit_check_noalloc", "ee_calibration_read", "ee_calibration_mfma",
-           "ee_calibration_mfma_tile", "ee_calibration_intake"]
+           "ee_calibration_mfma_tile", "ee_calibration_intake", "ee_rotary_frequencies", "ee_rotary", "ee_kv_quant_append",
+           "ee_kv_quant_read", "ee_paged_attention_quant_bytes", "ee_paged_attention_quant", "ee_kv_quant_evict_bytes",
+           "ee_kv_quant_evict"]
+EE_ROTARY_HALF, EE_ROTARY_INTERLEAVED = 0, 1
+EE_ROTARY_PLAIN, EE_ROTARY_LINEAR, EE_ROTARY_TURNS = 0, 1, 2
+EE_QUANT_INT8, EE_QUANT_E4M3 = 0, 1
 EE_NOALLOC_SCRATCH_BYTES = 8 << 20
 KERNEL_CLASSES = ["norm", "qkv", "attention", "o_proj", "gate_up", "down", "head", "combine", "kv_fill", "other"]
 
@@ -50,6 +55,23 @@ class ee_batch(C.Structure):
     _fields_ = [("batch", C.c_int32), ("tokens", C.c_void_p), ("context_lens", C.c_void_p),
                 ("block_tables", C.c_void_p), ("max_blocks", C.c_int32), ("max_context", C.c_int32),
                 ("row_table", C.c_void_p)]
+
+
+class ee_rotary_desc(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rotary_dim", C.c_int32), ("layout", C.c_int32), ("scaling", C.c_int32),
+                ("original_context", C.c_int32), ("theta", C.c_double), ("factor", C.c_double), ("turns_low", C.c_double),
+                ("turns_high", C.c_double), ("amplitude", C.c_double)]
+
+
+class ee_rotary_rows(C.Structure):
+    _fields_ = [("in_", C.c_void_p), ("out", C.c_void_p), ("in_stride", C.c_int64), ("out_stride", C.c_int64),
+                ("n_heads", C.c_int32)]
+
+
+class ee_quant_cache(C.Structure):
+    _fields_ = [("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("scales", C.c_void_p), ("n_layers", C.c_int32),
+                ("num_blocks", C.c_int32), ("block_size", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("format", C.c_int32)]
 
 
 class EEError(RuntimeError):
@@ -103,6 +125,25 @@ def lib() -> C.CDLL:
         L.ee_profile_read.argtypes = [C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.POINTER(C.c_float), C.c_int32]
         L.ee_profile_enable.restype = C.c_int
         L.ee_profile_read.restype = C.c_int
+        L.ee_rotary_frequencies.argtypes = [C.POINTER(ee_rotary_desc), C.c_void_p, C.c_void_p]
+        L.ee_rotary.argtypes = [C.POINTER(ee_rotary_desc), C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.POINTER(ee_rotary_rows),
+                                C.POINTER(ee_rotary_rows), C.c_int32, C.c_void_p]
+        L.ee_kv_quant_append.argtypes = [C.POINTER(ee_quant_cache), C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                         C.c_int32, C.POINTER(ee_batch), C.c_void_p]
+        L.ee_kv_quant_read.argtypes = [C.POINTER(ee_quant_cache), C.c_int32, C.POINTER(ee_batch), C.c_void_p, C.c_void_p,
+                                       C.c_int32, C.c_void_p]
+        L.ee_paged_attention_quant_bytes.argtypes = [C.POINTER(ee_quant_cache), C.c_int32, C.c_int32, C.c_int32, C.c_int32]
+        L.ee_paged_attention_quant_bytes.restype = C.c_size_t
+        L.ee_paged_attention_quant.argtypes = [C.POINTER(ee_quant_cache), C.c_int32, C.c_int32, C.c_void_p, C.POINTER(ee_batch),
+                                               C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.ee_kv_quant_evict_bytes.argtypes = [C.POINTER(ee_quant_cache), C.c_int32, C.c_int32]
+        L.ee_kv_quant_evict_bytes.restype = C.c_size_t
+        L.ee_kv_quant_evict.argtypes = [C.POINTER(ee_quant_cache), C.c_int32, C.POINTER(ee_batch), C.c_void_p, C.c_int32, C.c_void_p,
+                                        C.c_int32, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
+                                        C.c_size_t, C.c_void_p]
+        for name in ("ee_rotary_frequencies", "ee_rotary", "ee_kv_quant_append", "ee_kv_quant_read", "ee_paged_attention_quant",
+                     "ee_kv_quant_evict"):
+            getattr(L, name).restype = C.c_int
         for name in ("ee_pack_weight", "ee_decode_iteration", "ee_exit_check", "ee_kv_fill", "ee_paged_attention_decode",
                      "ee_exit_check_noalloc", "ee_noalloc_init"):
             getattr(L, name).restype = C.c_int
@@ -290,6 +331,143 @@ def ee_paged_attention_decode(desc: ee_model_desc, cache: PagedKV, layer: int, q
                               ws: Optional[Workspace] = None):
     _check(lib().ee_paged_attention_decode(C.byref(desc), C.byref(cache.c), layer, _ptr(q), C.byref(batch), _ptr(out),
                                            _ptr(ws.buf) if ws else None, ws.bytes if ws else 0, _stream()))
+
+
+# ---- 8-bit cache, rotary embedding on its own ------------------------------------------------------------
+def _row_view(t: torch.Tensor):
+    """Pointer, row stride and element type of [rows][heads][channels] whose heads and channels are consecutive."""
+    assert t.is_cuda and t.dim() == 3 and t.dtype in (torch.float32, torch.bfloat16), "rows are CUDA tensors [rows][heads][channels]"
+    rows, heads, dh = t.shape
+    assert rows == 0 or ((dh == 1 or t.stride(2) == 1) and (heads == 1 or t.stride(1) == dh)), "heads and channels must be consecutive"
+    return t.data_ptr(), t.stride(0) if rows > 1 else heads * dh, EE_FP32 if t.dtype == torch.float32 else EE_BF16
+
+
+def make_rotary_desc(head_dim: int, rotary_dim: Optional[int] = None, layout: str = "half", theta: float = 10000.0,
+                     scaling: str = "plain", factor: float = 1.0, original_context: int = 1, turns=(1.0, 4.0),
+                     amplitude: float = 1.0) -> ee_rotary_desc:
+    layouts = {"half": EE_ROTARY_HALF, "interleaved": EE_ROTARY_INTERLEAVED}
+    scalings = {"plain": EE_ROTARY_PLAIN, "linear": EE_ROTARY_LINEAR, "turns": EE_ROTARY_TURNS}
+    return ee_rotary_desc(head_dim, head_dim if rotary_dim is None else rotary_dim, layouts[layout], scalings[scaling],
+                          original_context, theta, factor, turns[0], turns[1], amplitude)
+
+
+def ee_rotary_frequencies(desc: ee_rotary_desc, device="cuda") -> torch.Tensor:
+    """The frequencies every later ee_rotary call with this desc takes (a new float64 tensor [rotary_dim / 2])."""
+    freqs = torch.empty(max(0, desc.rotary_dim // 2), dtype=torch.float64, device=device)
+    _check(lib().ee_rotary_frequencies(C.byref(desc), _ptr(freqs), _stream()))
+    return freqs
+
+
+def ee_rotary(desc: ee_rotary_desc, freqs: torch.Tensor, positions: torch.Tensor, q: Optional[torch.Tensor],
+              q_out: Optional[torch.Tensor], k: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+              transpose: bool = False):
+    """Rows [rows][heads][head_dim] of any row stride; q_out may be q, k_out may be k."""
+    assert freqs.dtype == torch.float64 and freqs.numel() == desc.rotary_dim // 2
+    rows, records, kinds = int(positions.shape[0]), [], set()
+    for x, y in ((q, q_out), (k, k_out)):
+        if x is None:
+            records.append(None)
+            continue
+        assert x.shape == y.shape and x.shape[0] == rows and x.shape[2] == desc.head_dim
+        (px, sx, tx), (py, sy, ty) = _row_view(x), _row_view(y)
+        kinds |= {tx, ty}
+        records.append(ee_rotary_rows(px, py, sx, sy, int(x.shape[1])))
+    assert len(kinds) <= 1, "q, k and the results have one type"
+    _check(lib().ee_rotary(C.byref(desc), _ptr(freqs), _ptr(_i32(positions)), rows, kinds.pop() if kinds else EE_FP32,
+                           C.byref(records[0]) if records[0] else None, C.byref(records[1]) if records[1] else None,
+                           int(bool(transpose)), _stream()))
+
+
+class QuantKV:
+    """8-bit paged cache: k [n_layers][num_blocks][Hkv][16][dh], v [n_layers][num_blocks][Hkv][dh][16] (int8 or
+    float8_e4m3fn) and scales [n_layers][num_blocks][Hkv][2] float."""
+
+    def __init__(self, n_layers: int, num_blocks: int, n_kv_heads: int, head_dim: int, format: str = "int8", device="cuda"):
+        t = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn}[format]
+        self._hold(torch.zeros((n_layers, num_blocks, n_kv_heads, 16, head_dim), dtype=torch.int8, device=device).view(t),
+                   torch.zeros((n_layers, num_blocks, n_kv_heads, head_dim, 16), dtype=torch.int8, device=device).view(t),
+                   torch.zeros((n_layers, num_blocks, n_kv_heads, 2), device=device))
+
+    @classmethod
+    def of(cls, k: torch.Tensor, v: torch.Tensor, scales: torch.Tensor) -> "QuantKV":
+        """The record of a cache that is there already."""
+        c = cls.__new__(cls)
+        c._hold(k, v, scales)
+        return c
+
+    def _hold(self, k, v, scales):
+        n, nb, h, bs, dh = k.shape
+        assert k.dtype == v.dtype and k.dtype in (torch.int8, torch.float8_e4m3fn) and scales.dtype == torch.float32
+        assert v.shape == (n, nb, h, dh, bs) and scales.shape == (n, nb, h, 2)
+        self.k, self.v, self.scales, self.num_blocks = k, v, scales, nb
+        self.c = ee_quant_cache(_ptr(k), _ptr(v), _ptr(scales), n, nb, bs, h, dh,
+                                EE_QUANT_INT8 if k.dtype == torch.int8 else EE_QUANT_E4M3)
+
+
+class QuantWorkspace:
+    """Scratch of ee_paged_attention_quant calls up to these sizes, or of ee_kv_quant_evict in place (`evicting`)."""
+
+    def __init__(self, cache: QuantKV, n_heads: int, max_batch: int, max_context: int, with_weights: bool = False,
+                 evicting: bool = False):
+        L = lib()
+        if evicting:
+            self.bytes = L.ee_kv_quant_evict_bytes(C.byref(cache.c), max_batch, max_context)
+            bad = self.bytes == 0
+        else:
+            self.bytes = L.ee_paged_attention_quant_bytes(C.byref(cache.c), n_heads, max_batch, max_context, int(with_weights))
+            bad = self.bytes == 0 and (max_batch < 1 or max_context < 1 or n_heads < 1 or n_heads % cache.c.n_kv_heads != 0)
+        if bad:
+            raise EEError(EE_ERR_INVALID_ARG, ee_last_error())
+        self.buf = torch.empty(max(self.bytes, 256), dtype=torch.uint8, device=cache.k.device)
+        assert self.buf.data_ptr() % 256 == 0
+
+
+def ee_kv_quant_append(cache: QuantKV, layer: int, k: torch.Tensor, v: torch.Tensor, batch: ee_batch):
+    """k, v [rows][Hkv][dh], float32 or bfloat16, any (even) row stride."""
+    shape = (batch.batch, cache.c.n_kv_heads, cache.c.head_dim)
+    assert k.shape == shape and v.shape == shape
+    (pk, sk, tk), (pv, sv, tv) = _row_view(k), _row_view(v)
+    assert tk == tv, "k and v have one type"
+    _check(lib().ee_kv_quant_append(C.byref(cache.c), layer, pk, sk, pv, sv, tk, C.byref(batch), _stream()))
+
+
+def ee_kv_quant_read(cache: QuantKV, layer: int, batch: ee_batch, k: torch.Tensor, v: torch.Tensor):
+    shape = (batch.batch, cache.c.n_kv_heads, cache.c.head_dim)
+    assert k.shape == shape and v.shape == shape and k.dtype == v.dtype and k.dtype in (torch.float32, torch.bfloat16)
+    _check(lib().ee_kv_quant_read(C.byref(cache.c), layer, C.byref(batch), _ptr(k), _ptr(v),
+                                  EE_FP32 if k.dtype == torch.float32 else EE_BF16, _stream()))
+
+
+def ee_paged_attention_quant(cache: QuantKV, layer: int, q: torch.Tensor, batch: ee_batch, out: torch.Tensor,
+                             ws: Optional[QuantWorkspace] = None, weights_in: Optional[torch.Tensor] = None,
+                             weights_out: Optional[torch.Tensor] = None):
+    """q, out [rows][H][dh] float32; weights [rows][Hkv][pitch] float32."""
+    assert q.dim() == 3 and q.shape == out.shape and q.shape[0] == batch.batch and q.shape[2] == cache.c.head_dim
+    assert q.dtype == torch.float32 and out.dtype == torch.float32
+    pitch = 0
+    for w in (weights_in, weights_out):
+        if w is not None:
+            assert w.dtype == torch.float32 and w.shape[:2] == (batch.batch, cache.c.n_kv_heads) and pitch in (0, w.shape[2])
+            pitch = int(w.shape[2])
+    _check(lib().ee_paged_attention_quant(C.byref(cache.c), layer, int(q.shape[1]), _ptr(q), C.byref(batch), _ptr(out),
+                                          _ptr(weights_in), _ptr(weights_out), pitch, _ptr(ws.buf) if ws else None,
+                                          ws.bytes if ws else 0, _stream()))
+
+
+def ee_kv_quant_evict(cache: QuantKV, layer: int, batch: ee_batch, weights_in: torch.Tensor, weights_out: Optional[torch.Tensor],
+                      keep: int, recent: int, kept: torch.Tensor, out_lens: torch.Tensor, ws: Optional[QuantWorkspace] = None,
+                      dst_tables: Optional[torch.Tensor] = None):
+    """weights [B][Hkv][pitch] float32, kept [B][Hkv][keep] int32, out_lens [B] int32, dst_tables [B][blocks] int32."""
+    head = (batch.batch, cache.c.n_kv_heads)
+    for w in (weights_in, weights_out):
+        assert w is None or (w.dtype == torch.float32 and w.shape[:2] == head)
+    assert kept.shape == head + (keep,) and out_lens.shape == (batch.batch,)
+    assert dst_tables is None or dst_tables.shape[0] == batch.batch
+    _check(lib().ee_kv_quant_evict(C.byref(cache.c), layer, C.byref(batch), _ptr(_i32(dst_tables)) if dst_tables is not None else None,
+                                   int(dst_tables.shape[1]) if dst_tables is not None else 0, _ptr(weights_in),
+                                   int(weights_in.shape[2]), _ptr(weights_out),
+                                   int(weights_out.shape[2]) if weights_out is not None else 0, keep, recent, _ptr(_i32(kept)),
+                                   _ptr(_i32(out_lens)), _ptr(ws.buf) if ws else None, ws.bytes if ws else 0, _stream()))
 
 
 def ee_profile_enable(on: bool):

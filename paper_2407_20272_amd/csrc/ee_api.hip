@@ -6,7 +6,7 @@
 #include <mutex>
 #include <vector>
 
-#include "ee_common.h"
+#include "quant.h"
 
 // Scratch of ee_exit_check_noalloc (see noalloc_scratch below).
 static __device__ __align__(256) unsigned char scratch[EE_NOALLOC_SCRATCH_BYTES];
@@ -980,6 +980,279 @@ int ee_paged_attention_decode(const ee_model_desc* desc, const ee_kv_cache* cach
   }
   const Pred always{nullptr, 0};
   if ((rc = launch_attention(at, desc->dtype, always, reinterpret_cast<hipStream_t>(stream)))) return rc;
+  EE_HIP(hipGetLastError());
+  return EE_OK;
+}
+
+// ---- 8-bit cache, rotary embedding on its own ------------------------------------------------------------------
+namespace {
+
+int check_rotary_desc(const ee_rotary_desc* D) {
+  if (!D) EE_FAIL(EE_ERR_INVALID_ARG, "rotary description is NULL");
+  if (D->head_dim < 2 || D->head_dim > 1024) EE_FAIL(EE_ERR_UNSUPPORTED, "rotary: head_dim %d outside 2..1024", D->head_dim);
+  if (D->rotary_dim < 2 || D->rotary_dim > D->head_dim || D->rotary_dim % 2)
+    EE_FAIL(EE_ERR_SHAPE, "rotary_dim %d: an even number within 2..head_dim %d", D->rotary_dim, D->head_dim);
+  if (D->layout != EE_ROTARY_HALF && D->layout != EE_ROTARY_INTERLEAVED) EE_FAIL(EE_ERR_INVALID_ARG, "rotary: unknown layout %d", D->layout);
+  if (D->scaling < EE_ROTARY_PLAIN || D->scaling > EE_ROTARY_TURNS) EE_FAIL(EE_ERR_INVALID_ARG, "rotary: unknown scaling %d", D->scaling);
+  if (!(D->theta > 0.0) || !(D->theta <= 1e300)) EE_FAIL(EE_ERR_INVALID_ARG, "rotary: theta must be positive and finite");
+  if (D->scaling != EE_ROTARY_PLAIN && (!(D->factor > 0.0) || !(D->factor <= 1e300)))
+    EE_FAIL(EE_ERR_INVALID_ARG, "rotary: factor must be positive and finite");
+  if (D->scaling == EE_ROTARY_TURNS &&
+      (D->original_context < 1 || !(D->turns_low < D->turns_high) || !(D->turns_low >= -1e300) || !(D->turns_high <= 1e300)))
+    EE_FAIL(EE_ERR_INVALID_ARG, "rotary: by turns needs original_context >= 1 and turns_low < turns_high");
+  if (!(D->amplitude >= -3e38 && D->amplitude <= 3e38)) EE_FAIL(EE_ERR_INVALID_ARG, "rotary: amplitude must be finite");
+  return EE_OK;
+}
+
+// What the `rows` rows of one side take up, in bytes.
+uint64_t rows_span(int rows, int64_t stride, int64_t row, int size) { return ((uint64_t)(rows - 1) * stride + row) * size; }
+
+int check_rotary_rows(const ee_rotary_rows* R, const char* name, int rows, int head_dim, int size, RotaryRows* out) {
+  *out = RotaryRows{nullptr, nullptr, 0, 0, 0};
+  if (!R) return EE_OK;
+  if (R->n_heads < 1 || R->n_heads > 65536) EE_FAIL(EE_ERR_INVALID_ARG, "rotary: %s has %d heads", name, R->n_heads);
+  if (!R->in || !R->out) EE_FAIL(EE_ERR_INVALID_ARG, "rotary: %s has a NULL pointer", name);
+  const int64_t row = (int64_t)R->n_heads * head_dim, far = INT64_MAX / 16 / (rows > 0 ? rows : 1);
+  if (R->in_stride < row || R->out_stride < row || R->in_stride > far || R->out_stride > far)
+    EE_FAIL(EE_ERR_SHAPE, "rotary: strides %lld, %lld of %s for rows of %lld", (long long)R->in_stride, (long long)R->out_stride, name, (long long)row);
+  const uintptr_t in = reinterpret_cast<uintptr_t>(R->in), res = reinterpret_cast<uintptr_t>(R->out);
+  if ((in | res) % size) EE_FAIL(EE_ERR_INVALID_ARG, "rotary: %s is not aligned to its type", name);
+  if (in == res) {
+    if (R->in_stride != R->out_stride && rows > 1) EE_FAIL(EE_ERR_INVALID_ARG, "rotary: %s in place with two strides", name);
+  } else if (R->in_stride == R->out_stride && rows > 1) {
+    // two views of one buffer may interleave: what counts is whether their rows meet
+    const uint64_t period = (uint64_t)R->in_stride * size, span = rows_span(rows, R->in_stride, row, size);
+    const uint64_t far_apart = in < res ? res - in : in - res, off = far_apart % period;
+    if (far_apart < span && (off < (uint64_t)row * size || off > period - (uint64_t)row * size))
+      EE_FAIL(EE_ERR_INVALID_ARG, "rotary: in and out of %s overlap", name);
+  } else if (in < res + rows_span(rows, R->out_stride, row, size) && res < in + rows_span(rows, R->in_stride, row, size)) {
+    EE_FAIL(EE_ERR_INVALID_ARG, "rotary: in and out of %s overlap", name);
+  }
+  *out = RotaryRows{R->in, R->out, R->in_stride, R->out_stride, R->n_heads};
+  return EE_OK;
+}
+
+int check_quant_cache(const ee_quant_cache* C) {
+  if (!C || !C->k_pool || !C->v_pool || !C->scales) EE_FAIL(EE_ERR_INVALID_ARG, "8-bit cache or one of its pools is NULL");
+  if (C->block_size != 16) EE_FAIL(EE_ERR_UNSUPPORTED, "block_size %d: only 16", C->block_size);
+  if (C->n_layers < 1 || C->num_blocks < 1 || C->n_kv_heads < 1) EE_FAIL(EE_ERR_INVALID_ARG, "8-bit cache: sizes must be positive");
+  if (C->n_kv_heads > 4096) EE_FAIL(EE_ERR_UNSUPPORTED, "8-bit cache: n_kv_heads %d exceeds 4096", C->n_kv_heads);
+  if (C->head_dim < 16 || C->head_dim > kQuantMaxHeadDim || C->head_dim % 16)
+    EE_FAIL(EE_ERR_UNSUPPORTED, "8-bit cache: head_dim %d: a multiple of 16 up to %d", C->head_dim, kQuantMaxHeadDim);
+  if (C->format != EE_QUANT_INT8 && C->format != EE_QUANT_E4M3) EE_FAIL(EE_ERR_INVALID_ARG, "8-bit cache: unknown format %d", C->format);
+  if ((reinterpret_cast<uintptr_t>(C->k_pool) | reinterpret_cast<uintptr_t>(C->v_pool)) & 15)
+    EE_FAIL(EE_ERR_INVALID_ARG, "8-bit cache: pools must start on 16 bytes");
+  if (reinterpret_cast<uintptr_t>(C->scales) & 7) EE_FAIL(EE_ERR_INVALID_ARG, "8-bit cache: scales must start on 8 bytes");
+  return EE_OK;
+}
+
+int check_quant_call(const ee_quant_cache* C, int32_t layer, const ee_batch* Bt, QuantCache* c, QuantRows* r) {
+  int rc;
+  if ((rc = check_quant_cache(C)) || (rc = check_batch(Bt, false))) return rc;
+  if (layer < 1 || layer > C->n_layers) EE_FAIL(EE_ERR_INVALID_ARG, "layer %d outside 1..%d", layer, C->n_layers);
+  const size_t units = (size_t)C->num_blocks * C->n_kv_heads * (layer - 1);
+  *c = QuantCache{reinterpret_cast<int8_t*>(C->k_pool) + units * 16 * C->head_dim, reinterpret_cast<int8_t*>(C->v_pool) + units * 16 * C->head_dim,
+                  C->scales + units * 2, C->num_blocks, C->n_kv_heads, C->head_dim, C->format};
+  *r = QuantRows{Bt->context_lens, Bt->block_tables, Bt->row_table, Bt->batch, Bt->max_blocks};
+  if ((int64_t)Bt->batch * C->n_kv_heads > (1 << 29)) EE_FAIL(EE_ERR_UNSUPPORTED, "%d rows of %d heads in one call", Bt->batch, C->n_kv_heads);
+  return EE_OK;
+}
+
+int check_pair_type(int32_t dtype, const void* a, const void* b, const char* what) {
+  if (dtype != EE_FP32 && dtype != EE_BF16) EE_FAIL(EE_ERR_INVALID_ARG, "%s: dtype must be EE_FP32 or EE_BF16", what);
+  if (!a || !b) EE_FAIL(EE_ERR_INVALID_ARG, "%s: NULL pointer", what);
+  if ((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) & (dtype == EE_BF16 ? 3 : 7))
+    EE_FAIL(EE_ERR_INVALID_ARG, "%s: rows must start on two elements", what);
+  return EE_OK;
+}
+
+int check_quant_heads(const ee_quant_cache* C, int32_t n_heads) {
+  if (n_heads < 1 || n_heads % C->n_kv_heads) EE_FAIL(EE_ERR_SHAPE, "n_heads %d is no multiple of n_kv_heads %d", n_heads, C->n_kv_heads);
+  if (n_heads / C->n_kv_heads > 1024 || n_heads > 65536) EE_FAIL(EE_ERR_UNSUPPORTED, "%d heads over %d K/V heads", n_heads, C->n_kv_heads);
+  return EE_OK;
+}
+
+int check_raw_workspace(void* ws, size_t have, size_t need) {
+  if (need == 0) return EE_OK;
+  if (!ws) EE_FAIL(EE_ERR_WORKSPACE, "workspace is NULL");
+  if (reinterpret_cast<uintptr_t>(ws) & 255) EE_FAIL(EE_ERR_WORKSPACE, "workspace is not 256-byte aligned");
+  if (have < need) EE_FAIL(EE_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", have, need);
+  return EE_OK;
+}
+
+size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+size_t evict_slots(int keep, int max_context) { return (size_t)((keep < max_context ? keep : max_context) + 15) / 16; }
+
+}  // namespace
+
+int ee_rotary_frequencies(const ee_rotary_desc* desc, double* freqs, void* stream) {
+  if (int rc = check_rotary_desc(desc)) return rc;
+  if (!freqs || (reinterpret_cast<uintptr_t>(freqs) & 7)) EE_FAIL(EE_ERR_INVALID_ARG, "ee_rotary_frequencies: NULL or misaligned pointer");
+  launch_rotary_frequencies(*desc, freqs, reinterpret_cast<hipStream_t>(stream));
+  EE_HIP(hipGetLastError());
+  return EE_OK;
+}
+
+int ee_rotary(const ee_rotary_desc* desc, const double* freqs, const int32_t* positions, int32_t rows, int32_t dtype, const ee_rotary_rows* q,
+              const ee_rotary_rows* k, int32_t transpose, void* stream) {
+  int rc;
+  if ((rc = check_rotary_desc(desc))) return rc;
+  if (dtype != EE_FP32 && dtype != EE_BF16) EE_FAIL(EE_ERR_INVALID_ARG, "rotary: dtype must be EE_FP32 or EE_BF16");
+  if (rows < 0) EE_FAIL(EE_ERR_INVALID_ARG, "rotary: %d rows", rows);
+  if (!q && !k) EE_FAIL(EE_ERR_INVALID_ARG, "rotary: neither q nor k");
+  if (transpose != 0 && transpose != 1) EE_FAIL(EE_ERR_INVALID_ARG, "rotary: transpose must be 0 or 1");
+  if (rows == 0) return EE_OK;
+  if (!freqs || !positions || (reinterpret_cast<uintptr_t>(freqs) & 7)) EE_FAIL(EE_ERR_INVALID_ARG, "rotary: NULL or misaligned pointer");
+  RotaryArgs a{freqs, positions, {}, {}, rows, desc->head_dim, desc->rotary_dim, (float)desc->amplitude, transpose ? -1.0f : 1.0f};
+  const int size = dtype == EE_BF16 ? 2 : 4;
+  if ((rc = check_rotary_rows(q, "q", rows, desc->head_dim, size, &a.q)) || (rc = check_rotary_rows(k, "k", rows, desc->head_dim, size, &a.k))) return rc;
+  const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  {
+    ProfScope ps(EE_K_OTHER, 0, st);
+    launch_rotary(a, dtype, desc->layout, st);
+  }
+  EE_HIP(hipGetLastError());
+  return EE_OK;
+}
+
+int ee_kv_quant_append(const ee_quant_cache* cache, int32_t layer, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int32_t dtype,
+                       const ee_batch* batch, void* stream) {
+  int rc;
+  QuantAppendArgs a{};
+  if ((rc = check_quant_call(cache, layer, batch, &a.c, &a.r))) return rc;
+  if (batch->batch == 0) return EE_OK;
+  if ((rc = check_pair_type(dtype, k, v, "ee_kv_quant_append"))) return rc;
+  const int64_t row = (int64_t)cache->n_kv_heads * cache->head_dim, far = INT64_MAX / 16 / batch->batch;
+  if (k_stride < row || v_stride < row || k_stride % 2 || v_stride % 2 || k_stride > far || v_stride > far)
+    EE_FAIL(EE_ERR_SHAPE, "ee_kv_quant_append: strides %lld, %lld for rows of %lld", (long long)k_stride, (long long)v_stride, (long long)row);
+  a.k = k;
+  a.v = v;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  {
+    ProfScope ps(EE_K_KVFILL, layer, st);
+    launch_quant_append(a, dtype, st);
+  }
+  EE_HIP(hipGetLastError());
+  return EE_OK;
+}
+
+int ee_kv_quant_read(const ee_quant_cache* cache, int32_t layer, const ee_batch* batch, void* k, void* v, int32_t dtype, void* stream) {
+  int rc;
+  QuantReadArgs a{};
+  if ((rc = check_quant_call(cache, layer, batch, &a.c, &a.r))) return rc;
+  if (batch->batch == 0) return EE_OK;
+  if ((rc = check_pair_type(dtype, k, v, "ee_kv_quant_read"))) return rc;
+  a.k = k;
+  a.v = v;
+  const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  {
+    ProfScope ps(EE_K_OTHER, layer, st);
+    launch_quant_read(a, dtype, st);
+  }
+  EE_HIP(hipGetLastError());
+  return EE_OK;
+}
+
+size_t ee_paged_attention_quant_bytes(const ee_quant_cache* cache, int32_t n_heads, int32_t max_batch, int32_t max_context, int32_t with_weights) {
+  if (check_quant_cache(cache) || check_quant_heads(cache, n_heads)) return 0;
+  if (max_batch < 1 || max_context < 1 || max_context > kAttnMaxBlocks * 16) {
+    set_error("ee_paged_attention_quant_bytes: batch %d, context %d", max_batch, max_context);
+    return 0;
+  }
+  const QuantCache c{nullptr, nullptr, nullptr, 0, cache->n_kv_heads, cache->head_dim, cache->format};
+  const size_t parts = align256(quant_attn_part_floats(c, n_heads, max_batch, max_context, with_weights != 0) * sizeof(float));
+  return parts + (with_weights ? align256((size_t)max_batch * n_heads * quant_score_pitch(max_context) * sizeof(float)) : 0);
+}
+
+int ee_paged_attention_quant(const ee_quant_cache* cache, int32_t layer, int32_t n_heads, const float* q, const ee_batch* batch, float* out,
+                             const float* weights_in, float* weights_out, int32_t weights_pitch, void* workspace, size_t workspace_bytes,
+                             void* stream) {
+  int rc;
+  QuantAttnArgs a{};
+  if ((rc = check_quant_call(cache, layer, batch, &a.c, &a.r)) || (rc = check_quant_heads(cache, n_heads))) return rc;
+  if (batch->batch == 0) return EE_OK;
+  if (!q || !out || ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 15))
+    EE_FAIL(EE_ERR_INVALID_ARG, "ee_paged_attention_quant: q and out must start on 16 bytes");
+  if (weights_in && !weights_out) EE_FAIL(EE_ERR_INVALID_ARG, "ee_paged_attention_quant: weights_in without weights_out");
+  if (weights_out && batch->row_table) EE_FAIL(EE_ERR_UNSUPPORTED, "ee_paged_attention_quant: weights with row_table");
+  if (weights_out && weights_pitch < batch->max_context)
+    EE_FAIL(EE_ERR_SHAPE, "ee_paged_attention_quant: weights_pitch %d below max_context %d", weights_pitch, batch->max_context);
+  a.n_heads = n_heads;
+  a.max_context = batch->max_context;
+  a.q = q;
+  a.out = out;
+  a.weights_in = weights_in;
+  a.weights_out = weights_out;
+  a.weights_pitch = weights_pitch;
+  if ((int64_t)batch->batch * ((n_heads + 15) / 16) > 65535)   // (the launch's second dimension)
+    EE_FAIL(EE_ERR_UNSUPPORTED, "ee_paged_attention_quant: %d rows of %d heads in one call", batch->batch, n_heads);
+  quant_attn_plan(a);
+  const size_t columns = (size_t)batch->batch * n_heads;
+  const size_t part_bytes = weights_out || a.n_parts > 1 ? align256(columns * a.n_parts * (cache->head_dim + 4) * sizeof(float)) : 0;
+  const size_t score_bytes = weights_out ? align256(columns * quant_score_pitch(a.max_context) * sizeof(float)) : 0;
+  if ((rc = check_raw_workspace(workspace, workspace_bytes, part_bytes + score_bytes))) return rc;
+  if (part_bytes) a.parts = reinterpret_cast<float*>(workspace);
+  if (score_bytes) a.scores = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + part_bytes);
+  const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  {
+    ProfScope ps(EE_K_ATTN, layer, st);
+    launch_quant_attention(a, st);
+  }
+  EE_HIP(hipGetLastError());
+  return EE_OK;
+}
+
+size_t ee_kv_quant_evict_bytes(const ee_quant_cache* cache, int32_t max_batch, int32_t keep) {
+  if (check_quant_cache(cache)) return 0;
+  if (max_batch < 1 || keep < 1 || keep > kAttnMaxBlocks * 16) {
+    set_error("ee_kv_quant_evict_bytes: batch %d, keep %d", max_batch, keep);
+    return 0;
+  }
+  const size_t units = (size_t)max_batch * cache->n_kv_heads * evict_slots(keep, keep) * 2;
+  return align256(units * 16 * cache->head_dim) + align256(units * sizeof(float));
+}
+
+int ee_kv_quant_evict(const ee_quant_cache* cache, int32_t layer, const ee_batch* batch, const int32_t* dst_tables, int32_t dst_max_blocks,
+                      const float* weights_in, int32_t weights_pitch, float* weights_out, int32_t weights_out_pitch, int32_t keep, int32_t recent,
+                      int32_t* kept, int32_t* out_lens, void* workspace, size_t workspace_bytes, void* stream) {
+  int rc;
+  QuantEvictArgs a{};
+  if ((rc = check_quant_call(cache, layer, batch, &a.c, &a.r))) return rc;
+  if (keep < 1 || recent < 0 || recent > keep) EE_FAIL(EE_ERR_INVALID_ARG, "ee_kv_quant_evict: keep %d, recent %d", keep, recent);
+  if (batch->batch == 0) return EE_OK;
+  if (batch->row_table) EE_FAIL(EE_ERR_INVALID_ARG, "ee_kv_quant_evict takes no row_table");
+  if (!weights_in || !kept || !out_lens) EE_FAIL(EE_ERR_INVALID_ARG, "ee_kv_quant_evict: NULL pointer");
+  if (batch->batch > 65535) EE_FAIL(EE_ERR_UNSUPPORTED, "ee_kv_quant_evict: %d sequences in one call", batch->batch);
+  if (weights_pitch < batch->max_context || (weights_out && weights_out_pitch < keep))
+    EE_FAIL(EE_ERR_SHAPE, "ee_kv_quant_evict: pitches %d, %d for contexts of %d, %d kept", weights_pitch, weights_out_pitch, batch->max_context, keep);
+  if (weights_out == weights_in && weights_out_pitch != weights_pitch) EE_FAIL(EE_ERR_SHAPE, "ee_kv_quant_evict: weights in place with two pitches");
+  const size_t slots = evict_slots(keep, batch->max_context);
+  if (dst_tables && (dst_max_blocks < 0 || (size_t)dst_max_blocks < slots))
+    EE_FAIL(EE_ERR_SHAPE, "ee_kv_quant_evict: dst_max_blocks %d below %zu", dst_max_blocks, slots);
+  const size_t units = (size_t)batch->batch * cache->n_kv_heads * slots * 2, image_bytes = align256(units * 16 * cache->head_dim);
+  if (!dst_tables && (rc = check_raw_workspace(workspace, workspace_bytes, image_bytes + align256(units * sizeof(float))))) return rc;
+  a.dst_tables = dst_tables;
+  a.dst_max_blocks = dst_max_blocks;
+  a.weights_in = weights_in;
+  a.weights_out = weights_out;
+  a.pitch_in = weights_pitch;
+  a.pitch_out = weights_out_pitch;
+  a.max_context = batch->max_context;
+  a.keep = keep;
+  a.recent = recent;
+  a.kept = kept;
+  a.out_lens = out_lens;
+  if (!dst_tables) {
+    a.images = reinterpret_cast<int8_t*>(workspace);
+    a.image_scales = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + image_bytes);
+  }
+  const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  {
+    ProfScope ps(EE_K_OTHER, layer, st);
+    launch_quant_evict(a, st);
+  }
   EE_HIP(hipGetLastError());
   return EE_OK;
 }

@@ -1,0 +1,109 @@
+// Shared declarations of the 8-bit cache and of the rotary embedding on its own (rotary.hip, quant_cache.hip,
+// quant_attention.hip): launch interfaces, and what a byte of the cache stands for.
+#pragma once
+
+#include "ee_common.h"
+
+namespace ee {
+
+typedef _Float16 half_t;
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef bf16_t bf16x2 __attribute__((ext_vector_type(2)));
+
+constexpr float kQuantScaleFloor = 1.17549435e-38f;   // 2^-126: a block of zeros; its reciprocal is finite
+constexpr int kQuantMaxHeadDim = 256;
+
+// rotary.hip
+struct RotaryRows {
+  const void* in;
+  void* out;
+  int64_t in_stride, out_stride;   // elements
+  int n_heads;
+};
+struct RotaryArgs {
+  const double* freqs;
+  const int32_t* positions;
+  RotaryRows q, k;   // n_heads == 0: none
+  int rows, head_dim, rotary_dim;
+  float amplitude;
+  float sign;        // +1, or -1 for the transposed rotation
+};
+void launch_rotary_frequencies(const ee_rotary_desc& d, double* freqs, hipStream_t st);
+void launch_rotary(const RotaryArgs& a, int dtype, int layout, hipStream_t st);
+
+// One layer of an 8-bit cache.
+struct QuantCache {
+  int8_t* k;       // [num_blocks][heads][16][dh]
+  int8_t* v;       // [num_blocks][heads][dh][16]
+  float* scales;   // [num_blocks][heads][2]
+  int num_blocks, heads, dh, format;
+};
+// Rows of a call and where their positions live.
+struct QuantRows {
+  const int32_t* context_lens;
+  const int32_t* block_tables;
+  const int32_t* row_table;   // nullptr: row m is sequence m
+  int rows, max_blocks;
+};
+
+// quant_cache.hip
+struct QuantAppendArgs {
+  QuantCache c;
+  QuantRows r;
+  const void *k, *v;
+  int64_t k_stride, v_stride;
+};
+void launch_quant_append(const QuantAppendArgs& a, int dtype, hipStream_t st);
+struct QuantReadArgs {
+  QuantCache c;
+  QuantRows r;
+  void *k, *v;
+};
+void launch_quant_read(const QuantReadArgs& a, int dtype, hipStream_t st);
+struct QuantEvictArgs {
+  QuantCache c;
+  QuantRows r;
+  const int32_t* dst_tables;   // nullptr: in place, by way of `images`
+  int dst_max_blocks;
+  const float* weights_in;
+  float* weights_out;
+  int pitch_in, pitch_out;
+  int max_context, keep, recent;
+  int32_t* kept;
+  int32_t* out_lens;
+  int8_t* images;              // [B][heads][blocks of keep][2][16 * dh]
+  float* image_scales;         // [B][heads][blocks of keep][2]
+};
+void launch_quant_evict(const QuantEvictArgs& a, hipStream_t st);
+
+// quant_attention.hip
+struct QuantAttnArgs {
+  QuantCache c;
+  QuantRows r;
+  int n_heads, max_context;
+  const float* q;
+  float* out;
+  const float* weights_in;
+  float* weights_out;          // nullptr: none
+  int weights_pitch;
+  float* parts;                // [rows][n_heads][n_parts][dh + 4]: running maximum, sum, -, -, unnormalised result of a part
+  float* scores;               // [rows][n_heads][quant_score_pitch(max_context)], in units of log 2
+  int tiles;                   // 16-column tiles of a workgroup
+  int n_parts, part_steps;     // parts of a context, and 64-position steps of a part
+};
+__host__ __device__ inline size_t quant_score_pitch(int max_context) { return (size_t)((max_context + 63) / 64) * 64; }
+// How a call is split (sets tiles, n_parts, part_steps), and the floats of `parts` that calls of up to so many rows and positions take.
+void quant_attn_plan(QuantAttnArgs& a);
+size_t quant_attn_part_floats(const QuantCache& c, int n_heads, int max_rows, int max_context, bool weights);
+void launch_quant_attention(const QuantAttnArgs& a, hipStream_t st);
+
+#ifdef __HIPCC__
+__device__ inline int quant_seq(const QuantRows& r, int m) { return r.row_table ? safe_row(r.row_table[m], r.rows) : m; }
+#endif
+
+}  // namespace ee
