@@ -2,6 +2,8 @@
 // quant_attention.hip): launch interfaces, and what a byte of the cache stands for.
 #pragma once
 
+#include <type_traits>
+
 #include "ee_common.h"
 
 namespace ee {
@@ -93,16 +95,29 @@ struct QuantAttnArgs {
   int weights_pitch;
   float* parts;                // [rows][n_heads][n_parts][dh + 4]: running maximum, sum, -, -, unnormalised result of a part
   float* scores;               // [rows][n_heads][quant_score_pitch(max_context)], in units of log 2
-  int tiles;                   // 16-column tiles of a workgroup
   int n_parts, part_steps;     // parts of a context, and 64-position steps of a part
 };
 __host__ __device__ inline size_t quant_score_pitch(int max_context) { return (size_t)((max_context + 63) / 64) * 64; }
-// How a call is split (sets tiles, n_parts, part_steps), and the floats of `parts` that calls of up to so many rows and positions take.
+// How a call is split (sets n_parts, part_steps), and the floats of `parts` that calls of up to so many rows and positions take.
 void quant_attn_plan(QuantAttnArgs& a);
 size_t quant_attn_part_floats(const QuantCache& c, int n_heads, int max_rows, int max_context, bool weights);
 void launch_quant_attention(const QuantAttnArgs& a, hipStream_t st);
 
 #ifdef __HIPCC__
+// The maximum of a wavefront's 64 values (of magnitudes' bits, which are ordered like integers), on the cross-lane network.
+__device__ inline uint32_t wave_max(uint32_t v) {
+  auto with = [&](auto ctrl, auto rows) { v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, decltype(rows)::value, 0xf, false)); };
+  with(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});   // row_shr 1, 2, 4, 8: lane 15 of each 16 has theirs
+  with(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
+  with(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+  with(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+  with(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // row_bcast 15, 31: lane 63 has all
+  with(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
+  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+__device__ inline int lane_value(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+__device__ inline float lane_value(float v, int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane)); }
+
 __device__ inline int quant_seq(const QuantRows& r, int m) { return r.row_table ? safe_row(r.row_table[m], r.rows) : m; }
 #endif
 

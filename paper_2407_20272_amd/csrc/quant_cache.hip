@@ -55,36 +55,35 @@ __device__ inline uint32_t quantise_pair(f32x2 x, float s, float inv) {
   }
 }
 
-__device__ inline uint32_t wave_max(uint32_t v) {
-#pragma unroll
-  for (int x = 1; x < 64; x <<= 1) v = max(v, (uint32_t)__shfl_xor((int)v, x));
-  return v;
-}
 // The larger of two scales; NaN if either is.
 __device__ inline float scale_max(float a, float b) { return a != a || b != b ? __builtin_nanf("") : fmaxf(a, b); }
 
-// The run of rows a wavefront has: rows m .. m + n - 1 are consecutive positions of one block, `off` the first one's place in it.  n = 0: row m is not the
-// first of its run (the wavefront of that one has it), or is skipped.
+// Rows that go into (or come from) one block are taken together: a run is rows at consecutive positions of one block.  A workgroup has kGroup
+// rows (where every row is a sequence of its own, two) of one head and takes the runs that begin among them; wavefronts 0 and 2 K's, 1 and 3 V's.
+constexpr int kGroup = 8, kApart = 2;
 struct Run {
-  int n, off, seq, logical;
+  int m, n, off, seq, logical;   // first row, rows, the first one's place in its block
 };
-__device__ inline Run run_of(const QuantRows& r, int m) {
-  const int lane = threadIdx.x & 63;
-  const int at = m - 1 + lane;                       // lane 0: the row in front
-  const bool there = lane <= 16 && at >= 0 && at < r.rows;
-  const int pos = there ? r.context_lens[at] : -1;
-  const int seq = there ? quant_seq(r, at) : -1;
-  const int pos0 = __shfl(pos, 1), seq0 = __shfl(seq, 1);
-  // lane i stands for position pos0 + i - 1 if row m - 1 + i goes on with the run
-  const bool goes = there && seq == seq0 && pos >= 0 && pos == pos0 + lane - 1 && (pos >> 4) == (pos0 >> 4);
-  const uint64_t on = __ballot(goes);
-  Run run{0, pos0 & 15, seq0, pos0 >> 4};
-  if (pos0 >= 0 && !(on & 1)) {
-    const uint64_t stop = ~(on >> 1);
-    run.n = __ffsll((unsigned long long)stop) - 1;   // (lanes from 17 on never go)
+struct Runs {
+  int base, pos, seq;            // lane i stands for row base - 1 + i
+  uint64_t goes_on, first;       // the lanes whose row goes on with the run of the row in front; that begin a run of this workgroup
+
+  __device__ Runs(const QuantRows& r, int base_, int group) : base(base_) {
+    const int lane = threadIdx.x & 63, at = base - 1 + lane;
+    const bool there = lane <= group + 15 && at >= 0 && at < r.rows;
+    pos = there ? r.context_lens[at] : -1;
+    seq = there ? quant_seq(r, at) : -1;
+    const int pos_before = __shfl_up(pos, 1), seq_before = __shfl_up(seq, 1);
+    const bool on = lane > 0 && pos > 0 && pos_before == pos - 1 && seq_before == seq && (pos & 15) != 0;
+    goes_on = __ballot(on);
+    first = __ballot(lane > 0 && lane <= group && pos >= 0 && !on);
   }
-  return run;
-}
+  __device__ Run of(int lane) const {
+    const uint64_t stop = ~(goes_on >> (lane + 1));            // (lanes behind group + 15 never go on)
+    const int p = lane_value(pos, lane);
+    return Run{base - 1 + lane, __ffsll((unsigned long long)stop), p & 15, lane_value(seq, lane), p >> 4};
+  }
+};
 
 template <class T>
 __device__ inline f32x2 load_pair(const T* p);
@@ -99,19 +98,13 @@ __device__ inline f32x2 load_pair<bf16_t>(const bf16_t* p) {
 __device__ inline uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu; }
 
 template <int FMT, class T, int CP>
-__global__ __launch_bounds__(kThreads) void quant_append_kernel(QuantAppendArgs a) {
+__device__ inline void append_run(const QuantAppendArgs& a, const Run& run, int head, int which) {
   const int lane = threadIdx.x & 63;
-  const int task = blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-  const int per_row = 2 * a.c.heads;
-  const int m = task / per_row;
-  if (m >= a.r.rows) return;
-  const int which = (task - m * per_row) & 1, head = (task - m * per_row) >> 1;
-  const Run run = run_of(a.r, m);
-  if (run.n == 0 || run.logical >= a.r.max_blocks) return;
+  if (run.logical >= a.r.max_blocks) return;
   const int blk = a.r.block_tables[(size_t)run.seq * a.r.max_blocks + run.logical];
   if ((unsigned)blk >= (unsigned)a.c.num_blocks) return;
   const int dh = a.c.dh;
-  const T* src = reinterpret_cast<const T*>(which ? a.v : a.k) + (size_t)m * (which ? a.v_stride : a.k_stride) + (size_t)head * dh;
+  const T* src = reinterpret_cast<const T*>(which ? a.v : a.k) + (size_t)run.m * (which ? a.v_stride : a.k_stride) + (size_t)head * dh;
   const int64_t stride = which ? a.v_stride : a.k_stride;
   const size_t unit = (size_t)blk * a.c.heads + head;
   float* sp = a.c.scales + unit * 2 + which;
@@ -185,6 +178,15 @@ __global__ __launch_bounds__(kThreads) void quant_append_kernel(QuantAppendArgs 
   }
 }
 
+template <int FMT, class T, int CP>
+__global__ __launch_bounds__(kThreads) void quant_append_kernel(QuantAppendArgs a, int group) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Runs runs(a.r, blockIdx.x * group, group);
+  int i = 0;
+  for (uint64_t left = runs.first; left; left &= left - 1, ++i)
+    if ((i & 1) == (wave >> 1)) append_run<FMT, T, CP>(a, runs.of(__ffsll((unsigned long long)left) - 1), blockIdx.y, wave & 1);
+}
+
 template <class T>
 __device__ inline void store_pair(T* p, f32x2 x);
 template <>
@@ -193,24 +195,11 @@ template <>
 __device__ inline void store_pair<bf16_t>(bf16_t* p, f32x2 x) { *reinterpret_cast<bf16x2*>(p) = bf16x2{(bf16_t)x[0], (bf16_t)x[1]}; }
 
 template <int FMT, class T, int CP>
-__global__ __launch_bounds__(kThreads) void quant_read_kernel(QuantReadArgs a) {
+__device__ inline void read_run(const QuantReadArgs& a, const Run& run, int head, int which) {
   const int lane = threadIdx.x & 63;
-  const int task = blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-  const int per_row = 2 * a.c.heads;
-  const int m = task / per_row;
-  if (m >= a.r.rows) return;
-  const int which = (task - m * per_row) & 1, head = (task - m * per_row) >> 1;
   const int dh = a.c.dh;
-  Run run = run_of(a.r, m);
-  T* dst = reinterpret_cast<T*>(which ? a.v : a.k) + ((size_t)m * a.c.heads + head) * dh;
+  T* dst = reinterpret_cast<T*>(which ? a.v : a.k) + ((size_t)run.m * a.c.heads + head) * dh;
   const size_t stride = (size_t)a.c.heads * dh;
-  if (run.n == 0) {
-    if (a.r.context_lens[m] < 0)
-#pragma unroll
-      for (int i = 0; i < CP; ++i)
-        if (2 * lane + 128 * i < dh) store_pair<T>(dst + 2 * lane + 128 * i, f32x2{0.0f, 0.0f});
-    return;
-  }
   const int logical = min(run.logical, a.r.max_blocks - 1);
   const int blk = safe_block(a.r.block_tables[(size_t)run.seq * a.r.max_blocks + logical], a.c.num_blocks);
   const size_t unit = (size_t)blk * a.c.heads + head;
@@ -241,6 +230,21 @@ __global__ __launch_bounds__(kThreads) void quant_read_kernel(QuantReadArgs a) {
           store_pair<T>(dst + (t - run.off) * stride + c, f32x2{q[0] * s, q[1] * s});
         }
     }
+  }
+}
+
+template <int FMT, class T, int CP>
+__global__ __launch_bounds__(kThreads) void quant_read_kernel(QuantReadArgs a, int group) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Runs runs(a.r, blockIdx.x * group, group);
+  int i = 0;
+  for (uint64_t left = runs.first; left; left &= left - 1, ++i)
+    if ((i & 1) == (wave >> 1)) read_run<FMT, T, CP>(a, runs.of(__ffsll((unsigned long long)left) - 1), blockIdx.y, wave & 1);
+  // rows that read nothing
+  for (uint64_t left = __ballot(lane > 0 && lane <= group && runs.base - 1 + lane < a.r.rows && runs.pos < 0); left; left &= left - 1) {
+    const size_t m = runs.base + __ffsll((unsigned long long)left) - 2;
+    T* dst = reinterpret_cast<T*>(wave & 1 ? a.v : a.k) + (m * a.c.heads + blockIdx.y) * a.c.dh;
+    for (int c = 2 * lane; c < a.c.dh && wave < 2; c += 128) store_pair<T>(dst + c, f32x2{0.0f, 0.0f});
   }
 }
 
@@ -369,7 +373,7 @@ __global__ __launch_bounds__(kThreads) void quant_build_kernel(QuantEvictArgs a,
   float need = kQuantScaleFloor;
 #pragma unroll
   for (int t = 0; t < 16; ++t) {
-    const int pt = __shfl(pos, t), bt = __shfl(blk, t);
+    const int pt = lane_value(pos, t), bt = lane_value(blk, t);
     const int8_t* p = (which ? a.c.v : a.c.k) + ((size_t)max(bt, 0) * a.c.heads + head) * 16 * dh;
 #pragma unroll
     for (int i = 0; i < CP; ++i) {
@@ -388,7 +392,7 @@ __global__ __launch_bounds__(kThreads) void quant_build_kernel(QuantEvictArgs a,
   }
 #pragma unroll
   for (int t = 0; t < 16; ++t) {
-    const float wt = __shfl(was, t);
+    const float wt = lane_value(was, t);
     uint32_t most = 0;
 #pragma unroll
     for (int i = 0; i < CP; ++i) {
@@ -398,7 +402,7 @@ __global__ __launch_bounds__(kThreads) void quant_build_kernel(QuantEvictArgs a,
     const float top = __builtin_bit_cast(float, wave_max(most));
     float nt = scale_for<FMT>(top * wt);
     if (FMT == EE_QUANT_INT8 && top >= 127.0f) nt = wt;
-    if (__shfl(pos, t) >= 0) need = scale_max(need, nt);
+    if (lane_value(pos, t) >= 0) need = scale_max(need, nt);
   }
   const float s = need, inv = 1.0f / s;
   int8_t* out;
@@ -461,11 +465,12 @@ int groups(int64_t tasks) { return (int)((tasks + kThreads / 64 - 1) / (kThreads
 
 template <int FMT, class T>
 static void append_as(const QuantAppendArgs& a, hipStream_t st) {
-  const int g = groups((int64_t)a.r.rows * a.c.heads * 2);
+  const int group = a.r.row_table ? kGroup : kApart;
+  const dim3 grid((a.r.rows + group - 1) / group, a.c.heads);
   if (a.c.dh <= 128)
-    quant_append_kernel<FMT, T, 1><<<g, kThreads, 0, st>>>(a);
+    quant_append_kernel<FMT, T, 1><<<grid, kThreads, 0, st>>>(a, group);
   else
-    quant_append_kernel<FMT, T, 2><<<g, kThreads, 0, st>>>(a);
+    quant_append_kernel<FMT, T, 2><<<grid, kThreads, 0, st>>>(a, group);
 }
 void launch_quant_append(const QuantAppendArgs& a, int dtype, hipStream_t st) {
   if (a.c.format == EE_QUANT_INT8)
@@ -476,11 +481,12 @@ void launch_quant_append(const QuantAppendArgs& a, int dtype, hipStream_t st) {
 
 template <int FMT, class T>
 static void read_as(const QuantReadArgs& a, hipStream_t st) {
-  const int g = groups((int64_t)a.r.rows * a.c.heads * 2);
+  const int group = a.r.row_table ? kGroup : kApart;
+  const dim3 grid((a.r.rows + group - 1) / group, a.c.heads);
   if (a.c.dh <= 128)
-    quant_read_kernel<FMT, T, 1><<<g, kThreads, 0, st>>>(a);
+    quant_read_kernel<FMT, T, 1><<<grid, kThreads, 0, st>>>(a, group);
   else
-    quant_read_kernel<FMT, T, 2><<<g, kThreads, 0, st>>>(a);
+    quant_read_kernel<FMT, T, 2><<<grid, kThreads, 0, st>>>(a, group);
 }
 void launch_quant_read(const QuantReadArgs& a, int dtype, hipStream_t st) {
   if (a.c.format == EE_QUANT_INT8)
