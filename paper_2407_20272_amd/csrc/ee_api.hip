@@ -1163,7 +1163,8 @@ size_t ee_paged_attention_quant_bytes(const ee_quant_cache* cache, int32_t n_hea
   }
   const QuantCache c{nullptr, nullptr, nullptr, 0, cache->n_kv_heads, cache->head_dim, cache->format};
   const size_t parts = align256(quant_attn_part_floats(c, n_heads, max_batch, max_context, with_weights != 0) * sizeof(float));
-  return parts + (with_weights ? align256((size_t)max_batch * n_heads * quant_score_pitch(max_context) * sizeof(float)) : 0);
+  // (only with parts: the spans of dealt-out rows)
+  return parts + (parts ? align256(kQuantMostSpans * sizeof(int2)) : 0) + (with_weights ? align256((size_t)max_batch * n_heads * quant_score_pitch(max_context) * sizeof(float)) : 0);
 }
 
 int ee_paged_attention_quant(const ee_quant_cache* cache, int32_t layer, int32_t n_heads, const float* q, const ee_batch* batch, float* out,
@@ -1188,13 +1189,14 @@ int ee_paged_attention_quant(const ee_quant_cache* cache, int32_t layer, int32_t
   a.weights_pitch = weights_pitch;
   if ((int64_t)batch->batch * ((n_heads + 15) / 16) > 65535)   // (the launch's second dimension)
     EE_FAIL(EE_ERR_UNSUPPORTED, "ee_paged_attention_quant: %d rows of %d heads in one call", batch->batch, n_heads);
-  quant_attn_plan(a);
-  const size_t columns = (size_t)batch->batch * n_heads;
-  const size_t part_bytes = weights_out || a.n_parts > 1 ? align256(columns * a.n_parts * (cache->head_dim + 4) * sizeof(float)) : 0;
-  const size_t score_bytes = weights_out ? align256(columns * quant_score_pitch(a.max_context) * sizeof(float)) : 0;
-  if ((rc = check_raw_workspace(workspace, workspace_bytes, part_bytes + score_bytes))) return rc;
-  if (part_bytes) a.parts = reinterpret_cast<float*>(workspace);
-  if (score_bytes) a.scores = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + part_bytes);
+  size_t spans;
+  const size_t part_bytes = align256(quant_attn_plan(a, &spans) * sizeof(float)), span_bytes = align256(spans * sizeof(int2));
+  const size_t score_bytes = weights_out ? align256((size_t)batch->batch * n_heads * quant_score_pitch(a.max_context) * sizeof(float)) : 0;
+  if ((rc = check_raw_workspace(workspace, workspace_bytes, part_bytes + span_bytes + score_bytes))) return rc;
+  char* ws = reinterpret_cast<char*>(workspace);
+  if (part_bytes) a.parts = reinterpret_cast<float*>(ws);
+  if (span_bytes) a.spans = reinterpret_cast<int2*>(ws + part_bytes);
+  if (score_bytes) a.scores = reinterpret_cast<float*>(ws + part_bytes + span_bytes);
   const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   {
     ProfScope ps(EE_K_ATTN, layer, st);

@@ -93,14 +93,21 @@ struct QuantAttnArgs {
   const float* weights_in;
   float* weights_out;          // nullptr: none
   int weights_pitch;
-  float* parts;                // [rows][n_heads][n_parts][dh + 4]: running maximum, sum, -, -, unnormalised result of a part
-  float* scores;               // [rows][n_heads][quant_score_pitch(max_context)], in units of log 2
-  int n_parts, part_steps;     // parts of a context, and 64-position steps of a part
+  // A context's parts leave records of head_dim + 4 floats: running maximum, sum, -, -, unnormalised result.
+  //   row_table: [rows][n_heads][n_parts], n_parts > 1;   else [kv heads][slots][columns of a tile] (see quant_attn_plan).
+  float* parts;                // nullptr: none
+  int2* spans;                 // dealt: [rows * tiles] first workgroup and number of workgroups that have a unit's steps
+  float* scores;               // weights: [rows][n_heads][quant_score_pitch(max_context)], in units of log 2
+  int n_parts, part_steps;     // row_table: parts of a context, and 64-position steps of a part
+  int dealt;                   // else: 0, or workgroups of a K/V head that all rows' steps are dealt out to
+  int slots;
 };
 __host__ __device__ inline size_t quant_score_pitch(int max_context) { return (size_t)((max_context + 63) / 64) * 64; }
-// How a call is split (sets n_parts, part_steps), and the floats of `parts` that calls of up to so many rows and positions take.
-void quant_attn_plan(QuantAttnArgs& a);
+// How a call's work is divided (sets n_parts, part_steps, dealt, slots), and the floats of `parts` that it needs, and entries of `spans`; the former for
+// all calls of up to so many rows and positions.
+size_t quant_attn_plan(QuantAttnArgs& a, size_t* spans);
 size_t quant_attn_part_floats(const QuantCache& c, int n_heads, int max_rows, int max_context, bool weights);
+constexpr int kQuantMostSpans = 1024;
 void launch_quant_attention(const QuantAttnArgs& a, hipStream_t st);
 
 #ifdef __HIPCC__

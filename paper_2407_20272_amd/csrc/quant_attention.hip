@@ -1,7 +1,7 @@
 // Attention over the 8-bit cache, on the matrix cores.
 //
-// A workgroup has up to 16 * NT columns, (row, query head) pairs that read the same K/V head: the grouped heads of one row, or of a run of
-// prompt rows.  A wavefront takes 64 positions (four blocks T_0..T_3) a step and multiplies
+// A workgroup has up to 16 or 32 columns, (row, query head) pairs that read the same K/V head: the grouped heads of one row, or of prompt rows.
+// A wavefront takes 64 positions (four blocks T_0..T_3) a step and multiplies
 //   S = K Q^T:  16 positions x 32 channels x 16 columns an instruction, the positions of instruction i being 4i..4i+3 of each block, so that
 //               lane (column n, group g) ends up with the scores of all 16 positions of block T_g;
 //   O += V^T P: 16 channels x 32 positions x 16 columns, contracted over positions 8h..8h+7 of each block: lane (n, g) has those
@@ -9,16 +9,17 @@
 // No value crosses lanes but the running maxima, and every load is 16 bytes a lane.  Bytes become fp16 without error.  q (scaled by a power of two
 // to 2^13..2^14) and the probabilities (times the block's scale, relative to the largest scale so far) are split into an fp16 head and
 // remainder, 22 bits together: the products are float in effect, as in the float cache's attention.
-// Softmax statistics and results are float, running over a wavefront's steps; the four wavefronts and the parts of a long context are
-// joined in a fixed order.
+// Softmax statistics and results are float, running over a wavefront's steps; the four wavefronts, and the parts of a context that
+// several workgroups have, are joined in a fixed order.
 #include "quant.h"
 
 namespace ee {
 
 namespace {
 
-constexpr int kWaves = 4;
-constexpr int kMinPart = 4, kMaxPart = 256;   // 64-position steps of a part of a context: one a wavefront, and what the tables in LDS hold
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kTableSteps = 256;     // steps whose block ids and scales are in LDS at a time
+constexpr int kDealtRows = kQuantMostSpans;   // rows (tiles of them) whose steps are dealt out evenly, at most: every workgroup adds up their lengths
 constexpr float kLog2e = 1.4426950408889634f;
 
 // Eight bytes -> eight fp16.
@@ -45,6 +46,12 @@ __device__ inline half8_t widen(uint32_t a, uint32_t b) {
 
 __device__ inline f32x4 mma(half8_t a, half8_t b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
+// Two floats as an fp16 head and remainder.
+__device__ inline void split(f32x2 x, half2_t& hi, half2_t& lo) {
+  hi = __builtin_convertvector(x, half2_t);
+  lo = __builtin_convertvector(f32x2{x[0] - (float)hi[0], x[1] - (float)hi[1]}, half2_t);
+}
+
 // The maximum over the four lanes that share a column.
 __device__ inline float max_over_groups(float v) {
   v = fmaxf(v, __shfl_xor(v, 16));
@@ -59,441 +66,589 @@ __device__ inline u32x4 load16(const int8_t* p) {
     return *reinterpret_cast<const u32x4*>(p);
 }
 
-// The last position row m attends: -1 for none.
-__device__ inline int last_position(const QuantAttnArgs& a, int m) {
-  return max(-1, min(a.r.context_lens[m], min(a.max_context, a.r.max_blocks * 16) - 1));
+// The last position that a row with this context length attends: -1 for none.
+__device__ inline int last_position(const QuantAttnArgs& a, int context_len) {
+  return max(-1, min(context_len, min(a.max_context, a.r.max_blocks * 16) - 1));
+}
+__device__ inline int steps_to(int last) { return (last >> 6) + 1; }   // (-1: 0)
+
+// Rows without row_table are cut into tiles of up to 16 of a K/V head's query heads ("units": row * tiles + tile).
+__host__ __device__ inline int unit_tiles(int group) { return (group + 15) / 16; }
+__host__ __device__ inline int unit_columns(int group) { return group < 16 ? group : 16; }
+
+// The steps of all units behind each other, dealt out to `a.dealt` workgroups a K/V head: start[u] = steps of the units in front of u, and
+// workgroup w has steps bound(w) .. bound(w + 1) - 1.
+struct Deal {
+  int total, workgroups;
+  __device__ int bound(int w) const { return (int)((int64_t)w * total / workgroups); }
+  __device__ int owner(int step) const { return (int)((((int64_t)step + 1) * workgroups + total - 1) / total) - 1; }
+};
+__device__ inline Deal deal_out(const QuantAttnArgs& a, int tiles, int* start /* LDS [kDealtRows + 1] */, int* scratch /* LDS [kWaves] */) {
+  const int units = a.r.rows * tiles, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int n[4], sum = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int u = 4 * tid + e;
+    n[e] = u < units ? steps_to(last_position(a, a.r.context_lens[u / tiles])) : 0;
+    sum += n[e];
+  }
+  int upto = sum;
+#pragma unroll
+  for (int x = 1; x < 64; x <<= 1) {
+    const int o = __shfl_up(upto, x);
+    if (lane >= x) upto += o;
+  }
+  if (lane == 63) scratch[wave] = upto;
+  __syncthreads();
+  int before = upto - sum, total = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) before += scratch[w];
+    total += scratch[w];
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (4 * tid + e <= units) start[4 * tid + e] = before;
+    before += n[e];
+  }
+  if (tid == kThreads - 1 && units == kDealtRows) start[units] = before;
+  __syncthreads();
+  // (a workgroup has a step a wavefront at least)
+  return Deal{__builtin_amdgcn_readfirstlane(total), __builtin_amdgcn_readfirstlane(max(1, min(a.dealt, total / kWaves)))};
 }
 
 // DH: the head's channels, or 0 for a.c.dh; NL: loads of 16 bytes a lane and position (64 channels each).  SHARED: rows that may share a sequence,
-// 32 columns; else the grouped heads of one row, 16 columns.
+// 32 columns; else units, 16 columns.
 constexpr int quant_tiles(bool shared) { return shared ? 2 : 1; }
 template <int FMT, int DH, int NL, bool SHARED, bool WEIGHTS>
-__global__ __launch_bounds__(64 * kWaves, NL * quant_tiles(SHARED) <= 2 ? 2 : 1) void quant_attn_kernel(QuantAttnArgs a) {
+__global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(QuantAttnArgs a) {
   constexpr int NT = quant_tiles(SHARED), C = 16 * NT, CT = 4 * NL;
-  constexpr bool QREG = NT == 1;        // q's fragments in registers, or in LDS
+  constexpr bool QREG = !SHARED;        // q's fragments in registers, or in LDS
   __shared__ half8_t q_lds[QREG ? 1 : NT * NL * 2 * 2 * 64];
   __shared__ float stat[2][kWaves][C];
   __shared__ f32x4 meet[kWaves][4][NT][64];
-  __shared__ int block_id[kMaxPart * 4];         // the part's blocks, and their scales of K and V
-  __shared__ f32x2 block_scale[kMaxPart * 4];
-  const int lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int dh = DH ? DH : a.c.dh, G = a.n_heads / a.c.heads, hk = blockIdx.x, part = blockIdx.z;
-  int f0, f1;
-  if constexpr (SHARED) {
-    f0 = blockIdx.y * C;
-    f1 = min(f0 + C, a.r.rows * G);
-  } else {
-    const int per_row = (G + C - 1) / C, m = blockIdx.y / per_row;
-    f0 = m * G + (blockIdx.y - m * per_row) * C;
-    f1 = min(f0 + C, (m + 1) * G);
-  }
-  // The tile's rows, one a lane.  What a wavefront needs before its first bytes (positions, block ids, q) is asked for at once: the ids of a
-  // row of its own without waiting for its length (entries behind it may be anything, see block_of).
-  const int r0 = f0 / G, n_rows = (f1 - 1) / G - r0 + 1;
-  const int m_lane = r0 + min(lane, n_rows - 1);
-  const int ctx = a.r.context_lens[m_lane];
-  const int first = part * a.part_steps, last_entry = a.r.max_blocks - 1;
-  int own_block = 0;
-  if constexpr (!SHARED) own_block = a.r.block_tables[(size_t)r0 * a.r.max_blocks + min(first * 4 + (int)threadIdx.x, last_entry)];
-  f32x4 qx[NT][2 * NL][2];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int f = min(f0 + nt * 16 + col, f1 - 1), m = f / G;
-    const float* q = a.q + ((size_t)m * a.n_heads + hk * G + (f - m * G)) * dh;
-#pragma unroll
-    for (int k = 0; k < 2 * NL; ++k) {
-      const int c = (k >> 1) * 64 + g * 16 + (k & 1) * 8;
-#pragma unroll
-      for (int e = 0; e < 2; ++e) qx[nt][k][e] = *reinterpret_cast<const f32x4*>(q + (c < dh ? c : 0) + 4 * e);
-    }
-  }
-  const int row_seq = quant_seq(a.r, m_lane), row_pos = max(-1, min(ctx, min(a.max_context, a.r.max_blocks * 16) - 1));
-  if (part > 0 && !__any((row_pos >> 6) >= part * a.part_steps)) return;
-
-  // q, split; the factor that turns a product back into a score in units of log 2
-  half8_t qf[QREG ? 2 * NL : 1][2];
-  float to_score[NT], m_run[NT], l_run[NT];
-  int col_row[NT], col_pos[NT];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int f = f0 + nt * 16 + col;
-    const bool valid = f < f1;
-    col_row[nt] = (valid ? f / G : r0) - r0;
-    col_pos[nt] = __shfl(row_pos, col_row[nt]);
-    if (!valid) col_pos[nt] = -1;
-    float most = 0.0f;
-#pragma unroll
-    for (int k = 0; k < 2 * NL; ++k)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        if (!valid || (k >> 1) * 64 + g * 16 >= dh) qx[nt][k][e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) most = fmaxf(most, fabsf(qx[nt][k][e][j]));
-      }
-    most = max_over_groups(most);
-    int ex = 14;
-    if (most < INFINITY && most > 0.0f) (void)frexpf(most, &ex);
-    ex = max(ex, -100);
-    const float up = ldexpf(1.0f, 14 - ex);
-    to_score[nt] = ldexpf(1.0f, ex - 14) * (kLog2e / sqrtf((float)dh));
-    m_run[nt] = -INFINITY;
-    l_run[nt] = 0.0f;
-#pragma unroll
-    for (int k = 0; k < 2 * NL; ++k) {
-      half8_t hi, lo;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float y = qx[nt][k][j >> 2][j & 3] * up;
-        hi[j] = (half_t)y;
-        lo[j] = (half_t)(y - (float)hi[j]);
-      }
-      if constexpr (QREG) {
-        qf[k][0] = hi;
-        qf[k][1] = lo;
-      } else if (wave == nt) {
-        q_lds[((nt * 2 * NL + k) * 2 + 0) * 64 + lane] = hi;
-        q_lds[((nt * 2 * NL + k) * 2 + 1) * 64 + lane] = lo;
-      }
-    }
-  }
-  if constexpr (!QREG) __syncthreads();
-
-  f32x4 o[CT][NT];
-#pragma unroll
-  for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) o[ct][nt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  float v_ref = 0.0f, v_up = 0.0f;      // the power of two that is at least every scale of V so far; 2^14 / v_ref
-
+  __shared__ int block_id[kTableSteps * 4];      // blocks of the steps at hand, and their scales of K and V
+  __shared__ f32x2 block_scale[kTableSteps * 4];
+  __shared__ int start[SHARED ? 1 : kDealtRows + 1], scratch[kWaves];
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int dh = DH ? DH : a.c.dh, G = a.n_heads / a.c.heads, hk = blockIdx.x, last_entry = a.r.max_blocks - 1;
+  const int tiles = SHARED ? 1 : unit_tiles(G);
   const size_t block_bytes = (size_t)16 * dh, block_pitch = block_bytes * a.c.heads;
   const int8_t* k_base = a.c.k + hk * block_bytes;
   const int8_t* v_base = a.c.v + hk * block_bytes;
 
-  // the scores' rows of the tile's columns
-  const size_t score_pitch = quant_score_pitch(a.max_context) * sizeof(float);
-  const auto score_rows = __builtin_amdgcn_make_buffer_rsrc(
-      reinterpret_cast<char*>(a.scores) + ((size_t)r0 * a.n_heads + hk * G + (f0 - r0 * G)) * score_pitch, 0, (int)((f1 - f0) * score_pitch), 0x00020000);
-  const uint32_t score_at = f0 + col < f1 ? (uint32_t)(col * score_pitch) : 0x80000000u;
-
-  // runs of rows that share a sequence, one after the other
-  for (int r = 0; r < n_rows;) {
-    int seq = r0, longest = __builtin_amdgcn_readfirstlane(row_pos);
-    int limit[NT];
-    if constexpr (!SHARED) {
-      r = n_rows;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) limit[nt] = col_pos[nt];
+  int unit = blockIdx.y, at = 0, stop = 0, early = 0;
+  Deal deal{};
+  const bool dealt = !SHARED && a.dealt;
+  if (dealt) {
+    deal = deal_out(a, tiles, start, scratch);
+    if ((int)blockIdx.y >= deal.workgroups || deal.total == 0) return;
+    if (blockIdx.x == 0 && blockIdx.y == 0)      // for the launch that joins the parts
+      for (int u = tid; u < a.r.rows * tiles; u += kThreads) {
+        const int first = start[u + 1] > start[u] ? deal.owner(start[u]) : 0;
+        a.spans[u] = make_int2(first, start[u + 1] > start[u] ? deal.owner(start[u + 1] - 1) - first + 1 : 0);
+      }
+    at = deal.bound(blockIdx.y);
+    stop = deal.bound(blockIdx.y + 1);
+    int lower = 0;                               // the unit that step `at` belongs to: units that end in front of it
+    for (int u = tid; u < a.r.rows * tiles; u += kThreads) lower += start[u + 1] <= at;
+    for (int x = 1; x < 64; x <<= 1) lower += __shfl_xor(lower, x);
+    if (lane == 0) scratch[wave] = lower;
+    __syncthreads();
+    unit = __builtin_amdgcn_readfirstlane(scratch[0] + scratch[1] + scratch[2] + scratch[3]);
+  } else if (!SHARED) {
+    // block ids are asked for beside the row's length (entries behind it may be anything, see below)
+    early = a.r.block_tables[(size_t)(unit / tiles) * a.r.max_blocks + min(tid, last_entry)];
+  }
+  do {
+    // ---- a piece: columns f0 .. f1 - 1, steps s0 .. s1 - 1 ----
+    int f0, f1, s0 = 0, s1 = 0, unit_steps = 0;
+    if constexpr (SHARED) {
+      f0 = blockIdx.y * C;
+      f1 = min(f0 + C, a.r.rows * G);
+      s0 = blockIdx.z * a.part_steps;
     } else {
-      seq = __shfl(row_seq, r);
-      const uint64_t other = ~__ballot(row_seq == seq && lane < n_rows) >> r;
-      const int r_end = min(n_rows, r + (other ? __ffsll((unsigned long long)other) - 1 : 64));
-      longest = lane >= r && lane < r_end ? row_pos : -1;
-#pragma unroll
-      for (int x = 1; x < 64; x <<= 1) longest = max(longest, __shfl_xor(longest, x));
-      longest = __builtin_amdgcn_readfirstlane(longest);
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) limit[nt] = col_row[nt] >= r && col_row[nt] < r_end ? col_pos[nt] : -1;
-      r = r_end;
+      const int m = unit / tiles;
+      f0 = m * G + (unit - m * tiles) * C;
+      f1 = min(f0 + C, (m + 1) * G);
     }
-    const int steps = min(a.part_steps, (longest >> 6) + 1 - first);      // (longest = -1: none)
-    if (steps <= 0) continue;
-
-    // The part's block ids, then their scales, go to LDS: a step's loads from memory are then its bytes alone.  (Loads return in the order they were
-    // asked for: waiting for an id behind a step's bytes would be waiting for the bytes.)
-    // Blocks behind the sequence's last one may be any of the pool's: none of their positions passes a limit, their scales and V's bytes are
-    // replaced by zeros.
-    const int32_t* table = a.r.block_tables + (size_t)seq * a.r.max_blocks + first * 4;
-    if constexpr (SHARED) __syncthreads();     // (the run in front has been read)
-    for (int i = threadIdx.x; i < steps * 4; i += 64 * kWaves) {
-      if (SHARED || i >= 64 * kWaves) own_block = table[min(i, last_entry - first * 4)];
-      block_id[i] = safe_block(own_block, a.c.num_blocks);
-    }
-    __syncthreads();
-    auto scales_of = [&](int i) {
-      const f32x2 sc = *reinterpret_cast<const f32x2*>(a.c.scales + ((size_t)block_id[min(i, steps * 4 - 1)] * a.c.heads + hk) * 2);
-      return (first * 4 + i) * 16 > longest ? f32x2{0.0f, 0.0f} : sc;
-    };
-    const f32x2 own_scale = scales_of(threadIdx.x);
-    u32x4 kr[4][NL], vr[CT];
-    // (channels and channel tiles from dh on are read as the first ones: the former meet zeros of q, the latter's results are dropped.  Every
-    // load is made, behind the last step from one place, so that what is in flight is known when the program is compiled.)
-    auto load_k = [&](int blk, bool there) {
-      const int8_t* p = there ? k_base + (size_t)blk * block_pitch + (col & 3) * dh : k_base;
+    const int r0 = f0 / G, n_rows = (f1 - 1) / G - r0 + 1;
+    const int m_lane = r0 + min(lane, n_rows - 1);   // the piece's rows, one a lane
+    const int ctx = a.r.context_lens[m_lane];
+    f32x4 qx[NT][2 * NL][2];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+    for (int nt = 0; nt < NT; ++nt) {
+      const int f = min(f0 + nt * 16 + col, f1 - 1), m = f / G;
+      const float* q = a.q + ((size_t)m * a.n_heads + hk * G + (f - m * G)) * dh;
 #pragma unroll
-        for (int l = 0; l < NL; ++l) {
-          const int c = l * 64 + g * 16;
-          kr[i][l] = load16<!SHARED>(p + 4 * i * dh + (DH || c < dh ? c : 0));
-        }
-    };
-    auto load_v = [&](int blk, bool there) {
-      const int8_t* p = there ? v_base + (size_t)blk * block_pitch + col * 16 : v_base;
+      for (int k = 0; k < 2 * NL; ++k) {
+        const int c = (k >> 1) * 64 + g * 16 + (k & 1) * 8;
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) vr[ct] = load16<!SHARED>(p + (DH || ct * 16 < dh ? ct * 256 : 0));
-    };
-
-    load_k(block_id[min(wave, steps - 1) * 4 + (col >> 2)], wave < steps);
-    load_v(block_id[min(wave, steps - 1) * 4 + g], wave < steps);
-    if ((int)threadIdx.x < steps * 4) block_scale[threadIdx.x] = own_scale;
-    for (int i = threadIdx.x + 64 * kWaves; i < steps * 4; i += 64 * kWaves) block_scale[i] = scales_of(i);
-    __syncthreads();
-    // results are kept relative to the largest scale of V so far
-    float most_v = 0.0f;
-    for (int i = lane; i < steps * 4; i += 64) most_v = fmaxf(most_v, block_scale[i][1]);
-    most_v = __builtin_bit_cast(float, wave_max(__builtin_bit_cast(uint32_t, most_v)));
-    if (most_v > v_ref) {
-      int e;
-      (void)frexpf(most_v, &e);
-      const float next = ldexpf(1.0f, max(-100, min(e, 127)));
-      const float f = v_ref / next;
-      v_ref = next;
-      v_up = 16384.0f / next;
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) o[ct][nt] *= f;
-    }
-    // a step asks for the next one's bytes as soon as its own have been used
-    for (int s = wave; s < steps; s += kWaves) {
-      const bool more = s + kWaves < steps;
-      const int ahead = min(s + kWaves, steps - 1) * 4;
-      const int pos0 = ((first + s) * 4 + g) * 16;
-      const f32x2 sc = block_scale[s * 4 + g];
-      const int k_blk = block_id[ahead + (col >> 2)], v_blk = block_id[ahead + g];
-      // S = K Q^T
-      f32x4 sd[NT][4];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sd[nt][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int l = 0; l < NL; ++l)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          half8_t kh[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) kh[i] = widen<FMT>(kr[i][l][2 * h], kr[i][l][2 * h + 1]);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              half8_t qv;
-              if constexpr (QREG)
-                qv = qf[2 * l + h][e];
-              else
-                qv = q_lds[((nt * 2 * NL + 2 * l + h) * 2 + e) * 64 + lane];
-#pragma unroll
-              for (int i = 0; i < 4; ++i) sd[nt][i] = mma(kh[i], qv, sd[nt][i]);
-            }
-          __builtin_amdgcn_sched_barrier(0);   // (else every byte is widened first, and there are not as many registers)
-        }
-      load_k(k_blk, more);
-      __builtin_amdgcn_sched_barrier(0);
-      const float v_factor = sc[1] * v_up;
-      half8_t ph[NT][2], pl[NT][2];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const float f = sc[0] * to_score[nt];
-        float mx = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float t = pos0 + 4 * i + e <= limit[nt] ? sd[nt][i][e] * f : -INFINITY;
-            sd[nt][i][e] = t;
-            mx = fmaxf(mx, t);
-          }
-        if constexpr (WEIGHTS) {   // lanes of no column are out of the buffer's range: their stores are dropped, and every store is made
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, sd[nt][i]), score_rows, score_at + (uint32_t)(pos0 + 4 * i) * 4, 0, 0);
-        }
-        const float m_new = fmaxf(m_run[nt], max_over_groups(mx));
-        const float base = m_new == -INFINITY ? 0.0f : m_new;
-        const float alpha = __builtin_amdgcn_exp2f(m_run[nt] - base);
-        if (__any(m_new != m_run[nt])) {
-#pragma unroll
-          for (int ct = 0; ct < CT; ++ct) o[ct][nt] *= alpha;
-        }
-        m_run[nt] = m_new;
-        float sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float p = __builtin_amdgcn_exp2f(sd[nt][i][e] - base);
-            sum += p;
-            const float w = p == 0.0f ? 0.0f : p * v_factor;   // (a masked position's scale may be anything)
-            const half_t hi = (half_t)w;
-            ph[nt][i >> 1][(i & 1) * 4 + e] = hi;
-            pl[nt][i >> 1][(i & 1) * 4 + e] = (half_t)(w - (float)hi);
-          }
-        l_run[nt] = l_run[nt] * alpha + sum;
+        for (int e = 0; e < 2; ++e) qx[nt][k][e] = *reinterpret_cast<const f32x4*>(q + (c < dh ? c : 0) + 4 * e);
       }
-      __builtin_amdgcn_sched_barrier(0);
-      // O += V^T P
-      if constexpr (FMT == EE_QUANT_E4M3) {
-        if ((first + s) * 64 + 63 > longest) {    // bytes that hold no position may be NaN, which zero weights do not cover
-#pragma unroll
-          for (int wd = 0; wd < 4; ++wd) {
-            const int n = longest + 1 - pos0 - 4 * wd;
-            const uint32_t keep = n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << (8 * n)) - 1;
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) vr[ct][wd] &= keep;
-          }
-        }
+    }
+    const int row_seq = quant_seq(a.r, m_lane), row_pos = last_position(a, ctx);
+    if constexpr (SHARED) {
+      if (blockIdx.z > 0 && !__any((row_pos >> 6) >= s0)) return;
+    } else {
+      unit_steps = __builtin_amdgcn_readfirstlane(steps_to(row_pos));
+      s1 = unit_steps;
+      if (dealt) {
+        const int begin = __builtin_amdgcn_readfirstlane(start[unit]);
+        unit_steps = __builtin_amdgcn_readfirstlane(start[unit + 1]) - begin;
+        s0 = at - begin;
+        s1 = min(stop - begin, unit_steps);
+        at = begin + s1;
       }
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const half8_t vh = widen<FMT>(vr[ct][2 * h], vr[ct][2 * h + 1]);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            o[ct][nt] = mma(vh, ph[nt][h], o[ct][nt]);
-            o[ct][nt] = mma(vh, pl[nt][h], o[ct][nt]);
-          }
-          if (h == 1 && (ct & 1)) __builtin_amdgcn_sched_barrier(0);
-        }
-      load_v(v_blk, more);
     }
-  }
 
-  // the wavefronts' results, joined in their order
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    l_run[nt] += __shfl_xor(l_run[nt], 16);
-    l_run[nt] += __shfl_xor(l_run[nt], 32);
-    if (g == 0) {
-      stat[0][wave][nt * 16 + col] = m_run[nt];
-      stat[1][wave][nt * 16 + col] = l_run[nt];
-    }
-  }
-  __syncthreads();
-  float m_all[NT], l_all[NT];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    float mm = -INFINITY, ll = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, stat[0][w][nt * 16 + col]);
-    const float base = mm == -INFINITY ? 0.0f : mm;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) ll += stat[1][w][nt * 16 + col] * __builtin_amdgcn_exp2f(stat[0][w][nt * 16 + col] - base);
-    m_all[nt] = mm;
-    l_all[nt] = ll;
-    const float f = __builtin_amdgcn_exp2f(m_run[nt] - base) * v_ref * (1.0f / 16384.0f);
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) o[ct][nt] *= f;
-  }
-  const bool direct = a.parts == nullptr;
-#pragma unroll
-  for (int c0 = 0; c0 < CT; c0 += 4) {
-    if (c0) __syncthreads();
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) meet[wave][c][nt][lane] = o[c0 + c][nt];
-    __syncthreads();
-    const int ch = (c0 + wave) * 16 + g * 4;
+    // q, split; the factor that turns a product back into a score in units of log 2
+    half8_t qf[QREG ? 2 * NL : 1][2];
+    float to_score[NT], m_run[NT], l_run[NT];
+    int col_row[NT], col_pos[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int f = f0 + nt * 16 + col;
-      f32x4 sum = meet[0][wave][nt][lane];
+      const bool valid = f < f1;
+      col_row[nt] = (valid ? f / G : r0) - r0;
+      col_pos[nt] = __shfl(row_pos, col_row[nt]);
+      if (!valid) col_pos[nt] = -1;
+      float most = 0.0f;
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) sum += meet[w][wave][nt][lane];
-      if (f >= f1 || ch >= dh) continue;
-      const int m = f / G;
-      const size_t at = (size_t)m * a.n_heads + hk * G + (f - m * G);
-      if (direct) {
-        const float inv = l_all[nt] == 0.0f ? 0.0f : 1.0f / l_all[nt];
-        *reinterpret_cast<f32x4*>(a.out + at * dh + ch) = sum * inv;
-      } else {
-        float* p = a.parts + (at * a.n_parts + part) * (dh + 4);
-        if (ch == 0) *reinterpret_cast<f32x2*>(p) = f32x2{m_all[nt], l_all[nt]};
-        *reinterpret_cast<f32x4*>(p + 4 + ch) = sum;
+      for (int k = 0; k < 2 * NL; ++k)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          if (!valid || (k >> 1) * 64 + g * 16 >= dh) qx[nt][k][e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) most = fmaxf(most, fabsf(qx[nt][k][e][j]));
+        }
+      most = max_over_groups(most);
+      int ex = 14;
+      if (most < INFINITY && most > 0.0f) (void)frexpf(most, &ex);
+      ex = max(ex, -100);
+      const float up = ldexpf(1.0f, 14 - ex);
+      to_score[nt] = ldexpf(1.0f, ex - 14) * (kLog2e / sqrtf((float)dh));
+      m_run[nt] = -INFINITY;
+      l_run[nt] = 0.0f;
+#pragma unroll
+      for (int k = 0; k < 2 * NL; ++k) {
+        half8_t hi, lo;
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+          half2_t h, l;
+          split(f32x2{qx[nt][k][j >> 2][j & 3] * up, qx[nt][k][j >> 2][(j & 3) + 1] * up}, h, l);
+          hi[j] = h[0], hi[j + 1] = h[1];
+          lo[j] = l[0], lo[j + 1] = l[1];
+        }
+        if constexpr (QREG) {
+          qf[k][0] = hi;
+          qf[k][1] = lo;
+        } else if (wave == nt) {
+          q_lds[((nt * 2 * NL + k) * 2 + 0) * 64 + lane] = hi;
+          q_lds[((nt * 2 * NL + k) * 2 + 1) * 64 + lane] = lo;
+        }
       }
     }
-  }
+    if constexpr (!QREG) __syncthreads();
+
+    f32x4 o[CT][NT];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) o[ct][nt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    float v_ref = 0.0f, v_up = 0.0f;      // the power of two that is at least every scale of V so far; 2^14 / v_ref
+
+    // The scores' rows of the piece's columns.  A wavefront collects 16 rows of 64 in LDS before it stores them: stores are counted in line with loads,
+    // and one in every step holds up the bytes behind it.
+    const size_t score_pitch = quant_score_pitch(a.max_context) * sizeof(float);
+    const auto score_rows = __builtin_amdgcn_make_buffer_rsrc(
+        reinterpret_cast<char*>(a.scores) + ((size_t)r0 * a.n_heads + hk * G + (f0 - r0 * G)) * score_pitch, 0, (int)((f1 - f0) * score_pitch), 0x00020000);
+    f32x4* const collected = meet[wave][0][0];
+    const int held_most = max(1, 16 / (f1 - f0));   // steps
+    int held = 0;
+
+    // runs of rows that share a sequence, one after the other
+    for (int r = 0; r < n_rows;) {
+      int seq = r0, longest = __builtin_amdgcn_readfirstlane(row_pos), shortest = longest;
+      int limit[NT];
+      if constexpr (!SHARED) {
+        r = n_rows;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) limit[nt] = col_pos[nt];
+      } else {
+        seq = lane_value(row_seq, r);
+        const uint64_t other = ~__ballot(row_seq == seq && lane < n_rows) >> r;
+        const int r_end = min(n_rows, r + (other ? __ffsll((unsigned long long)other) - 1 : 64));
+        longest = (int)wave_max((uint32_t)((lane >= r && lane < r_end ? row_pos : -1) + 1)) - 1;
+        // (columns of other runs have no position in this one)
+        shortest = r_end - r < n_rows ? -1 : -(int)wave_max((uint32_t)(lane < n_rows ? 0x40000000 - row_pos : 0)) + 0x40000000;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) limit[nt] = col_row[nt] >= r && col_row[nt] < r_end ? col_pos[nt] : -1;
+        r = r_end;
+        s1 = min(s0 + a.part_steps, steps_to(longest));
+      }
+      const int32_t* table = a.r.block_tables + (size_t)seq * a.r.max_blocks;
+      for (int c0 = s0; c0 < s1; c0 += kTableSteps) {
+        // Block ids, then their scales, go to LDS: a step's loads from memory are then its bytes alone.  (Loads return in the order they were
+        // asked for: waiting for an id behind a step's bytes would be waiting for the bytes.)
+        // Blocks behind the sequence's last one may be any of the pool's: none of their positions passes a limit; they get scales of 1
+        // and 0.
+        const int steps = min(kTableSteps, s1 - c0);
+        if (SHARED || dealt || c0 > s0) __syncthreads();   // (the tables in front have been read)
+        for (int i = tid; i < steps * 4; i += kThreads) {
+          const int blk = SHARED || dealt || c0 > 0 || i >= kThreads ? table[min(c0 * 4 + i, last_entry)] : early;
+          block_id[i] = safe_block(blk, a.c.num_blocks);
+        }
+        __syncthreads();
+        auto scales_of = [&](int i) {
+          const f32x2 sc = *reinterpret_cast<const f32x2*>(a.c.scales + ((size_t)block_id[min(i, steps * 4 - 1)] * a.c.heads + hk) * 2);
+          return (c0 * 4 + i) * 16 > longest ? f32x2{1.0f, 0.0f} : sc;
+        };
+        const f32x2 own_scale = scales_of(tid);
+        u32x4 kr[4][NL], vr[CT];
+        // (channels and channel tiles from dh on are read as the first ones: the former meet zeros of q, the latter's results are dropped.
+        // Every load is made, behind the last step from one place, so that what is in flight is known when the program is compiled.)
+        auto load_k = [&](int blk, bool there) {
+          const int8_t* p = there ? k_base + (size_t)blk * block_pitch + (col & 3) * dh : k_base;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int l = 0; l < NL; ++l) {
+              const int c = l * 64 + g * 16;
+              kr[i][l] = load16<!SHARED>(p + 4 * i * dh + (DH || c < dh ? c : 0));
+            }
+        };
+        auto load_v = [&](int blk, bool there) {
+          const int8_t* p = there ? v_base + (size_t)blk * block_pitch + col * 16 : v_base;
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) vr[ct] = load16<!SHARED>(p + (DH || ct * 16 < dh ? ct * 256 : 0));
+        };
+        load_k(block_id[min(wave, steps - 1) * 4 + (col >> 2)], wave < steps);
+        load_v(block_id[min(wave, steps - 1) * 4 + g], wave < steps);
+        if (tid < steps * 4) block_scale[tid] = own_scale;
+        for (int i = tid + kThreads; i < steps * 4; i += kThreads) block_scale[i] = scales_of(i);
+        __syncthreads();
+        // results are kept relative to the largest scale of V so far
+        float most_v = 0.0f;
+        for (int i = lane; i < steps * 4; i += 64) most_v = fmaxf(most_v, block_scale[i][1]);
+        most_v = __builtin_bit_cast(float, wave_max(__builtin_bit_cast(uint32_t, most_v)));
+        if (most_v > v_ref) {
+          int e;
+          (void)frexpf(most_v, &e);
+          const float next = ldexpf(1.0f, max(-100, min(e, 127)));
+          const float f = v_ref / next;
+          v_ref = next;
+          v_up = 16384.0f / next;
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) o[ct][nt] *= f;
+        }
+        // a step asks for the next one's bytes as soon as its own have been used
+        for (int s = wave; s < steps; s += kWaves) {
+          const bool more = s + kWaves < steps;
+          const int ahead = min(s + kWaves, steps - 1) * 4;
+          const int pos0 = ((c0 + s) * 4 + g) * 16;
+          const f32x2 sc = block_scale[s * 4 + g];
+          const int k_blk = block_id[ahead + (col >> 2)], v_blk = block_id[ahead + g];
+          // S = K Q^T
+          f32x4 sd[NT][4];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sd[nt][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int l = 0; l < NL; ++l)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              half8_t kh[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) kh[i] = widen<FMT>(kr[i][l][2 * h], kr[i][l][2 * h + 1]);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                  half8_t qv;
+                  if constexpr (QREG)
+                    qv = qf[2 * l + h][e];
+                  else
+                    qv = q_lds[((nt * 2 * NL + 2 * l + h) * 2 + e) * 64 + lane];
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) sd[nt][i] = mma(kh[i], qv, sd[nt][i]);
+                }
+              __builtin_amdgcn_sched_barrier(0);   // (else every byte is widened first, and there are not as many registers)
+            }
+          load_k(k_blk, more);
+          __builtin_amdgcn_sched_barrier(0);
+          const bool ragged = (c0 + s) * 64 + 63 > shortest;   // some positions are behind some column's last one
+          half8_t ph[NT][2], pl[NT][2];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            // scales are positive: the largest product gives the largest score.  A block without a position for a column has
+            // none of its scales in the column's result.
+            float f = sc[0] * to_score[nt], v_factor = sc[1] * v_up;
+            if (ragged) {
+              if (pos0 > limit[nt]) f = 1.0f, v_factor = 0.0f;
+              if (f == 0.0f) f = kQuantScaleFloor;   // (times minus infinity)
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  if (pos0 + 4 * i + e > limit[nt]) sd[nt][i][e] = -INFINITY;
+            }
+            float mx = sd[nt][0][0];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) mx = fmaxf(mx, sd[nt][i][e]);
+            if constexpr (WEIGHTS) {
+              if (f0 + col < f1) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) collected[(held * (f1 - f0) + col) * 16 + ((g * 4 + i) ^ col)] = sd[nt][i] * f;
+              }
+            }
+            const float m_new = fmaxf(m_run[nt], max_over_groups(mx * f));
+            const float base = m_new == -INFINITY ? 0.0f : m_new;
+            const float alpha = __builtin_amdgcn_exp2f(m_run[nt] - base);
+            if (__any(m_new != m_run[nt])) {
+#pragma unroll
+              for (int ct = 0; ct < CT; ++ct) o[ct][nt] *= alpha;
+            }
+            m_run[nt] = m_new;
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; e += 2) {
+                const float p0 = __builtin_amdgcn_exp2f(fmaf(sd[nt][i][e], f, -base)), p1 = __builtin_amdgcn_exp2f(fmaf(sd[nt][i][e + 1], f, -base));
+                sum += p0;
+                sum += p1;
+                half2_t hi, lo;
+                split(f32x2{p0 * v_factor, p1 * v_factor}, hi, lo);
+                ph[nt][i >> 1][(i & 1) * 4 + e] = hi[0], ph[nt][i >> 1][(i & 1) * 4 + e + 1] = hi[1];
+                pl[nt][i >> 1][(i & 1) * 4 + e] = lo[0], pl[nt][i >> 1][(i & 1) * 4 + e + 1] = lo[1];
+              }
+            l_run[nt] = l_run[nt] * alpha + sum;
+          }
+          __builtin_amdgcn_sched_barrier(0);
+          // O += V^T P
+          if constexpr (FMT == EE_QUANT_E4M3) {
+            if ((c0 + s) * 64 + 63 > longest) {    // bytes that hold no position may be NaN, which zero weights do not cover
+#pragma unroll
+              for (int wd = 0; wd < 4; ++wd) {
+                const int n = longest + 1 - pos0 - 4 * wd;
+                const uint32_t keep = n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << (8 * n)) - 1;
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) vr[ct][wd] &= keep;
+              }
+            }
+          }
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const half8_t vh = widen<FMT>(vr[ct][2 * h], vr[ct][2 * h + 1]);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                o[ct][nt] = mma(vh, ph[nt][h], o[ct][nt]);
+                o[ct][nt] = mma(vh, pl[nt][h], o[ct][nt]);
+              }
+              if (h == 1 && (ct & 1)) __builtin_amdgcn_sched_barrier(0);
+            }
+          load_v(v_blk, more);
+          if constexpr (WEIGHTS) {
+            if (++held == held_most || !more) {
+              const int columns = f1 - f0;
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const int row = 4 * j + g, step = row / columns, c = row - step * columns;   // (rows behind the last are out of the buffer's range)
+                const uint32_t to = (uint32_t)(c * score_pitch) + (uint32_t)((c0 + s - (held - 1 - step) * kWaves) * 64 + 4 * col) * 4;
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, collected[row * 16 + (col ^ c)]), score_rows,
+                                                       row < held * columns ? to : 0x80000000u, 0, 0);
+              }
+              held = 0;
+            }
+          }
+        }
+      }
+    }
+
+    // ---- the wavefronts' results, joined in their order ----
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      l_run[nt] += __shfl_xor(l_run[nt], 16);
+      l_run[nt] += __shfl_xor(l_run[nt], 32);
+      if (g == 0) {
+        stat[0][wave][nt * 16 + col] = m_run[nt];
+        stat[1][wave][nt * 16 + col] = l_run[nt];
+      }
+    }
+    __syncthreads();
+    float m_all[NT], l_all[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      float mm = -INFINITY, ll = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, stat[0][w][nt * 16 + col]);
+      const float base = mm == -INFINITY ? 0.0f : mm;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) ll += stat[1][w][nt * 16 + col] * __builtin_amdgcn_exp2f(stat[0][w][nt * 16 + col] - base);
+      m_all[nt] = mm;
+      l_all[nt] = ll;
+      const float f = __builtin_amdgcn_exp2f(m_run[nt] - base) * v_ref * (1.0f / 16384.0f);
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) o[ct][nt] *= f;
+    }
+    const bool whole = SHARED ? a.parts == nullptr : s0 == 0 && s1 == unit_steps;
+    const bool leaves_part = SHARED ? !whole : !whole || WEIGHTS;
+#pragma unroll
+    for (int c0 = 0; c0 < CT; c0 += 4) {
+      if (c0) __syncthreads();
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) meet[wave][c][nt][lane] = o[c0 + c][nt];
+      __syncthreads();
+      const int ch = (c0 + wave) * 16 + g * 4;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const int f = f0 + nt * 16 + col;
+        f32x4 sum = meet[0][wave][nt][lane];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) sum += meet[w][wave][nt][lane];
+        if (f >= f1 || ch >= dh) continue;
+        const int m = f / G;
+        const size_t row = (size_t)m * a.n_heads + hk * G + (f - m * G);
+        if (whole) {
+          const float inv = l_all[nt] == 0.0f ? 0.0f : 1.0f / l_all[nt];
+          *reinterpret_cast<f32x4*>(a.out + row * dh + ch) = sum * inv;
+        }
+        if (leaves_part) {
+          const size_t slot = SHARED ? row * a.n_parts + blockIdx.z
+                                     : ((size_t)hk * a.slots + unit + (dealt ? blockIdx.y : 0)) * unit_columns(G) + col;
+          float* p = a.parts + slot * (dh + 4);
+          if (ch == 0) *reinterpret_cast<f32x2*>(p) = f32x2{m_all[nt], l_all[nt]};
+          if (!whole) *reinterpret_cast<f32x4*>(p + 4 + ch) = sum;
+        }
+      }
+    }
+    if (!dealt) break;
+    do ++unit;
+    while (at < stop && __builtin_amdgcn_readfirstlane(start[unit + 1]) <= at);
+  } while (at < stop);
 }
 
-// The parts of a context joined in their order, a (row, head) a workgroup: a lane has the statistics of a part, each wavefront adds every fourth
-// part's result, the four sums meet in LDS.  In workgroups behind those: the attention every position got, four positions a thread.
-constexpr int kWeightPositions = 1024;
-__global__ __launch_bounds__(256) void quant_join_kernel(QuantAttnArgs a) {
+// The parts of contexts joined in their order, a (row, head) a workgroup: each wavefront adds every fourth part's result, the four sums meet in
+// LDS.  In workgroups behind those: the attention every position got, twice four positions a thread.
+constexpr int kWeightPositions = 8 * kThreads, kMostParts = 512;
+template <bool SHARED>
+__global__ __launch_bounds__(kThreads) void quant_join_kernel(QuantAttnArgs a) {
   extern __shared__ f32x2 head_stat[];   // [G] maximum, 1 / sum
   __shared__ f32x4 meet[kWaves][64];
+  __shared__ float factors[kMostParts];
   const int m = blockIdx.y, G = a.n_heads / a.c.heads, dh = a.c.dh, tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int last = last_position(a, m);
-  const int n = last < 0 ? 0 : (last >> 6) / a.part_steps + 1;
-  const size_t pitch = dh + 4;
-  // the factor of each lane's part, relative to the maximum over the parts, and the sum of all of them
-  auto factor = [&](int head, float* base, float* sum) {
-    const float* p = a.parts + (((size_t)m * a.n_heads + head) * a.n_parts + min(lane, a.n_parts - 1)) * pitch;
-    const f32x2 stat = *reinterpret_cast<const f32x2*>(p);
-    float mm = lane < n ? stat[0] : -INFINITY;
+  const int tiles = SHARED ? 1 : unit_tiles(G);
+  const int last = last_position(a, a.r.context_lens[m]);
+  const int joined = SHARED || a.dealt ? a.n_heads : 0;
+  const bool joins = (int)blockIdx.x < joined;
+  const int chunks = (a.max_context + kWeightPositions - 1) / kWeightPositions;
+  const int job = blockIdx.x - joined, j0 = joins ? 0 : (job % chunks) * kWeightPositions;
+  if (!joins && j0 > last) return;
+  // a head's parts: n records, `pitch` floats apart
+  const size_t pitch = (size_t)(dh + 4) * (SHARED ? 1 : unit_columns(G));
+  auto parts_of = [&](int head, int* n) {
+    if constexpr (SHARED) {
+      *n = last < 0 ? 0 : (last >> 6) / a.part_steps + 1;
+      return a.parts + ((size_t)m * a.n_heads + head) * a.n_parts * pitch;
+    } else {
+      const int hk = head / G, h = head - hk * G, u = m * tiles + h / 16;
+      const int2 span = a.dealt ? a.spans[u] : make_int2(0, last >= 0);
+      const int slot = u + span.x;
+      *n = span.y;
+      return a.parts + (((size_t)hk * a.slots + slot) * unit_columns(G) + h % 16) * (dh + 4);
+    }
+  };
+  // maximum and sum over a head's parts, and the parts' factors relative to the maximum
+  auto statistics = [&](const float* p, int n, bool keep) {
+    float mm = -INFINITY, sum = 0.0f;
+    for (int z = lane; z < n; z += 64) mm = fmaxf(mm, p[z * pitch]);
 #pragma unroll
     for (int x = 1; x < 64; x <<= 1) mm = fmaxf(mm, __shfl_xor(mm, x));
-    *base = mm == -INFINITY ? 0.0f : mm;
-    const float f = lane < n ? __builtin_amdgcn_exp2f(stat[0] - *base) : 0.0f;
-    float s = lane < n ? stat[1] * f : 0.0f;
+    const float base = mm == -INFINITY ? 0.0f : mm;
+    for (int z = lane; z < n; z += 64) {
+      const f32x2 st = *reinterpret_cast<const f32x2*>(p + z * pitch);
+      const float f = __builtin_amdgcn_exp2f(st[0] - base);
+      sum += st[1] * f;
+      if (keep) factors[z] = f;
+    }
 #pragma unroll
-    for (int x = 1; x < 64; x <<= 1) s += __shfl_xor(s, x);
-    *sum = s;
-    return f;
+    for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x);
+    return f32x2{base, sum};
   };
-  if ((int)blockIdx.x < a.n_heads) {
+  if (joins) {
     const int head = blockIdx.x, c = min(lane * 4, dh - 4);
-    const float* p = a.parts + ((size_t)m * a.n_heads + head) * a.n_parts * pitch + 4 + c;
-    float base, sum;
-    const float f = factor(head, &base, &sum);
+    int n;
+    const float* p = parts_of(head, &n);
+    float* out = a.out + ((size_t)m * a.n_heads + head) * dh;
+    if (n == 0 && wave == 0 && lane * 4 < dh) *reinterpret_cast<f32x4*>(out + c) = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (n == 0 || (!SHARED && n == 1)) return;   // (whole contexts have their results)
+    const f32x2 st = statistics(p, n, wave == 0);
+    __syncthreads();
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int z = wave; z < n; z += kWaves) o += *reinterpret_cast<const f32x4*>(p + z * pitch) * __shfl(f, z);
+    for (int z0 = wave; z0 < n; z0 += 4 * kWaves) {   // four parts in flight (behind the last: that one again, times 0)
+      f32x4 x[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = *reinterpret_cast<const f32x4*>(p + min(z0 + e * kWaves, n - 1) * pitch + 4 + c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o += x[e] * (z0 + e * kWaves < n ? factors[z0 + e * kWaves] : 0.0f);
+    }
     meet[wave][lane] = o;
     __syncthreads();
     if (wave || lane * 4 >= dh) return;
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) o += meet[w][lane];
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    *reinterpret_cast<f32x4*>(a.out + ((size_t)m * a.n_heads + head) * dh + c) = o * inv;
+    *reinterpret_cast<f32x4*>(out + c) = o * (st[1] == 0.0f ? 0.0f : 1.0f / st[1]);
     return;
   }
-  const int chunks = (a.max_context + kWeightPositions - 1) / kWeightPositions;
-  const int job = blockIdx.x - a.n_heads, hk = job / chunks, j = (job - hk * chunks) * kWeightPositions + 4 * tid;
-  if (j - 4 * tid > last) return;
+  const int hk = job / chunks;
   for (int h = wave; h < G; h += kWaves) {
-    float base, sum;
-    (void)factor(hk * G + h, &base, &sum);
-    if (lane == 0) head_stat[h] = f32x2{base, 1.0f / sum};
+    int n;
+    const float* p = parts_of(hk * G + h, &n);
+    const f32x2 st = statistics(p, n, false);
+    if (lane == 0) head_stat[h] = f32x2{st[0], 1.0f / st[1]};
   }
   __syncthreads();
-  if (j > last) return;
   const size_t sp = quant_score_pitch(a.max_context);
-  const float* s = a.scores + ((size_t)m * a.n_heads + hk * G) * sp + j;   // (rows of 64 positions: four are there)
-  const size_t row = ((size_t)m * a.c.heads + hk) * a.weights_pitch + j;
-  f32x4 w = {0.0f, 0.0f, 0.0f, 0.0f};
+  const float* s = a.scores + ((size_t)m * a.n_heads + hk * G) * sp;
+  const size_t row = ((size_t)m * a.c.heads + hk) * a.weights_pitch;
+#pragma unroll
+  for (int i = 0; i < kWeightPositions / (4 * kThreads); ++i) {
+    const int j = j0 + (i * kThreads + tid) * 4;   // (rows are of whole 64 positions: four are there)
+    if (j > last) continue;
+    f32x4 w = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
-  for (int h = 0; h < G; ++h) {
-    const f32x4 x = *reinterpret_cast<const f32x4*>(s + h * sp);
-    const f32x2 stat = head_stat[h];
+    for (int h = 0; h < G; ++h) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(s + h * sp + j);
+      const f32x2 st = head_stat[h];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] += __builtin_amdgcn_exp2f(x[e] - stat[0]) * stat[1];
+      for (int e = 0; e < 4; ++e) w[e] += __builtin_amdgcn_exp2f(x[e] - st[0]) * st[1];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (j + e <= last) a.weights_out[row + j + e] = a.weights_in && j + e < last ? a.weights_in[row + j + e] + w[e] : w[e];
   }
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (j + e <= last) a.weights_out[row + e] = a.weights_in && j + e < last ? a.weights_in[row + e] + w[e] : w[e];
 }
 
 template <int FMT, int DH, int NL>
 void launch_rows(const QuantAttnArgs& a, dim3 grid, hipStream_t st) {
   if (a.r.row_table)
-    quant_attn_kernel<FMT, DH, NL, true, false><<<grid, 64 * kWaves, 0, st>>>(a);
+    quant_attn_kernel<FMT, DH, NL, true, false><<<grid, kThreads, 0, st>>>(a);
   else if (a.scores)
-    quant_attn_kernel<FMT, DH, NL, false, true><<<grid, 64 * kWaves, 0, st>>>(a);
+    quant_attn_kernel<FMT, DH, NL, false, true><<<grid, kThreads, 0, st>>>(a);
   else
-    quant_attn_kernel<FMT, DH, NL, false, false><<<grid, 64 * kWaves, 0, st>>>(a);
+    quant_attn_kernel<FMT, DH, NL, false, false><<<grid, kThreads, 0, st>>>(a);
 }
 // Heads of 64 and 128 channels have kernels of their own: offsets within a block are then part of the load instructions.
 template <int FMT>
@@ -513,50 +668,82 @@ void launch_format(const QuantAttnArgs& a, dim3 grid, hipStream_t st) {
     launch_rows<FMT, 0, 4>(a, grid, st);
 }
 
-constexpr int kTarget = 512;             // workgroups to aim at by splitting contexts: two a compute unit
-constexpr int kMostParts = 64;           // (a lane each where they are joined)
+// Workgroups that dealing out aims at: two a compute unit, as many as are there at once.
+constexpr int kResident = 512;
+constexpr int kSharedParts = 64;
 
-// Workgroups of an unsplit call.
-int64_t plan_units(int rows, int G, int kv, bool shared) {
-  const int64_t C = 16 * quant_tiles(shared);
-  return (shared ? ((int64_t)rows * G + C - 1) / C : rows * ((G + C - 1) / C)) * kv;
+int deal_workgroups(int kv) { return kResident / kv > 1 ? kResident / kv : 1; }
+// Contexts of up to 16 steps are whole pieces: a workgroup's four wavefronts have four steps each, which takes no longer than a second launch
+// would.  With four times the resident workgroups in whole contexts, the order in which they end evens them out.
+bool deals(int rows, int group, int kv, int steps) {
+  const int64_t units = (int64_t)rows * unit_tiles(group);
+  return steps > 16 && units <= kDealtRows && units * kv < 4 * kResident;
 }
-int plan_parts(int64_t units, int steps) {
-  const int64_t most = steps / kMinPart, want = kTarget / units, least = (steps + kMaxPart - 1) / kMaxPart;
-  int64_t parts = want < 1 || most < 1 ? 1 : want < most ? want : most;
-  if (parts > kMostParts) parts = kMostParts;
-  return (int)(parts > least ? parts : least);
+int shared_parts(int rows, int group, int kv, int steps) {
+  const int64_t units = ((int64_t)rows * group + 31) / 32 * kv, want = kResident / units, most = steps / kWaves;
+  const int64_t parts = want < most ? want : most;
+  return (int)(parts < 1 ? 1 : parts > kSharedParts ? kSharedParts : parts);
 }
 
 }  // namespace
 
-void quant_attn_plan(QuantAttnArgs& a) {
-  const int steps = (a.max_context + 63) / 64;
-  const int64_t units = plan_units(a.r.rows, a.n_heads / a.c.heads, a.c.heads, a.r.row_table != nullptr);
-  const int parts = plan_parts(units, steps);
-  a.part_steps = ((steps + parts - 1) / parts + kMinPart - 1) / kMinPart * kMinPart;
-  a.n_parts = (steps + a.part_steps - 1) / a.part_steps;
+size_t quant_attn_plan(QuantAttnArgs& a, size_t* spans) {
+  *spans = 0;
+  const int steps = (a.max_context + 63) / 64, rows = a.r.rows, G = a.n_heads / a.c.heads, kv = a.c.heads;
+  const size_t record = a.c.dh + 4;
+  a.n_parts = 1;
+  a.part_steps = steps;
+  a.dealt = a.slots = 0;
+  if (a.r.row_table) {
+    const int parts = shared_parts(rows, G, kv, steps);
+    a.part_steps = (steps + parts - 1) / parts;
+    a.n_parts = (steps + a.part_steps - 1) / a.part_steps;
+    return a.n_parts > 1 ? (size_t)rows * a.n_heads * a.n_parts * record : 0;
+  }
+  a.slots = rows * unit_tiles(G);
+  if (deals(rows, G, kv, steps)) {
+    a.dealt = deal_workgroups(kv);
+    *spans = a.slots;
+    a.slots += a.dealt;                    // (unit u's part in workgroup w is in slot u + w: either grows from one piece to the next)
+  }
+  return a.dealt || a.weights_out ? (size_t)kv * a.slots * unit_columns(G) * record : 0;
 }
 
-// A call of fewer rows may be split into more parts: what all of them together take is bounded by the workgroups aimed at.
+// An upper bound that grows with its arguments: a call of fewer rows may be split where one of more is not.
 size_t quant_attn_part_floats(const QuantCache& c, int n_heads, int max_rows, int max_context, bool weights) {
-  const int steps = (max_context + 63) / 64;
-  const size_t pitch = c.dh + 4, columns = (size_t)max_rows * n_heads;
-  if (plan_parts(1, steps) == 1) return weights ? columns * pitch : 0;
-  // at most 32 columns a workgroup
-  const size_t split = columns * (size_t)(steps / kMinPart), aim = (size_t)kTarget * 32;
-  const size_t least = columns * (size_t)((steps + kMaxPart - 1) / kMaxPart);
-  return (split < aim ? split : least > aim ? least : aim) * pitch;
+  const int steps = (max_context + 63) / 64, G = n_heads / c.heads, kv = c.heads;
+  const size_t record = c.dh + 4, columns = (size_t)kv * unit_columns(G);
+  const int64_t units = (int64_t)max_rows * unit_tiles(G);
+  size_t most = weights ? (size_t)units * columns * record : 0;
+  if (steps > 16) {
+    // dealt out: units in front of the bounds of `deals`
+    int64_t u = units < kDealtRows ? units : kDealtRows;
+    const int64_t cap = (4 * kResident + kv - 1) / kv;
+    if (u > cap) u = cap;
+    const size_t dealt = (size_t)(u + deal_workgroups(kv)) * columns * record;
+    if (dealt > most) most = dealt;
+  }
+  // row_table: rows * heads * parts <= 32 columns a workgroup x the workgroups aimed at, and <= rows * heads * parts by steps
+  if (steps / kWaves > 1) {
+    const size_t by_steps = (size_t)max_rows * n_heads * (steps / kWaves < kSharedParts ? steps / kWaves : kSharedParts), aim = (size_t)32 * kResident;
+    const size_t shared = (by_steps < aim ? by_steps : aim) * record;
+    if (shared > most) most = shared;
+  }
+  return most;
 }
 
 void launch_quant_attention(const QuantAttnArgs& a, hipStream_t st) {
-  const int G = a.n_heads / a.c.heads, C = 16 * quant_tiles(a.r.row_table != nullptr);
-  const int y = a.r.row_table ? (int)(((int64_t)a.r.rows * G + C - 1) / C) : a.r.rows * ((G + C - 1) / C);
+  const int G = a.n_heads / a.c.heads;
+  const int y = a.r.row_table ? (int)(((int64_t)a.r.rows * G + 31) / 32) : a.dealt ? a.dealt : a.r.rows * unit_tiles(G);
   const dim3 grid(a.c.heads, y, a.n_parts);
   a.c.format == EE_QUANT_INT8 ? launch_format<EE_QUANT_INT8>(a, grid, st) : launch_format<EE_QUANT_E4M3>(a, grid, st);
   if (!a.parts) return;
-  const int chunks = a.weights_out ? (a.max_context + kWeightPositions - 1) / kWeightPositions : 0;
-  quant_join_kernel<<<dim3(a.n_heads + a.c.heads * chunks, a.r.rows), 256, (size_t)G * sizeof(f32x2), st>>>(a);
+  if (a.r.row_table) {
+    quant_join_kernel<true><<<dim3(a.n_heads, a.r.rows), kThreads, 0, st>>>(a);
+  } else {
+    const int chunks = a.weights_out ? (a.max_context + kWeightPositions - 1) / kWeightPositions : 0;
+    quant_join_kernel<false><<<dim3((a.dealt ? a.n_heads : 0) + a.c.heads * chunks, a.r.rows), kThreads, (size_t)G * sizeof(f32x2), st>>>(a);
+  }
 }
 
 }  // namespace ee
