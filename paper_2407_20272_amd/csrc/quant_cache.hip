@@ -34,24 +34,49 @@ __device__ inline float scale_for(float largest) {
   }
 }
 
-// The bytes nearest to x / s, ties to even.  INT8: x / s is estimated by a product with 1/s and then set right by the exact remainder x - q s
-// (one fma: |remainder| <= s and a multiple of the smaller operand's last place, so it has 24 bits), because the quotient
-// rounded to float may land on a tie that x / s is not on.  E4M3: s is a power of two, the product is exact and the conversion rounds once.
-template <int FMT>
-__device__ inline uint32_t quantise_pair(f32x2 x, float s, float inv) {
-  if (s != s) return 0;
-  if constexpr (FMT == EE_QUANT_INT8) {
-    uint32_t r = 0;
+// The bytes nearest to x / s, ties to even, of a number of pairs (inv = 1 / s).
+// E4M3: s is a power of two, so the product with inv is exact and the conversion rounds once.
+// INT8: adding 1.5 * 2^23 to the product leaves its nearest integer in the sum's low byte.  The product is up to 2.3e-5 away from x / s, which
+// matters where it lies that near to the middle between two integers (one wavefront in eight): there the exact remainder x - q s decides (one fma:
+// |remainder| <= s and a multiple of the smaller operand's last place, so it has 24 bits).
+template <int FMT, int N, class F>
+__device__ inline void quantise(F&& value, uint32_t (&out)[N], float s, float inv) {
+  if (s != s) {
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      float q = rintf(x[e] * inv);
-      const float rem = fmaf(-q, s, x[e]), twice = 2.0f * fabsf(rem);
-      if (twice > s || (twice == s && ((int)q & 1))) q += copysignf(1.0f, rem);
-      r |= (uint32_t)((int)fminf(fmaxf(q, -127.0f), 127.0f) & 0xff) << (8 * e);
+    for (int i = 0; i < N; ++i) out[i] = 0;
+    return;
+  }
+  if constexpr (FMT == EE_QUANT_E4M3) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const f32x2 x = value(i);
+      out[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[0] * inv, x[1] * inv, 0, false) & 0xffff;
     }
-    return r;
   } else {
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[0] * inv, x[1] * inv, 0, false) & 0xffff;
+    constexpr float kInteger = 12582912.0f;
+    float off = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const f32x2 x = value(i);
+      const float y0 = fmaf(x[0], inv, kInteger), y1 = fmaf(x[1], inv, kInteger);
+      off = fmaxf(off, fmaxf(fabsf(fmaf(x[0], inv, kInteger - y0)), fabsf(fmaf(x[1], inv, kInteger - y1))));
+      out[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, y1), __builtin_bit_cast(uint32_t, y0), 0x0c0c0400u);
+    }
+    if (__any(off > 0.49997f)) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const f32x2 x = value(i);
+        uint32_t r = 0;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float q = rintf(x[e] * inv);
+          const float rem = fmaf(-q, s, x[e]), twice = 2.0f * fabsf(rem);
+          if (twice > s || (twice == s && ((int)q & 1))) q += copysignf(1.0f, rem);
+          r |= (uint32_t)((int)q & 0xff) << (8 * e);
+        }
+        out[i] = r;
+      }
+    }
   }
 }
 
@@ -59,8 +84,9 @@ __device__ inline uint32_t quantise_pair(f32x2 x, float s, float inv) {
 __device__ inline float scale_max(float a, float b) { return a != a || b != b ? __builtin_nanf("") : fmaxf(a, b); }
 
 // Rows that go into (or come from) one block are taken together: a run is rows at consecutive positions of one block.  A workgroup has kGroup
-// rows (where every row is a sequence of its own, two) of one head and takes the runs that begin among them; wavefronts 0 and 2 K's, 1 and 3 V's.
-constexpr int kGroup = 8, kApart = 2;
+// rows (one, where every row is a sequence of its own) of two heads and takes the runs that begin among them, one after the other;
+// a wavefront for K and V of either head.  (Groups of 8: a chunk's runs of 16 leave every second workgroup empty, rows of many sequences take eight turns.)
+constexpr int kGroup = 8;
 struct Run {
   int m, n, off, seq, logical;   // first row, rows, the first one's place in its block
 };
@@ -97,84 +123,149 @@ __device__ inline f32x2 load_pair<bf16_t>(const bf16_t* p) {
 
 __device__ inline uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu; }
 
-template <int FMT, class T, int CP>
-__device__ inline void append_run(const QuantAppendArgs& a, const Run& run, int head, int which) {
-  const int lane = threadIdx.x & 63;
-  if (run.logical >= a.r.max_blocks) return;
-  const int blk = a.r.block_tables[(size_t)run.seq * a.r.max_blocks + run.logical];
-  if ((unsigned)blk >= (unsigned)a.c.num_blocks) return;
-  const int dh = a.c.dh;
-  const T* src = reinterpret_cast<const T*>(which ? a.v : a.k) + (size_t)run.m * (which ? a.v_stride : a.k_stride) + (size_t)head * dh;
-  const int64_t stride = which ? a.v_stride : a.k_stride;
-  const size_t unit = (size_t)blk * a.c.heads + head;
-  float* sp = a.c.scales + unit * 2 + which;
-  const float was = run.off ? *sp : kQuantScaleFloor;
+// What a run's rows are to become: where they are, their block, its scale in front.
+template <class T>
+struct AppendTo {
+  const T* src;
+  int64_t stride;
+  int8_t* block;
+  float* scale;
+  bool there;
+  __device__ AppendTo(const QuantAppendArgs& a, const Run& run, int head, int which) {
+    src = reinterpret_cast<const T*>(which ? a.v : a.k) + (size_t)run.m * (which ? a.v_stride : a.k_stride) + (size_t)head * a.c.dh;
+    stride = which ? a.v_stride : a.k_stride;
+    const int blk = run.logical < a.r.max_blocks ? a.r.block_tables[(size_t)run.seq * a.r.max_blocks + run.logical] : -1;
+    there = (unsigned)blk < (unsigned)a.c.num_blocks;
+    const size_t unit = (size_t)(there ? blk : 0) * a.c.heads + head;
+    block = (which ? a.c.v : a.c.k) + unit * 16 * a.c.dh;
+    scale = a.c.scales + unit * 2 + which;
+  }
+};
+template <class T>
+struct RawPair;
+template <>
+struct RawPair<float> {
+  typedef f32x2 type;
+  static __device__ f32x2 value(f32x2 r) { return r; }
+};
+template <>
+struct RawPair<bf16_t> {
+  typedef uint32_t type;
+  static __device__ f32x2 value(uint32_t u) { return f32x2{__builtin_bit_cast(float, u << 16), __builtin_bit_cast(float, u & 0xffff0000u)}; }
+};
 
-  const int end = run.off + run.n;
-  f32x2 x[16][CP];                                   // by place in the block
+// Four positions' bytes of channels c and c + 1 -> the two channels' words.
+__device__ inline void words_of(uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t& lo, uint32_t& hi) {
+  const uint32_t first = a0 | a1 << 16, second = a2 | a3 << 16;
+  lo = __builtin_amdgcn_perm(second, first, 0x06040200u);
+  hi = __builtin_amdgcn_perm(second, first, 0x07050301u);
+}
+
+// A whole block.
+template <int FMT, class T, int CP>
+__device__ inline void append_block(const QuantAppendArgs& a, const Run& run, int head, int which) {
+  typedef typename RawPair<T>::type raw_t;
+  const int lane = threadIdx.x & 63, dh = a.c.dh;
+  const AppendTo<T> to(a, run, head, which);
+  raw_t x[16 * CP];
   uint32_t most = 0;
 #pragma unroll
   for (int t = 0; t < 16; ++t)
 #pragma unroll
     for (int i = 0; i < CP; ++i) {
       const int c = 2 * lane + 128 * i;
-      x[t][i] = f32x2{0.0f, 0.0f};
-      if (t >= run.off && t < end && c < dh) x[t][i] = load_pair<T>(src + (t - run.off) * stride + c);
+      x[t * CP + i] = raw_t{};
+      if (c < dh) x[t * CP + i] = *reinterpret_cast<const raw_t*>(to.src + t * to.stride + c);
     }
+  if (!to.there) return;
 #pragma unroll
-  for (int t = 0; t < 16; ++t)
-#pragma unroll
-    for (int i = 0; i < CP; ++i) most = max(most, max(magnitude(x[t][i][0]), magnitude(x[t][i][1])));
-  const float need = scale_for<FMT>(__builtin_bit_cast(float, wave_max(most)));
-  const float s = run.off ? scale_max(was, need) : need, inv = 1.0f / s;
-  const bool grew = run.off && !(s == was);
-  if (lane == 0) *sp = s;
-
-  // what stood in front of the call's positions rounds again where the scale grew
-  if (which == 0) {
-    int8_t* kp = a.c.k + unit * 16 * dh;
-#pragma unroll
-    for (int t = 0; t < 16; ++t)
-#pragma unroll
-      for (int i = 0; i < CP; ++i) {
-        const int c = 2 * lane + 128 * i;
-        uint16_t* p = reinterpret_cast<uint16_t*>(kp + t * dh + c);
-        f32x2 y = x[t][i];
-        if (c >= dh || t >= end || (t < run.off && !grew)) continue;
-        if (t < run.off) {
-          y = byte_pair<FMT>(*p);
-          y = f32x2{y[0] * was, y[1] * was};
-        }
-        *p = (uint16_t)quantise_pair<FMT>(y, s, inv);
-      }
-    return;
+  for (int i = 0; i < 16 * CP; ++i) {
+    const f32x2 y = RawPair<T>::value(x[i]);
+    most = max(most, max(magnitude(y[0]), magnitude(y[1])));
   }
-  int8_t* vp = a.c.v + unit * 16 * dh;
+  const float s = scale_for<FMT>(__builtin_bit_cast(float, wave_max(most)));
+  if (lane == 0) *to.scale = s;
+  uint32_t two[16 * CP];
+  quantise<FMT>([&](int i) { return RawPair<T>::value(x[i]); }, two, s, 1.0f / s);
 #pragma unroll
   for (int i = 0; i < CP; ++i) {
     const int c = 2 * lane + 128 * i;
     if (c >= dh) continue;
-    int8_t* line = vp + (size_t)c * 16;              // channels c and c + 1: 32 bytes
-    u32x4 lo{}, hi{};
-    if (run.n < 16) {                                // (what stands behind the call's positions stays as it is)
-      lo = *reinterpret_cast<const u32x4*>(line);
-      hi = *reinterpret_cast<const u32x4*>(line + 16);
-    }
+    if (which == 0) {
 #pragma unroll
-    for (int t = 0; t < 16; ++t) {
-      const int sh = 8 * (t & 3);
-      f32x2 y = x[t][i];
-      if (t >= end || (t < run.off && !grew)) continue;
-      if (t < run.off) {
-        y = byte_pair<FMT>(((lo[t >> 2] >> sh) & 0xff) | (((hi[t >> 2] >> sh) & 0xff) << 8));
-        y = f32x2{y[0] * was, y[1] * was};
+      for (int t = 0; t < 16; ++t) *reinterpret_cast<uint16_t*>(to.block + t * dh + c) = (uint16_t)two[t * CP + i];
+    } else {
+      u32x4 lo, hi;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        uint32_t l, h;
+        words_of(two[(4 * w) * CP + i], two[(4 * w + 1) * CP + i], two[(4 * w + 2) * CP + i], two[(4 * w + 3) * CP + i], l, h);
+        lo[w] = l;
+        hi[w] = h;
       }
-      const uint32_t q = quantise_pair<FMT>(y, s, inv);
-      lo[t >> 2] = (lo[t >> 2] & ~(0xffu << sh)) | ((q & 0xff) << sh);
-      hi[t >> 2] = (hi[t >> 2] & ~(0xffu << sh)) | ((q >> 8) << sh);
+      *reinterpret_cast<u32x4*>(to.block + (size_t)c * 16) = lo;
+      *reinterpret_cast<u32x4*>(to.block + (size_t)c * 16 + 16) = hi;
     }
-    *reinterpret_cast<u32x4*>(line) = lo;
-    *reinterpret_cast<u32x4*>(line + 16) = hi;
+  }
+}
+
+// Part of a block, position by position.  What stood in front of the call's positions rounds again where the scale grew; what stands behind them stays
+// as it is.
+template <int FMT, class T, int CP>
+__device__ inline void append_positions(const QuantAppendArgs& a, const Run& run, int head, int which) {
+  const int lane = threadIdx.x & 63, dh = a.c.dh;
+  const AppendTo<T> to(a, run, head, which);
+  if (!to.there) return;
+  const float was = run.off ? *to.scale : kQuantScaleFloor;
+  // (lanes without channels read the last two)
+  auto channel = [&](int i) { return min(2 * lane + 128 * i, dh - 2); };
+  uint32_t most = 0;
+  for (int t0 = 0; t0 < run.n; t0 += 4) {            // (four positions in flight; behind the last: that one again)
+    f32x2 y[4][CP];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int i = 0; i < CP; ++i) y[e][i] = load_pair<T>(to.src + min(t0 + e, run.n - 1) * to.stride + channel(i));
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int i = 0; i < CP; ++i) most = max(most, max(magnitude(y[e][i][0]), magnitude(y[e][i][1])));
+  }
+  const float need = scale_for<FMT>(__builtin_bit_cast(float, wave_max(most)));
+  const float s = run.off ? scale_max(was, need) : need, inv = 1.0f / s;
+  if (lane == 0) *to.scale = s;
+  // bytes of channels c, c + 1 of a position are `apart` from those of the next, and `beside` from each other
+  const int apart = which ? 1 : dh, beside = which ? 16 : 1;
+  const int from = run.off && !(s == was) ? 0 : run.off;
+  const int end = run.off + run.n;
+  for (int t0 = from; t0 < end; t0 += 4) {
+    f32x2 y[4 * CP];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int i = 0; i < CP; ++i) {
+        const int t = min(t0 + e, end - 1);
+        if (t < run.off) {
+          const uint8_t* p = reinterpret_cast<const uint8_t*>(to.block) + t * apart + channel(i) * (which ? 16 : 1);
+          const f32x2 o = byte_pair<FMT>(p[0] | (uint32_t)p[beside] << 8);
+          y[e * CP + i] = f32x2{o[0] * was, o[1] * was};
+        } else {
+          y[e * CP + i] = load_pair<T>(to.src + (t - run.off) * to.stride + channel(i));
+        }
+      }
+    uint32_t two[4 * CP];
+    quantise<FMT>([&](int k) { return y[k]; }, two, s, inv);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int i = 0; i < CP; ++i) {
+        const int t = t0 + e, c = 2 * lane + 128 * i;
+        uint8_t* p = reinterpret_cast<uint8_t*>(to.block) + t * apart + c * (which ? 16 : 1);
+        if (t < end && c < dh) {
+          p[0] = (uint8_t)(two[e * CP + i] & 0xff);
+          p[beside] = (uint8_t)(two[e * CP + i] >> 8);
+        }
+      }
   }
 }
 
@@ -182,9 +273,15 @@ template <int FMT, class T, int CP>
 __global__ __launch_bounds__(kThreads) void quant_append_kernel(QuantAppendArgs a, int group) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Runs runs(a.r, blockIdx.x * group, group);
-  int i = 0;
-  for (uint64_t left = runs.first; left; left &= left - 1, ++i)
-    if ((i & 1) == (wave >> 1)) append_run<FMT, T, CP>(a, runs.of(__ffsll((unsigned long long)left) - 1), blockIdx.y, wave & 1);
+  const int head = blockIdx.y * 2 + (wave >> 1);
+  if (head >= a.c.heads) return;
+  for (uint64_t left = runs.first; left; left &= left - 1) {
+    const Run run = runs.of(__ffsll((unsigned long long)left) - 1);
+    if (run.n == 16)
+      append_block<FMT, T, CP>(a, run, head, wave & 1);
+    else
+      append_positions<FMT, T, CP>(a, run, head, wave & 1);
+  }
 }
 
 template <class T>
@@ -237,14 +334,14 @@ template <int FMT, class T, int CP>
 __global__ __launch_bounds__(kThreads) void quant_read_kernel(QuantReadArgs a, int group) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Runs runs(a.r, blockIdx.x * group, group);
-  int i = 0;
-  for (uint64_t left = runs.first; left; left &= left - 1, ++i)
-    if ((i & 1) == (wave >> 1)) read_run<FMT, T, CP>(a, runs.of(__ffsll((unsigned long long)left) - 1), blockIdx.y, wave & 1);
+  const int head = blockIdx.y * 2 + (wave >> 1);
+  if (head >= a.c.heads) return;
+  for (uint64_t left = runs.first; left; left &= left - 1) read_run<FMT, T, CP>(a, runs.of(__ffsll((unsigned long long)left) - 1), head, wave & 1);
   // rows that read nothing
   for (uint64_t left = __ballot(lane > 0 && lane <= group && runs.base - 1 + lane < a.r.rows && runs.pos < 0); left; left &= left - 1) {
     const size_t m = runs.base + __ffsll((unsigned long long)left) - 2;
-    T* dst = reinterpret_cast<T*>(wave & 1 ? a.v : a.k) + (m * a.c.heads + blockIdx.y) * a.c.dh;
-    for (int c = 2 * lane; c < a.c.dh && wave < 2; c += 128) store_pair<T>(dst + c, f32x2{0.0f, 0.0f});
+    T* dst = reinterpret_cast<T*>(wave & 1 ? a.v : a.k) + (m * a.c.heads + head) * a.c.dh;
+    for (int c = 2 * lane; c < a.c.dh; c += 128) store_pair<T>(dst + c, f32x2{0.0f, 0.0f});
   }
 }
 
@@ -259,10 +356,13 @@ __device__ inline uint32_t order_key(float w) {
 }
 
 // Which positions of one (sequence, head) stay.  The key of the last one that stays for its weight is found eight bits at a time (a histogram in
-// LDS over the keys that agree so far); a second walk numbers what stays in ascending order.
+// LDS over the keys that agree so far); another walk numbers what stays in ascending order.  The first kSelKeys keys are held in LDS: five
+// walks over memory, one load behind the other, took three times as long.
+constexpr int kEach = 12, kSelKeys = kEach * kSelThreads;
 __global__ __launch_bounds__(kSelThreads) void quant_select_kernel(QuantEvictArgs a) {
+  __shared__ uint32_t keys[kSelKeys];
   __shared__ uint32_t hist[256];
-  __shared__ int wave_n[2][kSelThreads / 64];
+  __shared__ uint32_t wave_n[kSelThreads / 64];
   __shared__ uint32_t chosen;
   __shared__ int above;
   const int b = blockIdx.y, head = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -275,12 +375,15 @@ __global__ __launch_bounds__(kSelThreads) void quant_select_kernel(QuantEvictArg
   const int old = n > a.keep ? n - a.recent : n;     // positions that are chosen from; the others stay
   int want = n > a.keep ? a.keep - a.recent : n;     // how many of them stay
   uint32_t prefix = 0;
+  auto key_of = [&](int i) { return i < kSelKeys ? keys[i] : order_key(w[i]); };
   if (want < old && want > 0) {
+#pragma unroll 4
+    for (int i = tid; i < min(n, kSelKeys); i += kSelThreads) keys[i] = order_key(w[i]);
     for (int shift = 24; shift >= 0; shift -= 8) {
       for (int i = tid; i < 256; i += kSelThreads) hist[i] = 0;
       __syncthreads();
       for (int i = tid; i < old; i += kSelThreads) {
-        const uint32_t k = order_key(w[i]);
+        const uint32_t k = key_of(i);
         if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255], 1u);
       }
       __syncthreads();
@@ -309,95 +412,138 @@ __global__ __launch_bounds__(kSelThreads) void quant_select_kernel(QuantEvictArg
       want -= above;                                 // those with a larger key all stay
     }
   }
-  // `want` positions whose key is `prefix` stay, the lowest ones
+  // `want` positions whose key is `prefix` stay, the lowest ones.  A thread numbers kEach neighbours at a time: of those in front, the ones that stay for
+  // certain, and of the ties as many as may.
   const bool all = want >= old, none = n > a.keep && a.keep == a.recent;
-  int at = 0, ties = 0;
-  for (int i0 = 0; i0 < n; i0 += kSelThreads) {
-    const int i = i0 + tid;
-    const float x = i < n ? w[i] : 0.0f;
-    const uint32_t k = order_key(x);
-    const bool sure = i < n && (all || i >= old || (!none && k > prefix));
-    const bool tie = i < old && !all && !none && k == prefix;
-    const uint64_t mine = (1ull << lane) - 1;
-    const uint64_t t = __ballot(tie);
-    if (lane == 0) wave_n[0][wave] = __popcll(t);
+  int sures = 0, ties = 0;
+  for (int i0 = 0; i0 < n; i0 += kSelKeys) {
+    const int each = (min(n - i0, kSelKeys) + kSelThreads - 1) / kSelThreads, begin = i0 + tid * each;
+    uint32_t mine = 0, held = 0;                     // counts: certain in the low half, ties in the high half; the kinds of this thread's positions
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const int i = begin + e;
+      if (e >= each || i >= n) continue;
+      uint32_t kind = 1;
+      if (!all && i < old) {
+        const uint32_t k = none ? 0 : key_of(i);
+        kind = none || k < prefix ? 0 : k == prefix ? 0x10000u : 1;
+      }
+      mine += kind;
+      held |= (kind == 1 ? 1u : kind ? 2u : 0u) << (2 * e);
+    }
+    uint32_t upto = mine;
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) {
+      const uint32_t o = __shfl_up(upto, x);
+      if (lane >= x) upto += o;
+    }
+    if (lane == 63) wave_n[wave] = upto;
     __syncthreads();
-    int t0 = ties, t_all = ties;
+    uint32_t before = upto - mine, total = 0;
+#pragma unroll
     for (int v = 0; v < kSelThreads / 64; ++v) {
-      if (v < wave) t0 += wave_n[0][v];
-      t_all += wave_n[0][v];
+      if (v < wave) before += wave_n[v];
+      total += wave_n[v];
     }
-    const bool stays = sure || (tie && t0 + __popcll(t & mine) < want);
-    const uint64_t s = __ballot(stays);
-    if (lane == 0) wave_n[1][wave] = __popcll(s);
-    __syncthreads();
-    int s0 = at, s_all = at;
-    for (int v = 0; v < kSelThreads / 64; ++v) {
-      if (v < wave) s0 += wave_n[1][v];
-      s_all += wave_n[1][v];
+    int sure_at = sures + (int)(before & 0xffff), tie_at = ties + (int)(before >> 16);
+    float x[kEach];
+    int to[kEach];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const uint32_t kind = (held >> (2 * e)) & 3;
+      to[e] = kind == 1 || (kind == 2 && tie_at < want) ? sure_at + min(tie_at, all ? 0 : want) : -1;
+      sure_at += kind == 1;
+      tie_at += kind == 2;
+      x[e] = to[e] >= 0 && w_out ? w[begin + e] : 0.0f;
     }
-    if (stays) {
-      const int to = s0 + __popcll(s & mine);        // <= i, and everything up to i0 + 1023 has been read
-      kept[to] = i;
-      if (w_out) w_out[to] = x;
-    }
-    at = s_all;
-    ties = t_all;
+    __syncthreads();                                 // (w_out may be w: everything up to here has been read, and no place is behind its position)
+#pragma unroll
+    for (int e = 0; e < kEach; ++e)
+      if (to[e] >= 0) {
+        kept[to[e]] = begin + e;
+        if (w_out) w_out[to[e]] = x[e];
+      }
+    sures += (int)(total & 0xffff);
+    ties += (int)(total >> 16);
   }
-  for (int i = at + tid; i < a.keep; i += kSelThreads) kept[i] = -1;
+  for (int i = min(n, a.keep) + tid; i < a.keep; i += kSelThreads) kept[i] = -1;
 }
 
 // One block of what stays: 16 positions from up to 16 blocks.  A position needs the scale with which its largest byte fits; one that fills its
 // block's range needs that block's scale itself, so a block that stays whole keeps its bytes.
 template <int FMT, int CP>
-__global__ __launch_bounds__(kThreads) void quant_build_kernel(QuantEvictArgs a, int slots) {
+__global__ __launch_bounds__(kThreads, CP == 1 ? 6 : 4) void quant_build_kernel(QuantEvictArgs a, int slots) {
   const int lane = threadIdx.x & 63;
-  const int task = blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+  const int task = blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int b = blockIdx.y;
   if (task >= slots * 2 * a.c.heads) return;
   const int which = task & 1, head = (task >> 1) % a.c.heads, slot = (task >> 1) / a.c.heads;
   const int dh = a.c.dh;
-  const int n = max(0, min(a.r.context_lens[b], min(a.max_context, a.r.max_blocks * 16)));
-  const int stay = min(n, a.keep);
-  if (slot * 16 >= stay || (!a.dst_tables && n <= a.keep)) return;
   const size_t row = (size_t)b * a.c.heads + head;
   const int mine = slot * 16 + (lane & 15);
-  const int pos = mine < stay ? a.kept[row * a.keep + mine] : -1;
-  int blk = -1;
+  const int n = a.r.context_lens[b];
+  const int pos = mine < a.keep ? a.kept[row * a.keep + mine] : -1;   // (-1 behind what stays)
+  if (lane_value(pos, 0) < 0 || (!a.dst_tables && n <= a.keep)) return;
+  int blk = 0;
   float was = kQuantScaleFloor;
   if (pos >= 0) {
     blk = safe_block(a.r.block_tables[(size_t)b * a.r.max_blocks + (pos >> 4)], a.c.num_blocks);
     was = a.c.scales[((size_t)blk * a.c.heads + head) * 2 + which];
   }
-  f32x2 x[16][CP];
-  float need = kQuantScaleFloor;
+  uint32_t two[16][CP];                              // a position's bytes of channels c and c + 1
+  if (which == 0) {
 #pragma unroll
-  for (int t = 0; t < 16; ++t) {
-    const int pt = lane_value(pos, t), bt = lane_value(blk, t);
-    const int8_t* p = (which ? a.c.v : a.c.k) + ((size_t)max(bt, 0) * a.c.heads + head) * 16 * dh;
+    for (int t = 0; t < 16; ++t) {
+      const int pt = lane_value(pos, t);
+      const int8_t* p = a.c.k + ((size_t)lane_value(blk, t) * a.c.heads + head) * 16 * dh + (pt & 15) * dh;
 #pragma unroll
-    for (int i = 0; i < CP; ++i) {
-      const int c = 2 * lane + 128 * i;
-      uint32_t two = 0;
-      if (pt >= 0 && c < dh) {
-        if (which == 0) {
-          two = *reinterpret_cast<const uint16_t*>(p + (pt & 15) * dh + c);
-        } else {
-          const uint8_t* line = reinterpret_cast<const uint8_t*>(p) + (size_t)c * 16 + (pt & 15);
-          two = line[0] | ((uint32_t)line[16] << 8);
-        }
+      for (int i = 0; i < CP; ++i) {
+        const int c = 2 * lane + 128 * i;
+        two[t][i] = pt >= 0 && c < dh ? *reinterpret_cast<const uint16_t*>(p + c) : 0;
       }
-      x[t][i] = byte_pair<FMT>(two);
+    }
+  } else {
+    // a channel's 16 positions are one load: a block that several of ours come from is read once, the next one while this one is taken apart
+    const int before = __shfl_up(pos, 1);
+    const uint32_t begins = (uint32_t)__ballot(lane < 16 && pos >= 0 && (lane == 0 || (pos >> 4) != (before >> 4)));
+    u32x4 now[CP][2], next[CP][2];
+    auto load = [&](uint32_t left, u32x4 (&to)[CP][2]) {
+      const int8_t* p = a.c.v + ((size_t)lane_value(blk, left ? __ffs(left) - 1 : 0) * a.c.heads + head) * 16 * dh;
+#pragma unroll
+      for (int i = 0; i < CP; ++i) {
+        const int c = 2 * lane + 128 * i;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) to[i][e] = *reinterpret_cast<const u32x4*>(p + (size_t)(c < dh ? c + e : 0) * 16);
+      }
+    };
+    load(begins, next);
+#pragma unroll
+    for (int t = 0; t < 16; ++t) {
+      if (begins >> t & 1) {
+#pragma unroll
+        for (int i = 0; i < CP; ++i) now[i][0] = next[i][0], now[i][1] = next[i][1];
+        load(begins >> (t + 1) << (t + 1), next);
+      }
+      const int pt = lane_value(pos, t), word = (pt >> 2) & 3, sh = 8 * (pt & 3);
+#pragma unroll
+      for (int i = 0; i < CP; ++i) {
+        uint32_t lo = now[i][0][0], hi = now[i][1][0];
+#pragma unroll
+        for (int w = 1; w < 4; ++w)
+          if (word == w) lo = now[i][0][w], hi = now[i][1][w];
+        two[t][i] = pt >= 0 && 2 * lane + 128 * i < dh ? ((lo >> sh) & 0xff) | (((hi >> sh) & 0xff) << 8) : 0;
+      }
     }
   }
+  float need = kQuantScaleFloor;
 #pragma unroll
   for (int t = 0; t < 16; ++t) {
     const float wt = lane_value(was, t);
     uint32_t most = 0;
 #pragma unroll
     for (int i = 0; i < CP; ++i) {
-      most = max(most, max(magnitude(x[t][i][0]), magnitude(x[t][i][1])));
-      x[t][i] = f32x2{x[t][i][0] * wt, x[t][i][1] * wt};
+      const f32x2 q = byte_pair<FMT>(two[t][i]);
+      most = max(most, max(magnitude(q[0]), magnitude(q[1])));
     }
     const float top = __builtin_bit_cast(float, wave_max(most));
     float nt = scale_for<FMT>(top * wt);
@@ -419,20 +565,27 @@ __global__ __launch_bounds__(kThreads) void quant_build_kernel(QuantEvictArgs a,
     sp = a.image_scales + unit;
   }
   if (lane == 0) *sp = s;
+  uint32_t again[16 * CP];
+  quantise<FMT>([&](int k) {
+    const f32x2 q = byte_pair<FMT>(two[k / CP][k % CP]);
+    const float wt = lane_value(was, k / CP);
+    return f32x2{q[0] * wt, q[1] * wt};
+  }, again, s, inv);
 #pragma unroll
   for (int i = 0; i < CP; ++i) {
     const int c = 2 * lane + 128 * i;
     if (c >= dh) continue;
     if (which == 0) {
 #pragma unroll
-      for (int t = 0; t < 16; ++t) *reinterpret_cast<uint16_t*>(out + t * dh + c) = (uint16_t)quantise_pair<FMT>(x[t][i], s, inv);
+      for (int t = 0; t < 16; ++t) *reinterpret_cast<uint16_t*>(out + t * dh + c) = (uint16_t)again[t * CP + i];
     } else {
-      u32x4 lo{}, hi{};
+      u32x4 lo, hi;
 #pragma unroll
-      for (int t = 0; t < 16; ++t) {
-        const uint32_t q = quantise_pair<FMT>(x[t][i], s, inv);
-        lo[t >> 2] |= (q & 0xff) << (8 * (t & 3));
-        hi[t >> 2] |= (q >> 8) << (8 * (t & 3));
+      for (int w = 0; w < 4; ++w) {
+        uint32_t l, h;
+        words_of(again[(4 * w) * CP + i], again[(4 * w + 1) * CP + i], again[(4 * w + 2) * CP + i], again[(4 * w + 3) * CP + i], l, h);
+        lo[w] = l;
+        hi[w] = h;
       }
       *reinterpret_cast<u32x4*>(out + (size_t)c * 16) = lo;
       *reinterpret_cast<u32x4*>(out + (size_t)c * 16 + 16) = hi;
@@ -465,8 +618,8 @@ int groups(int64_t tasks) { return (int)((tasks + kThreads / 64 - 1) / (kThreads
 
 template <int FMT, class T>
 static void append_as(const QuantAppendArgs& a, hipStream_t st) {
-  const int group = a.r.row_table ? kGroup : kApart;
-  const dim3 grid((a.r.rows + group - 1) / group, a.c.heads);
+  const int group = a.r.row_table ? kGroup : 1;
+  const dim3 grid((a.r.rows + group - 1) / group, (a.c.heads + 1) / 2);
   if (a.c.dh <= 128)
     quant_append_kernel<FMT, T, 1><<<grid, kThreads, 0, st>>>(a, group);
   else
@@ -481,8 +634,8 @@ void launch_quant_append(const QuantAppendArgs& a, int dtype, hipStream_t st) {
 
 template <int FMT, class T>
 static void read_as(const QuantReadArgs& a, hipStream_t st) {
-  const int group = a.r.row_table ? kGroup : kApart;
-  const dim3 grid((a.r.rows + group - 1) / group, a.c.heads);
+  const int group = a.r.row_table ? kGroup : 1;
+  const dim3 grid((a.r.rows + group - 1) / group, (a.c.heads + 1) / 2);
   if (a.c.dh <= 128)
     quant_read_kernel<FMT, T, 1><<<grid, kThreads, 0, st>>>(a, group);
   else
