@@ -334,12 +334,27 @@ def ee_paged_attention_decode(desc: ee_model_desc, cache: PagedKV, layer: int, q
 
 
 # ---- 8-bit cache, rotary embedding on its own ------------------------------------------------------------
+# One of these calls takes a few microseconds on the GPU at decode sizes, so the wrappers are kept short: a tensor is looked at once.
+_KIND = {torch.float32: EE_FP32, torch.bfloat16: EE_BF16}
+
+
+def _here(t: torch.Tensor) -> int:
+    """The address of a contiguous tensor on the current device (whose current stream the call goes to)."""
+    assert t.is_cuda and t.is_contiguous() and t.get_device() == torch._C._cuda_getDevice(), "contiguous CUDA tensors of the current device"
+    return t.data_ptr()
+
+
+def _raw_stream() -> int:
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+
 def _row_view(t: torch.Tensor):
-    """Pointer, row stride and element type of [rows][heads][channels] whose heads and channels are consecutive."""
-    assert t.is_cuda and t.dim() == 3 and t.dtype in (torch.float32, torch.bfloat16), "rows are CUDA tensors [rows][heads][channels]"
+    """Address, row stride and element type of [rows][heads][channels] whose heads and channels are consecutive."""
     rows, heads, dh = t.shape
-    assert rows == 0 or ((dh == 1 or t.stride(2) == 1) and (heads == 1 or t.stride(1) == dh)), "heads and channels must be consecutive"
-    return t.data_ptr(), t.stride(0) if rows > 1 else heads * dh, EE_FP32 if t.dtype == torch.float32 else EE_BF16
+    s = t.stride()
+    assert t.is_cuda and t.get_device() == torch._C._cuda_getDevice(), "CUDA tensors of the current device"
+    assert (s[2] == 1 or dh == 1) and (s[1] == dh or heads == 1) or rows == 0, "heads and channels must be consecutive"
+    return t.data_ptr(), s[0] if rows > 1 else heads * dh, _KIND[t.dtype]
 
 
 def make_rotary_desc(head_dim: int, rotary_dim: Optional[int] = None, layout: str = "half", theta: float = 10000.0,
@@ -358,24 +373,25 @@ def ee_rotary_frequencies(desc: ee_rotary_desc, device="cuda") -> torch.Tensor:
     return freqs
 
 
+def _rotary_side(x, y, rows, dh):
+    if x is None:
+        return None, None
+    assert x.shape == y.shape and x.shape[0] == rows and x.shape[2] == dh and x.dtype == y.dtype
+    (px, sx, kind), (py, sy, _) = _row_view(x), _row_view(y)
+    return C.byref(ee_rotary_rows(px, py, sx, sy, x.shape[1])), kind
+
+
 def ee_rotary(desc: ee_rotary_desc, freqs: torch.Tensor, positions: torch.Tensor, q: Optional[torch.Tensor],
               q_out: Optional[torch.Tensor], k: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
               transpose: bool = False):
     """Rows [rows][heads][head_dim] of any row stride; q_out may be q, k_out may be k."""
-    assert freqs.dtype == torch.float64 and freqs.numel() == desc.rotary_dim // 2
-    rows, records, kinds = int(positions.shape[0]), [], set()
-    for x, y in ((q, q_out), (k, k_out)):
-        if x is None:
-            records.append(None)
-            continue
-        assert x.shape == y.shape and x.shape[0] == rows and x.shape[2] == desc.head_dim
-        (px, sx, tx), (py, sy, ty) = _row_view(x), _row_view(y)
-        kinds |= {tx, ty}
-        records.append(ee_rotary_rows(px, py, sx, sy, int(x.shape[1])))
-    assert len(kinds) <= 1, "q, k and the results have one type"
-    _check(lib().ee_rotary(C.byref(desc), _ptr(freqs), _ptr(_i32(positions)), rows, kinds.pop() if kinds else EE_FP32,
-                           C.byref(records[0]) if records[0] else None, C.byref(records[1]) if records[1] else None,
-                           int(bool(transpose)), _stream()))
+    assert freqs.dtype == torch.float64 and freqs.shape[0] == desc.rotary_dim // 2 and positions.dtype == torch.int32
+    rows = positions.shape[0]
+    rq, tq = _rotary_side(q, q_out, rows, desc.head_dim)
+    rk, tk = _rotary_side(k, k_out, rows, desc.head_dim)
+    assert rq is None or rk is None or tq == tk, "q, k and the results have one type"
+    kind = tk if tq is None else tq
+    _check(lib().ee_rotary(desc, _here(freqs), _here(positions), rows, EE_FP32 if kind is None else kind, rq, rk, bool(transpose), _raw_stream()))
 
 
 class QuantKV:
@@ -399,7 +415,7 @@ class QuantKV:
         n, nb, h, bs, dh = k.shape
         assert k.dtype == v.dtype and k.dtype in (torch.int8, torch.float8_e4m3fn) and scales.dtype == torch.float32
         assert v.shape == (n, nb, h, dh, bs) and scales.shape == (n, nb, h, 2)
-        self.k, self.v, self.scales, self.num_blocks = k, v, scales, nb
+        self.k, self.v, self.scales, self.num_blocks, self.head = k, v, scales, nb, (h, dh)
         self.c = ee_quant_cache(_ptr(k), _ptr(v), _ptr(scales), n, nb, bs, h, dh,
                                 EE_QUANT_INT8 if k.dtype == torch.int8 else EE_QUANT_E4M3)
 
@@ -424,50 +440,50 @@ class QuantWorkspace:
 
 def ee_kv_quant_append(cache: QuantKV, layer: int, k: torch.Tensor, v: torch.Tensor, batch: ee_batch):
     """k, v [rows][Hkv][dh], float32 or bfloat16, any (even) row stride."""
-    shape = (batch.batch, cache.c.n_kv_heads, cache.c.head_dim)
+    shape = (batch.batch, *cache.head)
     assert k.shape == shape and v.shape == shape
     (pk, sk, tk), (pv, sv, tv) = _row_view(k), _row_view(v)
     assert tk == tv, "k and v have one type"
-    _check(lib().ee_kv_quant_append(C.byref(cache.c), layer, pk, sk, pv, sv, tk, C.byref(batch), _stream()))
+    _check(lib().ee_kv_quant_append(cache.c, layer, pk, sk, pv, sv, tk, batch, _raw_stream()))
 
 
 def ee_kv_quant_read(cache: QuantKV, layer: int, batch: ee_batch, k: torch.Tensor, v: torch.Tensor):
-    shape = (batch.batch, cache.c.n_kv_heads, cache.c.head_dim)
-    assert k.shape == shape and v.shape == shape and k.dtype == v.dtype and k.dtype in (torch.float32, torch.bfloat16)
-    _check(lib().ee_kv_quant_read(C.byref(cache.c), layer, C.byref(batch), _ptr(k), _ptr(v),
-                                  EE_FP32 if k.dtype == torch.float32 else EE_BF16, _stream()))
+    shape = (batch.batch, *cache.head)
+    assert k.shape == shape and v.shape == shape and k.dtype == v.dtype
+    _check(lib().ee_kv_quant_read(cache.c, layer, batch, _here(k), _here(v), _KIND[k.dtype], _raw_stream()))
 
 
 def ee_paged_attention_quant(cache: QuantKV, layer: int, q: torch.Tensor, batch: ee_batch, out: torch.Tensor,
                              ws: Optional[QuantWorkspace] = None, weights_in: Optional[torch.Tensor] = None,
                              weights_out: Optional[torch.Tensor] = None):
     """q, out [rows][H][dh] float32; weights [rows][Hkv][pitch] float32."""
-    assert q.dim() == 3 and q.shape == out.shape and q.shape[0] == batch.batch and q.shape[2] == cache.c.head_dim
+    rows, heads, dh = q.shape
+    assert q.shape == out.shape and rows == batch.batch and dh == cache.head[1]
     assert q.dtype == torch.float32 and out.dtype == torch.float32
     pitch = 0
     for w in (weights_in, weights_out):
         if w is not None:
-            assert w.dtype == torch.float32 and w.shape[:2] == (batch.batch, cache.c.n_kv_heads) and pitch in (0, w.shape[2])
-            pitch = int(w.shape[2])
-    _check(lib().ee_paged_attention_quant(C.byref(cache.c), layer, int(q.shape[1]), _ptr(q), C.byref(batch), _ptr(out),
-                                          _ptr(weights_in), _ptr(weights_out), pitch, _ptr(ws.buf) if ws else None,
-                                          ws.bytes if ws else 0, _stream()))
+            assert w.dtype == torch.float32 and w.shape[:2] == (rows, cache.head[0]) and pitch in (0, w.shape[2])
+            pitch = w.shape[2]
+    _check(lib().ee_paged_attention_quant(cache.c, layer, heads, _here(q), batch, _here(out), None if weights_in is None else _here(weights_in),
+                                          None if weights_out is None else _here(weights_out), pitch, _here(ws.buf) if ws else None,
+                                          ws.bytes if ws else 0, _raw_stream()))
 
 
 def ee_kv_quant_evict(cache: QuantKV, layer: int, batch: ee_batch, weights_in: torch.Tensor, weights_out: Optional[torch.Tensor],
                       keep: int, recent: int, kept: torch.Tensor, out_lens: torch.Tensor, ws: Optional[QuantWorkspace] = None,
                       dst_tables: Optional[torch.Tensor] = None):
     """weights [B][Hkv][pitch] float32, kept [B][Hkv][keep] int32, out_lens [B] int32, dst_tables [B][blocks] int32."""
-    head = (batch.batch, cache.c.n_kv_heads)
-    for w in (weights_in, weights_out):
-        assert w is None or (w.dtype == torch.float32 and w.shape[:2] == head)
-    assert kept.shape == head + (keep,) and out_lens.shape == (batch.batch,)
-    assert dst_tables is None or dst_tables.shape[0] == batch.batch
-    _check(lib().ee_kv_quant_evict(C.byref(cache.c), layer, C.byref(batch), _ptr(_i32(dst_tables)) if dst_tables is not None else None,
-                                   int(dst_tables.shape[1]) if dst_tables is not None else 0, _ptr(weights_in),
-                                   int(weights_in.shape[2]), _ptr(weights_out),
-                                   int(weights_out.shape[2]) if weights_out is not None else 0, keep, recent, _ptr(_i32(kept)),
-                                   _ptr(_i32(out_lens)), _ptr(ws.buf) if ws else None, ws.bytes if ws else 0, _stream()))
+    head = (batch.batch, cache.head[0])
+    assert weights_in.dtype == torch.float32 and weights_in.shape[:2] == head
+    assert weights_out is None or weights_out.dtype == torch.float32 and weights_out.shape[:2] == head
+    assert kept.shape == (*head, keep) and out_lens.shape == head[:1] and kept.dtype == torch.int32 and out_lens.dtype == torch.int32
+    assert dst_tables is None or dst_tables.shape[0] == head[0] and dst_tables.dtype == torch.int32
+    _check(lib().ee_kv_quant_evict(cache.c, layer, batch, None if dst_tables is None else _here(dst_tables),
+                                   0 if dst_tables is None else dst_tables.shape[1], _here(weights_in), weights_in.shape[2],
+                                   None if weights_out is None else _here(weights_out), 0 if weights_out is None else weights_out.shape[2],
+                                   keep, recent, _here(kept), _here(out_lens), _here(ws.buf) if ws else None, ws.bytes if ws else 0,
+                                   _raw_stream()))
 
 
 def ee_profile_enable(on: bool):
