@@ -117,6 +117,24 @@ __device__ inline Deal deal_out(const QuantAttnArgs& a, int tiles, int* start /*
   return Deal{__builtin_amdgcn_readfirstlane(total), __builtin_amdgcn_readfirstlane(max(1, min(a.dealt, total / kWaves)))};
 }
 
+// The attention that positions j .. j + 3 got from the G heads whose maximum and 1 / sum are in head_stat.
+__device__ inline void add_weights(const QuantAttnArgs& a, const f32x2* head_stat, int m, int hk, int G, int last, int j) {
+  const size_t sp = quant_score_pitch(a.max_context);
+  const float* s = a.scores + ((size_t)m * a.n_heads + hk * G) * sp + j;   // (rows are of whole 64 positions: four are there)
+  const size_t at = ((size_t)m * a.c.heads + hk) * a.weights_pitch + j;
+  f32x4 w = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int h = 0; h < G; ++h) {
+    const f32x4 x = *reinterpret_cast<const f32x4*>(s + h * sp);
+    const f32x2 st = head_stat[h];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] += __builtin_amdgcn_exp2f(x[e] - st[0]) * st[1];
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (j + e <= last) a.weights_out[at + e] = a.weights_in && j + e < last ? a.weights_in[at + e] + w[e] : w[e];
+}
+
 // DH: the head's channels, or 0 for a.c.dh; NL: loads of 16 bytes a lane and position (64 channels each).  SHARED: rows that may share a sequence,
 // 32 columns; else units, 16 columns.
 constexpr int quant_tiles(bool shared) { return shared ? 2 : 1; }
@@ -130,9 +148,10 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
   __shared__ int block_id[kTableSteps * 4];      // blocks of the steps at hand, and their scales of K and V
   __shared__ f32x2 block_scale[kTableSteps * 4];
   __shared__ int start[SHARED ? 1 : kDealtRows + 1], scratch[kWaves];
+  __shared__ f32x2 head_stat[C];                 // maximum, 1 / sum
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int dh = DH ? DH : a.c.dh, G = a.n_heads / a.c.heads, hk = blockIdx.x, last_entry = a.r.max_blocks - 1;
+  const int dh = DH ? DH : a.c.dh, G = __builtin_amdgcn_readfirstlane(a.n_heads / a.c.heads), hk = blockIdx.x, last_entry = a.r.max_blocks - 1;
   const int tiles = SHARED ? 1 : unit_tiles(G);
   const size_t block_bytes = (size_t)16 * dh, block_pitch = block_bytes * a.c.heads;
   const int8_t* k_base = a.c.k + hk * block_bytes;
@@ -169,11 +188,11 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
       f1 = min(f0 + C, a.r.rows * G);
       s0 = blockIdx.z * a.part_steps;
     } else {
-      const int m = unit / tiles;
+      const int m = __builtin_amdgcn_readfirstlane(unit / tiles);
       f0 = m * G + (unit - m * tiles) * C;
       f1 = min(f0 + C, (m + 1) * G);
     }
-    const int r0 = f0 / G, n_rows = (f1 - 1) / G - r0 + 1;
+    const int r0 = __builtin_amdgcn_readfirstlane(f0 / G), n_rows = __builtin_amdgcn_readfirstlane((f1 - 1) / G) - r0 + 1;
     const int m_lane = r0 + min(lane, n_rows - 1);   // the piece's rows, one a lane
     const int ctx = a.r.context_lens[m_lane];
     f32x4 qx[NT][2 * NL][2];
@@ -265,7 +284,7 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
     const auto score_rows = __builtin_amdgcn_make_buffer_rsrc(
         reinterpret_cast<char*>(a.scores) + ((size_t)r0 * a.n_heads + hk * G + (f0 - r0 * G)) * score_pitch, 0, (int)((f1 - f0) * score_pitch), 0x00020000);
     f32x4* const collected = meet[wave][0][0];
-    const int held_most = max(1, 16 / (f1 - f0));   // steps
+    const int held_shift = 31 - __builtin_clz(max(1, 16 / (f1 - f0)));   // row of column c, step k: (c << held_shift) + k
     int held = 0;
 
     // runs of rows that share a sequence, one after the other
@@ -405,7 +424,7 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
             if constexpr (WEIGHTS) {
               if (f0 + col < f1) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) collected[(held * (f1 - f0) + col) * 16 + ((g * 4 + i) ^ col)] = sd[nt][i] * f;
+                for (int i = 0; i < 4; ++i) collected[((col << held_shift) + held) * 16 + ((g * 4 + i) ^ col)] = sd[nt][i] * f;
               }
             }
             const float m_new = fmaxf(m_run[nt], max_over_groups(mx * f));
@@ -458,14 +477,18 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
             }
           load_v(v_blk, more);
           if constexpr (WEIGHTS) {
-            if (++held == held_most || !more) {
-              const int columns = f1 - f0;
+            __builtin_amdgcn_sched_barrier(0);
+            if (++held >> held_shift || !more) {
+              int again = lane;                      // (else the addresses are computed in front of the loop, and there are not as many registers)
+              asm("" : "+v"(again));
+              const int piece = again & 15;
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
-                const int row = 4 * j + g, step = row / columns, c = row - step * columns;   // (rows behind the last are out of the buffer's range)
-                const uint32_t to = (uint32_t)(c * score_pitch) + (uint32_t)((c0 + s - (held - 1 - step) * kWaves) * 64 + 4 * col) * 4;
-                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, collected[row * 16 + (col ^ c)]), score_rows,
-                                                       row < held * columns ? to : 0x80000000u, 0, 0);
+                const int row = 4 * j + (again >> 4), step = row & ((1 << held_shift) - 1), c = row >> held_shift;
+                const uint32_t to = (uint32_t)c * (uint32_t)score_pitch + (uint32_t)((c0 + s - (held - 1 - step) * kWaves) * 64 + 4 * piece) * 4;
+                // (rows of no column or step are out of the buffer's range: not stored)
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, collected[row * 16 + (piece ^ c)]), score_rows,
+                                                       step < held && c < f1 - f0 ? to : 0x80000000u, 0, 0);
               }
               held = 0;
             }
@@ -501,7 +524,7 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
       for (int ct = 0; ct < CT; ++ct) o[ct][nt] *= f;
     }
     const bool whole = SHARED ? a.parts == nullptr : s0 == 0 && s1 == unit_steps;
-    const bool leaves_part = SHARED ? !whole : !whole || WEIGHTS;
+    const bool leaves_part = SHARED ? !whole : !whole || (WEIGHTS && (dealt || tiles > 1));
 #pragma unroll
     for (int c0 = 0; c0 < CT; c0 += 4) {
       if (c0) __syncthreads();
@@ -533,10 +556,21 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
         }
       }
     }
+    if constexpr (WEIGHTS) {
+      if (wave == 0 && g == 0) head_stat[col] = f32x2{m_all[0] == -INFINITY ? 0.0f : m_all[0], 1.0f / l_all[0]};
+    }
     if (!dealt) break;
     do ++unit;
     while (at < stop && __builtin_amdgcn_readfirstlane(start[unit + 1]) <= at);
   } while (at < stop);
+  if constexpr (WEIGHTS) {
+    // a context that one workgroup has whole, with all heads that share it
+    if (!dealt && tiles == 1) {
+      __syncthreads();                               // (scores and statistics that the other wavefronts have written)
+      const int m = blockIdx.y, last = last_position(a, a.r.context_lens[m]);
+      for (int j = 4 * tid; j <= last; j += 4 * kThreads) add_weights(a, head_stat, m, hk, G, last, j);
+    }
+  }
 }
 
 // The parts of contexts joined in their order, a (row, head) a workgroup: each wavefront adds every fourth part's result, the four sums meet in
@@ -613,6 +647,10 @@ __global__ __launch_bounds__(kThreads) void quant_join_kernel(QuantAttnArgs a) {
     return;
   }
   const int hk = job / chunks;
+  if constexpr (!SHARED) {
+    // (contexts that one workgroup had whole are done)
+    if (tiles == 1 && !a.dealt) return;
+  }
   for (int h = wave; h < G; h += kWaves) {
     int n;
     const float* p = parts_of(hk * G + h, &n);
@@ -620,24 +658,10 @@ __global__ __launch_bounds__(kThreads) void quant_join_kernel(QuantAttnArgs a) {
     if (lane == 0) head_stat[h] = f32x2{st[0], 1.0f / st[1]};
   }
   __syncthreads();
-  const size_t sp = quant_score_pitch(a.max_context);
-  const float* s = a.scores + ((size_t)m * a.n_heads + hk * G) * sp;
-  const size_t row = ((size_t)m * a.c.heads + hk) * a.weights_pitch;
 #pragma unroll
   for (int i = 0; i < kWeightPositions / (4 * kThreads); ++i) {
-    const int j = j0 + (i * kThreads + tid) * 4;   // (rows are of whole 64 positions: four are there)
-    if (j > last) continue;
-    f32x4 w = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-    for (int h = 0; h < G; ++h) {
-      const f32x4 x = *reinterpret_cast<const f32x4*>(s + h * sp + j);
-      const f32x2 st = head_stat[h];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] += __builtin_amdgcn_exp2f(x[e] - st[0]) * st[1];
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (j + e <= last) a.weights_out[row + j + e] = a.weights_in && j + e < last ? a.weights_in[row + j + e] + w[e] : w[e];
+    const int j = j0 + (i * kThreads + tid) * 4;
+    if (j <= last) add_weights(a, head_stat, m, hk, G, last, j);
   }
 }
 
@@ -706,7 +730,7 @@ size_t quant_attn_plan(QuantAttnArgs& a, size_t* spans) {
     *spans = a.slots;
     a.slots += a.dealt;                    // (unit u's part in workgroup w is in slot u + w: either grows from one piece to the next)
   }
-  return a.dealt || a.weights_out ? (size_t)kv * a.slots * unit_columns(G) * record : 0;
+  return a.dealt || (a.weights_out && unit_tiles(G) > 1) ? (size_t)kv * a.slots * unit_columns(G) * record : 0;
 }
 
 // An upper bound that grows with its arguments: a call of fewer rows may be split where one of more is not.
