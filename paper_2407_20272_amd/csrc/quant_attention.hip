@@ -162,12 +162,13 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
   const bool dealt = !SHARED && a.dealt;
   if (dealt) {
     deal = deal_out(a, tiles, start, scratch);
-    if ((int)blockIdx.y >= deal.workgroups || deal.total == 0) return;
+    if ((int)blockIdx.y >= deal.workgroups) return;
     if (blockIdx.x == 0 && blockIdx.y == 0)      // for the launch that joins the parts
       for (int u = tid; u < a.r.rows * tiles; u += kThreads) {
         const int first = start[u + 1] > start[u] ? deal.owner(start[u]) : 0;
         a.spans[u] = make_int2(first, start[u + 1] > start[u] ? deal.owner(start[u + 1] - 1) - first + 1 : 0);
       }
+    if (deal.total == 0) return;
     at = deal.bound(blockIdx.y);
     stop = deal.bound(blockIdx.y + 1);
     int lower = 0;                               // the unit that step `at` belongs to: units that end in front of it

@@ -205,6 +205,12 @@ def test_append_chunks(fmt, dtype, heads, dh):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
+def test_append_rows_of_many_sequences(fmt):
+    """Single rows and short runs of 21 sequences next to each other, runs that end where another sequence's begins."""
+    run_append(fmt, torch.bfloat16, 3, 64, starts=[(7 * i) % 40 for i in range(21)], rows=[1, 1, 1, 2, 1, 5, 1] * 3, seed=21)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
 def test_append_one_by_one(fmt):
     """40 positions, one a call, magnitudes going up and down: blocks whose scale grows again and again."""
     run_append(fmt, torch.float32, 2, 128, starts=[0, 13], rows=[1, 1], seed=5, rounds=40,
@@ -350,6 +356,92 @@ def test_attention_of_a_split_context(fmt, n):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("heads,group,rows", [(2, 2, 40), (1, 20, 9), (4, 1, 70), (16, 1, 5)])
+def test_attention_of_a_ragged_batch(fmt, heads, group, rows):
+    """Rows whose steps are dealt out: workgroups with pieces of several rows, rows with pieces in several workgroups, empty rows at the ends and
+    between, rows of one position."""
+    lens = torch.randint(0, 1500, (rows,), generator=gen(rows)).tolist()
+    lens[0], lens[3], lens[4], lens[-1], lens[1] = -1, -1, 0, -1, 2000
+    check_attention(fmt, 64, heads, group, lens, seed=rows, width=130)
+
+
+@pytest.mark.parametrize("shared", [False, True])
+def test_attention_of_no_positions_at_all(shared):
+    tables, nb = tables_for([2000, 2000], 1)
+    kv = filled(1, nb, 2, 64, "int8", 1)
+    q = torch.randn(2, 4, 64, generator=gen(1)).cuda()
+    w = torch.full((2, 2, 2000), 3.0, device="cuda")
+    out = attend(kv, 1, q, [-1, -1], tables, [0, 1] if shared else None, weights=None if shared else w, max_context=2000)
+    assert torch.equal(out, torch.zeros_like(out)) and bool((w == 3.0).all())
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("shared", [False, True])
+def test_attention_of_more_blocks_than_a_table_holds(fmt, shared):
+    """Many heads, so that a workgroup walks a context of 18000 positions alone."""
+    n, heads = 18000, 512
+    tables, nb = tables_for([n], 2)
+    kv = filled(1, nb, heads, 16, fmt, 2)
+    q = torch.randn(1, heads, 16, generator=gen(3))
+    out = attend(kv, 1, q.cuda(), [n - 1], tables, [0] if shared else None)
+    few = [0, 1, 255, 256, 511]
+    kv_few = Q.Cache.of(kv)
+    part = Q.Cache(kv_few.k[:, few], kv_few.v[:, few], kv_few.scales[:, few], fmt)
+    want, _, bound = Q.attention(part, q[:, few].double(), [n - 1], tables)
+    assert bool(((out[:, few].cpu().double() - want).abs() <= bound).all())
+
+
+def test_attention_replays_with_other_lengths():
+    """One captured call, replayed as contexts grow: the work is divided by the lengths on the device."""
+    heads, group, dh, room = 2, 2, 64, 2100
+    tables, nb = tables_for([room, room, room], 5)
+    kv = filled(1, nb, heads, dh, "int8", 5)
+    q = torch.randn(3, heads * group, dh, generator=gen(6))
+    qd, lens, tb = q.cuda(), torch.zeros(3, dtype=torch.int32, device="cuda"), i32(tables)
+    out, weights = torch.empty_like(qd), torch.zeros(3, heads, room, device="cuda")
+    batch, ws = B.make_batch(None, lens, tb, room), B.QuantWorkspace(kv, heads * group, 3, room, True)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        B.ee_paged_attention_quant(kv, 1, qd, batch, out, ws, None, weights)
+    for now in ([0, -1, 2000], [2099, 2098, 1024], [5, 1023, 64], [-1, -1, -1]):
+        lens.copy_(torch.tensor(now, dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        w2 = torch.zeros_like(weights)
+        eager = attend(kv, 1, qd, now, tables, weights=w2, max_context=room)
+        assert torch.equal(out, eager)
+        for m, n in enumerate(now):
+            assert torch.equal(weights[m, :, :n + 1], w2[m, :, :n + 1])
+
+
+def test_calls_on_two_streams():
+    """Two chains of calls at once, each with buffers and a workspace of its own, give what they give alone."""
+    chains = []
+    for seed in (1, 2):
+        lens = [1700, 40, 900]
+        tables, nb = tables_for([n + 1 for n in lens], seed)
+        kv = filled(1, nb, 2, 64, "e4m3", seed)
+        q = torch.randn(3, 8, 64, generator=gen(seed)).cuda()
+        out, w = torch.empty_like(q), torch.zeros(3, 2, 1701, device="cuda")
+        batch, ws = B.make_batch(None, i32(lens), i32(tables), 1701), B.QuantWorkspace(kv, 8, 3, 1701, True)
+        chains.append((kv, q, batch, out, ws, w))
+    alone = []
+    for kv, q, batch, out, ws, w in chains:
+        B.ee_paged_attention_quant(kv, 1, q, batch, out, ws, None, w)
+        torch.cuda.synchronize()
+        alone.append((out.clone(), w.clone()))
+    streams = [torch.cuda.Stream() for _ in chains]
+    for _ in range(5):
+        for (kv, q, batch, out, ws, w), st in zip(chains, streams):
+            with torch.cuda.stream(st):
+                B.ee_paged_attention_quant(kv, 1, q, batch, out, ws, None, w)
+    torch.cuda.synchronize()
+    for (_, _, _, out, _, w), (o, x) in zip(chains, alone):
+        assert torch.equal(out, o) and torch.equal(w, x)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("q_scale", [0.0, 1e-20, 30.0, 1e4])
 def test_attention_extreme_queries(fmt, q_scale):
     check_attention(fmt, 64, 2, 2, lens=[100, 300], q_scale=q_scale)
@@ -421,7 +513,8 @@ def test_attention_bad_blocks_reach_nothing(fmt):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
-@pytest.mark.parametrize("heads,group,lens", [(2, 4, [0, 1, 63, 64, 500, -1]), (1, 20, [100, 3]), (2, 1, [5000]), (3, 2, [1500, 40])])
+@pytest.mark.parametrize("heads,group,lens", [(2, 4, [0, 1, 63, 64, 500, -1]), (1, 20, [100, 3]), (2, 1, [5000]), (3, 2, [1500, 40]),
+                                              (1, 18, [1400, -1, 3]), (2, 5, [1100, 64, 0, 1300])])
 @pytest.mark.parametrize("where", ["apart", "in place", "from nothing"])
 def test_attention_weights(fmt, heads, group, lens, where):
     tables, nb = tables_for([n + 1 for n in lens], 7)
@@ -550,6 +643,13 @@ def test_evict_order(kind):
         w[0, 1, 90:120] = -float("inf")
         w[0, 1, 120:130] = 1e-45
     run_evict("e4m3", 2, 64, [n], 70, 70 if kind == "recent only" else 15, seed=5, weights=w)
+
+
+@pytest.mark.parametrize("w_where", ["in place", "apart"])
+def test_evict_a_long_context(w_where):
+    """More positions than keys are held at once, with ties on both sides of that border."""
+    w = torch.randint(0, 4, (1, 1, 30000), generator=gen(4)).float()
+    run_evict("int8", 1, 16, [30000], 20000, 100, seed=1, weights=w, w_where=w_where)
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
