@@ -138,8 +138,10 @@ __device__ inline void add_weights(const QuantAttnArgs& a, const f32x2* head_sta
 // DH: the head's channels, or 0 for a.c.dh; NL: loads of 16 bytes a lane and position (64 channels each).  SHARED: rows that may share a sequence,
 // 32 columns; else units, 16 columns.
 constexpr int quant_tiles(bool shared) { return shared ? 2 : 1; }
-template <int FMT, int DH, int NL, bool SHARED, bool WEIGHTS>
+// KW: wavefronts of a unit.  With 2 a workgroup has two K/V heads of one row (the same blocks, so the loops stay in step).
+template <int FMT, int DH, int NL, bool SHARED, bool WEIGHTS, int KW>
 __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(QuantAttnArgs a) {
+  constexpr int UNITS = kWaves / KW;
   constexpr int NT = quant_tiles(SHARED), C = 16 * NT, CT = 4 * NL;
   constexpr bool QREG = !SHARED;        // q's fragments in registers, or in LDS
   __shared__ half8_t q_lds[QREG ? 1 : NT * NL * 2 * 2 * 64];
@@ -148,10 +150,10 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
   __shared__ int block_id[kTableSteps * 4];      // blocks of the steps at hand, and their scales of K and V
   __shared__ f32x2 block_scale[kTableSteps * 4];
   __shared__ int start[SHARED ? 1 : kDealtRows + 1], scratch[kWaves];
-  __shared__ f32x2 head_stat[C];                 // maximum, 1 / sum
+  __shared__ f32x2 head_stat[UNITS][C];          // maximum, 1 / sum
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, g = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int dh = DH ? DH : a.c.dh, G = __builtin_amdgcn_readfirstlane(a.n_heads / a.c.heads), hk = blockIdx.x, last_entry = a.r.max_blocks - 1;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), mine = UNITS > 1 ? wave / KW : 0, turn = wave - mine * KW;   // the unit, the wavefront's place in it
+  const int dh = DH ? DH : a.c.dh, G = __builtin_amdgcn_readfirstlane(a.n_heads / a.c.heads), hk = blockIdx.x * UNITS + mine, last_entry = a.r.max_blocks - 1;
   const int tiles = SHARED ? 1 : unit_tiles(G);
   const size_t block_bytes = (size_t)16 * dh, block_pitch = block_bytes * a.c.heads;
   const int8_t* k_base = a.c.k + hk * block_bytes;
@@ -159,7 +161,7 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
 
   int unit = blockIdx.y, at = 0, stop = 0, early = 0;
   Deal deal{};
-  const bool dealt = !SHARED && a.dealt;
+  const bool dealt = !SHARED && UNITS == 1 && a.dealt;
   if (dealt) {
     deal = deal_out(a, tiles, start, scratch);
     if ((int)blockIdx.y >= deal.workgroups) return;
@@ -309,23 +311,26 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
         s1 = min(s0 + a.part_steps, steps_to(longest));
       }
       const int32_t* table = a.r.block_tables + (size_t)seq * a.r.max_blocks;
-      for (int c0 = s0; c0 < s1; c0 += kTableSteps) {
+      for (int c0 = s0; c0 < s1; c0 += kTableSteps / UNITS) {
         // Block ids, then their scales, go to LDS: a step's loads from memory are then its bytes alone.  (Loads return in the order they were
         // asked for: waiting for an id behind a step's bytes would be waiting for the bytes.)
         // Blocks behind the sequence's last one may be any of the pool's: none of their positions passes a limit; they get scales of 1
         // and 0.
-        const int steps = min(kTableSteps, s1 - c0);
+        const int steps = min(kTableSteps / UNITS, s1 - c0);
+        f32x2* const scales = block_scale + mine * (kTableSteps / UNITS * 4);
         if (SHARED || dealt || c0 > s0) __syncthreads();   // (the tables in front have been read)
         for (int i = tid; i < steps * 4; i += kThreads) {
           const int blk = SHARED || dealt || c0 > 0 || i >= kThreads ? table[min(c0 * 4 + i, last_entry)] : early;
           block_id[i] = safe_block(blk, a.c.num_blocks);
         }
         __syncthreads();
+        // (a unit's scales are its own wavefronts' to fetch)
+        const int place = tid - mine * (64 * KW);
         auto scales_of = [&](int i) {
           const f32x2 sc = *reinterpret_cast<const f32x2*>(a.c.scales + ((size_t)block_id[min(i, steps * 4 - 1)] * a.c.heads + hk) * 2);
           return (c0 * 4 + i) * 16 > longest ? f32x2{1.0f, 0.0f} : sc;
         };
-        const f32x2 own_scale = scales_of(tid);
+        const f32x2 own_scale = scales_of(place);
         u32x4 kr[4][NL], vr[CT];
         // (channels and channel tiles from dh on are read as the first ones: the former meet zeros of q, the latter's results are dropped.
         // Every load is made, behind the last step from one place, so that what is in flight is known when the program is compiled.)
@@ -344,14 +349,14 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) vr[ct] = load16<!SHARED>(p + (DH || ct * 16 < dh ? ct * 256 : 0));
         };
-        load_k(block_id[min(wave, steps - 1) * 4 + (col >> 2)], wave < steps);
-        load_v(block_id[min(wave, steps - 1) * 4 + g], wave < steps);
-        if (tid < steps * 4) block_scale[tid] = own_scale;
-        for (int i = tid + kThreads; i < steps * 4; i += kThreads) block_scale[i] = scales_of(i);
+        load_k(block_id[min(turn, steps - 1) * 4 + (col >> 2)], turn < steps);
+        load_v(block_id[min(turn, steps - 1) * 4 + g], turn < steps);
+        if (place < steps * 4) scales[place] = own_scale;
+        for (int i = place + 64 * KW; i < steps * 4; i += 64 * KW) scales[i] = scales_of(i);
         __syncthreads();
         // results are kept relative to the largest scale of V so far
         float most_v = 0.0f;
-        for (int i = lane; i < steps * 4; i += 64) most_v = fmaxf(most_v, block_scale[i][1]);
+        for (int i = lane; i < steps * 4; i += 64) most_v = fmaxf(most_v, scales[i][1]);
         most_v = __builtin_bit_cast(float, wave_max(__builtin_bit_cast(uint32_t, most_v)));
         if (most_v > v_ref) {
           int e;
@@ -366,11 +371,11 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
             for (int nt = 0; nt < NT; ++nt) o[ct][nt] *= f;
         }
         // a step asks for the next one's bytes as soon as its own have been used
-        for (int s = wave; s < steps; s += kWaves) {
-          const bool more = s + kWaves < steps;
-          const int ahead = min(s + kWaves, steps - 1) * 4;
+        for (int s = turn; s < steps; s += KW) {
+          const bool more = s + KW < steps;
+          const int ahead = min(s + KW, steps - 1) * 4;
           const int pos0 = ((c0 + s) * 4 + g) * 16;
-          const f32x2 sc = block_scale[s * 4 + g];
+          const f32x2 sc = scales[s * 4 + g];
           const int k_blk = block_id[ahead + (col >> 2)], v_blk = block_id[ahead + g];
           // S = K Q^T
           f32x4 sd[NT][4];
@@ -486,7 +491,7 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
                 const int row = 4 * j + (again >> 4), step = row & ((1 << held_shift) - 1), c = row >> held_shift;
-                const uint32_t to = (uint32_t)c * (uint32_t)score_pitch + (uint32_t)((c0 + s - (held - 1 - step) * kWaves) * 64 + 4 * piece) * 4;
+                const uint32_t to = (uint32_t)c * (uint32_t)score_pitch + (uint32_t)((c0 + s - (held - 1 - step) * KW) * 64 + 4 * piece) * 4;
                 // (rows of no column or step are out of the buffer's range: not stored)
                 __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, collected[row * 16 + (piece ^ c)]), score_rows,
                                                        step < held && c < f1 - f0 ? to : 0x80000000u, 0, 0);
@@ -514,10 +519,10 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
     for (int nt = 0; nt < NT; ++nt) {
       float mm = -INFINITY, ll = 0.0f;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, stat[0][w][nt * 16 + col]);
+      for (int w = 0; w < KW; ++w) mm = fmaxf(mm, stat[0][mine * KW + w][nt * 16 + col]);
       const float base = mm == -INFINITY ? 0.0f : mm;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) ll += stat[1][w][nt * 16 + col] * __builtin_amdgcn_exp2f(stat[0][w][nt * 16 + col] - base);
+      for (int w = 0; w < KW; ++w) ll += stat[1][mine * KW + w][nt * 16 + col] * __builtin_amdgcn_exp2f(stat[0][mine * KW + w][nt * 16 + col] - base);
       m_all[nt] = mm;
       l_all[nt] = ll;
       const float f = __builtin_amdgcn_exp2f(m_run[nt] - base) * v_ref * (1.0f / 16384.0f);
@@ -534,31 +539,34 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) meet[wave][c][nt][lane] = o[c0 + c][nt];
       __syncthreads();
-      const int ch = (c0 + wave) * 16 + g * 4;
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const int f = f0 + nt * 16 + col;
-        f32x4 sum = meet[0][wave][nt][lane];
+      for (int c = turn * UNITS; c < (turn + 1) * UNITS; ++c) {   // (a unit's wavefronts share its channels)
+        const int ch = (c0 + c) * 16 + g * 4;
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) sum += meet[w][wave][nt][lane];
-        if (f >= f1 || ch >= dh) continue;
-        const int m = f / G;
-        const size_t row = (size_t)m * a.n_heads + hk * G + (f - m * G);
-        if (whole) {
-          const float inv = l_all[nt] == 0.0f ? 0.0f : 1.0f / l_all[nt];
-          *reinterpret_cast<f32x4*>(a.out + row * dh + ch) = sum * inv;
-        }
-        if (leaves_part) {
-          const size_t slot = SHARED ? row * a.n_parts + blockIdx.z
-                                     : ((size_t)hk * a.slots + unit + (dealt ? blockIdx.y : 0)) * unit_columns(G) + col;
-          float* p = a.parts + slot * (dh + 4);
-          if (ch == 0) *reinterpret_cast<f32x2*>(p) = f32x2{m_all[nt], l_all[nt]};
-          if (!whole) *reinterpret_cast<f32x4*>(p + 4 + ch) = sum;
+        for (int nt = 0; nt < NT; ++nt) {
+          const int f = f0 + nt * 16 + col;
+          f32x4 sum = meet[mine * KW][c][nt][lane];
+#pragma unroll
+          for (int w = 1; w < KW; ++w) sum += meet[mine * KW + w][c][nt][lane];
+          if (f >= f1 || ch >= dh) continue;
+          const int m = f / G;
+          const size_t row = (size_t)m * a.n_heads + hk * G + (f - m * G);
+          if (whole) {
+            const float inv = l_all[nt] == 0.0f ? 0.0f : 1.0f / l_all[nt];
+            *reinterpret_cast<f32x4*>(a.out + row * dh + ch) = sum * inv;
+          }
+          if (leaves_part) {
+            const size_t slot = SHARED ? row * a.n_parts + blockIdx.z
+                                       : ((size_t)hk * a.slots + unit + (dealt ? blockIdx.y : 0)) * unit_columns(G) + col;
+            float* p = a.parts + slot * (dh + 4);
+            if (ch == 0) *reinterpret_cast<f32x2*>(p) = f32x2{m_all[nt], l_all[nt]};
+            if (!whole) *reinterpret_cast<f32x4*>(p + 4 + ch) = sum;
+          }
         }
       }
     }
     if constexpr (WEIGHTS) {
-      if (wave == 0 && g == 0) head_stat[col] = f32x2{m_all[0] == -INFINITY ? 0.0f : m_all[0], 1.0f / l_all[0]};
+      if (turn == 0 && g == 0) head_stat[mine][col] = f32x2{m_all[0] == -INFINITY ? 0.0f : m_all[0], 1.0f / l_all[0]};
     }
     if (!dealt) break;
     do ++unit;
@@ -569,7 +577,7 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
     if (!dealt && tiles == 1) {
       __syncthreads();                               // (scores and statistics that the other wavefronts have written)
       const int m = blockIdx.y, last = last_position(a, a.r.context_lens[m]);
-      for (int j = 4 * tid; j <= last; j += 4 * kThreads) add_weights(a, head_stat, m, hk, G, last, j);
+      for (int j = 4 * (tid - mine * (64 * KW)); j <= last; j += 4 * 64 * KW) add_weights(a, head_stat[mine], m, hk, G, last, j);
     }
   }
 }
@@ -666,14 +674,27 @@ __global__ __launch_bounds__(kThreads) void quant_join_kernel(QuantAttnArgs a) {
   }
 }
 
+// Whether two K/V heads share a workgroup: where half as many workgroups still are as many as there can be at once.  Each has twice the steps then, and
+// its beginning and end take the same time.
+constexpr int kResident = 512;           // workgroups at once: two a compute unit
+bool pairs_heads(const QuantAttnArgs& a) {
+  return !a.r.row_table && !a.dealt && a.c.heads % 2 == 0 && (int64_t)a.slots * a.c.heads >= 2 * kResident;
+}
+template <int FMT, int DH, int NL, bool WEIGHTS>
+void launch_units(const QuantAttnArgs& a, dim3 grid, hipStream_t st) {
+  if (pairs_heads(a))
+    quant_attn_kernel<FMT, DH, NL, false, WEIGHTS, 2><<<dim3(grid.x / 2, grid.y), kThreads, 0, st>>>(a);
+  else
+    quant_attn_kernel<FMT, DH, NL, false, WEIGHTS, 4><<<grid, kThreads, 0, st>>>(a);
+}
 template <int FMT, int DH, int NL>
 void launch_rows(const QuantAttnArgs& a, dim3 grid, hipStream_t st) {
   if (a.r.row_table)
-    quant_attn_kernel<FMT, DH, NL, true, false><<<grid, kThreads, 0, st>>>(a);
+    quant_attn_kernel<FMT, DH, NL, true, false, 4><<<grid, kThreads, 0, st>>>(a);
   else if (a.scores)
-    quant_attn_kernel<FMT, DH, NL, false, true><<<grid, kThreads, 0, st>>>(a);
+    launch_units<FMT, DH, NL, true>(a, grid, st);
   else
-    quant_attn_kernel<FMT, DH, NL, false, false><<<grid, kThreads, 0, st>>>(a);
+    launch_units<FMT, DH, NL, false>(a, grid, st);
 }
 // Heads of 64 and 128 channels have kernels of their own: offsets within a block are then part of the load instructions.
 template <int FMT>
@@ -693,8 +714,6 @@ void launch_format(const QuantAttnArgs& a, dim3 grid, hipStream_t st) {
     launch_rows<FMT, 0, 4>(a, grid, st);
 }
 
-// Workgroups that dealing out aims at: two a compute unit, as many as are there at once.
-constexpr int kResident = 512;
 constexpr int kSharedParts = 64;
 
 int deal_workgroups(int kv) { return kResident / kv > 1 ? kResident / kv : 1; }

@@ -365,6 +365,23 @@ def test_attention_of_a_ragged_batch(fmt, heads, group, rows):
     check_attention(fmt, 64, heads, group, lens, seed=rows, width=130)
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dh,heads,group,rows,most", [(64, 32, 1, 36, 300), (128, 16, 2, 70, 130), (80, 64, 1, 17, 700), (32, 16, 17, 33, 70), (64, 33, 1, 33, 90)])
+def test_attention_of_many_heads(fmt, dh, heads, group, rows, most):
+    """Enough (row, K/V head) units that two share a workgroup (not with an odd number of heads), with and without weights."""
+    lens = torch.randint(-1, most, (rows,), generator=gen(rows)).tolist()
+    kv, tables, q, out = check_attention(fmt, dh, heads, group, lens, seed=rows, width=(most + 15) // 16, max_context=most)
+    w = torch.full((rows, heads, most), 2.0, device="cuda")
+    again = attend(kv, 2, q.cuda(), lens, tables, weights=w, max_context=most)
+    assert torch.equal(again, out)
+    _, probs, _ = Q.attention(Q.Cache.of(kv, 1), q.double(), lens, tables)
+    for m, n in enumerate(lens):
+        want = probs[m][0].view(heads, group, -1).sum(1)
+        # each probability by its head's slack, the sum of the heads 2^-24 a term
+        tol = (probs[m][0] * probs[m][1][:, None]).view(heads, group, -1).sum(1) + want * (group + 2) * 2.0 ** -24 + 1e-37
+        assert bool(((w[m, :, :n + 1].cpu().double() - want).abs() <= tol).all()) and bool((w[m, :, n + 1:] == 2.0).all())
+
+
 @pytest.mark.parametrize("shared", [False, True])
 def test_attention_of_no_positions_at_all(shared):
     tables, nb = tables_for([2000, 2000], 1)
