@@ -262,7 +262,8 @@ typedef struct ee_rotary_desc {
 } ee_rotary_desc;
 
 /* The rows of one tensor [rows][n_heads][head_dim]: heads and channels are consecutive, rows `stride` elements apart
- * (>= n_heads * head_dim).  in == out with equal strides works in place; otherwise the two must not overlap. */
+ * (>= n_heads * head_dim).  in == out with equal strides works in place; otherwise the two must not overlap, nor may the
+ * out of q overlap the in of k or the other way round. */
 typedef struct ee_rotary_rows {
   const void* in;      /* dev                                                                             */
   void* out;           /* dev                                                                             */
@@ -325,14 +326,16 @@ int ee_kv_quant_read(const ee_quant_cache* cache, int32_t layer, const ee_batch*
  *   out[m][h] = softmax_j(q[m][h] . K[j][h / g] / sqrt(head_dim)) . V[j][h / g],  j = 0..context_lens[m] INCLUSIVE,
  * with g = n_heads / n_kv_heads query heads to a K/V head.  Rows that share a sequence (row_table) are a causal chunk of a
  * prompt, and quickest when they stand next to each other.  A row with context_lens[m] < 0 attends nothing: its
- * result is 0.  q and out dev [rows][n_heads][head_dim] float, 16-byte aligned.
+ * result is 0.  q and out dev [rows][n_heads][head_dim] float, 16-byte aligned, not overlapping.
  * weights_out (dev [rows][n_kv_heads][weights_pitch] float, or NULL) receives the attention each cached position got, added
  * over the g heads that share it, for j <= p = context_lens[m]:
  *   weights_out[m][k][j] = weights_in[m][k][j] + sum_g probability   (j < p),   = sum_g probability   (j = p);
  * what lies behind is left as it was.  weights_in (same pitch) may be weights_out, or NULL for zeros.  Not with
  * row_table (EE_ERR_UNSUPPORTED).  weights_pitch >= max_context.
- * workspace: ee_paged_attention_quant_bytes for the call's sizes or larger ones (256-byte aligned; NULL where that is 0);
- * it needs no initialisation. */
+ * (weights_in and weights_out must not overlap in another way than being the same.)
+ * workspace: ee_paged_attention_quant_bytes for the call's sizes or larger ones, 256-byte aligned; it needs no
+ * initialisation and is dead between calls.  (Short contexts need none: NULL is refused only where something is needed.)
+ * The bytes are 0 only for sizes that are refused. */
 size_t ee_paged_attention_quant_bytes(const ee_quant_cache* cache, int32_t n_heads, int32_t max_batch, int32_t max_context,
                                       int32_t with_weights);
 int ee_paged_attention_quant(const ee_quant_cache* cache, int32_t layer, int32_t n_heads, const float* q,
@@ -343,13 +346,14 @@ int ee_paged_attention_quant(const ee_quant_cache* cache, int32_t layer, int32_t
  * (0 .. keep) positions stay, and of the others those with the largest weights_in (of equal ones the lowest position; NaN
  * counts as largest).  What stays moves together in its old order.  Here context_lens[b] is the NUMBER of cached
  * positions, at most max_context; row_table must be NULL; a sequence of `keep` positions or fewer keeps them all.
- * out_lens[b] = min(context_lens[b], keep) is the new number: the caller passes it on when every layer is done.
+ * out_lens[b] = min(context_lens[b], keep) is the new number: the caller passes it on when every layer is done (it must not
+ * be context_lens itself).
  *   dst_tables   dev [B][dst_max_blocks] or NULL.  NULL: the sequence's first blocks are written over (what lies behind
- *                out_lens[b] is free afterwards).  Else the result goes to these blocks, which must not be among the
+ *                out_lens[b] is free afterwards; no other sequence may share them).  Else the result goes to these blocks, which must not be among the
  *                blocks the batch's sequences are read from (for blocks that are shared, which must stay as they are).
  *   weights_in   dev [B][n_kv_heads][weights_pitch] float, weights_pitch >= max_context.
  *   weights_out  dev [B][n_kv_heads][weights_out_pitch] float or NULL, weights_out_pitch >= keep: the weights of what
- *                stays; may be weights_in (equal pitches).  Entries from out_lens[b] on are left as they were.
+ *                stays; may be weights_in (equal pitches; no other overlap).  Entries from out_lens[b] on are left as they were.
  *   kept         dev [B][n_kv_heads][keep] int32: the positions that stay, ascending, then -1.
  * A block that is written is built from its positions: its scale is the smallest that fits, and a position rounds
  * again (from the float its byte stood for) only where that scale differs from its old one.

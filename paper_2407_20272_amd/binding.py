@@ -428,13 +428,11 @@ class QuantWorkspace:
         L = lib()
         if evicting:
             self.bytes = L.ee_kv_quant_evict_bytes(C.byref(cache.c), max_batch, max_context)
-            bad = self.bytes == 0
         else:
             self.bytes = L.ee_paged_attention_quant_bytes(C.byref(cache.c), n_heads, max_batch, max_context, int(with_weights))
-            bad = self.bytes == 0 and (max_batch < 1 or max_context < 1 or n_heads < 1 or n_heads % cache.c.n_kv_heads != 0)
-        if bad:
+        if self.bytes == 0:
             raise EEError(EE_ERR_INVALID_ARG, ee_last_error())
-        self.buf = torch.empty(max(self.bytes, 256), dtype=torch.uint8, device=cache.k.device)
+        self.buf = torch.empty(self.bytes, dtype=torch.uint8, device=cache.k.device)
         assert self.buf.data_ptr() % 256 == 0
 
 

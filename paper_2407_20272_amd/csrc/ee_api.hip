@@ -1080,6 +1080,12 @@ int check_raw_workspace(void* ws, size_t have, size_t need) {
   return EE_OK;
 }
 
+// Whether two device ranges share a byte.
+bool ranges_meet(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + b_bytes && y < x + a_bytes;
+}
+
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 size_t evict_slots(int keep, int max_context) { return (size_t)((keep < max_context ? keep : max_context) + 15) / 16; }
 
@@ -1164,7 +1170,8 @@ size_t ee_paged_attention_quant_bytes(const ee_quant_cache* cache, int32_t n_hea
   const QuantCache c{nullptr, nullptr, nullptr, 0, cache->n_kv_heads, cache->head_dim, cache->format};
   const size_t parts = align256(quant_attn_part_floats(c, n_heads, max_batch, max_context, with_weights != 0) * sizeof(float));
   // (only with parts: the spans of dealt-out rows)
-  return parts + (parts ? align256(kQuantMostSpans * sizeof(int2)) : 0) + (with_weights ? align256((size_t)max_batch * n_heads * quant_score_pitch(max_context) * sizeof(float)) : 0);
+  const size_t all = parts + (parts ? align256(kQuantMostSpans * sizeof(int2)) : 0) + (with_weights ? align256((size_t)max_batch * n_heads * quant_score_pitch(max_context) * sizeof(float)) : 0);
+  return all ? all : 256;   // (0 says that the sizes are refused)
 }
 
 int ee_paged_attention_quant(const ee_quant_cache* cache, int32_t layer, int32_t n_heads, const float* q, const ee_batch* batch, float* out,
@@ -1176,10 +1183,15 @@ int ee_paged_attention_quant(const ee_quant_cache* cache, int32_t layer, int32_t
   if (batch->batch == 0) return EE_OK;
   if (!q || !out || ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 15))
     EE_FAIL(EE_ERR_INVALID_ARG, "ee_paged_attention_quant: q and out must start on 16 bytes");
+  const size_t q_bytes = (size_t)batch->batch * n_heads * cache->head_dim * sizeof(float);
+  if (ranges_meet(q, q_bytes, out, q_bytes)) EE_FAIL(EE_ERR_INVALID_ARG, "ee_paged_attention_quant: q and out overlap");
   if (weights_in && !weights_out) EE_FAIL(EE_ERR_INVALID_ARG, "ee_paged_attention_quant: weights_in without weights_out");
   if (weights_out && batch->row_table) EE_FAIL(EE_ERR_UNSUPPORTED, "ee_paged_attention_quant: weights with row_table");
   if (weights_out && weights_pitch < batch->max_context)
     EE_FAIL(EE_ERR_SHAPE, "ee_paged_attention_quant: weights_pitch %d below max_context %d", weights_pitch, batch->max_context);
+  const size_t weight_bytes = (size_t)batch->batch * cache->n_kv_heads * (size_t)weights_pitch * sizeof(float);
+  if (weights_in && weights_in != weights_out && ranges_meet(weights_in, weight_bytes, weights_out, weight_bytes))
+    EE_FAIL(EE_ERR_INVALID_ARG, "ee_paged_attention_quant: weights_in and weights_out overlap");
   a.n_heads = n_heads;
   a.max_context = batch->max_context;
   a.q = q;
@@ -1230,6 +1242,12 @@ int ee_kv_quant_evict(const ee_quant_cache* cache, int32_t layer, const ee_batch
   if (weights_pitch < batch->max_context || (weights_out && weights_out_pitch < keep))
     EE_FAIL(EE_ERR_SHAPE, "ee_kv_quant_evict: pitches %d, %d for contexts of %d, %d kept", weights_pitch, weights_out_pitch, batch->max_context, keep);
   if (weights_out == weights_in && weights_out_pitch != weights_pitch) EE_FAIL(EE_ERR_SHAPE, "ee_kv_quant_evict: weights in place with two pitches");
+  const size_t rows_in = (size_t)batch->batch * cache->n_kv_heads;
+  if (weights_out && weights_out != weights_in &&
+      ranges_meet(weights_in, rows_in * weights_pitch * sizeof(float), weights_out, rows_in * weights_out_pitch * sizeof(float)))
+    EE_FAIL(EE_ERR_INVALID_ARG, "ee_kv_quant_evict: weights_in and weights_out overlap");
+  if (ranges_meet(out_lens, batch->batch * sizeof(int32_t), batch->context_lens, batch->batch * sizeof(int32_t)))
+    EE_FAIL(EE_ERR_INVALID_ARG, "ee_kv_quant_evict: out_lens must not be context_lens (which later launches of the call read)");
   const size_t slots = evict_slots(keep, batch->max_context);
   if (dst_tables && (dst_max_blocks < 0 || (size_t)dst_max_blocks < slots))
     EE_FAIL(EE_ERR_SHAPE, "ee_kv_quant_evict: dst_max_blocks %d below %zu", dst_max_blocks, slots);

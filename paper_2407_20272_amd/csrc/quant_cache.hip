@@ -472,7 +472,7 @@ __global__ __launch_bounds__(kSelThreads) void quant_select_kernel(QuantEvictArg
 // One block of what stays: 16 positions from up to 16 blocks.  A position needs the scale with which its largest byte fits; one that fills its
 // block's range needs that block's scale itself, so a block that stays whole keeps its bytes.
 template <int FMT, int CP>
-__global__ __launch_bounds__(kThreads, CP == 1 ? 6 : 4) void quant_build_kernel(QuantEvictArgs a, int slots) {
+__global__ __launch_bounds__(kThreads, CP == 1 ? 6 : 3) void quant_build_kernel(QuantEvictArgs a, int slots) {
   const int lane = threadIdx.x & 63;
   const int task = blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int b = blockIdx.y;

@@ -31,11 +31,11 @@ def read(c=cache(), layer=1, b=batch(), k=P, v=P, dtype=B.EE_FP32):
     return B.lib().ee_kv_quant_read(ref(c), layer, ref(b), k, v, dtype, None)
 
 
-def attend(c=cache(), layer=1, heads=8, q=P, b=batch(), out=P, w_in=None, w_out=None, pitch=0, ws=None, size=0):
+def attend(c=cache(), layer=1, heads=8, q=P, b=batch(), out=1 << 30, w_in=None, w_out=None, pitch=0, ws=None, size=0):
     return B.lib().ee_paged_attention_quant(ref(c), layer, heads, q, ref(b), out, w_in, w_out, pitch, ws, size, None)
 
 
-def evict(c=cache(), layer=1, b=batch(), dst=None, dst_blocks=0, w=P, pitch=64, w_out=None, out_pitch=0, keep=20, recent=4, kept=P, lens=P,
+def evict(c=cache(), layer=1, b=batch(), dst=None, dst_blocks=0, w=P, pitch=64, w_out=None, out_pitch=0, keep=20, recent=4, kept=P, lens=1 << 20,
           ws=P, size=1 << 30):
     return B.lib().ee_kv_quant_evict(ref(c), layer, ref(b), dst, dst_blocks, w, pitch, w_out, out_pitch, keep, recent, kept, lens, ws, size, None)
 
@@ -78,10 +78,12 @@ def test_attention_refuses():
     assert attend(heads=6) == B.EE_ERR_SHAPE and attend(heads=0) == B.EE_ERR_SHAPE
     assert attend(c=cache(n_kv_heads=1), heads=1025) == B.EE_ERR_UNSUPPORTED
     assert attend(q=None) == B.EE_ERR_INVALID_ARG and attend(out=None) == B.EE_ERR_INVALID_ARG and attend(q=P + 4) == B.EE_ERR_INVALID_ARG
+    assert attend(q=P, out=P + 64) == B.EE_ERR_INVALID_ARG and "overlap" in B.ee_last_error()
     assert attend(w_in=P) == B.EE_ERR_INVALID_ARG
     assert attend(w_out=P, pitch=64, b=batch(row_table=P)) == B.EE_ERR_UNSUPPORTED
     assert attend(w_out=P, pitch=32) == B.EE_ERR_SHAPE
     assert attend(b=batch(rows=70000)) == B.EE_ERR_UNSUPPORTED
+    assert attend(w_in=P, w_out=P + 512, pitch=64) == B.EE_ERR_INVALID_ARG and "overlap" in B.ee_last_error()
     assert attend(w_out=P, pitch=64) == B.EE_ERR_WORKSPACE
     assert attend(w_out=P, pitch=64, ws=P + 128, size=1 << 30) == B.EE_ERR_WORKSPACE and "aligned" in B.ee_last_error()
     assert attend(w_out=P, pitch=64, ws=P, size=64) == B.EE_ERR_WORKSPACE and "needed" in B.ee_last_error()
@@ -94,10 +96,13 @@ def test_eviction_refuses():
     assert evict(b=batch(row_table=P)) == B.EE_ERR_INVALID_ARG
     for name in ("w", "kept", "lens"):
         assert evict(**{name: None}) == B.EE_ERR_INVALID_ARG
-    assert evict(pitch=32) == B.EE_ERR_SHAPE and evict(w_out=P + 64, out_pitch=19) == B.EE_ERR_SHAPE
+    assert evict(pitch=32) == B.EE_ERR_SHAPE and evict(w_out=1 << 21, out_pitch=19) == B.EE_ERR_SHAPE
     assert evict(w_out=P, out_pitch=63) == B.EE_ERR_SHAPE
     assert evict(dst=P, dst_blocks=1) == B.EE_ERR_SHAPE and evict(dst=P, dst_blocks=-1) == B.EE_ERR_SHAPE
     assert evict(b=batch(rows=70000)) == B.EE_ERR_UNSUPPORTED
+    assert evict(lens=P) == B.EE_ERR_INVALID_ARG and "out_lens" in B.ee_last_error()      # (context_lens are there)
+    assert evict(lens=P + 4) == B.EE_ERR_INVALID_ARG
+    assert evict(w_out=P + 256, out_pitch=64) == B.EE_ERR_INVALID_ARG and "overlap" in B.ee_last_error()
     assert evict(ws=None) == B.EE_ERR_WORKSPACE and evict(ws=P + 16) == B.EE_ERR_WORKSPACE and evict(size=100) == B.EE_ERR_WORKSPACE
 
 
@@ -113,7 +118,7 @@ def test_workspace_sizes_cover_smaller_calls():
             assert all(a <= b for line in table for a, b in zip(line, line[1:]))
             assert all(a <= b for up, down in zip(table, table[1:]) for a, b in zip(up, down))
             assert all(x % 256 == 0 for line in table for x in line)
-            assert not w or all(x > 0 for line in table for x in line)
+            assert all(x > 0 for line in table for x in line)
     assert L.ee_paged_attention_quant_bytes(None, 8, 1, 64, 0) == 0
     assert L.ee_paged_attention_quant_bytes(C.byref(cache()), 7, 1, 64, 0) == 0 and "n_heads" in B.ee_last_error()
     assert L.ee_paged_attention_quant_bytes(C.byref(cache()), 8, 1, 1 << 20, 0) == 0
