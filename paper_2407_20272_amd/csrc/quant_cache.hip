@@ -474,11 +474,11 @@ __global__ __launch_bounds__(kSelThreads) void quant_select_kernel(QuantEvictArg
   for (int i = min(n, a.keep) + tid; i < a.keep; i += kSelThreads) kept[i] = -1;
 }
 
-// One block of what stays: 16 positions from up to 16 blocks.  A position needs the scale with which its largest byte fits; one that fills its
-// block's range needs that block's scale itself, so a block that stays whole keeps its bytes.
+// One block of what stays: 16 positions from up to 16 blocks.  A value needs the scale with which it fits; an INT8 byte that fills its block's range
+// needs that block's scale itself, so a block that stays whole keeps its bytes.
 // Bound by a chain of loads (kept positions, block ids, scales, bytes) at six wavefronts a SIMD, and by V: a channel's 16 positions share a line, so
-// every block that anything stays of is read whole.  16 sequences of 700 to 6000 positions cut to 1000, 8 heads of 128: 37 us for 33 MB kept
-// (V byte by byte: 50; with the values as floats in registers, three wavefronts a SIMD: 54).
+// every block that anything stays of is read whole.  16 sequences of 700 to 6000 positions cut to 1000, 8 heads of 128: 33 us for 33 MB kept
+// (INT8 40; V byte by byte: 50; with the values as floats in registers, three wavefronts a SIMD: 54; a maximum of each position instead of all: 37).
 template <int FMT, int CP>
 __global__ __launch_bounds__(kThreads, CP == 1 ? 6 : 3) void quant_build_kernel(QuantEvictArgs a, int slots) {
   const int lane = threadIdx.x & 63;
@@ -543,21 +543,25 @@ __global__ __launch_bounds__(kThreads, CP == 1 ? 6 : 3) void quant_build_kernel(
       }
     }
   }
-  float need = kQuantScaleFloor;
+  // The largest value decides: scales grow with it.  (Magnitudes' bits are ordered as integers, NaN behind all of them.)
+  uint32_t most = 0, filled = 0;
 #pragma unroll
   for (int t = 0; t < 16; ++t) {
     const float wt = lane_value(was, t);
-    uint32_t most = 0;
 #pragma unroll
     for (int i = 0; i < CP; ++i) {
       const f32x2 q = byte_pair<FMT>(two[t][i]);
-      most = max(most, max(magnitude(q[0]), magnitude(q[1])));
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t value = magnitude(q[e] * wt);
+        const bool fills = FMT == EE_QUANT_INT8 && fabsf(q[e]) >= 127.0f;
+        most = max(most, fills ? 0u : value);
+        if (FMT == EE_QUANT_INT8) filled = max(filled, fills ? magnitude(wt) : 0u);
+      }
     }
-    const float top = __builtin_bit_cast(float, wave_max(most));
-    float nt = scale_for<FMT>(top * wt);
-    if (FMT == EE_QUANT_INT8 && top >= 127.0f) nt = wt;
-    if (lane_value(pos, t) >= 0) need = scale_max(need, nt);
   }
+  float need = scale_for<FMT>(__builtin_bit_cast(float, wave_max(most)));
+  if constexpr (FMT == EE_QUANT_INT8) need = scale_max(need, __builtin_bit_cast(float, wave_max(filled)));
   const float s = need, inv = 1.0f / s;
   int8_t* out;
   float* sp;
