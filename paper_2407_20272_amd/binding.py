@@ -338,23 +338,22 @@ def ee_paged_attention_decode(desc: ee_model_desc, cache: PagedKV, layer: int, q
 _KIND = {torch.float32: EE_FP32, torch.bfloat16: EE_BF16}
 
 
-def _here(t: torch.Tensor) -> int:
-    """The address of a contiguous tensor on the current device (whose current stream the call goes to)."""
-    assert t.is_cuda and t.is_contiguous() and t.get_device() == torch._C._cuda_getDevice(), "contiguous CUDA tensors of the current device"
+_device = torch._C._cuda_getDevice           # the current device ...
+_raw_stream = torch._C._cuda_getCurrentRawStream   # ... and its current stream, which the call goes to
+
+
+def _here(t: torch.Tensor, device: int) -> int:
+    """The address of a contiguous tensor on the current device."""
+    assert t.get_device() == device and t.is_contiguous(), "contiguous CUDA tensors of the current device"
     return t.data_ptr()
 
 
-def _raw_stream() -> int:
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
-
-
-def _row_view(t: torch.Tensor):
-    """Address, row stride and element type of [rows][heads][channels] whose heads and channels are consecutive."""
-    rows, heads, dh = t.shape
-    s = t.stride()
-    assert t.is_cuda and t.get_device() == torch._C._cuda_getDevice(), "CUDA tensors of the current device"
-    assert (s[2] == 1 or dh == 1) and (s[1] == dh or heads == 1) or rows == 0, "heads and channels must be consecutive"
-    return t.data_ptr(), s[0] if rows > 1 else heads * dh, _KIND[t.dtype]
+def _row_stride(t: torch.Tensor, rows: int, heads: int, dh: int, device: int) -> int:
+    """The row stride of [rows][heads][channels] whose heads and channels are consecutive."""
+    row, head, channel = t.stride()
+    assert t.get_device() == device, "CUDA tensors of the current device"
+    assert (channel == 1 or dh == 1) and (head == dh or heads == 1) or rows == 0, "heads and channels must be consecutive"
+    return row if rows > 1 else heads * dh
 
 
 def make_rotary_desc(head_dim: int, rotary_dim: Optional[int] = None, layout: str = "half", theta: float = 10000.0,
@@ -373,12 +372,11 @@ def ee_rotary_frequencies(desc: ee_rotary_desc, device="cuda") -> torch.Tensor:
     return freqs
 
 
-def _rotary_side(x, y, rows, dh):
-    if x is None:
-        return None, None
-    assert x.shape == y.shape and x.shape[0] == rows and x.shape[2] == dh and x.dtype == y.dtype
-    (px, sx, kind), (py, sy, _) = _row_view(x), _row_view(y)
-    return C.byref(ee_rotary_rows(px, py, sx, sy, x.shape[1])), kind
+def _rotary_side(x, y, rows, dh, device):
+    shape = x.shape
+    heads = shape[1]
+    assert shape == (rows, heads, dh) and y.shape == shape and x.dtype == y.dtype
+    return ee_rotary_rows(x.data_ptr(), y.data_ptr(), _row_stride(x, rows, heads, dh, device), _row_stride(y, rows, heads, dh, device), heads)
 
 
 def ee_rotary(desc: ee_rotary_desc, freqs: torch.Tensor, positions: torch.Tensor, q: Optional[torch.Tensor],
@@ -386,12 +384,12 @@ def ee_rotary(desc: ee_rotary_desc, freqs: torch.Tensor, positions: torch.Tensor
               transpose: bool = False):
     """Rows [rows][heads][head_dim] of any row stride; q_out may be q, k_out may be k."""
     assert freqs.dtype == torch.float64 and freqs.shape[0] == desc.rotary_dim // 2 and positions.dtype == torch.int32
-    rows = positions.shape[0]
-    rq, tq = _rotary_side(q, q_out, rows, desc.head_dim)
-    rk, tk = _rotary_side(k, k_out, rows, desc.head_dim)
-    assert rq is None or rk is None or tq == tk, "q, k and the results have one type"
-    kind = tk if tq is None else tq
-    _check(lib().ee_rotary(desc, _here(freqs), _here(positions), rows, EE_FP32 if kind is None else kind, rq, rk, bool(transpose), _raw_stream()))
+    device, rows, dh = _device(), positions.shape[0], desc.head_dim
+    assert q is None or k is None or q.dtype == k.dtype, "q, k and the results have one type"
+    some = k if q is None else q
+    _check(lib().ee_rotary(desc, _here(freqs, device), _here(positions, device), rows, EE_FP32 if some is None else _KIND[some.dtype],
+                           None if q is None else _rotary_side(q, q_out, rows, dh, device),
+                           None if k is None else _rotary_side(k, k_out, rows, dh, device), bool(transpose), _raw_stream(device)))
 
 
 class QuantKV:
@@ -438,50 +436,52 @@ class QuantWorkspace:
 
 def ee_kv_quant_append(cache: QuantKV, layer: int, k: torch.Tensor, v: torch.Tensor, batch: ee_batch):
     """k, v [rows][Hkv][dh], float32 or bfloat16, any (even) row stride."""
-    shape = (batch.batch, *cache.head)
-    assert k.shape == shape and v.shape == shape
-    (pk, sk, tk), (pv, sv, tv) = _row_view(k), _row_view(v)
-    assert tk == tv, "k and v have one type"
-    _check(lib().ee_kv_quant_append(cache.c, layer, pk, sk, pv, sv, tk, batch, _raw_stream()))
+    device, rows, (heads, dh) = _device(), batch.batch, cache.head
+    assert k.shape == (rows, heads, dh) and v.shape == k.shape and k.dtype == v.dtype, "k and v: rows of the batch, one type"
+    _check(lib().ee_kv_quant_append(cache.c, layer, k.data_ptr(), _row_stride(k, rows, heads, dh, device), v.data_ptr(),
+                                    _row_stride(v, rows, heads, dh, device), _KIND[k.dtype], batch, _raw_stream(device)))
 
 
 def ee_kv_quant_read(cache: QuantKV, layer: int, batch: ee_batch, k: torch.Tensor, v: torch.Tensor):
-    shape = (batch.batch, *cache.head)
-    assert k.shape == shape and v.shape == shape and k.dtype == v.dtype
-    _check(lib().ee_kv_quant_read(cache.c, layer, batch, _here(k), _here(v), _KIND[k.dtype], _raw_stream()))
+    device = _device()
+    assert k.shape == (batch.batch, *cache.head) and v.shape == k.shape and k.dtype == v.dtype, "k and v: rows of the batch, one type"
+    _check(lib().ee_kv_quant_read(cache.c, layer, batch, _here(k, device), _here(v, device), _KIND[k.dtype], _raw_stream(device)))
 
 
 def ee_paged_attention_quant(cache: QuantKV, layer: int, q: torch.Tensor, batch: ee_batch, out: torch.Tensor,
                              ws: Optional[QuantWorkspace] = None, weights_in: Optional[torch.Tensor] = None,
                              weights_out: Optional[torch.Tensor] = None):
     """q, out [rows][H][dh] float32; weights [rows][Hkv][pitch] float32."""
+    device = _device()
     rows, heads, dh = q.shape
-    assert q.shape == out.shape and rows == batch.batch and dh == cache.head[1]
+    assert out.shape == q.shape and rows == batch.batch and dh == cache.head[1]
     assert q.dtype == torch.float32 and out.dtype == torch.float32
     pitch = 0
     for w in (weights_in, weights_out):
         if w is not None:
             assert w.dtype == torch.float32 and w.shape[:2] == (rows, cache.head[0]) and pitch in (0, w.shape[2])
             pitch = w.shape[2]
-    _check(lib().ee_paged_attention_quant(cache.c, layer, heads, _here(q), batch, _here(out), None if weights_in is None else _here(weights_in),
-                                          None if weights_out is None else _here(weights_out), pitch, _here(ws.buf) if ws else None,
-                                          ws.bytes if ws else 0, _raw_stream()))
+    _check(lib().ee_paged_attention_quant(cache.c, layer, heads, _here(q, device), batch, _here(out, device),
+                                          None if weights_in is None else _here(weights_in, device),
+                                          None if weights_out is None else _here(weights_out, device), pitch,
+                                          None if ws is None else _here(ws.buf, device), 0 if ws is None else ws.bytes, _raw_stream(device)))
 
 
 def ee_kv_quant_evict(cache: QuantKV, layer: int, batch: ee_batch, weights_in: torch.Tensor, weights_out: Optional[torch.Tensor],
                       keep: int, recent: int, kept: torch.Tensor, out_lens: torch.Tensor, ws: Optional[QuantWorkspace] = None,
                       dst_tables: Optional[torch.Tensor] = None):
     """weights [B][Hkv][pitch] float32, kept [B][Hkv][keep] int32, out_lens [B] int32, dst_tables [B][blocks] int32."""
-    head = (batch.batch, cache.head[0])
+    device, head = _device(), (batch.batch, cache.head[0])
     assert weights_in.dtype == torch.float32 and weights_in.shape[:2] == head
     assert weights_out is None or weights_out.dtype == torch.float32 and weights_out.shape[:2] == head
     assert kept.shape == (*head, keep) and out_lens.shape == head[:1] and kept.dtype == torch.int32 and out_lens.dtype == torch.int32
     assert dst_tables is None or dst_tables.shape[0] == head[0] and dst_tables.dtype == torch.int32
-    _check(lib().ee_kv_quant_evict(cache.c, layer, batch, None if dst_tables is None else _here(dst_tables),
-                                   0 if dst_tables is None else dst_tables.shape[1], _here(weights_in), weights_in.shape[2],
-                                   None if weights_out is None else _here(weights_out), 0 if weights_out is None else weights_out.shape[2],
-                                   keep, recent, _here(kept), _here(out_lens), _here(ws.buf) if ws else None, ws.bytes if ws else 0,
-                                   _raw_stream()))
+    _check(lib().ee_kv_quant_evict(cache.c, layer, batch, None if dst_tables is None else _here(dst_tables, device),
+                                   0 if dst_tables is None else dst_tables.shape[1], _here(weights_in, device), weights_in.shape[2],
+                                   None if weights_out is None else _here(weights_out, device),
+                                   0 if weights_out is None else weights_out.shape[2], keep, recent, _here(kept, device),
+                                   _here(out_lens, device), None if ws is None else _here(ws.buf, device), 0 if ws is None else ws.bytes,
+                                   _raw_stream(device)))
 
 
 def ee_profile_enable(on: bool):
