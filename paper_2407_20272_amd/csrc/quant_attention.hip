@@ -27,6 +27,7 @@ namespace {
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kTableSteps = 256;     // steps whose block ids and scales are in LDS at a time
 constexpr int kDealtRows = kQuantMostSpans;   // rows (tiles of them) whose steps are dealt out evenly, at most: every workgroup adds up their lengths
+constexpr int kResident = 512;       // workgroups at once: two a compute unit
 constexpr float kLog2e = 1.4426950408889634f;
 
 // Eight bytes -> eight fp16.
@@ -120,8 +121,8 @@ __device__ inline Deal deal_out(const QuantAttnArgs& a, int tiles, int* start /*
   }
   if (tid == kThreads - 1 && units == kDealtRows) start[units] = before;
   __syncthreads();
-  // (a workgroup has a step a wavefront at least)
-  return Deal{__builtin_amdgcn_readfirstlane(total), __builtin_amdgcn_readfirstlane(max(1, min(a.dealt, total / kWaves)))};
+  // (a workgroup has two steps a wavefront at least: more parts take longer to join)
+  return Deal{__builtin_amdgcn_readfirstlane(total), __builtin_amdgcn_readfirstlane(max(1, min(a.dealt, total / (2 * kWaves))))};
 }
 
 // The attention that positions j .. j + 3 got from the G heads whose maximum and 1 / sum are in head_stat.
@@ -166,20 +167,30 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
   const int8_t* k_base = a.c.k + hk * block_bytes;
   const int8_t* v_base = a.c.v + hk * block_bytes;
 
-  int unit = blockIdx.y, at = 0, stop = 0, early = 0;
+  int unit = blockIdx.y, worker = blockIdx.y, at = 0, stop = 0, early = 0;
   Deal deal{};
   const bool dealt = !SHARED && UNITS == 1 && a.dealt;
+  if (!SHARED && tiles > 1) {
+    // the tiles of a row read the same bytes: workgroups whose ids differ by eight share a chiplet and its L2
+    if (dealt) {
+      if (a.dealt % 8 == 0) worker = (blockIdx.y % 8) * (a.dealt / 8) + blockIdx.y / 8;
+    } else {
+      const int whole = a.r.rows / 8 * 8, y = blockIdx.y, rest = y - whole * tiles;
+      const int row = rest < 0 ? y / (8 * tiles) * 8 + y % 8 : whole + rest % (a.r.rows - whole);
+      unit = __builtin_amdgcn_readfirstlane(row * tiles + (rest < 0 ? y / 8 % tiles : rest / (a.r.rows - whole)));
+    }
+  }
   if (dealt) {
     deal = deal_out(a, tiles, start, scratch);
-    if ((int)blockIdx.y >= deal.workgroups) return;
-    if (blockIdx.x == 0 && blockIdx.y == 0)      // for the launch that joins the parts
+    if (worker >= deal.workgroups) return;
+    if (blockIdx.x == 0 && worker == 0)          // for the launch that joins the parts
       for (int u = tid; u < a.r.rows * tiles; u += kThreads) {
         const int first = start[u + 1] > start[u] ? deal.owner(start[u]) : 0;
         a.spans[u] = make_int2(first, start[u + 1] > start[u] ? deal.owner(start[u + 1] - 1) - first + 1 : 0);
       }
     if (deal.total == 0) return;
-    at = deal.bound(blockIdx.y);
-    stop = deal.bound(blockIdx.y + 1);
+    at = deal.bound(worker);
+    stop = deal.bound(worker + 1);
     int lower = 0;                               // the unit that step `at` belongs to: units that end in front of it
     for (int u = tid; u < a.r.rows * tiles; u += kThreads) lower += start[u + 1] <= at;
     for (int x = 1; x < 64; x <<= 1) lower += __shfl_xor(lower, x);
@@ -564,7 +575,7 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
           }
           if (leaves_part) {
             const size_t slot = SHARED ? row * a.n_parts + blockIdx.z
-                                       : ((size_t)hk * a.slots + unit + (dealt ? blockIdx.y : 0)) * unit_columns(G) + col;
+                                       : ((size_t)hk * a.slots + unit + (dealt ? worker : 0)) * unit_columns(G) + col;
             float* p = a.parts + slot * (dh + 4);
             if (ch == 0) *reinterpret_cast<f32x2*>(p) = f32x2{m_all[nt], l_all[nt]};
             if (!whole) *reinterpret_cast<f32x4*>(p + 4 + ch) = sum;
@@ -589,13 +600,15 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
   }
 }
 
-// The parts of contexts joined in their order, a (row, head) a workgroup: each wavefront adds every fourth part's result, the four sums meet in
-// LDS.  In workgroups behind those: the attention every position got, twice four positions a thread.
-constexpr int kWeightPositions = 8 * kThreads, kMostParts = 512;
-template <bool SHARED>
-__global__ __launch_bounds__(kThreads) void quant_join_kernel(QuantAttnArgs a) {
+// The parts of contexts joined in their order, a (row, head) a workgroup: each of its WAVES wavefronts adds every WAVES-th part's result, their sums
+// meet in LDS.  In workgroups behind those: the attention every position got, four positions a thread, 2048 a workgroup.
+// Eight wavefronts where there are few (row, head) pairs (one row of 8 heads in 256 parts: 8 us instead of 11), else four (64 rows of 32 heads in two or
+// three parts: 6 us instead of 9).
+constexpr int kWeightPositions = 2048, kMostParts = kResident;
+template <bool SHARED, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void quant_join_kernel(QuantAttnArgs a) {
   extern __shared__ f32x2 head_stat[];   // [G] maximum, 1 / sum
-  __shared__ f32x4 meet[kWaves][64];
+  __shared__ f32x4 meet[WAVES][64];
   __shared__ float factors[kMostParts];
   const int m = blockIdx.y, G = a.n_heads / a.c.heads, dh = a.c.dh, tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -647,18 +660,18 @@ __global__ __launch_bounds__(kThreads) void quant_join_kernel(QuantAttnArgs a) {
     const f32x2 st = statistics(p, n, wave == 0);
     __syncthreads();
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int z0 = wave; z0 < n; z0 += 4 * kWaves) {   // four parts in flight (behind the last: that one again, times 0)
+    for (int z0 = wave; z0 < n; z0 += 4 * WAVES) {   // four parts in flight (behind the last: that one again, times 0)
       f32x4 x[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = *reinterpret_cast<const f32x4*>(p + min(z0 + e * kWaves, n - 1) * pitch + 4 + c);
+      for (int e = 0; e < 4; ++e) x[e] = *reinterpret_cast<const f32x4*>(p + min(z0 + e * WAVES, n - 1) * pitch + 4 + c);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o += x[e] * (z0 + e * kWaves < n ? factors[z0 + e * kWaves] : 0.0f);
+      for (int e = 0; e < 4; ++e) o += x[e] * (z0 + e * WAVES < n ? factors[z0 + e * WAVES] : 0.0f);
     }
     meet[wave][lane] = o;
     __syncthreads();
     if (wave || lane * 4 >= dh) return;
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) o += meet[w][lane];
+    for (int w = 1; w < WAVES; ++w) o += meet[w][lane];
     *reinterpret_cast<f32x4*>(out + c) = o * (st[1] == 0.0f ? 0.0f : 1.0f / st[1]);
     return;
   }
@@ -667,7 +680,7 @@ __global__ __launch_bounds__(kThreads) void quant_join_kernel(QuantAttnArgs a) {
     // (contexts that one workgroup had whole are done)
     if (tiles == 1 && !a.dealt) return;
   }
-  for (int h = wave; h < G; h += kWaves) {
+  for (int h = wave; h < G; h += WAVES) {
     int n;
     const float* p = parts_of(hk * G + h, &n);
     const f32x2 st = statistics(p, n, false);
@@ -675,15 +688,14 @@ __global__ __launch_bounds__(kThreads) void quant_join_kernel(QuantAttnArgs a) {
   }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kWeightPositions / (4 * kThreads); ++i) {
-    const int j = j0 + (i * kThreads + tid) * 4;
+  for (int i = 0; i < kWeightPositions / (256 * WAVES); ++i) {
+    const int j = j0 + 4 * (tid + i * 64 * WAVES);
     if (j <= last) add_weights(a, head_stat, m, hk, G, last, j);
   }
 }
 
 // Whether two K/V heads share a workgroup: where half as many workgroups still are as many as there can be at once.  Each has twice the steps then, and
 // its beginning and end take the same time.
-constexpr int kResident = 512;           // workgroups at once: two a compute unit
 bool pairs_heads(const QuantAttnArgs& a) {
   return !a.r.row_table && !a.dealt && a.c.heads % 2 == 0 && (int64_t)a.slots * a.c.heads >= 2 * kResident;
 }
@@ -789,11 +801,15 @@ void launch_quant_attention(const QuantAttnArgs& a, hipStream_t st) {
   const dim3 grid(a.c.heads, y, a.n_parts);
   a.c.format == EE_QUANT_INT8 ? launch_format<EE_QUANT_INT8>(a, grid, st) : launch_format<EE_QUANT_E4M3>(a, grid, st);
   if (!a.parts) return;
+  const bool few = (int64_t)a.r.rows * a.n_heads <= kResident;
   if (a.r.row_table) {
-    quant_join_kernel<true><<<dim3(a.n_heads, a.r.rows), kThreads, 0, st>>>(a);
+    const dim3 heads(a.n_heads, a.r.rows);
+    few ? quant_join_kernel<true, 8><<<heads, 512, 0, st>>>(a) : quant_join_kernel<true, 4><<<heads, 256, 0, st>>>(a);
   } else {
     const int chunks = a.weights_out ? (a.max_context + kWeightPositions - 1) / kWeightPositions : 0;
-    quant_join_kernel<false><<<dim3((a.dealt ? a.n_heads : 0) + a.c.heads * chunks, a.r.rows), kThreads, (size_t)G * sizeof(f32x2), st>>>(a);
+    const dim3 jobs((a.dealt ? a.n_heads : 0) + a.c.heads * chunks, a.r.rows);
+    const size_t lds = (size_t)G * sizeof(f32x2);
+    few ? quant_join_kernel<false, 8><<<jobs, 512, lds, st>>>(a) : quant_join_kernel<false, 4><<<jobs, 256, lds, st>>>(a);
   }
 }
 
