@@ -263,7 +263,7 @@ typedef struct ee_rotary_desc {
 
 /* The rows of one tensor [rows][n_heads][head_dim]: heads and channels are consecutive, rows `stride` elements apart
  * (>= n_heads * head_dim).  in == out with equal strides works in place; otherwise the two must not overlap, nor may the
- * out of q overlap the in of k or the other way round. */
+ * out of q overlap the in or out of k, or the out of k the in of q (rows of one buffer that lie between each other do not). */
 typedef struct ee_rotary_rows {
   const void* in;      /* dev                                                                             */
   void* out;           /* dev                                                                             */
@@ -342,7 +342,7 @@ int ee_paged_attention_quant(const ee_quant_cache* cache, int32_t layer, int32_t
                              const ee_batch* batch, float* out, const float* weights_in, float* weights_out,
                              int32_t weights_pitch, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Shortens the cache of every sequence of the batch to `keep` positions, for each K/V head by itself: the latest `recent`
+/* Shortens the cache of every sequence of the batch to `keep` (1 .. 262144) positions, for each K/V head by itself: the latest `recent`
  * (0 .. keep) positions stay, and of the others those with the largest weights_in (of equal ones the lowest position; NaN
  * counts as largest).  What stays moves together in its old order.  Here context_lens[b] is the NUMBER of cached
  * positions, at most max_context; row_table must be NULL; a sequence of `keep` positions or fewer keeps them all.

@@ -1004,8 +1004,16 @@ int check_rotary_desc(const ee_rotary_desc* D) {
   return EE_OK;
 }
 
-// What the `rows` rows of one side take up, in bytes.
-uint64_t rows_span(int rows, int64_t stride, int64_t row, int size) { return ((uint64_t)(rows - 1) * stride + row) * size; }
+// Whether `rows` rows of x_row and y_row elements share a byte (two views of one buffer may interleave).
+bool rows_meet(const void* x_rows, int64_t x_stride, int64_t x_row, const void* y_rows, int64_t y_stride, int64_t y_row, int rows, int size) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(x_rows), y = reinterpret_cast<uintptr_t>(y_rows);
+  const uint64_t x_span = ((uint64_t)(rows - 1) * x_stride + x_row) * size, y_span = ((uint64_t)(rows - 1) * y_stride + y_row) * size;
+  if (x >= y + y_span || y >= x + x_span) return false;
+  if (x_stride != y_stride || rows == 1) return true;
+  const uint64_t period = (uint64_t)x_stride * size;
+  const uint64_t off = y >= x ? (y - x) % period : (period - (x - y) % period) % period;   // from a row of x to the next of y
+  return off < (uint64_t)x_row * size || period - off < (uint64_t)y_row * size;
+}
 
 int check_rotary_rows(const ee_rotary_rows* R, const char* name, int rows, int head_dim, int size, RotaryRows* out) {
   *out = RotaryRows{nullptr, nullptr, 0, 0, 0};
@@ -1019,13 +1027,7 @@ int check_rotary_rows(const ee_rotary_rows* R, const char* name, int rows, int h
   if ((in | res) % size) EE_FAIL(EE_ERR_INVALID_ARG, "rotary: %s is not aligned to its type", name);
   if (in == res) {
     if (R->in_stride != R->out_stride && rows > 1) EE_FAIL(EE_ERR_INVALID_ARG, "rotary: %s in place with two strides", name);
-  } else if (R->in_stride == R->out_stride && rows > 1) {
-    // two views of one buffer may interleave: what counts is whether their rows meet
-    const uint64_t period = (uint64_t)R->in_stride * size, span = rows_span(rows, R->in_stride, row, size);
-    const uint64_t far_apart = in < res ? res - in : in - res, off = far_apart % period;
-    if (far_apart < span && (off < (uint64_t)row * size || off > period - (uint64_t)row * size))
-      EE_FAIL(EE_ERR_INVALID_ARG, "rotary: in and out of %s overlap", name);
-  } else if (in < res + rows_span(rows, R->out_stride, row, size) && res < in + rows_span(rows, R->in_stride, row, size)) {
+  } else if (rows_meet(R->in, R->in_stride, row, R->out, R->out_stride, row, rows, size)) {
     EE_FAIL(EE_ERR_INVALID_ARG, "rotary: in and out of %s overlap", name);
   }
   *out = RotaryRows{R->in, R->out, R->in_stride, R->out_stride, R->n_heads};
@@ -1112,6 +1114,13 @@ int ee_rotary(const ee_rotary_desc* desc, const double* freqs, const int32_t* po
   RotaryArgs a{freqs, positions, {}, {}, rows, desc->head_dim, desc->rotary_dim, (float)desc->amplitude, transpose ? -1.0f : 1.0f};
   const int size = dtype == EE_BF16 ? 2 : 4;
   if ((rc = check_rotary_rows(q, "q", rows, desc->head_dim, size, &a.q)) || (rc = check_rotary_rows(k, "k", rows, desc->head_dim, size, &a.k))) return rc;
+  if (q && k) {
+    const int64_t q_row = (int64_t)q->n_heads * desc->head_dim, k_row = (int64_t)k->n_heads * desc->head_dim;
+    if (rows_meet(q->out, q->out_stride, q_row, k->in, k->in_stride, k_row, rows, size) ||
+        rows_meet(k->out, k->out_stride, k_row, q->in, q->in_stride, q_row, rows, size) ||
+        rows_meet(q->out, q->out_stride, q_row, k->out, k->out_stride, k_row, rows, size))
+      EE_FAIL(EE_ERR_INVALID_ARG, "rotary: results of one of q and k overlap the other");
+  }
   const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   {
     ProfScope ps(EE_K_OTHER, 0, st);
@@ -1235,6 +1244,7 @@ int ee_kv_quant_evict(const ee_quant_cache* cache, int32_t layer, const ee_batch
   QuantEvictArgs a{};
   if ((rc = check_quant_call(cache, layer, batch, &a.c, &a.r))) return rc;
   if (keep < 1 || recent < 0 || recent > keep) EE_FAIL(EE_ERR_INVALID_ARG, "ee_kv_quant_evict: keep %d, recent %d", keep, recent);
+  if (keep > kAttnMaxBlocks * 16) EE_FAIL(EE_ERR_UNSUPPORTED, "ee_kv_quant_evict: keep %d exceeds the %d positions of a context", keep, kAttnMaxBlocks * 16);
   if (batch->batch == 0) return EE_OK;
   if (batch->row_table) EE_FAIL(EE_ERR_INVALID_ARG, "ee_kv_quant_evict takes no row_table");
   if (!weights_in || !kept || !out_lens) EE_FAIL(EE_ERR_INVALID_ARG, "ee_kv_quant_evict: NULL pointer");

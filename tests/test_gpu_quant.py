@@ -137,6 +137,25 @@ def test_rotary(dtype, layout, dh, r, h, kv, rows, transpose):
     assert torch.equal(buf[:, :h * dh], before[:, :h * dh]) and torch.equal(buf[:, (h + kv) * dh:], before[:, (h + kv) * dh:])
 
 
+def test_rotary_of_a_fused_buffer_in_place():
+    """q and k lie between each other's rows, both in place: the same results as apart, and V's rows stay."""
+    dh, h, kv, rows = 64, 6, 2, 9
+    desc = B.make_rotary_desc(dh)
+    freqs = B.ee_rotary_frequencies(desc)
+    pos = torch.arange(rows, dtype=torch.int32, device="cuda") * 7
+    buf = torch.randn(rows, (h + 2 * kv) * dh, generator=gen(5)).cuda()
+    before = buf.clone()
+
+    def parts(x):
+        return x[:, :h * dh].unflatten(1, (h, dh)), x[:, h * dh:(h + kv) * dh].unflatten(1, (kv, dh))
+    q, k = parts(buf)
+    q0, k0 = parts(before)
+    q_out, k_out = torch.empty(rows, h, dh, device="cuda"), torch.empty(rows, kv, dh, device="cuda")
+    B.ee_rotary(desc, freqs, pos, q0.contiguous(), q_out, k0.contiguous(), k_out)
+    B.ee_rotary(desc, freqs, pos, q, q, k, k)
+    assert torch.equal(q, q_out) and torch.equal(k, k_out) and torch.equal(buf[:, (h + kv) * dh:], before[:, (h + kv) * dh:])
+
+
 def test_rotary_addresses_off_sixteen_bytes():
     """The same results from an address that allows no wide loads."""
     desc = B.make_rotary_desc(64)

@@ -172,6 +172,24 @@ def test_rotary_refuses():
     assert B.lib().ee_rotary_frequencies(C.byref(desc()), None, None) == B.EE_ERR_INVALID_ARG
 
 
+def test_rotary_refuses_results_over_the_other_side():
+    far = 1 << 24
+
+    def both(q_in, q_out, k_in, k_out, stride=1024, n=4, q_heads=8, k_heads=4):
+        return rotate(n=n, q=rows(q_in, q_out, stride, stride, q_heads), k=rows(k_in, k_out, stride, stride, k_heads))
+    for bad in (dict(q_in=P, q_out=far, k_in=far, k_out=2 * far), dict(q_in=P, q_out=far, k_in=2 * far, k_out=P),
+                dict(q_in=P, q_out=far, k_in=2 * far, k_out=far), dict(q_in=P, q_out=far, k_in=far + 4 * 511, k_out=2 * far),
+                dict(q_in=P, q_out=far, k_in=far - 4 * 255, k_out=2 * far), dict(q_in=P, q_out=far, k_in=far + 3 * 4096, k_out=2 * far),
+                dict(q_in=P, q_out=P, k_in=P, k_out=P), dict(q_in=P, q_out=far, k_in=far, k_out=2 * far, n=1)):
+        assert both(**bad) == B.EE_ERR_INVALID_ARG and "overlap" in B.ee_last_error(), bad
+    # strides that differ: any shared range is refused
+    assert rotate(q=rows(P, far, 512, 512, 8), k=rows(far + 4 * 512, 2 * far, 1024, 1024, 4)) == B.EE_ERR_INVALID_ARG
+
+
+def test_eviction_refuses_more_than_a_context():
+    assert evict(keep=262145, w_out=None) == B.EE_ERR_UNSUPPORTED and evict(keep=2**31 - 1) == B.EE_ERR_UNSUPPORTED
+
+
 def test_names_of_the_binding():
     with pytest.raises(KeyError):
         B.make_rotary_desc(64, layout="quarter")
