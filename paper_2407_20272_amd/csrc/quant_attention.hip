@@ -215,20 +215,24 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
     }
     const int r0 = __builtin_amdgcn_readfirstlane(f0 / G), n_rows = __builtin_amdgcn_readfirstlane((f1 - 1) / G) - r0 + 1;
     const int m_lane = r0 + min(lane, n_rows - 1);   // the piece's rows, one a lane
-    const int ctx = a.r.context_lens[m_lane];
-    f32x4 qx[NT][2 * NL][2];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const int f = min(f0 + nt * 16 + col, f1 - 1), m = f / G;
+    const int ctx = a.r.context_lens[m_lane], row_seq = quant_seq(a.r, m_lane);
+    if constexpr (SHARED) early = a.r.block_tables[(size_t)__builtin_amdgcn_readfirstlane(row_seq) * a.r.max_blocks + min(s0 * 4 + tid, last_entry)];
+    // q: a wavefront's own in registers, or for LDS a quarter of the workgroup's (of one column tile, half of the channels): a load takes 16 bytes from
+    // each of up to 64 lines, so four times the loads are four times the time.
+    constexpr int QF = QREG ? 2 * NL : NL;         // fragments of 8 channels a lane
+    const int q_tile = QREG ? 0 : wave % NT, q_first = QREG ? 0 : wave / NT * QF, q_col = f0 + q_tile * 16 + col;
+    f32x4 qx[QF][2];
+    {
+      const int f = min(q_col, f1 - 1), m = f / G;
       const float* q = a.q + ((size_t)m * a.n_heads + hk * G + (f - m * G)) * dh;
 #pragma unroll
-      for (int k = 0; k < 2 * NL; ++k) {
-        const int c = (k >> 1) * 64 + g * 16 + (k & 1) * 8;
+      for (int k = 0; k < QF; ++k) {
+        const int c = ((q_first + k) >> 1) * 64 + g * 16 + ((q_first + k) & 1) * 8;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) qx[nt][k][e] = *reinterpret_cast<const f32x4*>(q + (c < dh ? c : 0) + 4 * e);
+        for (int e = 0; e < 2; ++e) qx[k][e] = *reinterpret_cast<const f32x4*>(q + (c < dh ? c : 0) + 4 * e);
       }
     }
-    const int row_seq = quant_seq(a.r, m_lane), row_pos = last_position(a, ctx);
+    const int row_pos = last_position(a, ctx);
     if constexpr (SHARED) {
       if (blockIdx.z > 0 && !__any((row_pos >> 6) >= s0)) return;
     } else {
@@ -247,6 +251,21 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
     half8_t qf[QREG ? 2 * NL : 1][2];
     float to_score[NT], m_run[NT], l_run[NT];
     int col_row[NT], col_pos[NT];
+    float most = 0.0f;
+#pragma unroll
+    for (int k = 0; k < QF; ++k)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        if (q_col >= f1 || ((q_first + k) >> 1) * 64 + g * 16 >= dh) qx[k][e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) most = fmaxf(most, fabsf(qx[k][e][j]));
+      }
+    most = max_over_groups(most);
+    if constexpr (!QREG) {
+      if (g == 0) stat[0][wave][col] = most;
+      __syncthreads();
+    }
+    float up = 0.0f;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int f = f0 + nt * 16 + col;
@@ -254,40 +273,31 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
       col_row[nt] = (valid ? f / G : r0) - r0;
       col_pos[nt] = __shfl(row_pos, col_row[nt]);
       if (!valid) col_pos[nt] = -1;
-      float most = 0.0f;
-#pragma unroll
-      for (int k = 0; k < 2 * NL; ++k)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          if (!valid || (k >> 1) * 64 + g * 16 >= dh) qx[nt][k][e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) most = fmaxf(most, fabsf(qx[nt][k][e][j]));
-        }
-      most = max_over_groups(most);
+      if constexpr (!QREG) most = fmaxf(stat[0][nt][col], stat[0][NT + nt][col]);
       int ex = 14;
       if (most < INFINITY && most > 0.0f) (void)frexpf(most, &ex);
       ex = max(ex, -100);
-      const float up = ldexpf(1.0f, 14 - ex);
+      if (nt == q_tile) up = ldexpf(1.0f, 14 - ex);
       to_score[nt] = ldexpf(1.0f, ex - 14) * (kLog2e / sqrtf((float)dh));
       m_run[nt] = -INFINITY;
       l_run[nt] = 0.0f;
+    }
 #pragma unroll
-      for (int k = 0; k < 2 * NL; ++k) {
-        half8_t hi, lo;
+    for (int k = 0; k < QF; ++k) {
+      half8_t hi, lo;
 #pragma unroll
-        for (int j = 0; j < 8; j += 2) {
-          half2_t h, l;
-          split(f32x2{qx[nt][k][j >> 2][j & 3] * up, qx[nt][k][j >> 2][(j & 3) + 1] * up}, h, l);
-          hi[j] = h[0], hi[j + 1] = h[1];
-          lo[j] = l[0], lo[j + 1] = l[1];
-        }
-        if constexpr (QREG) {
-          qf[k][0] = hi;
-          qf[k][1] = lo;
-        } else if (wave == nt) {
-          q_lds[((nt * 2 * NL + k) * 2 + 0) * 64 + lane] = hi;
-          q_lds[((nt * 2 * NL + k) * 2 + 1) * 64 + lane] = lo;
-        }
+      for (int j = 0; j < 8; j += 2) {
+        half2_t h, l;
+        split(f32x2{qx[k][j >> 2][j & 3] * up, qx[k][j >> 2][(j & 3) + 1] * up}, h, l);
+        hi[j] = h[0], hi[j + 1] = h[1];
+        lo[j] = l[0], lo[j + 1] = l[1];
+      }
+      if constexpr (QREG) {
+        qf[k][0] = hi;
+        qf[k][1] = lo;
+      } else {
+        q_lds[((q_tile * 2 * NL + q_first + k) * 2 + 0) * 64 + lane] = hi;
+        q_lds[((q_tile * 2 * NL + q_first + k) * 2 + 1) * 64 + lane] = lo;
       }
     }
     if constexpr (!QREG) __syncthreads();
@@ -310,6 +320,7 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
 
     // runs of rows that share a sequence, one after the other
     for (int r = 0; r < n_rows;) {
+      const bool first = r == 0;          // (block ids of the piece's first row are there)
       int seq = r0, longest = __builtin_amdgcn_readfirstlane(row_pos), shortest = longest;
       int limit[NT];
       if constexpr (!SHARED) {
@@ -336,9 +347,9 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
         // and 0.
         const int steps = min(kTableSteps / UNITS, s1 - c0);
         f32x2* const scales = block_scale + mine * (kTableSteps / UNITS * 4);
-        if (SHARED || dealt || c0 > s0) __syncthreads();   // (the tables in front have been read)
+        if (!(SHARED ? first : !dealt) || c0 > s0) __syncthreads();   // (the tables in front have been read)
         for (int i = tid; i < steps * 4; i += kThreads) {
-          const int blk = SHARED || dealt || c0 > 0 || i >= kThreads ? table[min(c0 * 4 + i, last_entry)] : early;
+          const int blk = !(SHARED ? first : !dealt) || c0 > s0 || i >= kThreads ? table[min(c0 * 4 + i, last_entry)] : early;
           block_id[i] = safe_block(blk, a.c.num_blocks);
         }
         __syncthreads();
