@@ -13,11 +13,12 @@
 // several workgroups have, are joined in a fixed order.
 //
 // Single rows are bound by the cache's bytes (head_dim 128, shuffled blocks; a plain read of this card makes 7.0 TB/s): one sequence of 131000 positions,
-// 8 K/V heads, 268 MB: 48.5 us (5.5 TB/s) and 4.9 to join 64 parts; 64 of 2000 to 6000: 95 us (5.5 TB/s) + 6; 32 of 576, 32 heads: 30 us (5.1).
+// 8 K/V heads, 268 MB: 48 us (5.6 TB/s) and 5 to join 64 parts; 64 of 2000 to 6000: 95 us (5.5 TB/s) + 6; 32 of 576, 32 heads: 30 us (5.1).
 // Without products, or without softmax, these times hardly change; two workgroups a compute unit with a step's 16 KB a wavefront in flight are
-// enough, three were no faster.  What is left is the beginning and end of a workgroup, about 4 us each.  512 prompt rows of four prompts up to
-// 3100 positions, 4 heads to a K/V head: 46 us, 25 GFLOP (12.6 in two pieces each): bound by instruction issue (a step is 590 vector and 128
-// matrix instructions).  Weights cost 27 us of the 64 sequences' call: 33 MB of scores written among 524 MB of reads, and 9 to read them.
+// enough, three were no faster.  What is left is the beginning and end of a workgroup, about 2 us each.  512 prompt rows of four prompts up to
+// 3100 positions, 4 heads to a K/V head: 45 us, 25 GFLOP (12.6 in two pieces each): bound by instruction issue (a step is 590 vector and 128
+// matrix instructions), 13 us are beginning and end.  Weights cost 27 us of the 64 sequences' call: 33 MB of scores written among 524 MB of reads (24 us;
+// with stores that are dropped the launch takes 98), and 9 to read them.
 #include "quant.h"
 
 namespace ee {
