@@ -327,6 +327,8 @@ int ee_kv_quant_read(const ee_quant_cache* cache, int32_t layer, const ee_batch*
  * with g = n_heads / n_kv_heads query heads to a K/V head.  Rows that share a sequence (row_table) are a causal chunk of a
  * prompt, and quickest when they stand next to each other.  A row with context_lens[m] < 0 attends nothing: its
  * result is 0.  q and out dev [rows][n_heads][head_dim] float, 16-byte aligned, not overlapping.
+ * Products and sums are float in effect; besides, a channel of q may be off by 2^-38 of the largest in its row and head, a probability times
+ * the scale of its block of V by 2^-37 of the largest such product among the positions that the row attends.
  * weights_out (dev [rows][n_kv_heads][weights_pitch] float, or NULL) receives the attention each cached position got, added
  * over the g heads that share it, for j <= p = context_lens[m]:
  *   weights_out[m][k][j] = weights_in[m][k][j] + sum_g probability   (j < p),   = sum_g probability   (j = p);

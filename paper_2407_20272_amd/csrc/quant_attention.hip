@@ -7,10 +7,16 @@
 //   O += V^T P: 16 channels x 32 positions x 16 columns, contracted over positions 8h..8h+7 of each block: lane (n, g) has those
 //               eight probabilities already, and the bytes of a channel's 16 positions are consecutive in V's blocks.
 // No value crosses lanes but the running maxima, and every load is 16 bytes a lane.  Bytes become fp16 without error.  q (scaled by a power of two
-// to 2^13..2^14) and the probabilities (times the block's scale, relative to the largest scale so far) are split into an fp16 head and
-// remainder, 22 bits together: the products are float in effect, as in the float cache's attention.
+// to 2^13..2^14) and the probabilities (times the block's scale of V, in units of their own) are split into an fp16 head and remainder: 22 bits
+// together, as far as the remainder's last place, 2^-24, allows.  A channel of q is off by 2^-38 of its row's largest at least, a weighted probability by 2^-37
+// of the largest probability times scale that its row has had.
 // Softmax statistics and results are float, running over a wavefront's steps; the wavefronts of a unit, and the parts of a context that
 // several workgroups have, are joined in a fixed order.
+// A column has two references, both whole powers of two, so that changing them rounds nothing:
+//   2^m for the sum: m is 32 below the largest score so far (in units of log 2, rounded up).  A probability is then a float, not 0, down to 2^-158 of
+//       the largest, and a block's scale times 2^(m - ..) stays a float where one with a small scale has the largest score;
+//   2^(m + d - 14) for the result: d follows the blocks' largest scores and scales together, over the positions that the column attends.  With the
+//       largest scale alone, a block that hardly counts (or another sequence's in the tile, or a later one's) would push all others into fp16's last places.
 //
 // Single rows are bound by the cache's bytes (head_dim 128, shuffled blocks; a plain read of this card makes 7.0 TB/s): one sequence of 131000 positions,
 // 8 K/V heads, 268 MB: 48 us (5.6 TB/s) and 5 to join 64 parts; 64 of 2000 to 6000: 95 us (5.5 TB/s) + 6; 32 of 576, 32 heads: 30 us (5.1).
@@ -30,6 +36,7 @@ constexpr int kTableSteps = 256;     // steps whose block ids and scales are in 
 constexpr int kDealtRows = kQuantMostSpans;   // rows (tiles of them) whose steps are dealt out evenly, at most: every workgroup adds up their lengths
 constexpr int kResident = 512;       // workgroups at once: two a compute unit
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kBelow = 32.0f;      // how far a column's reference is below its largest score
 
 // Eight bytes -> eight fp16.
 template <int FMT>
@@ -250,7 +257,7 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
 
     // q, split; the factor that turns a product back into a score in units of log 2
     half8_t qf[QREG ? 2 * NL : 1][2];
-    float to_score[NT], m_run[NT], l_run[NT];
+    float to_score[NT], m_run[NT], l_run[NT], d_run[NT];
     int col_row[NT], col_pos[NT];
     float most = 0.0f;
 #pragma unroll
@@ -280,7 +287,7 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
       ex = max(ex, -100);
       if (nt == q_tile) up = ldexpf(1.0f, 14 - ex);
       to_score[nt] = ldexpf(1.0f, ex - 14) * (kLog2e / sqrtf((float)dh));
-      m_run[nt] = -INFINITY;
+      m_run[nt] = d_run[nt] = -INFINITY;
       l_run[nt] = 0.0f;
     }
 #pragma unroll
@@ -308,7 +315,6 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) o[ct][nt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    float v_ref = 0.0f, v_up = 0.0f;      // the power of two that is at least every scale of V so far; 2^14 / v_ref
 
     // The scores' rows of the piece's columns.  A wavefront collects 16 rows of 64 in LDS before it stores them: stores are counted in line with loads,
     // and one in every step holds up the bytes behind it.
@@ -384,22 +390,6 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
         if (place < steps * 4) scales[place] = own_scale;
         for (int i = place + 64 * KW; i < steps * 4; i += 64 * KW) scales[i] = scales_of(i);
         __syncthreads();
-        // results are kept relative to the largest scale of V so far
-        float most_v = 0.0f;
-        for (int i = lane; i < steps * 4; i += 64) most_v = fmaxf(most_v, scales[i][1]);
-        most_v = __builtin_bit_cast(float, wave_max(__builtin_bit_cast(uint32_t, most_v)));
-        if (most_v > v_ref) {
-          int e;
-          (void)frexpf(most_v, &e);
-          const float next = ldexpf(1.0f, max(-100, min(e, 127)));
-          const float f = v_ref / next;
-          v_ref = next;
-          v_up = 16384.0f / next;
-#pragma unroll
-          for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) o[ct][nt] *= f;
-        }
         // a step asks for the next one's bytes as soon as its own have been used
         for (int s = turn; s < steps; s += KW) {
           const bool more = s + KW < steps;
@@ -437,14 +427,15 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
           load_k(k_blk, more);
           __builtin_amdgcn_sched_barrier(0);
           const bool ragged = (c0 + s) * 64 + 63 > shortest;   // some positions are behind some column's last one
+          const int v_exponent = __builtin_amdgcn_frexp_expf(sc[1]);   // sc[1] is below two to it
           half8_t ph[NT][2], pl[NT][2];
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
             // scales are positive: the largest product gives the largest score.  A block without a position for a column has
             // none of its scales in the column's result.
-            float f = sc[0] * to_score[nt], v_factor = sc[1] * v_up;
+            float f = sc[0] * to_score[nt];
             if (ragged) {
-              if (pos0 > limit[nt]) f = 1.0f, v_factor = 0.0f;
+              if (pos0 > limit[nt]) f = 1.0f;
               if (f == 0.0f) f = kQuantScaleFloor;   // (times minus infinity)
 #pragma unroll
               for (int i = 0; i < 4; ++i)
@@ -463,14 +454,26 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
                 for (int i = 0; i < 4; ++i) collected[((col << held_shift) + held) * 16 + ((g * 4 + i) ^ col)] = sd[nt][i] * f;
               }
             }
-            const float m_new = fmaxf(m_run[nt], max_over_groups(mx * f));
+            const float top = mx * f;              // of this lane's block
+            const float m_new = fmaxf(m_run[nt], ceilf(max_over_groups(top)) - kBelow);
             const float base = m_new == -INFINITY ? 0.0f : m_new;
             const float alpha = __builtin_amdgcn_exp2f(m_run[nt] - base);
-            if (__any(m_new != m_run[nt])) {
-#pragma unroll
-              for (int ct = 0; ct < CT; ++ct) o[ct][nt] *= alpha;
-            }
+            d_run[nt] += m_run[nt] - base;
             m_run[nt] = m_new;
+            // What the block adds to the result is below 2^adds times its bytes.  The unit is kept until that is past twice the unit; then a column that needs it
+            // takes another one.
+            const float adds = top - base + (float)v_exponent;
+            if (__any(adds > d_run[nt] + 1.0f)) {
+              const float reach = ceilf(max_over_groups(adds));
+              const float d_new = reach > d_run[nt] + 1.0f ? reach : d_run[nt];
+              const float beta = __builtin_amdgcn_exp2f(d_run[nt] - (d_new == -INFINITY ? 0.0f : d_new));
+#pragma unroll
+              for (int ct = 0; ct < CT; ++ct) o[ct][nt] *= beta;
+              d_run[nt] = d_new;
+            }
+            // (bounded where the probabilities are 0: those have to stay so)
+            float v_factor = __builtin_ldexpf(sc[1], min(14 - (int)fmaxf(d_run[nt], -1000.0f), 127 - v_exponent));
+            if (ragged && pos0 > limit[nt]) v_factor = 0.0f;
             float sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -555,9 +558,13 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
       for (int w = 0; w < KW; ++w) ll += stat[1][mine * KW + w][nt * 16 + col] * __builtin_amdgcn_exp2f(stat[0][mine * KW + w][nt * 16 + col] - base);
       m_all[nt] = mm;
       l_all[nt] = ll;
-      const float f = __builtin_amdgcn_exp2f(m_run[nt] - base) * v_ref * (1.0f / 16384.0f);
+      // divided by the sum first (the largest values' sums would be no floats), then in units of 1
+      const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
+      const int unit = (int)fmaxf(m_run[nt] - base + d_run[nt], -1000.0f) - 14;
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) o[ct][nt] *= f;
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[ct][nt][e] = __builtin_ldexpf(o[ct][nt][e] * inv, unit);
     }
     const bool whole = SHARED ? a.parts == nullptr : s0 == 0 && s1 == unit_steps;
     const bool leaves_part = SHARED ? !whole : !whole || (WEIGHTS && (dealt || tiles > 1));
@@ -581,10 +588,7 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
           if (f >= f1 || ch >= dh) continue;
           const int m = f / G;
           const size_t row = (size_t)m * a.n_heads + hk * G + (f - m * G);
-          if (whole) {
-            const float inv = l_all[nt] == 0.0f ? 0.0f : 1.0f / l_all[nt];
-            *reinterpret_cast<f32x4*>(a.out + row * dh + ch) = sum * inv;
-          }
+          if (whole) *reinterpret_cast<f32x4*>(a.out + row * dh + ch) = sum;
           if (leaves_part) {
             const size_t slot = SHARED ? row * a.n_parts + blockIdx.z
                                        : ((size_t)hk * a.slots + unit + (dealt ? worker : 0)) * unit_columns(G) + col;
@@ -621,7 +625,7 @@ template <bool SHARED, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void quant_join_kernel(QuantAttnArgs a) {
   extern __shared__ f32x2 head_stat[];   // [G] maximum, 1 / sum
   __shared__ f32x4 meet[WAVES][64];
-  __shared__ float factors[kMostParts];
+  __shared__ float shares[kMostParts];
   const int m = blockIdx.y, G = a.n_heads / a.c.heads, dh = a.c.dh, tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int tiles = SHARED ? 1 : unit_tiles(G);
@@ -645,7 +649,7 @@ __global__ __launch_bounds__(64 * WAVES) void quant_join_kernel(QuantAttnArgs a)
       return a.parts + (((size_t)hk * a.slots + slot) * unit_columns(G) + h % 16) * (dh + 4);
     }
   };
-  // maximum and sum over a head's parts, and the parts' factors relative to the maximum
+  // maximum and sum over a head's parts, and the parts' shares of the sum (before the division by it)
   auto statistics = [&](const float* p, int n, bool keep) {
     float mm = -INFINITY, sum = 0.0f;
     for (int z = lane; z < n; z += 64) mm = fmaxf(mm, p[z * pitch]);
@@ -654,9 +658,9 @@ __global__ __launch_bounds__(64 * WAVES) void quant_join_kernel(QuantAttnArgs a)
     const float base = mm == -INFINITY ? 0.0f : mm;
     for (int z = lane; z < n; z += 64) {
       const f32x2 st = *reinterpret_cast<const f32x2*>(p + z * pitch);
-      const float f = __builtin_amdgcn_exp2f(st[0] - base);
-      sum += st[1] * f;
-      if (keep) factors[z] = f;
+      const float share = st[1] * __builtin_amdgcn_exp2f(st[0] - base);
+      sum += share;
+      if (keep) shares[z] = share;
     }
 #pragma unroll
     for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x);
@@ -671,20 +675,21 @@ __global__ __launch_bounds__(64 * WAVES) void quant_join_kernel(QuantAttnArgs a)
     if (n == 0 || (!SHARED && n == 1)) return;   // (whole contexts have their results)
     const f32x2 st = statistics(p, n, wave == 0);
     __syncthreads();
+    const float inv = st[1] == 0.0f ? 0.0f : 1.0f / st[1];
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int z0 = wave; z0 < n; z0 += 4 * WAVES) {   // four parts in flight (behind the last: that one again, times 0)
       f32x4 x[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[e] = *reinterpret_cast<const f32x4*>(p + min(z0 + e * WAVES, n - 1) * pitch + 4 + c);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o += x[e] * (z0 + e * WAVES < n ? factors[z0 + e * WAVES] : 0.0f);
+      for (int e = 0; e < 4; ++e) o += x[e] * (z0 + e * WAVES < n ? shares[z0 + e * WAVES] * inv : 0.0f);
     }
     meet[wave][lane] = o;
     __syncthreads();
     if (wave || lane * 4 >= dh) return;
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) o += meet[w][lane];
-    *reinterpret_cast<f32x4*>(out + c) = o * (st[1] == 0.0f ? 0.0f : 1.0f / st[1]);
+    *reinterpret_cast<f32x4*>(out + c) = o;
     return;
   }
   const int hk = job / chunks;
