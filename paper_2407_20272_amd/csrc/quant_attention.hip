@@ -36,6 +36,8 @@ constexpr int kTableSteps = 256;     // steps whose block ids and scales are in 
 constexpr int kDealtRows = kQuantMostSpans;   // rows (tiles of them) whose steps are dealt out evenly, at most: every workgroup adds up their lengths
 constexpr int kResident = 512;       // workgroups at once: two a compute unit
 constexpr float kLog2e = 1.4426950408889634f;
+// Scores beyond this are rounded before the reference is taken off, as the largest one was; a fused subtraction would leave what that rounding took, a large number.
+constexpr float kLargeScore = 1048576.0f;
 constexpr float kBelow = 32.0f;      // how far a column's reference is below its largest score
 
 // Eight bytes -> eight fp16.
@@ -455,6 +457,11 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
               }
             }
             const float top = mx * f;              // of this lane's block
+            if (__any(fabsf(top) > kLargeScore && fabsf(top) < INFINITY)) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) sd[nt][i] *= f;
+              f = 1.0f;
+            }
             const float m_new = fmaxf(m_run[nt], ceilf(max_over_groups(top)) - kBelow);
             const float base = m_new == -INFINITY ? 0.0f : m_new;
             const float alpha = __builtin_amdgcn_exp2f(m_run[nt] - base);

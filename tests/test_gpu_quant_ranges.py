@@ -145,3 +145,27 @@ def test_values_next_to_the_largest_float(fmt, shared, n):
     out = T.attend(kv, 1, q.cuda(), [n - 1], tables, [0] if shared else None)
     check(kv, 1, q, out, [n - 1], tables, [0] if shared else None)
     assert bool(torch.isfinite(out).all())
+
+
+@pytest.mark.parametrize("fmt", T.FORMATS)
+@pytest.mark.parametrize("n,shared", [(300, False), (300, True), (3000, False), (3000, True)])
+def test_scores_of_any_size(fmt, n, shared):
+    """Scores of 10^8 and more, beside small scales of V: the position with the largest one is the result, and has the attention."""
+    tables, nb = T.tables_for([n], 2)
+    kv = T.filled(1, nb, 1, 64, fmt, 2)
+    kv.scales[..., 1] *= 2.0 ** -30
+    q = torch.randn(1, 2, 64, generator=T.gen(1))
+    q[0, 1] = q[0, 0] * 3.0
+    c = Q.Cache.of(kv)
+    z = c.gather(0, tables[0], 0, n) @ q[0, 0].double()
+    top = z.topk(2)
+    # (float scores: 2^-16 of the largest apart is far more than their errors, and e^(-z) of it is nothing)
+    assert float(top.values[0] - top.values[1]) > 2.0 ** -16 * float(z.abs().max())
+    best = int(top.indices[0])
+    want = c.gather(1, tables[0], 0, n)[best]
+    for size in (1e8, 1e12, 1e30):
+        w = None if shared else torch.full((1, 1, n), 7.0, device="cuda")
+        out = T.attend(kv, 1, (q * size).cuda(), [n - 1], tables, [0] if shared else None, weights=w).cpu().double()
+        assert bool(((out[0] - want).abs() <= want.abs() * 2.0 ** -20 + 1e-37).all())
+        if not shared:
+            assert bool(((w[0, 0].cpu().double() - 2.0 * (torch.arange(n) == best)).abs() <= 2.0 ** -20).all())
