@@ -307,6 +307,7 @@ typedef struct ee_quant_cache {
  * A block's scale is the smallest with which the largest magnitude ever appended to it fits,
  *   INT8: float(largest / 127), at least 2^-126;   E4M3: the smallest power of two with largest <= 448 * scale, at least
  *   2^-126,
+ * (the largest float included: INT8 scales end at 0x1.020406p+121, 127 times which is a float, and with 2^120, E4M3's last one, bytes end at 240)
  * and the first position of a block starts anew, whatever the block held.  Where a call makes a block's scale grow, the
  * positions in front of the call's are rounded again, from the floats their bytes stood for.  Every rounding is to the
  * nearest, ties to even, of the exact quotient.  An infinity or NaN makes the block's scale NaN (every result that

@@ -21,12 +21,16 @@ __device__ inline f32x2 byte_pair(uint32_t two) {   // bytes 0 and 1
   }
 }
 
+// The largest scales: 127 times this one is still a float; with the other a byte may be 240 at most (256 times it is none, the largest float divided by it is
+// next to 256).
+constexpr float kInt8ScaleMost = 0x1.020406p+121f, kE4m3ScaleMost = 0x1p120f;
+
 // The smallest scale with which `largest` fits; NaN for an infinity or NaN (a magnitude's bits are ordered as integers).
 template <int FMT>
 __device__ inline float scale_for(float largest) {
   if (!(largest < INFINITY)) return __builtin_nanf("");
   if constexpr (FMT == EE_QUANT_INT8) {
-    return fmaxf(largest / 127.0f, kQuantScaleFloor);
+    return fminf(fmaxf(largest / 127.0f, kQuantScaleFloor), kInt8ScaleMost);
   } else {
     int e;
     const float m = frexpf(largest, &e);             // 448 = 0.875 * 2^9
@@ -47,6 +51,14 @@ __device__ inline void quantise(F&& value, uint32_t (&out)[N], float s, float in
     return;
   }
   if constexpr (FMT == EE_QUANT_E4M3) {
+    if (s >= kE4m3ScaleMost) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const f32x2 x = value(i);
+        out[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(fminf(fmaxf(x[0] * inv, -240.0f), 240.0f), fminf(fmaxf(x[1] * inv, -240.0f), 240.0f), 0, false) & 0xffff;
+      }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const f32x2 x = value(i);
