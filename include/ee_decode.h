@@ -336,9 +336,10 @@ int ee_kv_quant_read(const ee_quant_cache* cache, int32_t layer, const ee_batch*
  * what lies behind is left as it was.  weights_in (same pitch) may be weights_out, or NULL for zeros.  Not with
  * row_table (EE_ERR_UNSUPPORTED).  weights_pitch >= max_context.
  * (weights_in and weights_out must not overlap in another way than being the same.)
+ * A call has at most 65535 / ceil(g / 16) rows, with row_table 65535 * 32 / g.
  * workspace: ee_paged_attention_quant_bytes for the call's sizes or larger ones, 256-byte aligned; it needs no
  * initialisation and is dead between calls.  (Short contexts need none: NULL is refused only where something is needed.)
- * The bytes are 0 only for sizes that are refused. */
+ * The bytes are 0 only for sizes that are refused (of rows: that the call refuses with row_table, or, with_weights, without). */
 size_t ee_paged_attention_quant_bytes(const ee_quant_cache* cache, int32_t n_heads, int32_t max_batch, int32_t max_context,
                                       int32_t with_weights);
 int ee_paged_attention_quant(const ee_quant_cache* cache, int32_t layer, int32_t n_heads, const float* q,

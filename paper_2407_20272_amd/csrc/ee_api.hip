@@ -1048,6 +1048,11 @@ int check_quant_cache(const ee_quant_cache* C) {
   return EE_OK;
 }
 
+int check_quant_rows(int rows, int kv_heads) {
+  if ((int64_t)rows * kv_heads > (1 << 29)) EE_FAIL(EE_ERR_UNSUPPORTED, "%d rows of %d heads in one call", rows, kv_heads);
+  return EE_OK;
+}
+
 int check_quant_call(const ee_quant_cache* C, int32_t layer, const ee_batch* Bt, QuantCache* c, QuantRows* r) {
   int rc;
   if ((rc = check_quant_cache(C)) || (rc = check_batch(Bt, false))) return rc;
@@ -1056,8 +1061,7 @@ int check_quant_call(const ee_quant_cache* C, int32_t layer, const ee_batch* Bt,
   *c = QuantCache{reinterpret_cast<int8_t*>(C->k_pool) + units * 16 * C->head_dim, reinterpret_cast<int8_t*>(C->v_pool) + units * 16 * C->head_dim,
                   C->scales + units * 2, C->num_blocks, C->n_kv_heads, C->head_dim, C->format};
   *r = QuantRows{Bt->context_lens, Bt->block_tables, Bt->row_table, Bt->batch, Bt->max_blocks};
-  if ((int64_t)Bt->batch * C->n_kv_heads > (1 << 29)) EE_FAIL(EE_ERR_UNSUPPORTED, "%d rows of %d heads in one call", Bt->batch, C->n_kv_heads);
-  return EE_OK;
+  return check_quant_rows(Bt->batch, C->n_kv_heads);
 }
 
 int check_pair_type(int32_t dtype, const void* a, const void* b, const char* what) {
@@ -1071,6 +1075,13 @@ int check_pair_type(int32_t dtype, const void* a, const void* b, const char* wha
 int check_quant_heads(const ee_quant_cache* C, int32_t n_heads) {
   if (n_heads < 1 || n_heads % C->n_kv_heads) EE_FAIL(EE_ERR_SHAPE, "n_heads %d is no multiple of n_kv_heads %d", n_heads, C->n_kv_heads);
   if (n_heads / C->n_kv_heads > 1024 || n_heads > 65536) EE_FAIL(EE_ERR_UNSUPPORTED, "%d heads over %d K/V heads", n_heads, C->n_kv_heads);
+  return EE_OK;
+}
+
+// A launch of the attention has its tiles in the second dimension.
+int check_attended_rows(int rows, int n_heads, int kv_heads, bool row_table) {
+  const int64_t tiles = quant_attn_tiles(rows, n_heads / kv_heads, row_table);
+  if (tiles > 65535) EE_FAIL(EE_ERR_UNSUPPORTED, "attention: %d rows of %d heads over %d in one call", rows, n_heads, kv_heads);
   return EE_OK;
 }
 
@@ -1176,6 +1187,8 @@ size_t ee_paged_attention_quant_bytes(const ee_quant_cache* cache, int32_t n_hea
     set_error("ee_paged_attention_quant_bytes: batch %d, context %d", max_batch, max_context);
     return 0;
   }
+  // (rows that share sequences may be more; weights are not for those)
+  if (check_quant_rows(max_batch, cache->n_kv_heads) || check_attended_rows(max_batch, n_heads, cache->n_kv_heads, !with_weights)) return 0;
   const QuantCache c{nullptr, nullptr, nullptr, 0, cache->n_kv_heads, cache->head_dim, cache->format};
   const size_t parts = align256(quant_attn_part_floats(c, n_heads, max_batch, max_context, with_weights != 0) * sizeof(float));
   // (only with parts: the spans of dealt-out rows)
@@ -1208,8 +1221,7 @@ int ee_paged_attention_quant(const ee_quant_cache* cache, int32_t layer, int32_t
   a.weights_in = weights_in;
   a.weights_out = weights_out;
   a.weights_pitch = weights_pitch;
-  if ((int64_t)batch->batch * ((n_heads + 15) / 16) > 65535)   // (the launch's second dimension)
-    EE_FAIL(EE_ERR_UNSUPPORTED, "ee_paged_attention_quant: %d rows of %d heads in one call", batch->batch, n_heads);
+  if ((rc = check_attended_rows(batch->batch, n_heads, cache->n_kv_heads, batch->row_table != nullptr))) return rc;
   size_t spans;
   const size_t part_bytes = align256(quant_attn_plan(a, &spans) * sizeof(float)), span_bytes = align256(spans * sizeof(int2));
   const size_t score_bytes = weights_out ? align256((size_t)batch->batch * n_heads * quant_score_pitch(a.max_context) * sizeof(float)) : 0;

@@ -108,6 +108,8 @@ __host__ __device__ inline size_t quant_score_pitch(int max_context) { return (s
 size_t quant_attn_plan(QuantAttnArgs& a, size_t* spans);
 size_t quant_attn_part_floats(const QuantCache& c, int n_heads, int max_rows, int max_context, bool weights);
 constexpr int kQuantMostSpans = 1024;
+// Tiles of a K/V head: of up to 16 heads of one row, or of 32 (row, head) pairs with row_table.
+int64_t quant_attn_tiles(int rows, int group, bool row_table);
 void launch_quant_attention(const QuantAttnArgs& a, hipStream_t st);
 
 #ifdef __HIPCC__

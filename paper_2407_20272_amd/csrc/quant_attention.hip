@@ -763,16 +763,18 @@ int deal_workgroups(int kv) { return kResident / kv > 1 ? kResident / kv : 1; }
 // Contexts of up to 16 steps are whole pieces: a workgroup's four wavefronts have four steps each, which takes no longer than a second launch
 // would.  With four times the resident workgroups in whole contexts, the order in which they end evens them out.
 bool deals(int rows, int group, int kv, int steps) {
-  const int64_t units = (int64_t)rows * unit_tiles(group);
+  const int64_t units = quant_attn_tiles(rows, group, false);
   return steps > 16 && units <= kDealtRows && units * kv < 4 * kResident;
 }
 int shared_parts(int rows, int group, int kv, int steps) {
-  const int64_t units = ((int64_t)rows * group + 31) / 32 * kv, want = kResident / units, most = steps / kWaves;
+  const int64_t units = quant_attn_tiles(rows, group, true) * kv, want = kResident / units, most = steps / kWaves;
   const int64_t parts = want < most ? want : most;
   return (int)(parts < 1 ? 1 : parts > kSharedParts ? kSharedParts : parts);
 }
 
 }  // namespace
+
+int64_t quant_attn_tiles(int rows, int group, bool row_table) { return row_table ? ((int64_t)rows * group + 31) / 32 : (int64_t)rows * unit_tiles(group); }
 
 size_t quant_attn_plan(QuantAttnArgs& a, size_t* spans) {
   *spans = 0;
@@ -800,7 +802,7 @@ size_t quant_attn_plan(QuantAttnArgs& a, size_t* spans) {
 size_t quant_attn_part_floats(const QuantCache& c, int n_heads, int max_rows, int max_context, bool weights) {
   const int steps = (max_context + 63) / 64, G = n_heads / c.heads, kv = c.heads;
   const size_t record = c.dh + 4, columns = (size_t)kv * unit_columns(G);
-  const int64_t units = (int64_t)max_rows * unit_tiles(G);
+  const int64_t units = quant_attn_tiles(max_rows, G, false);
   size_t most = weights ? (size_t)units * columns * record : 0;
   if (steps > 16) {
     // dealt out: units in front of the bounds of `deals`
@@ -821,7 +823,7 @@ size_t quant_attn_part_floats(const QuantCache& c, int n_heads, int max_rows, in
 
 void launch_quant_attention(const QuantAttnArgs& a, hipStream_t st) {
   const int G = a.n_heads / a.c.heads;
-  const int y = a.r.row_table ? (int)(((int64_t)a.r.rows * G + 31) / 32) : a.dealt ? a.dealt : a.r.rows * unit_tiles(G);
+  const int y = a.dealt ? a.dealt : (int)quant_attn_tiles(a.r.rows, G, a.r.row_table != nullptr);
   const dim3 grid(a.c.heads, y, a.n_parts);
   a.c.format == EE_QUANT_INT8 ? launch_format<EE_QUANT_INT8>(a, grid, st) : launch_format<EE_QUANT_E4M3>(a, grid, st);
   if (!a.parts) return;

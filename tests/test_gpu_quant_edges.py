@@ -40,3 +40,40 @@ def test_the_largest_float(fmt, later):
     B.ee_kv_quant_evict(kv, 1, B.make_batch(None, T.i32([20]), T.i32(tables), 20), torch.ones(1, 1, 20, device="cuda"), None, 20, 0, kept, lens, None, T.i32(dst))
     assert kept[0, 0].tolist() == list(range(20))
     check(dst)
+
+
+def some_of(kv, q, out, lens, tables, rows, heads, row_table=None):
+    """A few rows and K/V heads (one query head each) against the definition."""
+    c = Q.Cache.of(kv)
+    part = Q.Cache(c.k[:, heads], c.v[:, heads], c.scales[:, heads], c.fmt)
+    seq = [row_table[m] if row_table is not None else m for m in rows]
+    want, probs, bound = Q.attention(part, q[rows][:, heads].double(), [lens[m] for m in rows], tables, seq)
+    assert bool(((out[rows][:, heads].cpu().double() - want).abs() <= bound).all())
+    return probs
+
+
+def test_attention_of_tens_of_thousands_of_sequences():
+    heads, rows, most = 32, 33001, 40
+    kv = T.filled(1, 50, heads, 16, "int8", 1)
+    tables = torch.randint(0, 50, (rows, 3), generator=T.gen(2), dtype=torch.int32)       # (reading shares blocks)
+    lens = torch.randint(-1, most, (rows,), generator=T.gen(3)).tolist()
+    q = torch.randn(rows, heads, 16, generator=T.gen(4))
+    w = torch.full((rows, heads, most), 2.0, device="cuda")
+    out = T.attend(kv, 1, q.cuda(), lens, tables, weights=w, max_context=most)
+    some = [0, 1, 32767, 32768, 32769, 33000] + [m for m in range(40, 33000, 1500)]
+    probs = some_of(kv, q, out, lens, tables, some, [0, 17, 31])
+    for m, (p, slack) in zip(some, probs):
+        n = lens[m] + 1
+        assert bool(((w[m, [0, 17, 31], :n].cpu().double() - p).abs() <= p * slack[:, None] + p * 2.0 ** -22 + 1e-37).all())
+        assert bool((w[m, :, n:] == 2.0).all())
+
+
+def test_attention_of_a_long_prompt_chunk():
+    """More rows than 8191 of 128 heads: 282 tiles."""
+    heads, chunk = 128, [3000, 5, 6000]
+    tables, nb = T.tables_for(chunk, 1)
+    kv = T.filled(1, nb, heads, 16, "e4m3", 1)
+    lens, rt = [p for n in chunk for p in range(n)], [i for i, n in enumerate(chunk) for _ in range(n)]
+    q = torch.randn(len(lens), heads, 16, generator=T.gen(4))
+    out = T.attend(kv, 1, q.cuda(), lens, tables, rt)
+    some_of(kv, q, out, lens, tables, [0, 1, 2999, 3000, 3004, 3005, 8190, 8191, 8192, 9004], [0, 64, 127], rt)
