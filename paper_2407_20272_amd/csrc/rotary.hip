@@ -40,7 +40,7 @@ struct alignas(sizeof(T) * N) Piece {
 // head.  Bound by memory: it reads and writes every element once.  4096 rows of 40 heads of 128 bf16 channels, 84 MB: 15 us, 5.6 TB/s (a large copy
 // makes 5.1); one row of 64 heads 2.9 us, an empty launch 2.
 template <class T, int LAYOUT, int VEC>
-__global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, int rows_per_wg, int tasks_per_row) {
+__global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, int rows_per_wg, int tasks_per_row, int tasks_per_wg) {
   extern __shared__ float2 turn[];   // [rows_per_wg][rotary_dim / 2]
   const int pairs = a.rotary_dim / 2;
   const int m0 = blockIdx.x * rows_per_wg;
@@ -58,7 +58,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, int rows
   constexpr int STEP = LAYOUT == EE_ROTARY_HALF ? VEC : (VEC == 1 ? 2 : VEC);   // channels (of a half) that a rotated piece covers
   const int span = LAYOUT == EE_ROTARY_HALF ? pairs : a.rotary_dim;
   const int turned = span / STEP, pieces = turned + (a.head_dim - a.rotary_dim) / VEC;
-  const int first = blockIdx.y * kTasks, last = min(first + kTasks, tasks_per_row);
+  const int first = blockIdx.y * tasks_per_wg, last = min(first + tasks_per_wg, tasks_per_row);
   const int n = last - first;
   for (int i = threadIdx.x; i < n * n_rows; i += kThreads) {
     const int m = i / n, task = first + (i - m * n);
@@ -112,8 +112,20 @@ void launch(const RotaryArgs& a, hipStream_t st) {
   const int tasks = (a.q.n_heads + a.k.n_heads) * (span / step + (a.head_dim - a.rotary_dim) / VEC);
   int rows = kTasks / tasks;   // rows of few pieces share a workgroup
   rows = rows < 1 ? 1 : rows > kMaxRows ? kMaxRows : rows;
-  const dim3 grid((a.rows + rows - 1) / rows, (tasks + kTasks - 1) / kTasks);
-  rotary_kernel<T, LAYOUT, VEC><<<grid, kThreads, (size_t)rows * (a.rotary_dim / 2) * sizeof(float2), st>>>(a, rows, tasks);
+  // A launch has at most 65535 workgroups in the second dimension, and fewer than 2^32 threads in the first.
+  const int each = tasks > kTasks * 65535 ? (tasks + 65534) / 65535 : kTasks;
+  const int64_t slice = (int64_t)((1 << 24) - 1) * rows;
+  for (int64_t m = 0; m < a.rows; m += slice) {
+    RotaryArgs part = a;
+    part.positions += m;
+    part.rows = (int)(a.rows - m < slice ? a.rows - m : slice);
+    for (RotaryRows* r : {&part.q, &part.k}) {
+      r->in = reinterpret_cast<const T*>(r->in) + m * r->in_stride;
+      r->out = reinterpret_cast<T*>(r->out) + m * r->out_stride;
+    }
+    const dim3 grid((int)(((int64_t)part.rows + rows - 1) / rows), (tasks + each - 1) / each);
+    rotary_kernel<T, LAYOUT, VEC><<<grid, kThreads, (size_t)rows * (a.rotary_dim / 2) * sizeof(float2), st>>>(part, rows, tasks, each);
+  }
 }
 
 bool aligned(const RotaryRows& r, int size, int vec) {

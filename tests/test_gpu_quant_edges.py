@@ -1,4 +1,6 @@
 """The 8-bit cache at the borders of what its calls take: the largest floats, rows of no sequence."""
+import math
+
 import pytest
 import torch
 
@@ -77,3 +79,29 @@ def test_attention_of_a_long_prompt_chunk():
     q = torch.randn(len(lens), heads, 16, generator=T.gen(4))
     out = T.attend(kv, 1, q.cuda(), lens, tables, rt)
     some_of(kv, q, out, lens, tables, [0, 1, 2999, 3000, 3004, 3005, 8190, 8191, 8192, 9004], [0, 64, 127], rt)
+
+
+def test_rotary_of_more_rows_than_one_launch_has():
+    rows = (1 << 27) + 9
+    desc = B.make_rotary_desc(2)
+    freqs = B.ee_rotary_frequencies(desc)
+    pos = torch.arange(rows, dtype=torch.int32, device="cuda")
+    x = torch.tensor([1.0, 0.0], dtype=torch.bfloat16, device="cuda").repeat(rows).view(rows, 1, 2)
+    B.ee_rotary(desc, freqs, pos, x, x)
+    for m in (0, 1, 1000, (1 << 27) - 9, (1 << 27) - 8, 1 << 27, rows - 1):
+        want = torch.stack([torch.cos(pos[m].double()), torch.sin(pos[m].double())])
+        assert bool(((x[m, 0].double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -20).all()), m
+
+
+def test_rotary_of_more_pieces_than_one_launch_has():
+    """A row of 65536 query and 65536 key heads of 1024 channels, of which two are rotated: element by element."""
+    desc = B.make_rotary_desc(1024, 2)
+    freqs = B.ee_rotary_frequencies(desc)
+    pos = torch.tensor([3], dtype=torch.int32, device="cuda")
+    q, k = (torch.full((1, 65536, 1024), float(n), device="cuda") for n in (1, 2))
+    q_out, k_out = torch.zeros_like(q), torch.zeros_like(k)
+    B.ee_rotary(desc, freqs, pos, q, q_out, k, k_out)
+    c, s = math.cos(3.0), math.sin(3.0)
+    for out, n in ((q_out, 1.0), (k_out, 2.0)):
+        assert bool((out[..., 2:] == n).all())
+        assert bool(((out[..., 0].double() - n * (c - s)).abs() <= n * 2.0 ** -20).all()) and bool(((out[..., 1].double() - n * (c + s)).abs() <= n * 2.0 ** -20).all())
