@@ -286,9 +286,9 @@ __device__ inline void append_positions(const QuantAppendArgs& a, const Run& run
 // 2103 bf16 rows of 32 heads of 128 channels, E4M3: 17 us, 52 MB (3 TB/s; INT8 22); 256 rows of 256 sequences, 8 heads: 7.5 us, of which an empty
 // launch takes 2 and three dependent loads most of the rest.
 template <int FMT, class T, int CP>
-__global__ __launch_bounds__(kThreads) void quant_append_kernel(QuantAppendArgs a, int group) {
+__global__ __launch_bounds__(kThreads) void quant_append_kernel(QuantAppendArgs a, int group, int first) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Runs runs(a.r, blockIdx.x * group, group);
+  const Runs runs(a.r, (first + blockIdx.x) * group, group);
   const int head = blockIdx.y * 2 + (wave >> 1);
   if (head >= a.c.heads) return;
   for (uint64_t left = runs.first; left; left &= left - 1) {
@@ -348,9 +348,9 @@ __device__ inline void read_run(const QuantReadArgs& a, const Run& run, int head
 
 // Bound by what it writes: the same 2103 rows and what stands in their blocks as floats, 17 MB read and 70 MB written, 17 us.
 template <int FMT, class T, int CP>
-__global__ __launch_bounds__(kThreads) void quant_read_kernel(QuantReadArgs a, int group) {
+__global__ __launch_bounds__(kThreads) void quant_read_kernel(QuantReadArgs a, int group, int first) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Runs runs(a.r, blockIdx.x * group, group);
+  const Runs runs(a.r, (first + blockIdx.x) * group, group);
   const int head = blockIdx.y * 2 + (wave >> 1);
   if (head >= a.c.heads) return;
   for (uint64_t left = runs.first; left; left &= left - 1) read_run<FMT, T, CP>(a, runs.of(__ffsll((unsigned long long)left) - 1), head, wave & 1);
@@ -637,18 +637,24 @@ __global__ __launch_bounds__(kThreads) void quant_place_kernel(QuantEvictArgs a,
   if (lane == 0) a.c.scales[unit * 2 + which] = a.image_scales[from];
 }
 
+// A launch has fewer than 2^32 threads a dimension.
+constexpr int kLaunchGroups = (1 << 24) - 1;
+template <class F>
+void for_groups(const QuantRows& r, int heads, F&& launch) {
+  const int group = r.row_table ? kGroup : 1, all = (int)(((int64_t)r.rows + group - 1) / group);
+  for (int first = 0; first < all; first += kLaunchGroups) launch(dim3(min(all - first, kLaunchGroups), (heads + 1) / 2), group, first);
+}
+
 int groups(int64_t tasks) { return (int)((tasks + kThreads / 64 - 1) / (kThreads / 64)); }
 
 }  // namespace
 
 template <int FMT, class T>
 static void append_as(const QuantAppendArgs& a, hipStream_t st) {
-  const int group = a.r.row_table ? kGroup : 1;
-  const dim3 grid((a.r.rows + group - 1) / group, (a.c.heads + 1) / 2);
   if (a.c.dh <= 128)
-    quant_append_kernel<FMT, T, 1><<<grid, kThreads, 0, st>>>(a, group);
+    for_groups(a.r, a.c.heads, [&](dim3 grid, int group, int first) { quant_append_kernel<FMT, T, 1><<<grid, kThreads, 0, st>>>(a, group, first); });
   else
-    quant_append_kernel<FMT, T, 2><<<grid, kThreads, 0, st>>>(a, group);
+    for_groups(a.r, a.c.heads, [&](dim3 grid, int group, int first) { quant_append_kernel<FMT, T, 2><<<grid, kThreads, 0, st>>>(a, group, first); });
 }
 void launch_quant_append(const QuantAppendArgs& a, int dtype, hipStream_t st) {
   if (a.c.format == EE_QUANT_INT8)
@@ -659,12 +665,10 @@ void launch_quant_append(const QuantAppendArgs& a, int dtype, hipStream_t st) {
 
 template <int FMT, class T>
 static void read_as(const QuantReadArgs& a, hipStream_t st) {
-  const int group = a.r.row_table ? kGroup : 1;
-  const dim3 grid((a.r.rows + group - 1) / group, (a.c.heads + 1) / 2);
   if (a.c.dh <= 128)
-    quant_read_kernel<FMT, T, 1><<<grid, kThreads, 0, st>>>(a, group);
+    for_groups(a.r, a.c.heads, [&](dim3 grid, int group, int first) { quant_read_kernel<FMT, T, 1><<<grid, kThreads, 0, st>>>(a, group, first); });
   else
-    quant_read_kernel<FMT, T, 2><<<grid, kThreads, 0, st>>>(a, group);
+    for_groups(a.r, a.c.heads, [&](dim3 grid, int group, int first) { quant_read_kernel<FMT, T, 2><<<grid, kThreads, 0, st>>>(a, group, first); });
 }
 void launch_quant_read(const QuantReadArgs& a, int dtype, hipStream_t st) {
   if (a.c.format == EE_QUANT_INT8)

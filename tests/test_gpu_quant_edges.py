@@ -81,6 +81,21 @@ def test_attention_of_a_long_prompt_chunk():
     some_of(kv, q, out, lens, tables, [0, 1, 2999, 3000, 3004, 3005, 8190, 8191, 8192, 9004], [0, 64, 127], rt)
 
 
+def test_append_and_read_of_more_rows_than_one_launch_has():
+    """2^24 + 5 sequences of a block each."""
+    rows, dh = (1 << 24) + 5, 16
+    kv = B.QuantKV(1, rows, 1, dh, "int8")
+    tables = torch.arange(rows - 1, -1, -1, dtype=torch.int32, device="cuda")[:, None]
+    lens = torch.arange(rows, dtype=torch.int32, device="cuda").remainder_(16)
+    x = torch.randint(-127, 128, (rows, 1, dh), dtype=torch.int32, device="cuda").to(torch.bfloat16)
+    x[:, 0, 0] = 127.0                                   # the scale is 1: everything comes back as it was
+    batch = B.make_batch(None, lens, tables, 16)
+    B.ee_kv_quant_append(kv, 1, x, -x, batch)
+    k, v = torch.zeros_like(x), torch.zeros_like(x)
+    B.ee_kv_quant_read(kv, 1, batch, k, v)
+    assert torch.equal(k, x) and torch.equal(v, -x)
+
+
 def test_rotary_of_more_rows_than_one_launch_has():
     rows = (1 << 27) + 9
     desc = B.make_rotary_desc(2)
