@@ -346,7 +346,7 @@ int ee_paged_attention_quant(const ee_quant_cache* cache, int32_t layer, int32_t
                              const ee_batch* batch, float* out, const float* weights_in, float* weights_out,
                              int32_t weights_pitch, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Shortens the cache of every sequence of the batch to `keep` (1 .. 262144) positions, for each K/V head by itself: the latest `recent`
+/* Shortens the cache of every sequence of the batch to `keep` (1 .. 262144, ceil(keep / 16) * n_kv_heads < 2^25) positions, for each K/V head by itself: the latest `recent`
  * (0 .. keep) positions stay, and of the others those with the largest weights_in (of equal ones the lowest position; NaN
  * counts as largest).  What stays moves together in its old order.  Here context_lens[b] is the NUMBER of cached
  * positions, at most max_context; row_table must be NULL; a sequence of `keep` positions or fewer keeps them all.

@@ -1101,6 +1101,11 @@ bool ranges_meet(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
 
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 size_t evict_slots(int keep, int max_context) { return (size_t)((keep < max_context ? keep : max_context) + 15) / 16; }
+// (a launch has fewer than 2^32 threads a dimension, 128 for a block and head)
+int check_evict_blocks(size_t slots, int kv_heads) {
+  if (slots * kv_heads >= (size_t)1 << 25) EE_FAIL(EE_ERR_UNSUPPORTED, "ee_kv_quant_evict: %zu blocks of %d heads stay of a sequence", slots, kv_heads);
+  return EE_OK;
+}
 
 }  // namespace
 
@@ -1245,6 +1250,7 @@ size_t ee_kv_quant_evict_bytes(const ee_quant_cache* cache, int32_t max_batch, i
     set_error("ee_kv_quant_evict_bytes: batch %d, keep %d", max_batch, keep);
     return 0;
   }
+  if (check_evict_blocks(evict_slots(keep, keep), cache->n_kv_heads)) return 0;
   const size_t units = (size_t)max_batch * cache->n_kv_heads * evict_slots(keep, keep) * 2;
   return align256(units * 16 * cache->head_dim) + align256(units * sizeof(float));
 }
@@ -1271,6 +1277,7 @@ int ee_kv_quant_evict(const ee_quant_cache* cache, int32_t layer, const ee_batch
   if (ranges_meet(out_lens, batch->batch * sizeof(int32_t), batch->context_lens, batch->batch * sizeof(int32_t)))
     EE_FAIL(EE_ERR_INVALID_ARG, "ee_kv_quant_evict: out_lens must not be context_lens (which later launches of the call read)");
   const size_t slots = evict_slots(keep, batch->max_context);
+  if ((rc = check_evict_blocks(slots, cache->n_kv_heads))) return rc;
   if (dst_tables && (dst_max_blocks < 0 || (size_t)dst_max_blocks < slots))
     EE_FAIL(EE_ERR_SHAPE, "ee_kv_quant_evict: dst_max_blocks %d below %zu", dst_max_blocks, slots);
   const size_t units = (size_t)batch->batch * cache->n_kv_heads * slots * 2, image_bytes = align256(units * 16 * cache->head_dim);

@@ -27,3 +27,13 @@ def test_rows_that_share_sequences(heads, kv, rows):
     assert need(c, heads, rows) > 0
     assert need(c, heads, rows + 1) == 0 and "rows" in B.ee_last_error()
     assert attend(c=c, heads=heads, b=batch(rows=rows + 1, row_table=P), out=1 << 40) == B.EE_ERR_UNSUPPORTED and "rows" in B.ee_last_error()
+
+
+@pytest.mark.parametrize("dst", [None, P])
+def test_eviction_of_many_blocks_and_heads(dst):
+    from test_quant_abi import evict
+    c, b = cache(n_kv_heads=4096, head_dim=16, num_blocks=1 << 14), batch(max_blocks=1 << 14, max_context=1 << 18)
+    for keep in (1 << 17, 1 << 18):
+        assert evict(c=c, b=b, keep=keep, pitch=1 << 18, dst=dst, dst_blocks=1 << 14, size=1 << 50) == B.EE_ERR_UNSUPPORTED
+        assert B.lib().ee_kv_quant_evict_bytes(C.byref(c), 2, keep) == 0 and "blocks" in B.ee_last_error()
+    assert B.lib().ee_kv_quant_evict_bytes(C.byref(c), 2, (1 << 17) - 16) > 0
