@@ -303,7 +303,7 @@ typedef struct ee_quant_cache {
 
 /* Caches K and V of the batch's rows: row m goes to position context_lens[m] of its sequence.  With row_table several rows
  * may share a sequence; those that fall into one block stand next to each other in the batch, at consecutive ascending
- * positions.  A row with context_lens[m] < 0 is skipped (padding).
+ * positions.  A row with context_lens[m] < 0 is skipped (padding), and so is one whose row_table entry is none.
  * A block's scale is the smallest with which the largest magnitude ever appended to it fits,
  *   INT8: float(largest / 127), at least 2^-126;   E4M3: the smallest power of two with largest <= 448 * scale, at least
  *   2^-126,
@@ -319,7 +319,7 @@ int ee_kv_quant_append(const ee_quant_cache* cache, int32_t layer, const void* k
 
 /* The floats that the cache holds: row m reads position context_lens[m] of its sequence (row_table as above; any
  * order).  k, v dev [rows][n_kv_heads][head_dim] of `dtype`, starting on 8 (EE_FP32) or 4 bytes; zeros for
- * context_lens[m] < 0. */
+ * context_lens[m] < 0 or a row_table entry that is none. */
 int ee_kv_quant_read(const ee_quant_cache* cache, int32_t layer, const ee_batch* batch, void* k, void* v, int32_t dtype,
                      void* stream);
 

@@ -112,7 +112,8 @@ struct Runs {
     const int lane = threadIdx.x & 63, at = base - 1 + lane;
     const bool there = lane <= group + 15 && at >= 0 && at < r.rows;
     pos = there ? r.context_lens[at] : -1;
-    seq = there ? quant_seq(r, at) : -1;
+    seq = there && r.row_table ? r.row_table[at] : at;
+    if ((unsigned)seq >= (unsigned)r.rows) pos = -1; // (a row of no sequence is written nowhere)
     const int pos_before = __shfl_up(pos, 1), seq_before = __shfl_up(seq, 1);
     const bool on = lane > 0 && pos > 0 && pos_before == pos - 1 && seq_before == seq && (pos & 15) != 0;
     goes_on = __ballot(on);

@@ -120,3 +120,25 @@ def test_rotary_of_more_pieces_than_one_launch_has():
     for out, n in ((q_out, 1.0), (k_out, 2.0)):
         assert bool((out[..., 2:] == n).all())
         assert bool(((out[..., 0].double() - n * (c - s)).abs() <= n * 2.0 ** -20).all()) and bool(((out[..., 1].double() - n * (c + s)).abs() <= n * 2.0 ** -20).all())
+
+
+@pytest.mark.parametrize("fmt", T.FORMATS)
+def test_rows_of_no_sequence(fmt):
+    """Entries of row_table outside the batch: appending drops the row, no sequence's positions change, and reading is of nothing."""
+    kv = T.filled(1, 6, 2, 64, fmt, 9)
+    tables = torch.tensor([[0, 1], [2, 3], [4, 5], [0, 0], [0, 0], [0, 0]], dtype=torch.int32)
+    lens, rt = [3, 4, 5, 18, 0, 2], [-1, 0, 6, 1 << 30, 2, -(1 << 31)]
+    ref = Q.Cache.of(kv)
+    x = torch.randn(6, 2, 64, generator=T.gen(2)).cuda()
+    batch = B.make_batch(None, T.i32(lens), T.i32(tables), 32, T.i32(rt))
+    B.ee_kv_quant_append(kv, 1, x, -x, batch)
+    there = [0 <= s < 6 for s in rt]
+    Q.append(ref, x.cpu().double(), -x.cpu().double(), [n if ok else -1 for n, ok in zip(lens, there)], tables, [s if ok else 0 for s, ok in zip(rt, there)])
+    T.assert_cache(kv, ref)
+    k, v = torch.full_like(x, 7.0), torch.full_like(x, 7.0)
+    B.ee_kv_quant_read(kv, 1, batch, k, v)
+    for m, ok in enumerate(there):
+        for out, which in ((k, 0), (v, 1)):
+            for h in range(2):
+                want = ref.value(which, int(tables[rt[m], lens[m] // 16]), h, lens[m] % 16) if ok else torch.zeros(64, dtype=torch.float64)
+                assert torch.equal(out[m, h].cpu().double(), want)
