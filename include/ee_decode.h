@@ -318,7 +318,7 @@ int ee_kv_quant_append(const ee_quant_cache* cache, int32_t layer, const void* k
                        int64_t v_stride, int32_t dtype, const ee_batch* batch, void* stream);
 
 /* The floats that the cache holds: row m reads position context_lens[m] of its sequence (row_table as above; any
- * order).  k, v dev [rows][n_kv_heads][head_dim] of `dtype`, starting on 8 (EE_FP32) or 4 bytes; zeros for
+ * order).  k, v dev [rows][n_kv_heads][head_dim] of `dtype`, starting on 8 (EE_FP32) or 4 bytes, not overlapping; zeros for
  * context_lens[m] < 0 or a row_table entry that is none. */
 int ee_kv_quant_read(const ee_quant_cache* cache, int32_t layer, const ee_batch* batch, void* k, void* v, int32_t dtype,
                      void* stream);

@@ -1175,6 +1175,8 @@ int ee_kv_quant_read(const ee_quant_cache* cache, int32_t layer, const ee_batch*
   if ((rc = check_quant_call(cache, layer, batch, &a.c, &a.r))) return rc;
   if (batch->batch == 0) return EE_OK;
   if ((rc = check_pair_type(dtype, k, v, "ee_kv_quant_read"))) return rc;
+  const size_t bytes = (size_t)batch->batch * cache->n_kv_heads * cache->head_dim * (dtype == EE_BF16 ? 2 : 4);
+  if (ranges_meet(k, bytes, v, bytes)) EE_FAIL(EE_ERR_INVALID_ARG, "ee_kv_quant_read: k and v overlap");
   a.k = k;
   a.v = v;
   const hipStream_t st = reinterpret_cast<hipStream_t>(stream);

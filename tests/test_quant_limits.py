@@ -37,3 +37,9 @@ def test_eviction_of_many_blocks_and_heads(dst):
         assert evict(c=c, b=b, keep=keep, pitch=1 << 18, dst=dst, dst_blocks=1 << 14, size=1 << 50) == B.EE_ERR_UNSUPPORTED
         assert B.lib().ee_kv_quant_evict_bytes(C.byref(c), 2, keep) == 0 and "blocks" in B.ee_last_error()
     assert B.lib().ee_kv_quant_evict_bytes(C.byref(c), 2, (1 << 17) - 16) > 0
+
+
+def test_read_refuses_results_over_each_other():
+    from test_quant_abi import read
+    for k, v in ((P, P), (P, P + 8), (P + 2 * 256 * 4 - 8, P)):       # (2 rows of 4 heads of 64 channels)
+        assert read(k=k, v=v) == B.EE_ERR_INVALID_ARG and "overlap" in B.ee_last_error()
