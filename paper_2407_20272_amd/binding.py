@@ -338,8 +338,9 @@ def ee_paged_attention_decode(desc: ee_model_desc, cache: PagedKV, layer: int, q
 _KIND = {torch.float32: EE_FP32, torch.bfloat16: EE_BF16}
 
 
-_device = torch._C._cuda_getDevice           # the current device ...
-_raw_stream = torch._C._cuda_getCurrentRawStream   # ... and its current stream, which the call goes to
+# The current device, and its current stream, which a call goes to: by torch's own short ways where it has them (0.2 us together, the public ones 1.3).
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
 def _here(t: torch.Tensor, device: int) -> int:
