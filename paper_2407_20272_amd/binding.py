@@ -274,6 +274,8 @@ def make_batch(tokens: Optional[torch.Tensor], context_lens: torch.Tensor, block
                  _ptr(_i32(block_tables)), int(block_tables.shape[1]) if block_tables.dim() == 2 else 0, max_context,
                  _ptr(_i32(row_table)) if row_table is not None else None)
     b._keep = (tokens, context_lens, block_tables, row_table)   # the record only holds raw pointers: keep the tensors alive
+    b.device = context_lens.get_device()
+    assert all(t is None or t.get_device() == b.device for t in b._keep), "the tensors of a batch are on one device"
     return b
 
 
@@ -349,6 +351,13 @@ def _here(t: torch.Tensor, device: int) -> int:
     return t.data_ptr()
 
 
+def _current_device(cache: "QuantKV", batch: ee_batch) -> int:
+    """The current device, which is the cache's and the batch's."""
+    device = _device()
+    assert cache.device == device and getattr(batch, "device", device) == device, "a cache and a batch of the current device"
+    return device
+
+
 def _row_stride(t: torch.Tensor, rows: int, heads: int, dh: int, device: int) -> int:
     """The row stride of [rows][heads][channels] whose heads and channels are consecutive."""
     row, head, channel = t.stride()
@@ -369,7 +378,7 @@ def make_rotary_desc(head_dim: int, rotary_dim: Optional[int] = None, layout: st
 def ee_rotary_frequencies(desc: ee_rotary_desc, device="cuda") -> torch.Tensor:
     """The frequencies every later ee_rotary call with this desc takes (a new float64 tensor [rotary_dim / 2])."""
     freqs = torch.empty(max(0, desc.rotary_dim // 2), dtype=torch.float64, device=device)
-    _check(lib().ee_rotary_frequencies(C.byref(desc), _ptr(freqs), _stream()))
+    _check(lib().ee_rotary_frequencies(C.byref(desc), _here(freqs, _device()), _stream()))
     return freqs
 
 
@@ -415,6 +424,8 @@ class QuantKV:
         assert k.dtype == v.dtype and k.dtype in (torch.int8, torch.float8_e4m3fn) and scales.dtype == torch.float32
         assert v.shape == (n, nb, h, dh, bs) and scales.shape == (n, nb, h, 2)
         self.k, self.v, self.scales, self.num_blocks, self.head = k, v, scales, nb, (h, dh)
+        self.device = k.get_device()
+        assert v.get_device() == self.device and scales.get_device() == self.device, "the pools of a cache are on one device"
         self.c = ee_quant_cache(_ptr(k), _ptr(v), _ptr(scales), n, nb, bs, h, dh,
                                 EE_QUANT_INT8 if k.dtype == torch.int8 else EE_QUANT_E4M3)
 
@@ -437,14 +448,14 @@ class QuantWorkspace:
 
 def ee_kv_quant_append(cache: QuantKV, layer: int, k: torch.Tensor, v: torch.Tensor, batch: ee_batch):
     """k, v [rows][Hkv][dh], float32 or bfloat16, any (even) row stride."""
-    device, rows, (heads, dh) = _device(), batch.batch, cache.head
+    device, rows, (heads, dh) = _current_device(cache, batch), batch.batch, cache.head
     assert k.shape == (rows, heads, dh) and v.shape == k.shape and k.dtype == v.dtype, "k and v: rows of the batch, one type"
     _check(lib().ee_kv_quant_append(cache.c, layer, k.data_ptr(), _row_stride(k, rows, heads, dh, device), v.data_ptr(),
                                     _row_stride(v, rows, heads, dh, device), _KIND[k.dtype], batch, _raw_stream(device)))
 
 
 def ee_kv_quant_read(cache: QuantKV, layer: int, batch: ee_batch, k: torch.Tensor, v: torch.Tensor):
-    device = _device()
+    device = _current_device(cache, batch)
     assert k.shape == (batch.batch, *cache.head) and v.shape == k.shape and k.dtype == v.dtype, "k and v: rows of the batch, one type"
     _check(lib().ee_kv_quant_read(cache.c, layer, batch, _here(k, device), _here(v, device), _KIND[k.dtype], _raw_stream(device)))
 
@@ -453,7 +464,7 @@ def ee_paged_attention_quant(cache: QuantKV, layer: int, q: torch.Tensor, batch:
                              ws: Optional[QuantWorkspace] = None, weights_in: Optional[torch.Tensor] = None,
                              weights_out: Optional[torch.Tensor] = None):
     """q, out [rows][H][dh] float32; weights [rows][Hkv][pitch] float32."""
-    device = _device()
+    device = _current_device(cache, batch)
     rows, heads, dh = q.shape
     assert out.shape == q.shape and rows == batch.batch and dh == cache.head[1]
     assert q.dtype == torch.float32 and out.dtype == torch.float32
@@ -472,7 +483,7 @@ def ee_kv_quant_evict(cache: QuantKV, layer: int, batch: ee_batch, weights_in: t
                       keep: int, recent: int, kept: torch.Tensor, out_lens: torch.Tensor, ws: Optional[QuantWorkspace] = None,
                       dst_tables: Optional[torch.Tensor] = None):
     """weights [B][Hkv][pitch] float32, kept [B][Hkv][keep] int32, out_lens [B] int32, dst_tables [B][blocks] int32."""
-    device, head = _device(), (batch.batch, cache.head[0])
+    device, head = _current_device(cache, batch), (batch.batch, cache.head[0])
     assert weights_in.dtype == torch.float32 and weights_in.shape[:2] == head
     assert weights_out is None or weights_out.dtype == torch.float32 and weights_out.shape[:2] == head
     assert kept.shape == (*head, keep) and out_lens.shape == head[:1] and kept.dtype == torch.int32 and out_lens.dtype == torch.int32
