@@ -330,6 +330,7 @@ int ee_kv_quant_read(const ee_quant_cache* cache, int32_t layer, const ee_batch*
  * result is 0.  q and out dev [rows][n_heads][head_dim] float, 16-byte aligned, not overlapping.
  * Products and sums are float in effect; besides, a channel of q may be off by 2^-38 of the largest in its row and head, a probability times
  * the scale of its block of V by 2^-37 of the largest such product among the positions that the row attends.
+ * batch->max_context sizes the launches: a bound near the longest context is quickest (up to 8192 where there are many rows and heads).
  * weights_out (dev [rows][n_kv_heads][weights_pitch] float, or NULL) receives the attention each cached position got, added
  * over the g heads that share it, for j <= p = context_lens[m]:
  *   weights_out[m][k][j] = weights_in[m][k][j] + sum_g probability   (j < p),   = sum_g probability   (j = p);

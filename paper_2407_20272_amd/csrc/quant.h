@@ -99,11 +99,13 @@ struct QuantAttnArgs {
   int2* spans;                 // dealt: [rows * tiles] first workgroup and number of workgroups that have a unit's steps
   float* scores;               // weights: [rows][n_heads][quant_score_pitch(max_context)], in units of log 2
   int n_parts, part_steps;     // row_table: parts of a context, and 64-position steps of a part
-  int dealt;                   // else: 0, or workgroups of a K/V head that all rows' steps are dealt out to
+  bool whole;                  // else: whether there is a launch in which contexts are whole pieces
+  int dealt;                   // 0, or workgroups of a K/V head that all rows' steps are dealt out to
+  int long_steps;              // with both: contexts of more steps than this are dealt out (0: all)
   int slots;
 };
 __host__ __device__ inline size_t quant_score_pitch(int max_context) { return (size_t)((max_context + 63) / 64) * 64; }
-// How a call's work is divided (sets n_parts, part_steps, dealt, slots), and the floats of `parts` that it needs, and entries of `spans`; the former for
+// How a call's work is divided (sets n_parts, part_steps, whole, dealt, long_steps), and the floats of `parts` that it needs, and entries of `spans`; the former for
 // all calls of up to so many rows and positions.
 size_t quant_attn_plan(QuantAttnArgs& a, size_t* spans);
 size_t quant_attn_part_floats(const QuantCache& c, int n_heads, int max_rows, int max_context, bool weights);

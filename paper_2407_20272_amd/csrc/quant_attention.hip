@@ -89,6 +89,8 @@ __device__ inline int last_position(const QuantAttnArgs& a, int context_len) {
   return max(-1, min(context_len, min(a.max_context, a.r.max_blocks * 16) - 1));
 }
 __device__ inline int steps_to(int last) { return (last >> 6) + 1; }   // (-1: 0)
+// Whether a row of so many steps is this launch's: where long contexts are dealt out and the others are not, that is two launches.
+__device__ inline bool takes(const QuantAttnArgs& a, int steps) { return !a.long_steps || (steps > a.long_steps) == (a.dealt != 0); }
 
 // Rows without row_table are cut into tiles of up to 16 of a K/V head's query heads ("units": row * tiles + tile).
 __host__ __device__ inline int unit_tiles(int group) { return (group + 15) / 16; }
@@ -108,6 +110,7 @@ __device__ inline Deal deal_out(const QuantAttnArgs& a, int tiles, int* start /*
   for (int e = 0; e < 4; ++e) {
     const int u = 4 * tid + e;
     n[e] = u < units ? steps_to(last_position(a, a.r.context_lens[u / tiles])) : 0;
+    if (!takes(a, n[e])) n[e] = 0;
     sum += n[e];
   }
   int upto = sum;
@@ -248,6 +251,7 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
     } else {
       unit_steps = __builtin_amdgcn_readfirstlane(steps_to(row_pos));
       s1 = unit_steps;
+      if (!dealt && !takes(a, unit_steps)) return;
       if (dealt) {
         const int begin = __builtin_amdgcn_readfirstlane(start[unit]);
         unit_steps = __builtin_amdgcn_readfirstlane(start[unit + 1]) - begin;
@@ -637,6 +641,7 @@ __global__ __launch_bounds__(64 * WAVES) void quant_join_kernel(QuantAttnArgs a)
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int tiles = SHARED ? 1 : unit_tiles(G);
   const int last = last_position(a, a.r.context_lens[m]);
+  if (!SHARED && !takes(a, steps_to(last))) return;
   const int joined = SHARED || a.dealt ? a.n_heads : 0;
   const bool joins = (int)blockIdx.x < joined;
   const int chunks = (a.max_context + kWeightPositions - 1) / kWeightPositions;
@@ -761,10 +766,15 @@ constexpr int kSharedParts = 64;
 
 int deal_workgroups(int kv) { return kResident / kv > 1 ? kResident / kv : 1; }
 // Contexts of up to 16 steps are whole pieces: a workgroup's four wavefronts have four steps each, which takes no longer than a second launch
-// would.  With four times the resident workgroups in whole contexts, the order in which they end evens them out.
-bool deals(int rows, int group, int kv, int steps) {
-  const int64_t units = quant_attn_tiles(rows, group, false);
-  return steps > 16 && units <= kDealtRows && units * kv < 4 * kResident;
+// would.  With four times the resident workgroups in whole contexts, the order in which they end evens them out, as far as no context is much of the work.
+// Lengths are the device's; all the host knows is how long a context may be.  If that is more than kLongSteps (8192 positions), two further launches deal
+// out the contexts that are.  256 rows over 8 K/V heads, one of 131000 positions among 500 each: 109 us instead of 1790; one of 20000: 76 instead of 302; 1000 to 16000: 809
+// instead of 929.  The price: 110 instead of 105 where the longest is 1500, 1009 instead of 972 where all are 12000.  (All of them dealt out: 129, 90, - and 122.)
+constexpr int kLongSteps = 128;
+// Rows that are dealt out in one launch.
+int deal_rows(int rows, int group) {
+  const int most = kDealtRows / unit_tiles(group);
+  return rows < most ? rows : most;
 }
 int shared_parts(int rows, int group, int kv, int steps) {
   const int64_t units = quant_attn_tiles(rows, group, true) * kv, want = kResident / units, most = steps / kWaves;
@@ -782,20 +792,24 @@ size_t quant_attn_plan(QuantAttnArgs& a, size_t* spans) {
   const size_t record = a.c.dh + 4;
   a.n_parts = 1;
   a.part_steps = steps;
-  a.dealt = a.slots = 0;
+  a.whole = false;
+  a.dealt = a.slots = a.long_steps = 0;
   if (a.r.row_table) {
     const int parts = shared_parts(rows, G, kv, steps);
     a.part_steps = (steps + parts - 1) / parts;
     a.n_parts = (steps + a.part_steps - 1) / a.part_steps;
     return a.n_parts > 1 ? (size_t)rows * a.n_heads * a.n_parts * record : 0;
   }
-  a.slots = rows * unit_tiles(G);
-  if (deals(rows, G, kv, steps)) {
+  const int tiles = unit_tiles(G);
+  const bool many = quant_attn_tiles(rows, G, false) > kDealtRows || quant_attn_tiles(rows, G, false) * kv >= 4 * kResident;
+  a.whole = many || steps <= 16;
+  if (!a.whole || steps > kLongSteps) {
     a.dealt = deal_workgroups(kv);
-    *spans = a.slots;
-    a.slots += a.dealt;                    // (unit u's part in workgroup w is in slot u + w: either grows from one piece to the next)
+    *spans = (size_t)deal_rows(rows, G) * tiles;
   }
-  return a.dealt || (a.weights_out && unit_tiles(G) > 1) ? (size_t)kv * a.slots * unit_columns(G) * record : 0;
+  if (a.whole && a.dealt) a.long_steps = kLongSteps;
+  const size_t whole_slots = a.whole && a.weights_out && tiles > 1 ? (size_t)rows * tiles : 0, deal_slots = a.dealt ? *spans + a.dealt : 0;
+  return (size_t)kv * (whole_slots > deal_slots ? whole_slots : deal_slots) * unit_columns(G) * record;
 }
 
 // An upper bound that grows with its arguments: a call of fewer rows may be split where one of more is not.
@@ -808,7 +822,7 @@ size_t quant_attn_part_floats(const QuantCache& c, int n_heads, int max_rows, in
     // dealt out: units in front of the bounds of `deals`
     int64_t u = units < kDealtRows ? units : kDealtRows;
     const int64_t cap = (4 * kResident + kv - 1) / kv;
-    if (u > cap) u = cap;
+    if (u > cap && steps <= kLongSteps) u = cap;
     const size_t dealt = (size_t)(u + deal_workgroups(kv)) * columns * record;
     if (dealt > most) most = dealt;
   }
@@ -821,7 +835,9 @@ size_t quant_attn_part_floats(const QuantCache& c, int n_heads, int max_rows, in
   return most;
 }
 
-void launch_quant_attention(const QuantAttnArgs& a, hipStream_t st) {
+namespace {
+
+void launch_part(const QuantAttnArgs& a, hipStream_t st) {
   const int G = a.n_heads / a.c.heads;
   const int y = a.dealt ? a.dealt : (int)quant_attn_tiles(a.r.rows, G, a.r.row_table != nullptr);
   const dim3 grid(a.c.heads, y, a.n_parts);
@@ -836,6 +852,34 @@ void launch_quant_attention(const QuantAttnArgs& a, hipStream_t st) {
     const dim3 jobs((a.dealt ? a.n_heads : 0) + a.c.heads * chunks, a.r.rows);
     const size_t lds = (size_t)G * sizeof(f32x2);
     few ? quant_join_kernel<false, 8><<<jobs, 512, lds, st>>>(a) : quant_join_kernel<false, 4><<<jobs, 256, lds, st>>>(a);
+  }
+}
+
+}  // namespace
+
+void launch_quant_attention(const QuantAttnArgs& a, hipStream_t st) {
+  if (a.r.row_table) return launch_part(a, st);
+  const int G = a.n_heads / a.c.heads, tiles = unit_tiles(G);
+  if (a.whole) {
+    QuantAttnArgs part = a;
+    part.dealt = 0;
+    part.slots = a.r.rows * tiles;
+    if (!a.weights_out || tiles == 1) part.parts = nullptr;
+    launch_part(part, st);
+  }
+  const int each = deal_rows(a.r.rows, G);
+  for (int r = 0; a.dealt && r < a.r.rows; r += each) {   // (the workspace serves one after the other)
+    QuantAttnArgs part = a;
+    part.r.rows = each < a.r.rows - r ? each : a.r.rows - r;
+    part.r.context_lens += r;
+    part.r.block_tables += (size_t)r * a.r.max_blocks;
+    part.q += (size_t)r * a.n_heads * a.c.dh;
+    part.out += (size_t)r * a.n_heads * a.c.dh;
+    const size_t weights = (size_t)r * a.c.heads * a.weights_pitch;
+    if (a.weights_in) part.weights_in += weights;
+    if (a.weights_out) part.weights_out += weights;
+    part.slots = part.r.rows * tiles + a.dealt;           // (unit u's part in workgroup w is in slot u + w: either grows from one piece to the next)
+    launch_part(part, st);
   }
 }
 
