@@ -15,7 +15,7 @@
 // A column has two references, both whole powers of two, so that changing them rounds nothing:
 //   2^m for the sum: m is 32 below the largest score so far (in units of log 2, rounded up).  A probability is then a float, not 0, down to 2^-158 of
 //       the largest, and a block's scale times 2^(m - ..) stays a float where one with a small scale has the largest score;
-//   2^(m + d - 14) for the result: d follows the blocks' largest scores and scales together, over the positions that the column attends.  With the
+//   2^(m + r - 15) for the result: r follows the blocks' largest scores and scales together, over the positions that the column attends.  With the
 //       largest scale alone, a block that hardly counts (or another sequence's in the tile, or a later one's) would push all others into fp16's last places.
 //
 // Single rows are bound by the cache's bytes (head_dim 128, shuffled blocks; a plain read of this card makes 7.0 TB/s): one sequence of 131000 positions,
@@ -68,6 +68,15 @@ __device__ inline f32x4 mma(half8_t a, half8_t b, f32x4 c) { return __builtin_am
 __device__ inline void split(f32x2 x, half2_t& hi, half2_t& lo) {
   hi = __builtin_convertvector(x, half2_t);
   lo = __builtin_convertvector(f32x2{x[0] - (float)hi[0], x[1] - (float)hi[1]}, half2_t);
+}
+
+__device__ inline float largest(const f32x4 (&x)[4]) {
+  float v = x[0][0];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v = fmaxf(v, x[i][e]);
+  return v;
 }
 
 // The maximum over the four lanes that share a column.
@@ -263,7 +272,7 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
 
     // q, split; the factor that turns a product back into a score in units of log 2
     half8_t qf[QREG ? 2 * NL : 1][2];
-    float to_score[NT], m_run[NT], l_run[NT], d_run[NT];
+    float to_score[NT], m_run[NT], l_run[NT], r_run[NT];
     int col_row[NT], col_pos[NT];
     float most = 0.0f;
 #pragma unroll
@@ -293,7 +302,7 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
       ex = max(ex, -100);
       if (nt == q_tile) up = ldexpf(1.0f, 14 - ex);
       to_score[nt] = ldexpf(1.0f, ex - 14) * (kLog2e / sqrtf((float)dh));
-      m_run[nt] = d_run[nt] = -INFINITY;
+      m_run[nt] = r_run[nt] = -INFINITY;
       l_run[nt] = 0.0f;
     }
 #pragma unroll
@@ -433,15 +442,16 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
           load_k(k_blk, more);
           __builtin_amdgcn_sched_barrier(0);
           const bool ragged = (c0 + s) * 64 + 63 > shortest;   // some positions are behind some column's last one
-          const int v_exponent = __builtin_amdgcn_frexp_expf(sc[1]);   // sc[1] is below two to it
+          // sc[1] is below 2 to v_exponent, and times 2 to v_most still a float
+          const float v_exponent = (float)__builtin_amdgcn_frexp_expf(sc[1]), v_most = 127.0f - v_exponent;
           half8_t ph[NT][2], pl[NT][2];
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
             // scales are positive: the largest product gives the largest score.  A block without a position for a column has
             // none of its scales in the column's result.
-            float f = sc[0] * to_score[nt];
+            float f = sc[0] * to_score[nt], v_scale = sc[1];
             if (ragged) {
-              if (pos0 > limit[nt]) f = 1.0f;
+              if (pos0 > limit[nt]) f = 1.0f, v_scale = 0.0f;
               if (f == 0.0f) f = kQuantScaleFloor;   // (times minus infinity)
 #pragma unroll
               for (int i = 0; i < 4; ++i)
@@ -449,42 +459,37 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
                 for (int e = 0; e < 4; ++e)
                   if (pos0 + 4 * i + e > limit[nt]) sd[nt][i][e] = -INFINITY;
             }
-            float mx = sd[nt][0][0];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) mx = fmaxf(mx, sd[nt][i][e]);
+            const float mx = largest(sd[nt]);
             if constexpr (WEIGHTS) {
               if (f0 + col < f1) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) collected[((col << held_shift) + held) * 16 + ((g * 4 + i) ^ col)] = sd[nt][i] * f;
               }
             }
-            const float top = mx * f;              // of this lane's block
-            if (__any(fabsf(top) > kLargeScore && fabsf(top) < INFINITY)) {
-#pragma unroll
-              for (int i = 0; i < 4; ++i) sd[nt][i] *= f;
-              f = 1.0f;
-            }
-            const float m_new = fmaxf(m_run[nt], ceilf(max_over_groups(top)) - kBelow);
+            const float m_new = fmaxf(m_run[nt], ceilf(max_over_groups(mx * f)) - kBelow);
             const float base = m_new == -INFINITY ? 0.0f : m_new;
-            const float alpha = __builtin_amdgcn_exp2f(m_run[nt] - base);
-            d_run[nt] += m_run[nt] - base;
+            const float less = m_run[nt] - base, alpha = __builtin_amdgcn_exp2f(less);
             m_run[nt] = m_new;
+            r_run[nt] += less;
             // What the block adds to the result is below 2^adds times its bytes.  The unit is kept until that is past twice the unit; then a column that needs it
             // takes another one.
-            const float adds = top - base + (float)v_exponent;
-            if (__any(adds > d_run[nt] + 1.0f)) {
-              const float reach = ceilf(max_over_groups(adds));
-              const float d_new = reach > d_run[nt] + 1.0f ? reach : d_run[nt];
-              const float beta = __builtin_amdgcn_exp2f(d_run[nt] - (d_new == -INFINITY ? 0.0f : d_new));
+            float adds = fmaf(mx, f, -base) + v_exponent;
+            if (__any(adds > r_run[nt] || fabsf(base) > kLargeScore)) {
+              if (__any(fabsf(base) > kLargeScore)) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sd[nt][i] *= f;
+                f = 1.0f;
+                adds = largest(sd[nt]) - base + v_exponent;
+              }
+              const float reach = ceilf(max_over_groups(adds)) + 1.0f;
+              const float r_new = reach > r_run[nt] + 1.0f ? reach : r_run[nt];
+              const float beta = __builtin_amdgcn_exp2f(r_run[nt] - (r_new == -INFINITY ? 0.0f : r_new));
 #pragma unroll
               for (int ct = 0; ct < CT; ++ct) o[ct][nt] *= beta;
-              d_run[nt] = d_new;
+              r_run[nt] = r_new;
             }
-            // (bounded where the probabilities are 0: those have to stay so)
-            float v_factor = __builtin_ldexpf(sc[1], min(14 - (int)fmaxf(d_run[nt], -1000.0f), 127 - v_exponent));
-            if (ragged && pos0 > limit[nt]) v_factor = 0.0f;
+            // (bounded where the probabilities are 0, which have to stay so)
+            const float v_factor = __builtin_ldexpf(v_scale, (int)fminf(15.0f - r_run[nt], v_most));
             float sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -571,7 +576,7 @@ __global__ __launch_bounds__(kThreads, NL <= 2 ? 2 : 1) void quant_attn_kernel(Q
       l_all[nt] = ll;
       // divided by the sum first (the largest values' sums would be no floats), then in units of 1
       const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
-      const int unit = (int)fmaxf(m_run[nt] - base + d_run[nt], -1000.0f) - 14;
+      const int unit = (int)fmaxf(m_run[nt] - base + r_run[nt], -1000.0f) - 15;
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
