@@ -93,7 +93,7 @@ struct QuantAttnArgs {
   const float* weights_in;
   float* weights_out;          // nullptr: none
   int weights_pitch;
-  // A context's parts leave records of head_dim + 4 floats: running maximum, sum, -, -, unnormalised result.
+  // A context's parts leave records of head_dim + 4 floats: running maximum's reference, sum, -, -, the part's own result.
   //   row_table: [rows][n_heads][n_parts], n_parts > 1;   else [kv heads][slots][columns of a tile] (see quant_attn_plan).
   float* parts;                // nullptr: none
   int2* spans;                 // dealt: [rows * tiles] first workgroup and number of workgroups that have a unit's steps

@@ -18,12 +18,13 @@
 //   2^(m + r - 15) for the result: r follows the blocks' largest scores and scales together, over the positions that the column attends.  With the
 //       largest scale alone, a block that hardly counts (or another sequence's in the tile, or a later one's) would push all others into fp16's last places.
 //
-// Single rows are bound by the cache's bytes (head_dim 128, shuffled blocks; a plain read of this card makes 7.0 TB/s): one sequence of 131000 positions,
-// 8 K/V heads, 268 MB: 48 us (5.6 TB/s) and 5 to join 64 parts; 64 of 2000 to 6000: 95 us (5.5 TB/s) + 6; 32 of 576, 32 heads: 30 us (5.1).
+// Single rows are bound by the cache's bytes (head_dim 128, shuffled blocks; a plain read of this card makes 6.3 to 6.8 TB/s): one sequence of 131000 positions,
+// 8 K/V heads, 268 MB: 48 us (5.6 TB/s) and 5 to join 64 parts; 64 of 2000 to 6000: 96 us (5.4 TB/s) + 6; 32 of 576, 32 heads: 30 us (5.1).
 // Without products, or without softmax, these times hardly change; two workgroups a compute unit with a step's 16 KB a wavefront in flight are
 // enough, three were no faster.  What is left is the beginning and end of a workgroup, about 2 us each.  512 prompt rows of four prompts up to
-// 3100 positions, 4 heads to a K/V head: 45 us, 25 GFLOP (12.6 in two pieces each): bound by instruction issue (a step is 590 vector and 128
-// matrix instructions), 13 us are beginning and end.  Weights cost 27 us of the 64 sequences' call: 33 MB of scores written among 524 MB of reads (24 us;
+// 3100 positions, 4 heads to a K/V head: 46 us, 25 GFLOP (12.6 in two pieces each).  All tiles are resident at once, and a K/V head's 64 have 1 to 49 steps (mean 25): the
+// call takes as long as the longest and what shares its compute unit.  Within a step it is the issue of instructions (about 600 vector and 128 matrix ones): prompts of
+// 12000 positions, tiles of one length, make 860 TFLOP/s, three quarters of a large matrix product's.  Weights cost 27 us of the 64 sequences' call: 33 MB of scores written among 524 MB of reads (24 us;
 // with stores that are dropped the launch takes 98), and 9 to read them.
 #include "quant.h"
 

@@ -98,8 +98,9 @@ __device__ inline float scale_max(float a, float b) { return a != a || b != b ? 
 // Rows that go into (or come from) one block are taken together: a run is rows at consecutive positions of one block.  A workgroup has kGroup
 // rows (one, where every row is a sequence of its own) of two heads and takes the runs that begin among them, one after the other;
 // a wavefront for K and V of either head.  (Groups of 8: a chunk's runs of 16 leave every second workgroup empty, rows of many sequences take eight turns.
-// With a wavefront a row, 15 of 16 of them empty, 2103 rows took 43 us instead of 17; groups of 4, 16, 32: 20, 20, 18.  300 rows of 100
-// sequences: 13, 20, 28 instead of 15.)
+// With a wavefront a row, 15 of 16 of them empty, 2103 rows took 43 us instead of 17.  Groups of 4, 8, 16, E4M3: 2103 rows of three sequences 17.4, 14.3, 14.6 us where
+// no scale grows and 18.5, 18.1, 20.1 where those of the first blocks do; 300 rows of 100 sequences 6.2, 6.6, 11.4 and 14.2, 16.2, 25.8; 1000 rows of 500 sequences
+// 10.2, 11.7, 15.2 and 26, 32, 37.  INT8: 24, 20, 21 and 26, 23, 26; 7.0, 9.0, 14.0 and 14.9, 17.5, 29; 10.5, 12.6, 18.3 and 27, 33, 39.)
 constexpr int kGroup = 8;
 struct Run {
   int m, n, off, seq, logical;   // first row, rows, the first one's place in its block
@@ -284,8 +285,10 @@ __device__ inline void append_positions(const QuantAppendArgs& a, const Run& run
   }
 }
 
-// 2103 bf16 rows of 32 heads of 128 channels, E4M3: 17 us, 52 MB (3 TB/s; INT8 22); 256 rows of 256 sequences, 8 heads: 7.5 us, of which an empty
-// launch takes 2 and three dependent loads most of the rest.
+// 2103 bf16 rows of 32 heads of 128 channels, E4M3: 17 us, 52 MB (3 TB/s; INT8 22).  256 rows of 256 sequences, 8 heads: 6 to 7 us where no scale grows, of which an
+// empty launch takes 2 and three dependent loads most of the rest.  Where one does, what stands in front is rounded again, four positions at a time, each four
+// behind the stores of those before: with 1, 4, 8, 12, 15 positions in front 7, 10, 14, 18, 20 us (INT8; E4M3, whose scales grow in steps of two, 6 to 18).  In a decode some
+// wavefront of a large batch has a growing scale in nearly every call.
 template <int FMT, class T, int CP>
 __global__ __launch_bounds__(kThreads) void quant_append_kernel(QuantAppendArgs a, int group, int first) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);

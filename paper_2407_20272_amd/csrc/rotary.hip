@@ -38,7 +38,9 @@ struct alignas(sizeof(T) * N) Piece {
 // piece and its partner rotary_dim/2 further on, else a piece of VEC/2 neighbouring pairs (one pair where VEC is 1).
 // The workgroup's rows share the tables of (cos, sin): their double products, reductions and sincospi are done once a row and pair, not once a
 // head.  Bound by memory: it reads and writes every element once.  4096 rows of 40 heads of 128 bf16 channels, 84 MB: 15 us, 5.6 TB/s (a large copy
-// makes 5.1); one row of 64 heads 2.9 us, an empty launch 2.
+// makes 5.1; the 84 MB stay in the last-level cache between calls); one row of 64 heads 2.9 us, an empty launch 2.  1001 float rows with 48 of 80 channels interleaved, 16 MB:
+// 6.9 us, twice what memory takes: a thread's loads wait for the stores of its piece before (in and out may be one buffer).  Where halves are no whole number of 16 bytes
+// everything goes element by element.
 template <class T, int LAYOUT, int VEC>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, int rows_per_wg, int tasks_per_row, int tasks_per_wg) {
   extern __shared__ float2 turn[];   // [rows_per_wg][rotary_dim / 2]
