@@ -369,6 +369,105 @@ int ee_kv_quant_evict(const ee_quant_cache* cache, int32_t layer, const ee_batch
                       int32_t weights_out_pitch, int32_t keep, int32_t recent, int32_t* kept, int32_t* out_lens,
                       void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- Several continuations of a prompt ---------------------------------------------------------------------------
+ * Beam search, parallel samples, many questions about one text: block tables whose sequences share blocks, kept by counts of
+ * references on the device; the choice among beams; and an attention that reads what rows share once.  Same conventions as
+ * above.  One step of a beam search over a cache:
+ *   ee_beam_select -> ee_reorder_rows (what else belongs to a beam) -> ee_kv_pages_fork, releasing the old rows ->
+ *   ee_kv_pages_grow -> ee_kv_copy -> ee_kv_pages_shared -> the layers, each with ee_paged_attention_shared.
+ *
+ * refs dev [num_blocks] int32: how many table entries name a block; 0 (or less) is a free block.  The tables of a call and its refs
+ * belong together: an entry counts once for every row that names it within its length. */
+typedef struct ee_page_tables {
+  int32_t* block_tables; /* dev [rows][max_blocks]                                                        */
+  int32_t* lens;         /* dev [rows]: cached positions (0 .. max_blocks * 16); the first ceil(lens / 16) entries of a row are
+                            its blocks, what lies behind is never read                                     */
+  int32_t rows, max_blocks;
+} ee_page_tables;
+
+/* Scratch bytes of ee_kv_pages_grow and ee_kv_pages_compact for a pool of num_blocks (up to 2^23) and calls of up to max_rows rows.  256-byte
+ * aligned, no initialisation, dead between calls; calls that may overlap need one each. */
+size_t ee_kv_pages_bytes(int32_t num_blocks, int32_t max_rows);
+
+/* Row m of dst becomes a copy of row parents[m] of src: its blocks (one more reference each) and its length.  parents dev [dst->rows]; where
+ * it is no row of src, row m becomes empty.  Entries behind a row's blocks are left as they were.  release = 1: afterwards the rows of src give up theirs, as
+ * by ee_kv_pages_release.  dst->max_blocks >= src->max_blocks; the tables must not overlap. */
+int ee_kv_pages_fork(int32_t* refs, int32_t num_blocks, const ee_page_tables* src, const int32_t* parents, const ee_page_tables* dst,
+                     int32_t release, void* stream);
+
+/* Takes one reference from each block of every row, and sets the rows' lens to 0 (their entries stay as they are). */
+int ee_kv_pages_release(int32_t* refs, int32_t num_blocks, const ee_page_tables* tables, void* stream);
+
+/* Makes room for positions lens[m] .. new_lens[m] - 1 of every row (new_lens dev [rows], at most max_blocks * 16 count; a row with new_lens <= lens
+ * wants nothing).  lens stay as they are: the caller sets them when the positions are cached.
+ *   Blocks behind the row's are added.  A last block that is partly filled, and that other entries name too, is replaced by one of the row's own, and the
+ *   row is given a move (old, new) for ee_kv_copy; where all its references are rows of this call that want to write it, the last of these rows keeps it.
+ *   Free blocks are handed out in ascending order, to the rows in order and their entries in order.
+ *   moves   dev [rows][2] int32: (old, new), or (-1, -1).
+ *   missing dev [1] int32: 0, or how many blocks too few are free; then nothing has changed and every move is (-1, -1). */
+int ee_kv_pages_grow(int32_t* refs, int32_t num_blocks, const ee_page_tables* tables, const int32_t* new_lens, int32_t* moves, int32_t* missing,
+                     void* workspace, size_t workspace_bytes, void* stream);
+
+/* Packs the n blocks in use into 0 .. n - 1: those from n on move, in ascending order, to the free ones below n, in ascending order.  refs and the tables
+ * (NULL or rows == 0: none) follow.
+ *   remap   dev [num_blocks] int32: the new place of every block in use, -1 for a free one (for tables that are kept elsewhere).
+ *   moves   dev [num_blocks][2] int32: (old, new), then (-1, -1).     n_moves dev [1] int32.
+ * The contents are the caller's to move: ee_kv_copy with these moves. */
+int ee_kv_pages_compact(int32_t* refs, int32_t num_blocks, const ee_page_tables* tables, int32_t* remap, int32_t* moves, int32_t* n_moves,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* shared_blocks[g] = how many leading entries all rows first_row[g] .. first_row[g + 1] - 1 have in common, of those that every one of them has filled
+ * (16 positions); 0 for a group without rows.  first_row dev [n_groups + 1] int32, shared_blocks dev [n_groups] int32. */
+int ee_kv_pages_shared(const ee_page_tables* tables, const int32_t* first_row, int32_t n_groups, int32_t* shared_blocks, void* stream);
+
+/* Copies blocks of every layer, K and V (and scales): moves dev [n][2] int32 (from, to); a pair with an entry outside 0 .. num_blocks - 1 is skipped.  count
+ * dev [1] int32 or NULL: only the first *count of the n pairs.  No block may be written twice, or both read and written (but a pair of one block with itself
+ * does nothing).  Pools start on 16 bytes. */
+int ee_kv_copy(const ee_model_desc* desc, const ee_kv_cache* cache, const int32_t* moves, int32_t n, const int32_t* count, void* stream);
+int ee_kv_quant_copy(const ee_quant_cache* cache, const int32_t* moves, int32_t n, const int32_t* count, void* stream);
+
+/* One step of beam search.  Rows g * beams .. of the logits are group g's beams; candidate (row, t) has the score
+ *   scores[row] + (logits[row][t] - log sum_t' exp(logits[row][t'])),
+ * a row with finished[row] != 0 only the candidate (row, end_token) with scores[row] (its logits are not read).  A score that is not finite (a token masked by
+ * -inf; any of a row with a NaN or +inf among its logits) counts as -inf.  For every group the n_out best, best first; of equal scores the lower
+ * row, then the lower token first, so tokens and rows are given also where all that is left is -inf.  Scores are formed and compared in double, the sum's
+ * exponentials in float; among one row's tokens the order is that of the logits.
+ *   logits dev [groups * beams] rows of vocab values of `dtype` (EE_FP32 | EE_BF16), logits_stride (>= vocab) elements apart, any element alignment.
+ *   scores dev [groups * beams] float.  finished dev [groups * beams] int32 or NULL (none).  end_token: 0 .. vocab - 1, or -1 (none; not with finished).
+ *   tokens, parents (rows of the call), finished_out dev [groups][n_out] int32, scores_out float; finished_out (or NULL) is 1 where the row is finished or the token
+ *   is end_token.  Outputs must not overlap scores or finished.
+ * beams and n_out are 1 .. 128, n_out <= beams * vocab.  workspace: 256-byte aligned, ee_beam_select_bytes for the call's
+ * sizes or larger ones (0: refused sizes), no initialisation, dead between calls. */
+size_t ee_beam_select_bytes(int32_t groups, int32_t beams, int32_t vocab, int32_t n_out);
+int ee_beam_select(const void* logits, int64_t logits_stride, int32_t dtype, const float* scores, const int32_t* finished, int32_t groups, int32_t beams,
+                   int32_t vocab, int32_t n_out, int32_t end_token, int32_t* tokens, int32_t* parents, float* scores_out, int32_t* finished_out,
+                   void* workspace, size_t workspace_bytes, void* stream);
+
+/* out[m] = in[parents[m]], rows of row_bytes bytes, in_stride and out_stride (>= row_bytes) bytes apart: whatever else belongs to a beam.  Where parents[m] is
+ * none of 0 .. in_rows - 1 row m is left as it was.  in and out must not overlap. */
+int ee_reorder_rows(const void* in, int64_t in_stride, int32_t in_rows, const int32_t* parents, int32_t rows, int64_t row_bytes, void* out,
+                    int64_t out_stride, void* stream);
+
+/* Rows whose sequences begin with the same blocks.  Groups are rows first_row[g] .. first_row[g + 1] - 1 of the batch (ascending); the first shared_blocks[g]
+ * entries of their block tables are equal.  A group may have one row, or share nothing. */
+typedef struct ee_prefix_groups {
+  int32_t n_groups;             /* 0 .. 65536                                                                */
+  const int32_t* first_row;     /* dev [n_groups + 1] int32                                               */
+  const int32_t* shared_blocks; /* dev [n_groups] int32                                                   */
+  int32_t max_shared;           /* host-side upper bound of shared_blocks (more are not shared: read row by row) */
+} ee_prefix_groups;
+
+/* ee_paged_attention_decode for such rows, n_heads query heads over the desc->n_heads K/V heads of the cache (a multiple; g = n_heads / desc->n_heads):
+ *   out[m][h] = softmax_j(q[m][h] . K[j][h / g] / sqrt(head_dim)) . V[j][h / g],   j = 0..context_lens[m] INCLUSIVE,
+ * the same result as without groups; shared blocks are read once for up to 64 columns (a row and a query head) instead of once a row.  A row shorter than its group's shared
+ * blocks attends its own positions all the same; one with context_lens[m] < 0 attends nothing: its result is 0.  Rows of no group are left as they were.  row_table as in
+ * ee_paged_attention_decode (shared blocks are then those of the rows' sequences).
+ * q and out dev [rows][n_heads][head_dim] float, 16-byte aligned, not overlapping; pools start on 16 bytes.  Products and sums are float in effect.
+ * workspace: 256-byte aligned, ee_paged_attention_shared_bytes for the call's sizes or larger ones, no initialisation, dead between calls. */
+size_t ee_paged_attention_shared_bytes(const ee_model_desc* desc, int32_t n_heads, int32_t max_batch, int32_t max_groups, int32_t max_context);
+int ee_paged_attention_shared(const ee_model_desc* desc, const ee_kv_cache* cache, int32_t layer, int32_t n_heads, const float* q, const ee_batch* batch,
+                              const ee_prefix_groups* groups, float* out, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- Measurement helpers (not part of the decode path) ------------------------------------------------------
  * While enabled, every later ee_* call brackets the kernels it enqueues with pairs of HIP events on the call's
  * stream (the events add a few microseconds per kernel, so throughput is timed with profiling off).

@@ -23,7 +23,9 @@ EXPORTS = ["ee_last_error", "ee_packed_weight_bytes", "ee_pack_weight", "ee_work
            "ee_noalloc_init", "ee_exit_check_noalloc_bytes", "ee_exit_check_noalloc", "ee_calibration_read", "ee_calibration_mfma",
            "ee_calibration_mfma_tile", "ee_calibration_intake", "ee_rotary_frequencies", "ee_rotary", "ee_kv_quant_append",
            "ee_kv_quant_read", "ee_paged_attention_quant_bytes", "ee_paged_attention_quant", "ee_kv_quant_evict_bytes",
-           "ee_kv_quant_evict"]
+           "ee_kv_quant_evict", "ee_kv_pages_bytes", "ee_kv_pages_fork", "ee_kv_pages_release", "ee_kv_pages_grow", "ee_kv_pages_compact",
+           "ee_kv_pages_shared", "ee_kv_copy", "ee_kv_quant_copy", "ee_beam_select_bytes", "ee_beam_select", "ee_reorder_rows",
+           "ee_paged_attention_shared_bytes", "ee_paged_attention_shared"]
 EE_ROTARY_HALF, EE_ROTARY_INTERLEAVED = 0, 1
 EE_ROTARY_PLAIN, EE_ROTARY_LINEAR, EE_ROTARY_TURNS = 0, 1, 2
 EE_QUANT_INT8, EE_QUANT_E4M3 = 0, 1
@@ -72,6 +74,14 @@ class ee_quant_cache(C.Structure):
     _fields_ = [("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("scales", C.c_void_p), ("n_layers", C.c_int32),
                 ("num_blocks", C.c_int32), ("block_size", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
                 ("format", C.c_int32)]
+
+
+class ee_page_tables(C.Structure):
+    _fields_ = [("block_tables", C.c_void_p), ("lens", C.c_void_p), ("rows", C.c_int32), ("max_blocks", C.c_int32)]
+
+
+class ee_prefix_groups(C.Structure):
+    _fields_ = [("n_groups", C.c_int32), ("first_row", C.c_void_p), ("shared_blocks", C.c_void_p), ("max_shared", C.c_int32)]
 
 
 class EEError(RuntimeError):
@@ -141,6 +151,24 @@ def lib() -> C.CDLL:
         L.ee_kv_quant_evict.argtypes = [C.POINTER(ee_quant_cache), C.c_int32, C.POINTER(ee_batch), C.c_void_p, C.c_int32, C.c_void_p,
                                         C.c_int32, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
                                         C.c_size_t, C.c_void_p]
+        pool, tables, i32, ptr, size = [C.c_void_p, C.c_int32], C.POINTER(ee_page_tables), C.c_int32, C.c_void_p, C.c_size_t
+        L.ee_kv_pages_bytes.argtypes, L.ee_kv_pages_bytes.restype = [i32, i32], size
+        L.ee_kv_pages_fork.argtypes = pool + [tables, ptr, tables, i32, ptr]
+        L.ee_kv_pages_release.argtypes = pool + [tables, ptr]
+        L.ee_kv_pages_grow.argtypes = pool + [tables, ptr, ptr, ptr, ptr, size, ptr]
+        L.ee_kv_pages_compact.argtypes = pool + [tables, ptr, ptr, ptr, ptr, size, ptr]
+        L.ee_kv_pages_shared.argtypes = [tables, ptr, i32, ptr, ptr]
+        L.ee_kv_copy.argtypes = [C.POINTER(ee_model_desc), C.POINTER(ee_kv_cache), ptr, i32, ptr, ptr]
+        L.ee_kv_quant_copy.argtypes = [C.POINTER(ee_quant_cache), ptr, i32, ptr, ptr]
+        L.ee_beam_select_bytes.argtypes, L.ee_beam_select_bytes.restype = [i32] * 4, size
+        L.ee_beam_select.argtypes = [ptr, C.c_int64, i32, ptr, ptr] + [i32] * 5 + [ptr] * 5 + [size, ptr]
+        L.ee_reorder_rows.argtypes = [ptr, C.c_int64, i32, ptr, i32, C.c_int64, ptr, C.c_int64, ptr]
+        L.ee_paged_attention_shared_bytes.argtypes, L.ee_paged_attention_shared_bytes.restype = [C.POINTER(ee_model_desc)] + [i32] * 4, size
+        L.ee_paged_attention_shared.argtypes = [C.POINTER(ee_model_desc), C.POINTER(ee_kv_cache), i32, i32, ptr, C.POINTER(ee_batch),
+                                                C.POINTER(ee_prefix_groups), ptr, ptr, size, ptr]
+        for name in ("ee_kv_pages_fork", "ee_kv_pages_release", "ee_kv_pages_grow", "ee_kv_pages_compact", "ee_kv_pages_shared", "ee_kv_copy",
+                     "ee_kv_quant_copy", "ee_beam_select", "ee_reorder_rows", "ee_paged_attention_shared"):
+            getattr(L, name).restype = C.c_int
         for name in ("ee_rotary_frequencies", "ee_rotary", "ee_kv_quant_append", "ee_kv_quant_read", "ee_paged_attention_quant",
                      "ee_kv_quant_evict"):
             getattr(L, name).restype = C.c_int
@@ -265,6 +293,16 @@ class PagedKV:
         self.k = torch.full(shape, fill, dtype=cfg.torch_dtype, device=device)
         self.v = torch.full(shape, fill, dtype=cfg.torch_dtype, device=device)
         self.c = ee_kv_cache(self.k.data_ptr(), self.v.data_ptr(), num_blocks, cfg.block_size)
+
+    @classmethod
+    def of(cls, cfg, k: torch.Tensor, v: torch.Tensor) -> "PagedKV":
+        """The record of pools that are there already."""
+        c = cls.__new__(cls)
+        c.cfg, c.num_blocks, c.k, c.v = cfg, k.shape[1], k, v
+        assert k.shape == (cfg.n_layers, c.num_blocks, cfg.n_heads, cfg.block_size, cfg.head_dim) and v.shape == k.shape
+        assert k.dtype == v.dtype == cfg.torch_dtype and k.get_device() == v.get_device()
+        c.c = ee_kv_cache(_ptr(k), _ptr(v), c.num_blocks, cfg.block_size)
+        return c
 
 
 def make_batch(tokens: Optional[torch.Tensor], context_lens: torch.Tensor, block_tables: torch.Tensor,
@@ -494,6 +532,175 @@ def ee_kv_quant_evict(cache: QuantKV, layer: int, batch: ee_batch, weights_in: t
                                    0 if weights_out is None else weights_out.shape[2], keep, recent, _here(kept, device),
                                    _here(out_lens, device), None if ws is None else _here(ws.buf, device), 0 if ws is None else ws.bytes,
                                    _raw_stream(device)))
+
+
+# ---- several continuations of a prompt -------------------------------------------------------------------
+class PagePool:
+    """The references of a cache's blocks (int32 [num_blocks]), and the scratch of the calls that change them for up to max_rows rows.  Calls on one
+    pool are ordered among themselves (one stream, or events between streams): they change the same counts."""
+
+    def __init__(self, num_blocks: int, max_rows: int, device="cuda"):
+        self._hold(torch.zeros(num_blocks, dtype=torch.int32, device=device), max_rows)
+
+    @classmethod
+    def of(cls, refs: torch.Tensor, max_rows: int) -> "PagePool":
+        """The record of counts that are there already."""
+        c = cls.__new__(cls)
+        c._hold(refs, max_rows)
+        return c
+
+    def _hold(self, refs, max_rows):
+        assert refs.dtype == torch.int32 and refs.dim() == 1
+        self.refs, self.num_blocks, self.device = refs, refs.shape[0], refs.get_device()
+        self.address = _ptr(refs)
+        self.bytes = lib().ee_kv_pages_bytes(self.num_blocks, max_rows)
+        if self.bytes == 0:
+            raise EEError(EE_ERR_INVALID_ARG, ee_last_error())
+        self.ws = torch.empty(self.bytes, dtype=torch.uint8, device=refs.device)
+        assert self.ws.data_ptr() % 256 == 0
+
+
+class PageTables:
+    """Block tables [rows][max_blocks] and the cached positions [rows] of their rows, int32."""
+
+    def __init__(self, block_tables: torch.Tensor, lens: torch.Tensor):
+        assert block_tables.dtype == torch.int32 and lens.dtype == torch.int32 and block_tables.dim() == 2 and lens.shape == block_tables.shape[:1]
+        assert block_tables.get_device() == lens.get_device(), "tables and lengths are on one device"
+        self.block_tables, self.lens, self.rows, self.device = block_tables, lens, lens.shape[0], lens.get_device()
+        self.c = ee_page_tables(_ptr(block_tables), _ptr(lens), *block_tables.shape)
+
+
+def _pool_device(pool, *tables) -> int:
+    device = _device()
+    assert all(t is None or t.device == device for t in (pool, *tables)), "a pool and tables of the current device"
+    return device
+
+
+def _int32s(t: torch.Tensor, shape, device: int) -> int:
+    assert t.dtype == torch.int32 and t.shape == shape, "int32 of the call's sizes"
+    return _here(t, device)
+
+
+def ee_kv_pages_fork(pool: PagePool, src: PageTables, parents: torch.Tensor, dst: PageTables, release: bool = False):
+    """Row m of dst becomes row parents[m] of src; with release the rows of src give up their blocks."""
+    device = _pool_device(pool, src, dst)
+    _check(lib().ee_kv_pages_fork(pool.address, pool.num_blocks, src.c, _int32s(parents, (dst.rows,), device), dst.c, bool(release), _raw_stream(device)))
+
+
+def ee_kv_pages_release(pool: PagePool, tables: PageTables):
+    device = _pool_device(pool, tables)
+    _check(lib().ee_kv_pages_release(pool.address, pool.num_blocks, tables.c, _raw_stream(device)))
+
+
+def ee_kv_pages_grow(pool: PagePool, tables: PageTables, new_lens: torch.Tensor, moves: torch.Tensor, missing: torch.Tensor):
+    """new_lens [rows], moves [rows][2], missing [1], int32."""
+    device, rows = _pool_device(pool, tables), tables.rows
+    _check(lib().ee_kv_pages_grow(pool.address, pool.num_blocks, tables.c, _int32s(new_lens, (rows,), device), _int32s(moves, (rows, 2), device),
+                                  _int32s(missing, (1,), device), pool.ws.data_ptr(), pool.bytes, _raw_stream(device)))
+
+
+def ee_kv_pages_compact(pool: PagePool, tables: Optional[PageTables], remap: torch.Tensor, moves: torch.Tensor, n_moves: torch.Tensor):
+    """remap [num_blocks], moves [num_blocks][2], n_moves [1], int32."""
+    device, n = _pool_device(pool, tables), pool.num_blocks
+    _check(lib().ee_kv_pages_compact(pool.address, n, None if tables is None else tables.c, _int32s(remap, (n,), device), _int32s(moves, (n, 2), device),
+                                     _int32s(n_moves, (1,), device), pool.ws.data_ptr(), pool.bytes, _raw_stream(device)))
+
+
+def ee_kv_pages_shared(tables: PageTables, first_row: torch.Tensor, shared_blocks: torch.Tensor):
+    """first_row [groups + 1], shared_blocks [groups], int32."""
+    device, n = _pool_device(None, tables), shared_blocks.shape[0]
+    _check(lib().ee_kv_pages_shared(tables.c, _int32s(first_row, (n + 1,), device), n, _int32s(shared_blocks, (n,), device), _raw_stream(device)))
+
+
+def ee_kv_copy(desc: ee_model_desc, cache: PagedKV, moves: torch.Tensor, count: Optional[torch.Tensor] = None):
+    """moves [n][2] int32; count [1] int32: only the first of them."""
+    device, n = _device(), moves.shape[0]
+    assert cache.k.get_device() == device, "a cache of the current device"
+    _check(lib().ee_kv_copy(desc, cache.c, _int32s(moves, (n, 2), device), n, None if count is None else _int32s(count, (1,), device), _raw_stream(device)))
+
+
+def ee_kv_quant_copy(cache: QuantKV, moves: torch.Tensor, count: Optional[torch.Tensor] = None):
+    device, n = _device(), moves.shape[0]
+    assert cache.device == device, "a cache of the current device"
+    _check(lib().ee_kv_quant_copy(cache.c, _int32s(moves, (n, 2), device), n, None if count is None else _int32s(count, (1,), device), _raw_stream(device)))
+
+
+class BeamWorkspace:
+    """Scratch of ee_beam_select calls of these sizes."""
+
+    def __init__(self, groups: int, beams: int, vocab: int, n_out: int, device="cuda"):
+        self.bytes = lib().ee_beam_select_bytes(groups, beams, vocab, n_out)
+        if self.bytes == 0:
+            raise EEError(EE_ERR_INVALID_ARG, ee_last_error())
+        self.buf = torch.empty(self.bytes, dtype=torch.uint8, device=device)
+        assert self.buf.data_ptr() % 256 == 0
+
+
+def ee_beam_select(logits: torch.Tensor, scores: torch.Tensor, beams: int, tokens: torch.Tensor, parents: torch.Tensor, scores_out: torch.Tensor,
+                   ws: BeamWorkspace, finished: Optional[torch.Tensor] = None, finished_out: Optional[torch.Tensor] = None, end_token: int = -1):
+    """logits [groups * beams][vocab] float32 or bfloat16, any row stride; scores [groups * beams] float32; finished [groups * beams] int32; the results
+    [groups * n_out] (or [groups][n_out])."""
+    device, (rows, vocab) = _device(), logits.shape
+    assert beams > 0 and rows % beams == 0 and scores.shape == (rows,) and scores.dtype == torch.float32 and scores_out.dtype == torch.float32
+    assert logits.get_device() == device and (logits.stride(1) == 1 or vocab == 1), "rows of consecutive values on the current device"
+    groups = rows // beams
+    total = tokens.numel()
+    n_out = total // groups if groups else 1
+    assert total == groups * n_out and parents.numel() == total and scores_out.numel() == total and tokens.dtype == torch.int32 and parents.dtype == torch.int32
+    assert finished_out is None or finished_out.numel() == total and finished_out.dtype == torch.int32
+    _check(lib().ee_beam_select(logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, _KIND[logits.dtype], _here(scores, device),
+                                None if finished is None else _int32s(finished, (rows,), device), groups, beams, vocab, n_out, end_token,
+                                _here(tokens, device), _here(parents, device), _here(scores_out, device),
+                                None if finished_out is None else _here(finished_out, device), _here(ws.buf, device), ws.bytes, _raw_stream(device)))
+
+
+def ee_reorder_rows(x: torch.Tensor, parents: torch.Tensor, out: torch.Tensor):
+    """out[m] = x[parents[m]] of any type, rows of consecutive values at any row stride."""
+    device, rows = _device(), parents.shape[0]
+    assert x.dtype == out.dtype and x.shape[1:] == out.shape[1:] and out.shape[0] == rows and parents.dtype == torch.int32
+    size = x.element_size()
+    strides = []
+    for t in (x, out):
+        assert t.get_device() == device, "CUDA tensors of the current device"
+        if t.is_contiguous() or t.shape[0] == 0:
+            strides.append(t.numel() // t.shape[0] * size if t.shape[0] else 0)
+        else:
+            assert t[0].is_contiguous(), "rows of consecutive values"
+            strides.append(t.stride(0) * size)
+    row = out.numel() // rows * size if rows else 0
+    _check(lib().ee_reorder_rows(x.data_ptr(), strides[0], x.shape[0], _here(parents, device), rows, row, out.data_ptr(), strides[1], _raw_stream(device)))
+
+
+def make_prefix_groups(first_row: torch.Tensor, shared_blocks: torch.Tensor, max_shared: int) -> ee_prefix_groups:
+    """first_row [groups + 1], shared_blocks [groups], int32; max_shared bounds the latter."""
+    assert first_row.shape == (shared_blocks.shape[0] + 1,)
+    g = ee_prefix_groups(shared_blocks.shape[0], _ptr(_i32(first_row)), _ptr(_i32(shared_blocks)), max_shared)
+    g._keep = (first_row, shared_blocks)   # the record only holds raw pointers
+    g.device = first_row.get_device()
+    assert shared_blocks.get_device() == g.device, "the tensors of groups are on one device"
+    return g
+
+
+class SharedWorkspace:
+    """Scratch of ee_paged_attention_shared calls up to these sizes."""
+
+    def __init__(self, desc: ee_model_desc, n_heads: int, max_batch: int, max_groups: int, max_context: int, device="cuda"):
+        self.bytes = lib().ee_paged_attention_shared_bytes(desc, n_heads, max_batch, max_groups, max_context)
+        if self.bytes == 0:
+            raise EEError(EE_ERR_INVALID_ARG, ee_last_error())
+        self.buf = torch.empty(self.bytes, dtype=torch.uint8, device=device)
+        assert self.buf.data_ptr() % 256 == 0
+
+
+def ee_paged_attention_shared(desc: ee_model_desc, cache: PagedKV, layer: int, q: torch.Tensor, batch: ee_batch, groups: ee_prefix_groups,
+                              out: torch.Tensor, ws: SharedWorkspace):
+    """q, out [rows][n_heads][dh] float32; the cache has desc.n_heads K/V heads."""
+    device = _device()
+    assert cache.k.get_device() == device and batch.device == device and groups.device == device, "cache, batch and groups of the current device"
+    rows, heads, dh = q.shape
+    assert out.shape == q.shape and rows == batch.batch and dh == desc.head_dim and q.dtype == torch.float32 and out.dtype == torch.float32
+    _check(lib().ee_paged_attention_shared(desc, cache.c, layer, heads, _here(q, device), batch, groups, _here(out, device), _here(ws.buf, device), ws.bytes,
+                                           _raw_stream(device)))
 
 
 def ee_profile_enable(on: bool):

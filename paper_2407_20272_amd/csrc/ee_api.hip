@@ -7,6 +7,7 @@
 #include <vector>
 
 #include "quant.h"
+#include "beams.h"
 
 // Scratch of ee_exit_check_noalloc (see noalloc_scratch below).
 static __device__ __align__(256) unsigned char scratch[EE_NOALLOC_SCRATCH_BYTES];
@@ -1303,6 +1304,411 @@ int ee_kv_quant_evict(const ee_quant_cache* cache, int32_t layer, const ee_batch
   {
     ProfScope ps(EE_K_OTHER, layer, st);
     launch_quant_evict(a, st);
+  }
+  EE_HIP(hipGetLastError());
+  return EE_OK;
+}
+
+// ---- Several continuations of a prompt --------------------------------------------------------------------------
+namespace {
+
+constexpr int kMostPageRows = 1 << 20;
+constexpr int kMostPageBlocks = 1 << 23;   // (the chunks' counts are kept in LDS)
+
+int check_pool(const int32_t* refs, int32_t num_blocks, const char* what) {
+  if (!refs || (reinterpret_cast<uintptr_t>(refs) & 3)) EE_FAIL(EE_ERR_INVALID_ARG, "%s: refs NULL or misaligned", what);
+  if (num_blocks < 1) EE_FAIL(EE_ERR_INVALID_ARG, "%s: num_blocks must be positive", what);
+  if (num_blocks > kMostPageBlocks) EE_FAIL(EE_ERR_UNSUPPORTED, "%s: num_blocks %d exceeds %d", what, num_blocks, kMostPageBlocks);
+  return EE_OK;
+}
+
+int check_tables(const ee_page_tables* T, const char* what, PageRows* r) {
+  if (!T) EE_FAIL(EE_ERR_INVALID_ARG, "%s: tables are NULL", what);
+  if (T->rows < 0) EE_FAIL(EE_ERR_INVALID_ARG, "%s: %d rows", what, T->rows);
+  *r = PageRows{T->block_tables, T->lens, T->rows, T->max_blocks};
+  if (T->rows == 0) return EE_OK;
+  if (!T->block_tables || !T->lens || ((reinterpret_cast<uintptr_t>(T->block_tables) | reinterpret_cast<uintptr_t>(T->lens)) & 3))
+    EE_FAIL(EE_ERR_INVALID_ARG, "%s: tables NULL or misaligned", what);
+  if (T->rows > kMostPageRows) EE_FAIL(EE_ERR_UNSUPPORTED, "%s: %d rows in one call", what, T->rows);
+  if (T->max_blocks < 1) EE_FAIL(EE_ERR_INVALID_ARG, "%s: max_blocks must be positive", what);
+  if (T->max_blocks > kMostPageBlocks) EE_FAIL(EE_ERR_UNSUPPORTED, "%s: max_blocks %d exceeds %d", what, T->max_blocks, kMostPageBlocks);
+  return EE_OK;
+}
+
+size_t table_bytes(const PageRows& r) { return (size_t)r.rows * r.max_blocks * sizeof(int32_t); }
+size_t len_bytes(const PageRows& r) { return (size_t)r.rows * sizeof(int32_t); }
+
+int check_int32(const void* p, const char* what) {
+  if (!p || (reinterpret_cast<uintptr_t>(p) & 3)) EE_FAIL(EE_ERR_INVALID_ARG, "%s: NULL or misaligned pointer", what);
+  return EE_OK;
+}
+
+// The work area of a pool of num_blocks and calls of rows; its bytes.
+size_t carve_pages(int num_blocks, int rows, void* ws, PageWork* w) {
+  const size_t chunks = page_chunks(num_blocks);
+  char* at = reinterpret_cast<char*>(ws);
+  size_t used = 0;
+  auto take = [&](size_t bytes) {
+    char* p = at ? at + used : nullptr;
+    used += align256(bytes);
+    return p;
+  };
+  char* taken = take(chunks * 16 * sizeof(uint64_t));
+  char* counts = take(chunks * sizeof(int32_t));
+  char* claims = take((size_t)num_blocks * sizeof(int32_t));
+  char* latest = take((size_t)num_blocks * sizeof(int32_t));
+  char* row_first = take(((size_t)rows + 1) * sizeof(int32_t));
+  char* replaces = take((size_t)rows * sizeof(int32_t));
+  if (w)
+    *w = PageWork{reinterpret_cast<uint64_t*>(taken), reinterpret_cast<int32_t*>(counts), reinterpret_cast<int32_t*>(claims),
+                  reinterpret_cast<int32_t*>(latest), reinterpret_cast<int32_t*>(row_first), reinterpret_cast<int32_t*>(replaces)};
+  return used;
+}
+
+int copy_pages(PageCopyArgs a, const int32_t* moves, int32_t n, const int32_t* count, const char* what, void* stream) {
+  if (n < 0) EE_FAIL(EE_ERR_INVALID_ARG, "%s: %d moves", what, n);
+  if (n == 0) return EE_OK;
+  if (!moves || ((reinterpret_cast<uintptr_t>(moves) | reinterpret_cast<uintptr_t>(count)) & 3)) EE_FAIL(EE_ERR_INVALID_ARG, "%s: moves NULL or misaligned", what);
+  for (int p = 0; p < 2; ++p)
+    if (reinterpret_cast<uintptr_t>(a.pool[p].base) & 15) EE_FAIL(EE_ERR_INVALID_ARG, "%s: pools must start on 16 bytes", what);
+  a.moves = moves;
+  a.count = count;
+  a.n = n;
+  const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  {
+    ProfScope ps(EE_K_OTHER, 0, st);
+    launch_pages_copy(a, st);
+  }
+  EE_HIP(hipGetLastError());
+  return EE_OK;
+}
+
+int check_shared_heads(const ee_model_desc* D, int32_t n_heads) {
+  if (n_heads < 1 || n_heads % D->n_heads) EE_FAIL(EE_ERR_SHAPE, "n_heads %d is no multiple of the cache's %d", n_heads, D->n_heads);
+  if (n_heads > 65536) EE_FAIL(EE_ERR_UNSUPPORTED, "%d heads over %d K/V heads", n_heads, D->n_heads);
+  return EE_OK;
+}
+
+int check_shared_tiles(const SharedAttnArgs& a) {
+  if (a.tiles > 65535) EE_FAIL(EE_ERR_UNSUPPORTED, "attention: %d rows in %d groups, %d heads over %d, in one call", a.rows, a.n_groups, a.kv_heads * a.group, a.kv_heads);
+  return EE_OK;
+}
+
+}  // namespace
+
+size_t ee_kv_pages_bytes(int32_t num_blocks, int32_t max_rows) {
+  if (num_blocks < 1 || num_blocks > kMostPageBlocks || max_rows < 0 || max_rows > kMostPageRows) {
+    set_error("ee_kv_pages_bytes: %d blocks, %d rows", num_blocks, max_rows);
+    return 0;
+  }
+  return carve_pages(num_blocks, max_rows, nullptr, nullptr);
+}
+
+int ee_kv_pages_fork(int32_t* refs, int32_t num_blocks, const ee_page_tables* src, const int32_t* parents, const ee_page_tables* dst,
+                     int32_t release, void* stream) {
+  int rc;
+  PageRows from, to;
+  if ((rc = check_pool(refs, num_blocks, "ee_kv_pages_fork")) || (rc = check_tables(src, "ee_kv_pages_fork", &from)) || (rc = check_tables(dst, "ee_kv_pages_fork", &to)))
+    return rc;
+  if (release != 0 && release != 1) EE_FAIL(EE_ERR_INVALID_ARG, "ee_kv_pages_fork: release must be 0 or 1");
+  if (to.rows > 0) {
+    if ((rc = check_int32(parents, "ee_kv_pages_fork"))) return rc;
+    if (from.rows > 0 && to.max_blocks < from.max_blocks) EE_FAIL(EE_ERR_SHAPE, "ee_kv_pages_fork: %d entries a row for rows of %d", to.max_blocks, from.max_blocks);
+    if (ranges_meet(from.tables, table_bytes(from), to.tables, table_bytes(to)) || ranges_meet(from.lens, len_bytes(from), to.lens, len_bytes(to)) ||
+        ranges_meet(from.lens, len_bytes(from), to.tables, table_bytes(to)) || ranges_meet(from.tables, table_bytes(from), to.lens, len_bytes(to)) ||
+        ranges_meet(parents, len_bytes(to), to.tables, table_bytes(to)) || ranges_meet(parents, len_bytes(to), to.lens, len_bytes(to)))
+      EE_FAIL(EE_ERR_INVALID_ARG, "ee_kv_pages_fork: what is written overlaps what is read");
+  }
+  if (to.rows == 0 && !(release && from.rows > 0)) return EE_OK;
+  const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  {
+    ProfScope ps(EE_K_OTHER, 0, st);
+    if (to.rows > 0) launch_pages_fork(refs, num_blocks, from, parents, to, st);
+    if (release && from.rows > 0) launch_pages_release(refs, num_blocks, from, st);
+  }
+  EE_HIP(hipGetLastError());
+  return EE_OK;
+}
+
+int ee_kv_pages_release(int32_t* refs, int32_t num_blocks, const ee_page_tables* tables, void* stream) {
+  int rc;
+  PageRows r;
+  if ((rc = check_pool(refs, num_blocks, "ee_kv_pages_release")) || (rc = check_tables(tables, "ee_kv_pages_release", &r))) return rc;
+  if (r.rows == 0) return EE_OK;
+  const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  {
+    ProfScope ps(EE_K_OTHER, 0, st);
+    launch_pages_release(refs, num_blocks, r, st);
+  }
+  EE_HIP(hipGetLastError());
+  return EE_OK;
+}
+
+int ee_kv_pages_grow(int32_t* refs, int32_t num_blocks, const ee_page_tables* tables, const int32_t* new_lens, int32_t* moves, int32_t* missing,
+                     void* workspace, size_t workspace_bytes, void* stream) {
+  int rc;
+  PageRows r;
+  if ((rc = check_pool(refs, num_blocks, "ee_kv_pages_grow")) || (rc = check_tables(tables, "ee_kv_pages_grow", &r))) return rc;
+  if ((rc = check_int32(missing, "ee_kv_pages_grow"))) return rc;
+  if (r.rows > 0) {
+    if ((rc = check_int32(new_lens, "ee_kv_pages_grow")) || (rc = check_int32(moves, "ee_kv_pages_grow"))) return rc;
+    if (ranges_meet(new_lens, len_bytes(r), moves, 2 * len_bytes(r)) || ranges_meet(r.lens, len_bytes(r), moves, 2 * len_bytes(r)) ||
+        ranges_meet(new_lens, len_bytes(r), missing, sizeof(int32_t)) || ranges_meet(r.lens, len_bytes(r), missing, sizeof(int32_t)))
+      EE_FAIL(EE_ERR_INVALID_ARG, "ee_kv_pages_grow: moves or missing overlap the lengths");
+  }
+  PageWork w;
+  if ((rc = check_raw_workspace(workspace, workspace_bytes, carve_pages(num_blocks, r.rows, workspace, &w)))) return rc;
+  const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  {
+    ProfScope ps(EE_K_OTHER, 0, st);
+    launch_pages_grow(refs, num_blocks, r, new_lens, moves, missing, w, st);
+  }
+  EE_HIP(hipGetLastError());
+  return EE_OK;
+}
+
+int ee_kv_pages_compact(int32_t* refs, int32_t num_blocks, const ee_page_tables* tables, int32_t* remap, int32_t* moves, int32_t* n_moves,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+  int rc;
+  PageRows r{};
+  if ((rc = check_pool(refs, num_blocks, "ee_kv_pages_compact")) || (tables && (rc = check_tables(tables, "ee_kv_pages_compact", &r)))) return rc;
+  if ((rc = check_int32(remap, "ee_kv_pages_compact")) || (rc = check_int32(moves, "ee_kv_pages_compact")) || (rc = check_int32(n_moves, "ee_kv_pages_compact")))
+    return rc;
+  const size_t all = (size_t)num_blocks * sizeof(int32_t);
+  if (ranges_meet(remap, all, refs, all) || ranges_meet(moves, 2 * all, refs, all) || ranges_meet(remap, all, moves, 2 * all))
+    EE_FAIL(EE_ERR_INVALID_ARG, "ee_kv_pages_compact: refs, remap and moves overlap");
+  PageWork w;
+  if ((rc = check_raw_workspace(workspace, workspace_bytes, carve_pages(num_blocks, 0, workspace, &w)))) return rc;
+  const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  {
+    ProfScope ps(EE_K_OTHER, 0, st);
+    launch_pages_compact(refs, num_blocks, r, remap, moves, n_moves, w, st);
+  }
+  EE_HIP(hipGetLastError());
+  return EE_OK;
+}
+
+int ee_kv_pages_shared(const ee_page_tables* tables, const int32_t* first_row, int32_t n_groups, int32_t* shared_blocks, void* stream) {
+  int rc;
+  PageRows r;
+  if ((rc = check_tables(tables, "ee_kv_pages_shared", &r))) return rc;
+  if (n_groups < 0 || n_groups > kMostPageRows) EE_FAIL(EE_ERR_INVALID_ARG, "ee_kv_pages_shared: %d groups", n_groups);
+  if (n_groups == 0) return EE_OK;
+  if ((rc = check_int32(first_row, "ee_kv_pages_shared")) || (rc = check_int32(shared_blocks, "ee_kv_pages_shared"))) return rc;
+  const size_t bytes = (size_t)n_groups * sizeof(int32_t);
+  if (ranges_meet(first_row, bytes + sizeof(int32_t), shared_blocks, bytes)) EE_FAIL(EE_ERR_INVALID_ARG, "ee_kv_pages_shared: first_row and shared_blocks overlap");
+  const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  {
+    ProfScope ps(EE_K_OTHER, 0, st);
+    launch_pages_shared(r, first_row, n_groups, shared_blocks, st);
+  }
+  EE_HIP(hipGetLastError());
+  return EE_OK;
+}
+
+int ee_kv_copy(const ee_model_desc* desc, const ee_kv_cache* cache, const int32_t* moves, int32_t n, const int32_t* count, void* stream) {
+  int rc;
+  if ((rc = check_desc(desc)) || (rc = check_cache(cache))) return rc;
+  const size_t block = (size_t)desc->n_heads * 16 * desc->head_dim * elem_bytes(*desc);
+  PageCopyArgs a{};
+  a.pool[0] = PagePlane{reinterpret_cast<char*>(cache->k_pool), block, desc->n_layers};
+  a.pool[1] = PagePlane{reinterpret_cast<char*>(cache->v_pool), block, desc->n_layers};
+  a.n_pools = 2;
+  a.num_blocks = cache->num_blocks;
+  return copy_pages(a, moves, n, count, "ee_kv_copy", stream);
+}
+
+int ee_kv_quant_copy(const ee_quant_cache* cache, const int32_t* moves, int32_t n, const int32_t* count, void* stream) {
+  int rc;
+  if ((rc = check_quant_cache(cache))) return rc;
+  const size_t block = (size_t)cache->n_kv_heads * 16 * cache->head_dim;
+  PageCopyArgs a{};
+  a.pool[0] = PagePlane{reinterpret_cast<char*>(cache->k_pool), block, cache->n_layers};
+  a.pool[1] = PagePlane{reinterpret_cast<char*>(cache->v_pool), block, cache->n_layers};
+  a.pool[2] = PagePlane{reinterpret_cast<char*>(cache->scales), (size_t)cache->n_kv_heads * 2 * sizeof(float), cache->n_layers};
+  a.n_pools = 3;
+  a.num_blocks = cache->num_blocks;
+  return copy_pages(a, moves, n, count, "ee_kv_quant_copy", stream);
+}
+
+namespace {
+
+int check_beams(int32_t groups, int32_t beams, int32_t vocab, int32_t n_out) {
+  if (groups < 0 || beams < 1 || vocab < 1 || n_out < 1) EE_FAIL(EE_ERR_INVALID_ARG, "beam selection: %d groups of %d beams, vocab %d, n_out %d", groups, beams, vocab, n_out);
+  if (beams > kBeamMost || n_out > kBeamMost) EE_FAIL(EE_ERR_UNSUPPORTED, "beam selection: %d beams, n_out %d: up to %d", beams, n_out, kBeamMost);
+  if (n_out > (int64_t)beams * vocab) EE_FAIL(EE_ERR_SHAPE, "beam selection: n_out %d of %d beams and vocab %d", n_out, beams, vocab);
+  if ((int64_t)groups * beams > 65535) EE_FAIL(EE_ERR_UNSUPPORTED, "beam selection: %d groups of %d beams in one call", groups, beams);
+  if (vocab > 1 << 24) EE_FAIL(EE_ERR_UNSUPPORTED, "beam selection: vocab %d exceeds %d", vocab, 1 << 24);
+  return EE_OK;
+}
+
+size_t carve_beams(BeamArgs& a, void* ws) {
+  beam_plan(a);
+  const size_t pieces = (size_t)a.groups * a.beams * a.chunks, stats = align256(pieces * sizeof(double2));
+  a.stats = reinterpret_cast<double2*>(ws);
+  a.found = reinterpret_cast<uint64_t*>(reinterpret_cast<char*>(ws) + stats);
+  return stats + align256(pieces * a.n_out * sizeof(uint64_t));
+}
+
+}  // namespace
+
+size_t ee_beam_select_bytes(int32_t groups, int32_t beams, int32_t vocab, int32_t n_out) {
+  if (check_beams(groups, beams, vocab, n_out)) return 0;
+  BeamArgs a{};
+  a.groups = groups < 1 ? 1 : groups;
+  a.beams = beams;
+  a.vocab = vocab;
+  a.n_out = n_out;
+  size_t most = carve_beams(a, nullptr);
+  if (n_out > kBeamFewOut) {   // (fewer come back of smaller chunks)
+    a.n_out = kBeamFewOut;
+    const size_t few = carve_beams(a, nullptr);
+    most = few > most ? few : most;
+  }
+  return most;
+}
+
+int ee_beam_select(const void* logits, int64_t logits_stride, int32_t dtype, const float* scores, const int32_t* finished, int32_t groups, int32_t beams,
+                   int32_t vocab, int32_t n_out, int32_t end_token, int32_t* tokens, int32_t* parents, float* scores_out, int32_t* finished_out,
+                   void* workspace, size_t workspace_bytes, void* stream) {
+  int rc;
+  if (dtype != EE_FP32 && dtype != EE_BF16) EE_FAIL(EE_ERR_INVALID_ARG, "ee_beam_select: dtype must be EE_FP32 or EE_BF16");
+  if ((rc = check_beams(groups, beams, vocab, n_out))) return rc;
+  if (end_token < -1 || end_token >= vocab) EE_FAIL(EE_ERR_INVALID_ARG, "ee_beam_select: end_token %d outside -1..%d", end_token, vocab - 1);
+  if (finished && end_token < 0) EE_FAIL(EE_ERR_INVALID_ARG, "ee_beam_select: finished rows need an end_token");
+  if (groups == 0) return EE_OK;
+  const int size = dtype == EE_BF16 ? 2 : 4, rows = groups * beams;
+  if (!logits || reinterpret_cast<uintptr_t>(logits) % size) EE_FAIL(EE_ERR_INVALID_ARG, "ee_beam_select: logits NULL or misaligned");
+  if (logits_stride < vocab || logits_stride > INT64_MAX / 16 / rows) EE_FAIL(EE_ERR_SHAPE, "ee_beam_select: stride %lld for rows of %d", (long long)logits_stride, vocab);
+  if ((rc = check_int32(scores, "ee_beam_select")) || (rc = check_int32(tokens, "ee_beam_select")) || (rc = check_int32(parents, "ee_beam_select")) ||
+      (rc = check_int32(scores_out, "ee_beam_select")))
+    return rc;
+  if ((reinterpret_cast<uintptr_t>(finished) | reinterpret_cast<uintptr_t>(finished_out)) & 3) EE_FAIL(EE_ERR_INVALID_ARG, "ee_beam_select: misaligned pointer");
+  const size_t in = (size_t)rows * 4, out = (size_t)groups * n_out * 4;
+  const void* outs[4] = {tokens, parents, scores_out, finished_out};
+  for (int i = 0; i < 4; ++i) {
+    if (!outs[i]) continue;
+    if (ranges_meet(outs[i], out, scores, in) || (finished && ranges_meet(outs[i], out, finished, in)))
+      EE_FAIL(EE_ERR_INVALID_ARG, "ee_beam_select: results overlap scores or finished");
+    for (int k = 0; k < i; ++k)
+      if (outs[k] && ranges_meet(outs[i], out, outs[k], out)) EE_FAIL(EE_ERR_INVALID_ARG, "ee_beam_select: results overlap each other");
+  }
+  BeamArgs a{};
+  a.logits = logits;
+  a.stride = logits_stride;
+  a.scores = scores;
+  a.finished = finished;
+  a.groups = groups;
+  a.beams = beams;
+  a.vocab = vocab;
+  a.n_out = n_out;
+  a.end_token = end_token;
+  a.tokens = tokens;
+  a.parents = parents;
+  a.scores_out = scores_out;
+  a.finished_out = finished_out;
+  if ((rc = check_raw_workspace(workspace, workspace_bytes, carve_beams(a, workspace)))) return rc;
+  const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  {
+    ProfScope ps(EE_K_HEAD, 0, st);
+    launch_beam_select(a, dtype, st);
+  }
+  EE_HIP(hipGetLastError());
+  return EE_OK;
+}
+
+int ee_reorder_rows(const void* in, int64_t in_stride, int32_t in_rows, const int32_t* parents, int32_t rows, int64_t row_bytes, void* out,
+                    int64_t out_stride, void* stream) {
+  int rc;
+  if (in_rows < 0 || rows < 0 || row_bytes < 0) EE_FAIL(EE_ERR_INVALID_ARG, "ee_reorder_rows: %d rows of %d, %lld bytes", rows, in_rows, (long long)row_bytes);
+  if (rows == 0 || in_rows == 0 || row_bytes == 0) return EE_OK;
+  if (!in || !out) EE_FAIL(EE_ERR_INVALID_ARG, "ee_reorder_rows: NULL pointer");
+  if ((rc = check_int32(parents, "ee_reorder_rows"))) return rc;
+  const int64_t far = INT64_MAX / 16;
+  if (in_stride < row_bytes || out_stride < row_bytes || in_stride > far / in_rows || out_stride > far / rows)
+    EE_FAIL(EE_ERR_SHAPE, "ee_reorder_rows: strides %lld, %lld for rows of %lld bytes", (long long)in_stride, (long long)out_stride, (long long)row_bytes);
+  if (row_bytes > (int64_t)1 << 40 || (row_bytes + 16383) / 16384 * rows > (1 << 23)) EE_FAIL(EE_ERR_UNSUPPORTED, "ee_reorder_rows: %d rows of %lld bytes in one call", rows, (long long)row_bytes);
+  const size_t out_bytes = (size_t)(rows - 1) * out_stride + row_bytes;
+  if (ranges_meet(in, (size_t)(in_rows - 1) * in_stride + row_bytes, out, out_bytes) || ranges_meet(parents, (size_t)rows * 4, out, out_bytes))
+    EE_FAIL(EE_ERR_INVALID_ARG, "ee_reorder_rows: out overlaps in or parents");
+  const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  {
+    ProfScope ps(EE_K_OTHER, 0, st);
+    launch_reorder_rows(RowCopyArgs{reinterpret_cast<const char*>(in), reinterpret_cast<char*>(out), in_stride, out_stride, row_bytes, parents, in_rows, rows}, st);
+  }
+  EE_HIP(hipGetLastError());
+  return EE_OK;
+}
+
+size_t ee_paged_attention_shared_bytes(const ee_model_desc* desc, int32_t n_heads, int32_t max_batch, int32_t max_groups, int32_t max_context) {
+  if (check_desc(desc) || check_shared_heads(desc, n_heads)) return 0;
+  if (max_batch < 1 || max_groups < 1 || max_groups > 65536 || max_context < 1 || max_context > kAttnMaxBlocks * 16) {
+    set_error("ee_paged_attention_shared_bytes: batch %d, %d groups, context %d", max_batch, max_groups, max_context);
+    return 0;
+  }
+  SharedAttnArgs a{};
+  a.rows = max_batch;
+  a.kv_heads = desc->n_heads;
+  a.group = n_heads / desc->n_heads;
+  a.dh = desc->head_dim;
+  a.n_groups = max_groups;
+  a.max_context = max_context;
+  size_t tiles;
+  const size_t floats = shared_attn_most_floats(a, desc->dtype, &tiles);
+  if (check_shared_tiles(a)) return 0;
+  const size_t all = align256(tiles * sizeof(int4)) + align256(floats * sizeof(float));
+  return all ? all : 256;   // (0 says that the sizes are refused)
+}
+
+int ee_paged_attention_shared(const ee_model_desc* desc, const ee_kv_cache* cache, int32_t layer, int32_t n_heads, const float* q, const ee_batch* batch,
+                              const ee_prefix_groups* groups, float* out, void* workspace, size_t workspace_bytes, void* stream) {
+  int rc;
+  if ((rc = check_desc(desc)) || (rc = check_cache(cache)) || (rc = check_batch(batch, false)) || (rc = check_shared_heads(desc, n_heads))) return rc;
+  if (!groups) EE_FAIL(EE_ERR_INVALID_ARG, "ee_paged_attention_shared: groups are NULL");
+  if (groups->n_groups < 0 || groups->max_shared < 0) EE_FAIL(EE_ERR_INVALID_ARG, "ee_paged_attention_shared: %d groups, max_shared %d", groups->n_groups, groups->max_shared);
+  if (groups->n_groups > 65536) EE_FAIL(EE_ERR_UNSUPPORTED, "ee_paged_attention_shared: %d groups in one call", groups->n_groups);
+  if (batch->batch == 0 || groups->n_groups == 0) return EE_OK;
+  if (layer < 1 || layer > desc->n_layers) EE_FAIL(EE_ERR_INVALID_ARG, "layer %d outside 1..%d", layer, desc->n_layers);
+  if ((rc = check_int32(groups->first_row, "ee_paged_attention_shared")) || (rc = check_int32(groups->shared_blocks, "ee_paged_attention_shared"))) return rc;
+  if (!q || !out || ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 15))
+    EE_FAIL(EE_ERR_INVALID_ARG, "ee_paged_attention_shared: q and out must start on 16 bytes");
+  if ((reinterpret_cast<uintptr_t>(cache->k_pool) | reinterpret_cast<uintptr_t>(cache->v_pool)) & 15)
+    EE_FAIL(EE_ERR_INVALID_ARG, "ee_paged_attention_shared: pools must start on 16 bytes");
+  const size_t q_bytes = (size_t)batch->batch * n_heads * desc->head_dim * sizeof(float);
+  if (ranges_meet(q, q_bytes, out, q_bytes)) EE_FAIL(EE_ERR_INVALID_ARG, "ee_paged_attention_shared: q and out overlap");
+  const size_t off = pool_layer_elems(*desc, *cache) * elem_bytes(*desc) * (size_t)(layer - 1);
+  SharedAttnArgs a{};
+  a.q = q;
+  a.out = out;
+  a.k = reinterpret_cast<const char*>(cache->k_pool) + off;
+  a.v = reinterpret_cast<const char*>(cache->v_pool) + off;
+  a.context_lens = batch->context_lens;
+  a.block_tables = batch->block_tables;
+  a.row_table = batch->row_table;
+  a.max_blocks = batch->max_blocks;
+  a.rows = batch->batch;
+  a.kv_heads = desc->n_heads;
+  a.group = n_heads / desc->n_heads;
+  a.dh = desc->head_dim;
+  a.num_blocks = cache->num_blocks;
+  a.first_row = groups->first_row;
+  a.shared_blocks = groups->shared_blocks;
+  a.n_groups = groups->n_groups;
+  a.max_shared = groups->max_shared;
+  a.max_context = batch->max_context;
+  shared_attn_plan(a, desc->dtype);
+  if ((rc = check_shared_tiles(a))) return rc;
+  const size_t tile_bytes = a.parts > 1 ? align256((size_t)a.tiles * sizeof(int4)) : 0;
+  const size_t record_bytes = align256(shared_attn_record_floats(a) * sizeof(float));
+  if ((rc = check_raw_workspace(workspace, workspace_bytes, tile_bytes + record_bytes))) return rc;
+  if (a.parts > 1) {
+    a.tile_of = reinterpret_cast<int4*>(workspace);
+    a.records = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + tile_bytes);
+  }
+  const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  {
+    ProfScope ps(EE_K_ATTN, layer, st);
+    launch_shared_attention(a, desc->dtype, st);
   }
   EE_HIP(hipGetLastError());
   return EE_OK;
