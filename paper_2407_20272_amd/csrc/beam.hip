@@ -336,7 +336,7 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
 
 // A workgroup copies up to 16 KiB of a row, in the widest pieces that addresses, strides and the row allow.
 constexpr int kRowPiece = 16384;
-template <class V>
+template <class V>   // (a vector type of the compiler's: an array of structures would pass through LDS)
 __global__ __launch_bounds__(256) void reorder_rows_kernel(RowCopyArgs a, int pieces) {
   const int row = blockIdx.x / pieces, piece = blockIdx.x - row * pieces;
   const int p = a.parents[row];
@@ -382,7 +382,7 @@ void launch_reorder_rows(const RowCopyArgs& a, hipStream_t st) {
   const uint64_t all = reinterpret_cast<uintptr_t>(a.in) | reinterpret_cast<uintptr_t>(a.out) | a.in_stride | a.out_stride | a.row_bytes;
   const int pieces = (int)((a.row_bytes + kRowPiece - 1) / kRowPiece);
   const unsigned grid = (unsigned)((int64_t)a.rows * pieces);
-  if (all % 16 == 0) reorder_rows_kernel<uint4><<<grid, 256, 0, st>>>(a, pieces);
+  if (all % 16 == 0) reorder_rows_kernel<u32x4><<<grid, 256, 0, st>>>(a, pieces);
   else if (all % 4 == 0) reorder_rows_kernel<uint32_t><<<grid, 256, 0, st>>>(a, pieces);
   else reorder_rows_kernel<uint8_t><<<grid, 256, 0, st>>>(a, pieces);
 }

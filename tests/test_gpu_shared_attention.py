@@ -91,7 +91,7 @@ def test_groups_of_all_kinds(dtype, dh, heads, kv):
 
 
 @pytest.mark.parametrize("dtype,dh,heads,kv", HEADS)
-@pytest.mark.parametrize("rows", [1, 2, 15, 16, 17, 64, 65, 130])
+@pytest.mark.parametrize("rows", [1, 2, 15, 16, 17, 33, 64, 65, 130])
 def test_many_rows_of_one_group(dtype, dh, heads, kv, rows):
     Case(dtype, dh, heads, kv, [(5, [80 + (i * 7) % 45 for i in range(rows)])], seed=rows).check()
 
