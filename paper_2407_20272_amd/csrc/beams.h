@@ -83,10 +83,10 @@ struct SharedAttnArgs {
   int max_blocks, rows, kv_heads, group, dh, num_blocks;
   const int32_t *first_row, *shared_blocks;
   int n_groups, max_shared, max_context;
-  // Set by shared_attn_plan: columns (a row and one of its query heads) of a tile, tiles, and the parts that a tile's positions are divided into.
-  int columns, rows_per_tile, head_chunks, tiles, parts;
-  int4* tile_of;               // parts > 1: [tiles]: first row, rows, parts that have steps
-  float* records;              // parts > 1: [tiles][kv heads][head chunks][parts][columns][dh + 4]: maximum, sum, -, -, sums of V
+  // Set by shared_attn_plan: columns (a row and one of its query heads) of a tile, tiles, and workgroups of a K/V head that are dealt out to the tiles (0: one a tile).
+  int columns, rows_per_tile, head_chunks, tiles, dealt;
+  int4* tile_of;               // dealt: [tiles]: first row, rows, first workgroup and how many
+  float* records;              // dealt: [head chunks][kv heads][workgroup][columns][dh + 4]: maximum, sum, -, -, sums of V
 };
 void shared_attn_plan(SharedAttnArgs& a, int dtype);
 size_t shared_attn_record_floats(const SharedAttnArgs& a);

@@ -1698,10 +1698,10 @@ int ee_paged_attention_shared(const ee_model_desc* desc, const ee_kv_cache* cach
   a.max_context = batch->max_context;
   shared_attn_plan(a, desc->dtype);
   if ((rc = check_shared_tiles(a))) return rc;
-  const size_t tile_bytes = a.parts > 1 ? align256((size_t)a.tiles * sizeof(int4)) : 0;
+  const size_t tile_bytes = a.dealt ? align256((size_t)a.tiles * sizeof(int4)) : 0;
   const size_t record_bytes = align256(shared_attn_record_floats(a) * sizeof(float));
   if ((rc = check_raw_workspace(workspace, workspace_bytes, tile_bytes + record_bytes))) return rc;
-  if (a.parts > 1) {
+  if (a.dealt) {
     a.tile_of = reinterpret_cast<int4*>(workspace);
     a.records = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + tile_bytes);
   }

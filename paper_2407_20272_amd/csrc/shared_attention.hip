@@ -29,8 +29,9 @@ constexpr int kThreads = kWaves * 64;
 constexpr float kNegBig = -1.0e30f;
 constexpr int kMostColumns = 48;    // of a tile (64 columns' sums and what is multiplied with them are more than 256 registers)
 constexpr int kMostRows = kMostColumns;
-constexpr int kMostWgs = 256, kMostParts = 256, kFewSteps = 16;   // workgroups that run at once; parts of a tile; steps that are worth a part
-constexpr int kEarlyRows = 1024;    // up to so many rows' lengths are asked for together with the groups
+constexpr int kMostWgs = 256;   // workgroups that run at once
+constexpr int kWorthDealing = 64;   // steps of a tile
+constexpr int kDealRows = 1024, kDealGroups = 512, kDealTiles = 512;   // up to so many are dealt out
 
 // The upper halves of two words (two floats truncated to bf16), the first in the low half.
 __device__ inline uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
@@ -51,46 +52,148 @@ __device__ inline void split3(const float (&x)[8], u32x4 (&part)[3]) {
   }
 }
 
-// The tile's rows: found by the sums of the groups' tiles.  s_tile: first row, rows (0: there is no such tile), shared blocks.  The rows' lengths come along.
-__device__ inline void find_tile(const SharedAttnArgs& a, int tile, int* s_tile, int* s_lens) {
-  __shared__ int s_wave[kWaves];
+// Sums over the lanes up to each one, on the cross-lane network.
+__device__ inline int wave_sums(int v) {
+  auto add = [&](auto ctrl, auto rows) { v += __builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, decltype(rows)::value, 0xf, false); };
+  add(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});   // row_shr 1, 2, 4, 8
+  add(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
+  add(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+  add(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+  add(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // row_bcast 15, 31
+  add(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
+  return v;
+}
+
+// The sum of the values of the threads before each, over the workgroup, and of all.
+__device__ inline int block_sums(int v, int* s_wave, int& all) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int upto = wave_sums(v);
+  __syncthreads();
+  if (lane == 63) s_wave[wave] = upto;
+  __syncthreads();
+  int before = upto - v;
+  all = 0;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) {
+    if (i < wave) before += s_wave[i];
+    all += s_wave[i];
+  }
+  return before;
+}
+
+// The last of n ascending numbers that is at most x (the first where none is).
+__device__ inline int last_within(const int* s, int n, int x) {
+  int lo = 0, hi = n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (s[mid] <= x) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+
+struct Group {
+  int first, rows, shared;   // shared: blocks
+};
+__device__ inline Group group_of(const SharedAttnArgs& a, int g) {
+  Group r{0, 0, 0};
+  if (g < a.n_groups) {
+    const int first = a.first_row[g], next = a.first_row[g + 1], shared = a.shared_blocks[g];
+    r.first = min(max(first, 0), a.rows);
+    r.rows = min(max(next, r.first), a.rows) - r.first;
+    r.shared = min(min(max(shared, 0), a.max_shared), a.max_blocks);
+  }
+  return r;
+}
+// Rows from .. to of a group, and its shared blocks; no rows: there is no such tile.
+struct Tile {
+  int row0, rows, shared;
+};
+__device__ inline int positions_of(const SharedAttnArgs& a, int len) { return min(max(len, -1), a.max_blocks * 16 - 1) + 1; }
+
+// A tile by its number.  Up to 64 groups every wavefront looks for itself, by registers; else they meet in LDS.
+__device__ inline Tile find_tile(const SharedAttnArgs& a, int tile, int* s_wave, int* s_tile) {
+  const int lane = threadIdx.x & 63;
+  if (a.n_groups <= 64) {
+    const Group g = group_of(a, lane);
+    const int tiles = (g.rows + a.rows_per_tile - 1) / a.rows_per_tile, upto = wave_sums(tiles);
+    const unsigned long long here = __ballot(tile >= upto - tiles && tile < upto);
+    if (!here) return Tile{0, 0, 0};
+    const int at = __builtin_ctzll(here), r0 = (tile - (upto - tiles)) * a.rows_per_tile;
+    return Tile{__builtin_amdgcn_readlane(g.first + r0, at), __builtin_amdgcn_readlane(min(a.rows_per_tile, g.rows - r0), at), __builtin_amdgcn_readlane(g.shared, at)};
+  }
   if (threadIdx.x == 0) s_tile[1] = 0;
-  if (a.rows <= kEarlyRows)
-    for (int m = threadIdx.x; m < a.rows; m += kThreads) s_lens[m] = a.context_lens[m];
   int sum = 0;
   for (int g0 = 0; g0 < a.n_groups; g0 += kThreads) {
-    const int g = g0 + threadIdx.x;
-    int first = 0, rows = 0, shared = 0;
-    if (g < a.n_groups) {
-      shared = a.shared_blocks[g];
-      first = min(max(a.first_row[g], 0), a.rows);
-      rows = min(max(a.first_row[g + 1], first), a.rows) - first;
-    }
-    const int tiles = (rows + a.rows_per_tile - 1) / a.rows_per_tile;
-    int upto = tiles;
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) {
-      const int o = __shfl_up(upto, x);
-      if (lane >= x) upto += o;
-    }
-    if (g0) __syncthreads();
-    if (lane == 63) s_wave[wave] = upto;
-    __syncthreads();
-    int before = sum + upto - tiles;
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
-      if (i < wave) before += s_wave[i];
-      sum += s_wave[i];
-    }
+    const Group g = group_of(a, g0 + threadIdx.x);
+    const int tiles = (g.rows + a.rows_per_tile - 1) / a.rows_per_tile;
+    int all;
+    const int before = sum + block_sums(tiles, s_wave, all);
+    sum += all;
     if (tile >= before && tile < before + tiles) {
       const int r0 = (tile - before) * a.rows_per_tile;
-      s_tile[0] = first + r0;
-      s_tile[1] = min(a.rows_per_tile, rows - r0);
-      s_tile[2] = min(min(max(shared, 0), a.max_shared), a.max_blocks);
+      s_tile[0] = g.first + r0;
+      s_tile[1] = min(a.rows_per_tile, g.rows - r0);
+      s_tile[2] = g.shared;
     }
   }
   __syncthreads();
+  return Tile{__builtin_amdgcn_readfirstlane(s_tile[0]), __builtin_amdgcn_readfirstlane(s_tile[1]), __builtin_amdgcn_readfirstlane(s_tile[2])};
+}
+
+// All tiles of a call, and how many workgroups each gets: about as many as its share of the steps, in every workgroup's LDS.
+struct Deal {
+  int group_first[kDealGroups], group_tile[kDealGroups], group_rows[kDealGroups], group_shared[kDealGroups];   // of each group: first row, tiles before it, ..
+  int steps[kDealTiles], with[kDealTiles], first[kDealTiles], parts[kDealTiles];   // of each tile: steps, whether rows attend the shared blocks together, workgroups before it, its own
+};
+__device__ inline Tile dealt_tile(const SharedAttnArgs& a, const Deal& d, int tile) {
+  const int g = last_within(d.group_tile, a.n_groups, tile), r0 = (tile - d.group_tile[g]) * a.rows_per_tile;
+  return Tile{d.group_first[g] + r0, min(a.rows_per_tile, d.group_rows[g] - r0), d.group_shared[g]};
+}
+// Tiles; `all`: workgroups that have something to do.
+__device__ inline int deal_tiles(const SharedAttnArgs& a, Deal& d, int* s_wave, int& all) {
+  const int t = threadIdx.x;
+  const Group g = group_of(a, t);
+  constexpr int EACH = kDealRows / kThreads;
+  int lens[EACH];
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) lens[i] = t + i * kThreads < a.rows ? a.context_lens[t + i * kThreads] : 0;
+  for (int i = t; i < a.tiles; i += kThreads) d.steps[i] = d.with[i] = 0;
+  int tiles;
+  const int before = block_sums((g.rows + a.rows_per_tile - 1) / a.rows_per_tile, s_wave, tiles);
+  if (t < a.n_groups) {
+    d.group_first[t] = g.first;
+    d.group_tile[t] = before;
+    d.group_rows[t] = g.rows;
+    d.group_shared[t] = g.shared;
+  }
+  tiles = min(tiles, a.tiles);
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    const int m = t + i * kThreads;
+    if (m >= a.rows) break;
+    const int of = last_within(d.group_first, a.n_groups, m), r = m - d.group_first[of], tile = d.group_tile[of] + r / a.rows_per_tile;
+    if (r < 0 || r >= d.group_rows[of] || tile >= tiles) continue;   // a row of no group
+    const int npos = positions_of(a, lens[i]), shared = d.group_shared[of] * 16;
+    const bool with = shared > 0 && npos >= shared;
+    atomicAdd(&d.steps[tile], (npos - (with ? shared : 0) + 31) >> 5);
+    if (with) d.with[tile] = 1;
+  }
+  __syncthreads();
+  static_assert(kDealTiles <= kThreads && kDealGroups <= kThreads, "a thread a tile");
+  int steps = 0, sum;
+  if (t < tiles) steps = d.steps[t] + (d.with[t] ? (dealt_tile(a, d, t).shared * 16 + 31) >> 5 : 0);
+  block_sums(steps, s_wave, sum);
+  const int most = max(1, steps / kWaves);   // (a step a wavefront at least)
+  const int parts = t < tiles ? min(most, max(1, (int)((int64_t)a.dealt * steps / max(sum, 1)))) : 0;
+  const int first = block_sums(parts, s_wave, all);
+  if (t < tiles) {
+    d.first[t] = first;
+    d.parts[t] = parts;
+  }
+  __syncthreads();
+  return tiles;
 }
 
 // The maximum over the four lanes of a column.
@@ -129,64 +232,38 @@ __global__ __launch_bounds__(kThreads) void shared_attn_kernel(SharedAttnArgs a)
   constexpr int PITCH = DH + 4;                          // (of a column's sums in LDS: 16 columns' rows begin in 16 different groups of banks)
   constexpr size_t Q_BYTES = NT > 1 ? (size_t)NT * KS * QP * 1024 : 0, O_BYTES = (size_t)kWaves * 16 * PITCH * 4;
   __shared__ __align__(16) char s_space[Q_BYTES > O_BYTES ? Q_BYTES : O_BYTES];   // q [NT][KS][QP][64 lanes] of 16 bytes, then the wavefronts' sums
-  __shared__ int s_tile[3];
-  __shared__ int s_lens[kEarlyRows];
-  __shared__ int s_first[kMostRows + 2];                 // of every run (the shared blocks, then the rows' own positions): steps before it
-  __shared__ int s_from[kMostRows + 1], s_end[kMostRows + 1], s_seq[kMostRows + 1];   // its positions, and the block table that it walks
-  __shared__ int s_with[kMostRows];                      // whether a row attends all shared blocks with the others
+  // Of every run (the shared blocks, then the rows' own positions), each wavefront for itself: steps before it, its positions from .. to, the block table that it walks.
+  __shared__ int4 s_runs[kWaves][kMostRows + 2];
   __shared__ float s_m[kWaves][16], s_l[kWaves][16];
+  __shared__ int s_wave[kWaves], s_tile[3];
+  __shared__ Deal s_deal;
 
-  const int kvh = blockIdx.x % a.kv_heads, hc = blockIdx.x / a.kv_heads;
-  const int part = blockIdx.y, tile = blockIdx.z;   // (tiles that there are not come last)
+  const int kvh = blockIdx.x % a.kv_heads, hc = blockIdx.x / a.kv_heads, wg = blockIdx.y;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, j = lane >> 4;
-  find_tile(a, tile, s_tile, s_lens);
-  const int row0 = __builtin_amdgcn_readfirstlane(s_tile[0]), n_rows = __builtin_amdgcn_readfirstlane(s_tile[1]);
-  const bool writes_tile = a.parts > 1 && part == 0 && blockIdx.x == 0 && threadIdx.x == 0;
-  if (n_rows == 0) {
-    if (writes_tile) a.tile_of[tile] = make_int4(0, 0, 0, 0);
-    return;
+  int4* runs = s_runs[wave];
+  // What this workgroup does: tile number wg, or part `part` of `parts` of a tile.
+  const int early_len = a.rows <= 64 ? a.context_lens[min(lane, a.rows - 1)] : 0;   // (asked for together with the groups)
+  int tile = wg, part = 0, parts = 1;
+  Tile here;
+  if (a.dealt) {
+    int all;
+    const int n_tiles = deal_tiles(a, s_deal, s_wave, all);
+    if (wg == 0 && blockIdx.x == 0 && threadIdx.x < a.tiles) {
+      const int t = threadIdx.x;
+      const Tile x = t < n_tiles ? dealt_tile(a, s_deal, t) : Tile{0, 0, 0};
+      a.tile_of[t] = t < n_tiles ? make_int4(x.row0, x.rows, s_deal.first[t], s_deal.parts[t]) : make_int4(0, 0, 0, 0);
+    }
+    if (wg >= all) return;
+    tile = __builtin_amdgcn_readfirstlane(last_within(s_deal.first, n_tiles, wg));
+    part = wg - __builtin_amdgcn_readfirstlane(s_deal.first[tile]);
+    parts = __builtin_amdgcn_readfirstlane(s_deal.parts[tile]);
+    const Tile x = dealt_tile(a, s_deal, tile);
+    here = Tile{__builtin_amdgcn_readfirstlane(x.row0), __builtin_amdgcn_readfirstlane(x.rows), __builtin_amdgcn_readfirstlane(x.shared)};
+  } else {
+    here = find_tile(a, tile, s_wave, s_tile);
+    if (here.rows == 0) return;
   }
-  // The runs, by the first wavefront: lane r has row r.
-  if (wave == 0) {
-    const int m = row0 + min(lane, n_rows - 1);
-    const int seq = a.row_table ? safe_row(a.row_table[m], a.rows) : m;
-    const int len = a.rows <= kEarlyRows ? s_lens[m] : a.context_lens[m];
-    const int shared = s_tile[2] * 16;
-    const int npos = lane < n_rows ? min(max(len, -1), a.max_blocks * 16 - 1) + 1 : 0;
-    const bool with = lane < n_rows && shared > 0 && npos >= shared;
-    const unsigned long long who = __ballot(with);
-    const int prefix_steps = who ? (shared + 31) >> 5 : 0;
-    const int from = with ? shared : 0, steps = (npos - from + 31) >> 5;
-    int upto = lane < n_rows ? steps : 0;
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) {
-      const int o = __shfl_up(upto, x);
-      if (lane >= x) upto += o;
-    }
-    if (lane < n_rows) {
-      s_first[lane + 1] = prefix_steps + upto - steps;
-      s_from[lane + 1] = from;
-      s_end[lane + 1] = npos;
-      s_seq[lane + 1] = seq;
-      s_with[lane] = with;
-    }
-    if (lane == n_rows - 1) s_first[n_rows + 1] = prefix_steps + upto;
-    if (lane == (who ? __builtin_ctzll(who) : 0)) s_seq[0] = seq;
-    if (lane == 0) {
-      s_first[0] = 0;
-      s_from[0] = 0;
-      s_end[0] = shared;
-    }
-  }
-  __syncthreads();
-  const int total = __builtin_amdgcn_readfirstlane(s_first[n_rows + 1]);
-  const int per = max((total + a.parts - 1) / a.parts, kWaves);
-  const int live = max(1, (total + per - 1) / per);
-  if (writes_tile) a.tile_of[tile] = make_int4(row0, n_rows, live, 0);
-  if (part >= live) return;
-  const int lo = part * per, hi = min(total, lo + per);
-  const int nk = hi - lo > wave ? (hi - lo - wave + kWaves - 1) / kWaves : 0;   // steps of this wavefront: lo + wave + k * kWaves
 
   const size_t block_elems = (size_t)a.kv_heads * 16 * DH;
   const T* kpool = reinterpret_cast<const T*>(a.k) + (size_t)kvh * 16 * DH;
@@ -195,6 +272,27 @@ __global__ __launch_bounds__(kThreads) void shared_attn_kernel(SharedAttnArgs a)
   const int k_at = l16 * DH + j * (BF16 ? 8 : 4);     // position l16, channels + c * 32 (16)
   const int v_at = j * 4 * DH + l16 * CT;             // positions 4j + i, channels l16 * CT ..
 
+  int total;
+  const int row0 = here.row0, n_rows = here.rows;
+  {   // the runs: lane r has row r
+    const int m = row0 + min(lane, n_rows - 1);
+    const int seq = a.row_table ? safe_row(a.row_table[m], a.rows) : m;
+    const int len = a.rows <= 64 ? __shfl(early_len, m) : a.context_lens[m];
+    const int shared = here.shared * 16, npos = positions_of(a, len);
+    const bool with = lane < n_rows && shared > 0 && npos >= shared;
+    const unsigned long long who = __ballot(with);
+    const int prefix_steps = who ? (shared + 31) >> 5 : 0;
+    const int from = with ? shared : 0, steps = lane < n_rows ? (npos - from + 31) >> 5 : 0;
+    const int upto = wave_sums(steps);
+    total = prefix_steps + __builtin_amdgcn_readlane(upto, 63);
+    if (lane < n_rows) runs[lane + 1] = make_int4(prefix_steps + upto - steps, from, npos, seq);
+    if (lane == (who ? __builtin_ctzll(who) : 0)) runs[0] = make_int4(0, 0, shared, seq);
+    if (lane == 0) runs[n_rows + 1] = make_int4(total, 0, 0, 0);
+  }
+  const int per = (total + parts - 1) / parts, lo = min(part * per, total), hi = min(total, lo + per);
+  const bool alone = parts == 1;   // the tile's result is this workgroup's
+  const int nk = hi - lo > wave ? (hi - lo - wave + kWaves - 1) / kWaves : 0;   // steps of this wavefront: lo + wave + k * kWaves
+
   // The blocks of the wavefront's next 32 steps, two lanes a step (a step's second block may not be there: the first again, masked).
   int off_lo = 0, off_hi = 0;
   auto load_ids = [&](int k0) {
@@ -202,12 +300,12 @@ __global__ __launch_bounds__(kThreads) void shared_attn_kernel(SharedAttnArgs a)
     int r = 0, z = n_rows;           // the last run that begins at or before s (runs without steps lie in front of the next)
     while (r < z) {
       const int mid = (r + z + 1) >> 1;
-      if (s_first[mid] <= s) r = mid;
+      if (runs[mid].x <= s) r = mid;
       else z = mid - 1;
     }
-    const int at = s_from[r] + (s - s_first[r]) * 32 + (lane & 1) * 16;
-    const int b = min(at, s_end[r] - 1) >> 4;
-    const size_t off = (size_t)safe_block(a.block_tables[(size_t)s_seq[r] * a.max_blocks + b], a.num_blocks) * block_elems * sizeof(T);
+    const int4 of = runs[r];
+    const int b = min(of.y + (s - of.x) * 32 + (lane & 1) * 16, of.z - 1) >> 4;
+    const size_t off = (size_t)safe_block(a.block_tables[(size_t)of.w * a.max_blocks + b], a.num_blocks) * block_elems * sizeof(T);
     off_lo = (int)(uint32_t)off;
     off_hi = (int)(uint32_t)(off >> 32);
   };
@@ -289,7 +387,7 @@ __global__ __launch_bounds__(kThreads) void shared_attn_kernel(SharedAttnArgs a)
     const int column = t * 16 + l16;
     const bool ok = column < n_columns;
     col_row[t] = ok ? column / gc : -1;
-    col_with[t] = ok && s_with[ok ? col_row[t] : 0];
+    col_with[t] = ok && runs[(ok ? col_row[t] : 0) + 1].y > 0;
     all_with = all_with && __all(!ok || col_with[t]);
   }
 
@@ -430,34 +528,38 @@ __global__ __launch_bounds__(kThreads) void shared_attn_kernel(SharedAttnArgs a)
     }
     if (k + 1 < nk) load_v(k + 1);
   };
-  const int plain_steps = all_with ? __builtin_amdgcn_readfirstlane(s_end[0]) >> 5 : 0;
+  const int plain_steps = all_with ? __builtin_amdgcn_readfirstlane(runs[0].z) >> 5 : 0;
   int k = 0;
   for (; k < nk && lo + wave + k * kWaves < plain_steps; ++k) step(std::true_type{}, k, 0, 0, 0);
   for (int run = 0; k < nk; ++k) {
     const int at = lo + wave + k * kWaves;
-    while (at >= __builtin_amdgcn_readfirstlane(s_first[run + 1])) ++run;
-    const int tok0 = __builtin_amdgcn_readfirstlane(s_from[run]) + (at - __builtin_amdgcn_readfirstlane(s_first[run])) * 32;
-    step(std::false_type{}, k, run, tok0, __builtin_amdgcn_readfirstlane(s_end[run]));
+    while (at >= __builtin_amdgcn_readfirstlane(runs[run + 1].x)) ++run;
+    const int4 of = runs[run];
+    const int tok0 = __builtin_amdgcn_readfirstlane(of.y + (at - of.x) * 32);
+    step(std::false_type{}, k, run, tok0, __builtin_amdgcn_readfirstlane(of.z));
   }
 
-  // the four lanes of a column have sums over positions of their own; then the wavefronts, in order, 16 columns at a time
+  // the four lanes of a column have sums over positions of their own; then the wavefronts that had steps, in order, 16 columns at a time
+  const int n_waves = min(kWaves, hi - lo);
   typedef float sums_t[16][PITCH];
   sums_t* s_o = reinterpret_cast<sums_t*>(s_space);
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     if (t * 16 >= n_columns) break;
     if (t || NT > 1) __syncthreads();   // q, or the columns before, have been read
-    float l = l_run[t];
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
+    if (wave < n_waves) {
+      float l = l_run[t];
+      l += __shfl_xor(l, 16);
+      l += __shfl_xor(l, 32);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int u = 0; u < CT; u += 4)
-        *reinterpret_cast<f32x4*>(&s_o[wave][l16][(j * 4 + i) * CT + u]) = f32x4{o[t][u][i], o[t][u + 1][i], o[t][u + 2][i], o[t][u + 3][i]};
-    if (j == 0) {
-      s_m[wave][l16] = m_run[t];
-      s_l[wave][l16] = l;
+        for (int u = 0; u < CT; u += 4)
+          *reinterpret_cast<f32x4*>(&s_o[wave][l16][(j * 4 + i) * CT + u]) = f32x4{o[t][u][i], o[t][u + 1][i], o[t][u + 2][i], o[t][u + 3][i]};
+      if (j == 0) {
+        s_m[wave][l16] = m_run[t];
+        s_l[wave][l16] = l;
+      }
     }
     __syncthreads();
     for (int x = threadIdx.x; x < 16 * (DH / 4); x += kThreads) {
@@ -466,19 +568,21 @@ __global__ __launch_bounds__(kThreads) void shared_attn_kernel(SharedAttnArgs a)
       const int r = column / gc;
       float M = kNegBig, L = 0.0f;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_m[w][c]);
+      for (int w = 0; w < kWaves; ++w) M = w < n_waves ? fmaxf(M, s_m[w][c]) : M;
       f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
-        const float wgt = __builtin_amdgcn_exp2f(s_m[w][c] - M);
-        L += s_l[w][c] * wgt;
-        acc += *reinterpret_cast<const f32x4*>(&s_o[w][c][ch]) * wgt;
+        if (w < n_waves) {
+          const float wgt = __builtin_amdgcn_exp2f(s_m[w][c] - M);
+          L += s_l[w][c] * wgt;
+          acc += *reinterpret_cast<const f32x4*>(&s_o[w][c][ch]) * wgt;
+        }
       }
-      if (live == 1) {
-        const float inv = s_end[r + 1] > 0 ? 1.0f / L : 0.0f;      // a row without a position: 0
+      if (alone) {
+        const float inv = runs[r + 1].z > 0 ? 1.0f / L : 0.0f;      // a row without a position: 0
         *reinterpret_cast<f32x4*>(a.out + ((size_t)(row0 + r) * heads + head0 + column - r * gc) * DH + ch) = acc * inv;
       } else {
-        float* rec = a.records + ((((size_t)tile * a.head_chunks + hc) * a.kv_heads + kvh) * a.parts + part) * a.columns * PITCH + (size_t)column * PITCH;
+        float* rec = a.records + (((size_t)hc * a.kv_heads + kvh) * (a.dealt + a.tiles) + wg) * a.columns * PITCH + (size_t)column * PITCH;
         if (ch == 0) *reinterpret_cast<f32x4*>(rec) = f32x4{M, L, 0.0f, 0.0f};
         *reinterpret_cast<f32x4*>(rec + 4 + ch) = acc;
       }
@@ -486,7 +590,7 @@ __global__ __launch_bounds__(kThreads) void shared_attn_kernel(SharedAttnArgs a)
   }
 }
 
-// Adds the parts of a tile's columns: a workgroup has one column, DH / 4 threads to every eighth (sixteenth) part; then these, in order.
+// Adds the parts of the tiles that several workgroups had: a workgroup a column, DH / 4 threads to every eighth (sixteenth) part; then these, in order.
 template <int DH>
 __global__ __launch_bounds__(256) void shared_join_kernel(SharedAttnArgs a) {
   constexpr int TH = DH / 4, G = 256 / TH, PITCH = DH + 4;
@@ -495,13 +599,14 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedAttnArgs a) {
   const int kvh = blockIdx.x % a.kv_heads, hc = blockIdx.x / a.kv_heads, tile = blockIdx.y, c = blockIdx.z;
   const int4 td = a.tile_of[tile];
   const int gc = min(a.group - hc * a.columns, a.columns);
-  if (td.z < 2 || c >= td.y * gc) return;
+  const int parts = td.w;
+  if (parts < 2 || c >= td.y * gc) return;
   const int g = threadIdx.x / TH, ch = threadIdx.x % TH * 4, r = c / gc;
-  const float* rec = a.records + (((size_t)tile * a.head_chunks + hc) * a.kv_heads + kvh) * a.parts * a.columns * PITCH + (size_t)c * PITCH;
+  const float* rec = a.records + (((size_t)hc * a.kv_heads + kvh) * (a.dealt + a.tiles) + td.z) * a.columns * PITCH + (size_t)c * PITCH;
   const size_t pitch = (size_t)a.columns * PITCH;
   float M = kNegBig, L = 0.0f;
   f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int p = g; p < td.z; p += G) {
+  for (int p = g; p < parts; p += G) {
     const float m = rec[p * pitch], l = rec[p * pitch + 1];
     const f32x4 x = *reinterpret_cast<const f32x4*>(rec + p * pitch + 4 + ch);
     const float to = fmaxf(M, m), was = __builtin_amdgcn_exp2f(M - to), now = __builtin_amdgcn_exp2f(m - to);
@@ -534,8 +639,8 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedAttnArgs a) {
 
 template <class T, int DH, int NT>
 void launch_tiles(const SharedAttnArgs& a, hipStream_t st) {
-  shared_attn_kernel<T, DH, NT><<<dim3(a.kv_heads * a.head_chunks, a.parts, a.tiles), kThreads, 0, st>>>(a);
-  if (a.parts > 1) shared_join_kernel<DH><<<dim3(a.kv_heads * a.head_chunks, a.tiles, a.columns), 256, 0, st>>>(a);
+  shared_attn_kernel<T, DH, NT><<<dim3(a.kv_heads * a.head_chunks, a.dealt ? a.dealt + a.tiles : a.tiles), kThreads, 0, st>>>(a);
+  if (a.dealt) shared_join_kernel<DH><<<dim3(a.kv_heads * a.head_chunks, a.tiles, a.columns), 256, 0, st>>>(a);
 }
 
 template <class T, int DH>
@@ -566,34 +671,35 @@ void shared_attn_plan(SharedAttnArgs& a, int dtype) {
   const int64_t columns = ((int64_t)a.rows * a.group + a.n_groups - 1) / a.n_groups;
   tile_widths(a, columns > most ? most : (int)(columns + 15) / 16 * 16, most);
   a.tiles = most_tiles(a);
-  const int64_t wgs = (int64_t)a.tiles * a.kv_heads * a.head_chunks;
-  const int64_t steps = (a.max_context + 31) / 32;
-  int64_t parts = kMostWgs / wgs;
-  if (parts > steps / kFewSteps) parts = steps / kFewSteps;
-  if (parts > kMostParts) parts = kMostParts;
-  a.parts = parts < 2 ? 1 : (int)parts;
+  // Whole tiles a workgroup, or all tiles' steps dealt out evenly: where there are fewer tiles than run at once and they are long, and where they are few enough
+  // for a long one to be waited for.  (Lengths are the device's: these are bounds.)
+  const int64_t heads = (int64_t)a.kv_heads * a.head_chunks, wgs = a.tiles * heads;
+  const int64_t shared = a.max_shared < a.max_context / 16 ? a.max_shared : a.max_context / 16, own = a.max_context - shared * 16;
+  const int64_t steps = (shared * 16 + 31) / 32 + (int64_t)(a.rows < a.rows_per_tile ? a.rows : a.rows_per_tile) * ((own + 31) / 32);
+  const bool deal = wgs < kMostWgs ? steps >= kWorthDealing : wgs < 8 * kMostWgs && wgs * steps >= 8 * kWaves * kMostWgs;
+  const bool can = a.rows <= kDealRows && a.n_groups <= kDealGroups && a.tiles <= kDealTiles;
+  a.dealt = deal && can ? (heads < kMostWgs ? (int)(kMostWgs / heads) : 1) : 0;
 }
 
 size_t shared_attn_record_floats(const SharedAttnArgs& a) {
-  return a.parts > 1 ? (size_t)a.tiles * a.kv_heads * a.head_chunks * a.parts * a.columns * (a.dh + 4) : 0;
+  return a.dealt ? (size_t)a.kv_heads * a.head_chunks * (a.dealt + a.tiles) * a.columns * (a.dh + 4) : 0;
 }
 
-// For calls of fewer rows, groups and positions, which may have narrower tiles.  Of each width the tiles grow with rows and groups; the parts of all of them together
-// are at most kMostWgs where there are any.
+// For calls of fewer rows, groups and positions, which may have narrower tiles: of each width the tiles grow with rows and groups.
 size_t shared_attn_most_floats(SharedAttnArgs& a, int dtype, size_t* tiles) {
   size_t most = 0;
-  const int64_t steps = (a.max_context + 31) / 32, apart = steps / kFewSteps;
   const int widest = dtype == EE_FP32 ? 32 : kMostColumns;
   *tiles = 0;
   for (int columns = 16; columns <= widest; columns += 16) {
     tile_widths(a, columns, widest);
-    a.tiles = most_tiles(a);
-    if (*tiles < (size_t)a.tiles) *tiles = a.tiles;
-    const size_t floats = (size_t)kMostWgs * a.columns * (a.dh + 4);
+    const int64_t heads = (int64_t)a.kv_heads * a.head_chunks;
+    int64_t t = most_tiles(a);
+    if (t > kDealTiles) t = kDealTiles;
+    if (t * heads > 8 * kMostWgs) t = (8 * kMostWgs + heads - 1) / heads;
+    const size_t floats = (size_t)(kMostWgs + heads + t * heads) * a.columns * (a.dh + 4);
+    if (*tiles < (size_t)t) *tiles = t;
     if (most < floats) most = floats;
   }
-  if (apart < 2) most = *tiles = 0;
-  if (*tiles > kMostWgs) *tiles = kMostWgs;   // (more of them have one part each)
   shared_attn_plan(a, dtype);
   return most;
 }
