@@ -6,6 +6,8 @@
 // sum of exponentials and its n best, in order (within a beam the order of the scores is that of the logits, so this needs no sum of the whole row).
 // The join forms the rows' sums from the chunks', the scores of what was found, and the n best of these.
 // What is compared are scores in double: rounded to float many candidates of a beam would be equal, and beams' sums meet there.
+#include <type_traits>
+
 #include "beams.h"
 
 namespace ee {
@@ -21,6 +23,7 @@ __device__ inline uint32_t key_of(float z) {
   const uint32_t u = __float_as_uint(z + 0.0f);   // (-0 is 0)
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+constexpr uint32_t kLowestKey = 0x00800000u;   // of the lowest float
 __device__ inline float float_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
 __device__ inline uint64_t key_of(double s) {
   const uint64_t u = (uint64_t)__double_as_longlong(s + 0.0);
@@ -28,111 +31,148 @@ __device__ inline uint64_t key_of(double s) {
 }
 __device__ inline double double_of(uint64_t key) { return __longlong_as_double((long long)(key >> 63 ? key & ~(1ull << 63) : ~key)); }
 
-// The largest bound of which at least n of the keys are not below (each lane has K of them; the wavefront's together), to its upper `BITS` bits; at least 1.
-template <int K, int BITS>
+// The largest bound of which at least n of the keys are not below (each lane has K of them; the wavefront's together), to its upper 2 * PAIRS bits; at least 1.
+// (Two bits at a time: what a step takes is its chain of scalar instructions, and three counts go through it side by side.)
+template <int K, int PAIRS>
 __device__ inline uint32_t wave_bound(const uint32_t (&key)[K], int n) {
   uint32_t bound = 0;
-  for (int bit = 31; bit >= 32 - BITS; --bit) {
-    const uint32_t c = bound | 1u << bit;
-    int count = 0;
+  for (int bit = 30; bit >= 32 - 2 * PAIRS; bit -= 2) {
+    int count[3] = {0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < K; ++i) count += __popcll(__ballot(key[i] >= c));
-    if (count >= n) bound = c;
+    for (int i = 0; i < K; ++i)
+#pragma unroll
+      for (int q = 0; q < 3; ++q) count[q] += __popcll(__ballot(key[i] >= (bound | (uint32_t)(q + 1) << bit)));
+    bound |= (uint32_t)((count[0] >= n) + (count[1] >= n) + (count[2] >= n)) << bit;
   }
   return bound ? bound : 1u;
 }
 
+// The largest of a wavefront's values, and the sums of its numbers (in a fixed order), on the cross-lane network: every lane has them.
+__device__ inline uint32_t wave_largest(uint32_t v) {
+  auto with = [&](auto ctrl, auto rows) { v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, decltype(rows)::value, 0xf, false)); };
+  with(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});   // row_shr 1, 2, 4, 8
+  with(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
+  with(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+  with(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+  with(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // row_bcast 15, 31
+  with(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
+  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+__device__ inline int wave_total(int v) {
+  auto add = [&](auto ctrl, auto rows) { v += __builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, decltype(rows)::value, 0xf, false); };
+  add(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});
+  add(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
+  add(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+  add(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+  add(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});
+  add(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
+  return __builtin_amdgcn_readlane(v, 63);
+}
+__device__ inline double wave_sum(double v) {
+  auto add = [&](auto ctrl, auto rows) {
+    const uint64_t u = (uint64_t)__double_as_longlong(v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+    v += __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
+  };
+  add(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});
+  add(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
+  add(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+  add(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+  add(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});
+  add(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
+  const uint64_t u = (uint64_t)__double_as_longlong(v);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, 63), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), 63);
+  return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
+}
+
 constexpr int kScanList = 512;   // candidates of a chunk that are put in order
 
-// A chunk of THREADS * EACH values.  What falls behind the n-th largest of the threads' maxima is none of the n best; the others (n and a few) are
+// A chunk of THREADS * EACH values.  What falls behind the n-th largest of 256 parts' maxima is none of the n best; the others (n and a few) are
 // gathered and put in order by counting, for each, those in front of it.  Where they are too many (many equal values), the n-th of all is found bit by bit first.
 template <class T, int THREADS, int EACH>
-__global__ __launch_bounds__(THREADS) void beam_scan_kernel(BeamArgs a) {
+__global__ __launch_bounds__(THREADS, EACH > 16 ? 6 : 4) void beam_scan_kernel(BeamArgs a) {
   constexpr int VEC = 16 / sizeof(T), LOADS = EACH / VEC, WAVES = THREADS / 64;
-  __shared__ uint64_t s_list[kScanList];
-  __shared__ uint32_t s_most[THREADS];
+  __shared__ __align__(16) uint64_t s_list[kScanList + 8];
+  __shared__ uint32_t s_most[256];
   __shared__ double s_sum[WAVES];
-  __shared__ float s_max[WAVES];
+  __shared__ uint32_t s_top[WAVES];
+  __shared__ uint32_t s_bound;
   __shared__ int s_count, s_below[WAVES];
-  const int row = blockIdx.y, chunk = blockIdx.x;
-  if (a.finished && a.finished[row]) return;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int base = chunk * THREADS * EACH;
-  const T* z = reinterpret_cast<const T*>(a.logits) + (size_t)row * a.stride;
-  if (threadIdx.x == 0) s_count = 0;
-
-  // Values `at(l) + e` for piece l; the same places whether the row starts on 16 bytes or not, so that equal rows have equal sums.
+  const int chunk = blockIdx.x, row = blockIdx.y, base = chunk * THREADS * EACH, n = a.n_out, lists = a.beams * a.chunks;
+  const int done = a.finished ? a.finished[row] : 0;   // (looked at when the values have been asked for)
+  const char* z = reinterpret_cast<const char*>(a.logits) + (size_t)row * a.stride * sizeof(T);
+  // Values `at(l) + e` for part l; the same places whether the row starts on 16 bytes or not, so that equal rows have equal sums.
   auto at = [&](int l) { return base + (l * THREADS + (int)threadIdx.x) * VEC; };
   float x[EACH];
-  const bool aligned = ((reinterpret_cast<uintptr_t>(a.logits) | (a.stride * sizeof(T))) & 15) == 0;
-  if (aligned) {
+  constexpr uint32_t NONE = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;   // -inf
+  if ((reinterpret_cast<uintptr_t>(z) & 15) == 0 && (base + THREADS * EACH <= a.vocab || a.vocab % VEC == 0)) {
     u32x4 raw[LOADS];
 #pragma unroll
-    for (int l = 0; l < LOADS; ++l)
-      if (at(l) + VEC <= a.vocab) raw[l] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(z + at(l)));
-#pragma unroll
     for (int l = 0; l < LOADS; ++l) {
-      if (at(l) + VEC <= a.vocab) {
+      raw[l] = u32x4{NONE, NONE, NONE, NONE};
+      if (at(l) < a.vocab) raw[l] = *reinterpret_cast<const u32x4*>(z + (uint32_t)at(l) * (uint32_t)sizeof(T));
+    }
+    if (done) return;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          if constexpr (sizeof(T) == 4) x[l * VEC + e] = __uint_as_float(raw[l][e]);
-          else x[l * VEC + e] = __uint_as_float(e & 1 ? raw[l][e / 2] & 0xffff0000u : raw[l][e / 2] << 16);
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) x[l * VEC + e] = at(l) + e < a.vocab ? (float)z[at(l) + e] : -INFINITY;
-      }
+    for (int i = 0; i < EACH; ++i) {
+      if constexpr (sizeof(T) == 4) x[i] = __uint_as_float(raw[i / 4][i % 4]);
+      else x[i] = __uint_as_float(i & 1 ? raw[i / 8][i % 8 / 2] & 0xffff0000u : raw[i / 8][i % 8 / 2] << 16);
     }
   } else {
+    if (done) return;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
       const int t = at(i / VEC) + i % VEC;
-      x[i] = t < a.vocab ? (float)z[t] : -INFINITY;
+      x[i] = t < a.vocab ? (float)*reinterpret_cast<const T*>(z + (uint32_t)t * (uint32_t)sizeof(T)) : -INFINITY;
     }
   }
 
   float most = -INFINITY;
 #pragma unroll
   for (int i = 0; i < EACH; ++i) most = fmaxf(most, x[i]);
-  s_most[threadIdx.x] = key_of(most);
-  float top = most;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
-  if (lane == 0) s_max[wave] = top;
+  const uint32_t most_key = key_of(most);
+  if constexpr (THREADS == 256) {
+    s_most[threadIdx.x] = most_key;
+  } else {   // four threads' together: quad_perm [1,0,3,2], [2,3,0,1]
+    uint32_t four = max(most_key, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most_key, 0xB1, 0xf, 0xf, true));
+    four = max(four, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)four, 0x4E, 0xf, 0xf, true));
+    if ((threadIdx.x & 3) == 0) s_most[threadIdx.x / 4] = four;
+  }
+  uint32_t top_key = wave_largest(most_key);
+  if (lane == 0) s_top[wave] = top_key;
+  if (threadIdx.x == 0) s_count = 0;
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < WAVES; ++i) top = fmaxf(top, s_max[i]);
+  for (int i = 0; i < WAVES; ++i) top_key = max(top_key, s_top[i]);
+  const float top = top_key ? float_of(top_key) : -INFINITY;
   // (a chunk without a value has a sum of 0, one with a NaN or +inf a sum that is NaN: so has its row)
   const float ref = top == -INFINITY ? 0.0f : top;
   float part = 0.0f;
 #pragma unroll
   for (int i = 0; i < EACH; ++i) part += __expf(x[i] - ref);
-  double sum = part;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+  const double sum = wave_sum(part);
   if (lane == 0) s_sum[wave] = sum;
 
-  // the n-th largest of the threads' maxima, found by every wavefront for itself
-  const int n = a.n_out;
-  uint32_t bound;
-  {
-    uint32_t key[WAVES];
+  // the n-th largest of the 256 maxima: below it is none of the n best
+  if (wave == 0) {
+    uint32_t key[4];
 #pragma unroll
-    for (int i = 0; i < WAVES; ++i) key[i] = s_most[i * 64 + lane];
-    bound = wave_bound<WAVES, 20>(key, n);
+    for (int i = 0; i < 4; ++i) key[i] = s_most[i * 64 + lane];
+    const uint32_t bound = wave_bound<4, 9>(key, n);
+    if (lane == 0) s_bound = bound;
   }
+  __syncthreads();
+  const float bound = s_bound < kLowestKey ? -3.4028235e38f : float_of(s_bound);
   auto composite = [&](int i) { return (uint64_t)key_of(x[i]) << 32 | (0xffffffffu - (uint32_t)(at(i / VEC) + i % VEC)); };
-  auto gather = [&](uint64_t from) {
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-      const uint64_t c = composite(i);
-      if (c >= from) {
-        const int k = atomicAdd(&s_count, 1);
-        if (k < kScanList) s_list[k] = c;
-      }
-    }
+  auto take = [&](int i) {
+    const int k = atomicAdd(&s_count, 1);
+    if (k < kScanList) s_list[k] = composite(i);
   };
-  gather((uint64_t)bound << 32);
+#pragma unroll
+  for (int i = 0; i < EACH; ++i)
+    if (x[i] >= bound) take(i);
   __syncthreads();
   int count = s_count;
   if (count > kScanList) {
@@ -142,8 +182,7 @@ __global__ __launch_bounds__(THREADS) void beam_scan_kernel(BeamArgs a) {
       int mine = 0;
 #pragma unroll
       for (int i = 0; i < EACH; ++i) mine += composite(i) >= c;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) mine += __shfl_xor(mine, o);
+      mine = wave_total(mine);
       __syncthreads();
       if (lane == 0) s_below[wave] = mine;
       __syncthreads();
@@ -154,144 +193,237 @@ __global__ __launch_bounds__(THREADS) void beam_scan_kernel(BeamArgs a) {
     }
     if (threadIdx.x == 0) s_count = 0;
     __syncthreads();
-    gather(from);   // (composites differ: n of them)
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)
+      if (composite(i) >= from) take(i);   // (composites differ: n of them)
     __syncthreads();
     count = min(s_count, kScanList);
   }
-  const size_t piece = (size_t)row * a.chunks + chunk;
   if (threadIdx.x == 0) {
     double total = 0.0;
     for (int i = 0; i < WAVES; ++i) total += s_sum[i];
-    a.stats[piece] = make_double2(top, total);
+    a.stats[(size_t)row * a.chunks + chunk] = make_double2(top, total);
   }
-  uint64_t* found = a.found + piece * n;
+  // place k of this list among the group's: [k][beam][chunk]
+  uint64_t* found = a.found + (size_t)(row / a.beams) * n * lists + (size_t)(row % a.beams) * a.chunks + chunk;
+  if (threadIdx.x < 8) s_list[count + threadIdx.x] = 0;   // (whole eights are compared)
+  __syncthreads();
   for (int i = threadIdx.x; i < count; i += THREADS) {
     const uint64_t c = s_list[i];
     int rank = 0;
-    for (int j = 0; j < count; ++j) rank += s_list[j] > c;
-    if (rank < n) found[rank] = c;
+    for (int j = 0; j < count; j += 8)
+#pragma unroll
+      for (int u = 0; u < 8; ++u) rank += s_list[j + u] > c;
+    if (rank < n) found[(size_t)rank * lists] = c;
   }
-  for (int i = count + (int)threadIdx.x; i < n; i += THREADS) found[i] = 0;
+  for (int i = count + (int)threadIdx.x; i < n; i += THREADS) found[(size_t)i * lists] = 0;
 }
 
 constexpr int kJoinThreads = 1024;
 constexpr int kJoinList = 1024;
+constexpr int kJoinKept = 16384;  // candidates whose rough scores stay in LDS
+constexpr int kJoinFew = 128;    // so many are put in order without a look at which may count
 
-// A workgroup a group.
+// A workgroup a group.  The n best of its beams' chunks' are found as in the scan, by the n-th largest of 256 maxima; where beams are so unlike that this lets many
+// more through than n, the bound is moved up by halves until few are left.  Then by counting what is in front.
 __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int is_bf16) {
   constexpr int WAVES = kJoinThreads / 64;
-  __shared__ double s_lse[kBeamMost], s_base[kBeamMost];
+  struct alignas(16) Candidate {
+    uint64_t key, index;   // of the score in double, 0: none; beam of the group * vocab + token
+  };
+  __shared__ double s_off[kBeamMost], s_base[kBeamMost];   // of a beam: the logarithm of its sum; its score
   __shared__ int s_done[kBeamMost];
-  __shared__ uint32_t s_most[kJoinThreads];
-  __shared__ uint64_t s_key[kJoinList];
-  __shared__ uint64_t s_cand[kJoinList]; // index: beam * vocab + token
-  __shared__ int s_count, s_below[WAVES];
+  __shared__ float s_rough_off[kBeamMost];
+  __shared__ uint32_t s_most[kJoinThreads / 4];
+  __shared__ Candidate s_list[kJoinList + 4];
+  __shared__ uint32_t s_rough[kJoinKept];
+  __shared__ uint32_t s_bound;
+  __shared__ int s_count, s_below[2][WAVES];
   const int g = blockIdx.x, n = a.n_out, W = a.beams, row0 = g * W;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int lists = W * a.chunks, all = lists * n;
+  const uint64_t* found = a.found + (size_t)g * all;   // the lists' first ones, then the second ones, ..
   if (threadIdx.x == 0) s_count = 0;
-  // the rows' sums, a wavefront a row (a fixed order of additions)
-  for (int b = wave; b < W; b += WAVES) {
-    const int row = row0 + b;
-    const bool done = a.finished && a.finished[row];
-    double m = -INFINITY, sum = 0.0;
-    if (!done) {
-      for (int c = lane; c < a.chunks; c += 64) m = fmax(m, a.stats[(size_t)row * a.chunks + c].x);
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) m = fmax(m, __shfl_xor(m, o));
-      for (int c = lane; c < a.chunks; c += 64) {
-        const double2 s = a.stats[(size_t)row * a.chunks + c];
-        if (s.y != 0.0) sum += s.y * exp(s.x - m);   // (NaN stays)
-      }
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
-    }
-    if (lane == 0) {
-      s_lse[b] = m + log(sum);
-      s_base[b] = a.scores[row];
-      s_done[b] = done;
-    }
-  }
-  __syncthreads();
-  const int per_beam = a.chunks * n;
-  const int all = W * per_beam;
-  // key of candidate i (0: none), and its index
-  auto candidate = [&](int i, uint64_t& index) -> uint64_t {
-    const int b = i / per_beam, j = i - b * per_beam;
-    double s;
-    if (s_done[b]) {
-      if (j) return 0;
-      s = s_base[b];
-      index = (uint64_t)b * a.vocab + a.end_token;
-    } else {
-      const uint64_t c = a.found[(size_t)(row0 + b) * per_beam + j];
-      if (!(c >> 32)) return 0;
-      s = s_base[b] + ((double)float_of((uint32_t)(c >> 32)) - s_lse[b]);
-      index = (uint64_t)b * a.vocab + (0xffffffffu - (uint32_t)c);
-    }
-    return s - s == 0.0 ? key_of(s) : 0;   // what is not finite is none
-  };
-  uint32_t most = 0;
-  for (int i = threadIdx.x; i < all; i += kJoinThreads) {
-    uint64_t index;
-    most = max(most, (uint32_t)(candidate(i, index) >> 32));
-  }
-  s_most[threadIdx.x] = most;
-  __syncthreads();
-  uint32_t bound;
+  // The rows' sums: 2^p lanes a row, as many as it has chunks (in a fixed order of additions).
+  float far = 0.0f;   // the largest magnitude of what is added to logits
   {
-    uint32_t key[WAVES];
-#pragma unroll
-    for (int i = 0; i < WAVES; ++i) key[i] = s_most[i * 64 + lane];
-    bound = wave_bound<WAVES, 32>(key, n);
-  }
-  // in front: larger score, or an equal one and the lower index
-  auto gather = [&](uint64_t from, uint64_t up_to) {
-    for (int i = threadIdx.x; i < all; i += kJoinThreads) {
-      uint64_t index;
-      const uint64_t k = candidate(i, index);
-      if (k > from || (k == from && index <= up_to)) {
-        const int at = atomicAdd(&s_count, 1);
-        if (at < kJoinList) {
-          s_key[at] = k;
-          s_cand[at] = index;
+    int p = 0;
+    while (p < 6 && 1 << p < a.chunks) ++p;
+    const int c0 = lane & ((1 << p) - 1);
+    for (int b0 = wave << (6 - p); b0 < W; b0 += WAVES << (6 - p)) {
+      const int b = b0 + (lane >> p), row = row0 + min(b, W - 1);
+      const int done = a.finished ? a.finished[row] : 0;
+      const float base = a.scores[row];
+      const double2* stats = a.stats + (size_t)row * a.chunks;
+      double2 first = make_double2(-INFINITY, 0.0);
+      if (c0 < a.chunks && !done) first = stats[c0];
+      float m = (float)first.x;   // (maxima are floats)
+      if (!done)
+        for (int k = c0 + 64; k < a.chunks; k += 64) m = fmaxf(m, (float)stats[k].x);
+      for (int o = 1; o < 1 << p; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+      double sum = first.y != 0.0 ? first.y * exp(first.x - m) : 0.0;   // (NaN stays)
+      if (!done)
+        for (int k = c0 + 64; k < a.chunks; k += 64) {
+          const double2 s = stats[k];
+          if (s.y != 0.0) sum += s.y * exp(s.x - m);
         }
+      for (int o = 1; o < 1 << p; o <<= 1) sum += __shfl_xor(sum, o);
+      if (c0 == 0 && b < W) {
+        const double off = done ? 0.0 : m + log(sum), to = base - off;
+        s_off[b] = off;
+        s_base[b] = base;
+        s_done[b] = done != 0;
+        // what is not finite stands for rows that have no candidates; what no float is for the largest
+        s_rough_off[b] = to - to == 0.0 ? fminf(fmaxf((float)to, -3.4028235e38f), 3.4028235e38f) : NAN;
       }
     }
+  }
+  __syncthreads();
+  for (int b = 0; b < W; ++b) far = fmaxf(far, fabsf(s_rough_off[b]));
+  // A thread's candidates are 1024 apart: the list goes round, the beam is a quotient by a product of 32 bits (exact: lists * chunks is below 2^32).
+  const uint32_t by_chunks = a.chunks > 1 ? 0xffffffffu / (uint32_t)a.chunks + 1 : 0;
+  auto beam_of = [&](int list) { return a.chunks > 1 ? (int)__umulhi((uint32_t)list, by_chunks) : list; };
+  const int list0 = (int)threadIdx.x % lists, turn_by = kJoinThreads % lists;
+  auto next_list = [&](int list) {
+    list += turn_by;
+    return list >= lists ? list - lists : list;
   };
-  auto block_count = [&](auto&& test) {
-    int mine = 0;
-    for (int i = threadIdx.x; i < all; i += kJoinThreads) {
-      uint64_t index;
-      const uint64_t k = candidate(i, index);
-      mine += k != 0 && test(k, index);
+  auto candidate = [&](int list, uint64_t cc, bool first) {   // of this list, the first one or not; its logit and token are cc
+    const int b = beam_of(list);
+    double s;
+    Candidate r;
+    if (s_done[b]) {
+      s = first && list == b * a.chunks ? s_base[b] : -INFINITY;
+      r.index = (uint64_t)b * a.vocab + a.end_token;
+    } else {
+      s = cc >> 32 ? s_base[b] + ((double)float_of((uint32_t)(cc >> 32)) - s_off[b]) : -INFINITY;
+      r.index = (uint64_t)b * a.vocab + (0xffffffffu - (uint32_t)cc);
     }
+    r.key = s - s == 0.0 ? key_of(s) : 0;   // what is not finite is none
+    return r;
+  };
+  // The order of a float near the score, for the first look: the row's part is rounded, and the sum (to less than 2^-22 of the row's part and the score together).  0 for none.
+  auto rough = [&](int list, uint64_t cc, bool first) {
+    const int b = beam_of(list);
+    float f = s_rough_off[b];
+    if (s_done[b]) f = first && list == b * a.chunks ? f : NAN;
+    else f = cc >> 32 ? f + float_of((uint32_t)(cc >> 32)) : NAN;
+    return f == f ? key_of(fminf(fmaxf(f, -3.4028235e38f), 3.4028235e38f)) : 0u;
+  };
+  const int kept = min(all, kJoinKept);
+  uint32_t most = 0;
+  int list_far = list0, list_kept_end = 0;   // (the latter: of the thread's first candidate that is not kept)
+  for (int i0 = threadIdx.x; i0 < all; i0 += 4 * kJoinThreads) {
+    uint64_t c[4];
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) mine += __shfl_xor(mine, o);
-    __syncthreads();
-    if (lane == 0) s_below[wave] = mine;
+    for (int u = 0; u < 4; ++u) c[u] = i0 + u * kJoinThreads < all ? found[i0 + u * kJoinThreads] : 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = i0 + u * kJoinThreads;
+      if (i == kJoinKept + (int)threadIdx.x) list_kept_end = list_far;
+      if (i < all) {
+        const uint32_t k = rough(list_far, c[u], i < lists);
+        if (i < kJoinKept) s_rough[i] = k;   // (read by the same thread)
+        most = max(most, k);
+      }
+      list_far = next_list(list_far);
+    }
+  }
+  // use(rough score, its number, its list) of every candidate of this thread
+  auto each = [&](auto&& use) {
+    int list = list0;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < kept; i += kJoinThreads) {
+      use(s_rough[i], i, list);
+      list = next_list(list);
+    }
+    list = list_kept_end;
+    for (int i = kJoinKept + threadIdx.x; i < all; i += kJoinThreads) {
+      use(rough(list, found[i], i < lists), i, list);
+      list = next_list(list);
+    }
+  };
+  auto block_sum = [&](int mine, int turn) {   // (two rows of LDS in turn: one barrier a sum)
+    mine = wave_total(mine);
+    if (lane == 0) s_below[turn & 1][wave] = mine;
     __syncthreads();
     int sum = 0;
 #pragma unroll
-    for (int i = 0; i < WAVES; ++i) sum += s_below[i];
+    for (int i = 0; i < WAVES; ++i) sum += s_below[turn & 1][i];
     return sum;
   };
-  gather((uint64_t)bound << 32, ~0ull);
+  uint32_t bound = 1;
+  if (all > kJoinFew) {
+    // four threads' together: quad_perm [1,0,3,2], [2,3,0,1]
+    most = max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0xB1, 0xf, 0xf, true));
+    most = max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0x4E, 0xf, 0xf, true));
+    if ((threadIdx.x & 3) == 0) s_most[threadIdx.x / 4] = most;
+    __syncthreads();
+    uint32_t key[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) key[i] = s_most[i * 64 + lane];
+    if (wave == 0) {
+      const uint32_t b = wave_bound<4, 9>(key, n);
+      if (lane == 0) s_bound = b;
+    }
+    uint32_t above = wave_largest(max(max(key[0], key[1]), max(key[2], key[3]))) + 1;   // nothing is here or above
+    __syncthreads();
+    bound = s_bound;
+    for (int turn = 0;; ++turn) {   // n at least are at the bound or above, fewer from `above` on
+      uint32_t middle = bound;
+      if (turn) {
+        if (above - bound < 2) break;
+        middle = bound + (above - bound) / 2;
+      }
+      int mine = 0;
+      each([&](uint32_t k, int, int) { mine += k >= middle; });
+      const int there = block_sum(mine, turn);
+      if (there >= n || turn == 0) bound = middle;
+      else above = middle;
+      if (there <= max(2 * n, 64) && (there >= n || turn == 0)) break;
+    }
+  }
+  if (bound > 1) {   // whose score may be at the bound's
+    const float f = float_of(bound), least = f - (fabsf(f) + 2.0f * far) * 0x1p-20f;
+    bound = least > -3.4028235e38f ? key_of(least) : 1;
+  }
+  auto put_by = [&](const Candidate& x) {
+    if (!x.key) return;
+    const int at = atomicAdd(&s_count, 1);
+    if (at < kJoinList) s_list[at] = x;
+  };
+  each([&](uint32_t k, int i, int list) {
+    if (k >= bound) put_by(candidate(list, found[i], i < lists));   // (k of none is 0)
+  });
   __syncthreads();
   int count = s_count;
-  if (count > kJoinList) {   // many equal scores: the n-th bit by bit, then its index
+  if (count > kJoinList) {   // as many equal scores: the n-th bit by bit, then its index
+    int turn = 0;
+    auto block_count = [&](auto&& test) {
+      int mine = 0;
+      each([&](uint32_t k, int i, int list) {
+        if (k >= bound) mine += test(candidate(list, found[i], i < lists));
+      });
+      return block_sum(mine, turn++);
+    };
+    __syncthreads();   // (the sums' rows may still be read)
     uint64_t from = 0;
     for (int bit = 63; bit >= 0; --bit) {
-      const uint64_t c = from | 1ull << bit;
-      if (block_count([&](uint64_t k, uint64_t) { return k >= c; }) >= n) from = c;
+      const uint64_t f = from | 1ull << bit;
+      if (block_count([&](const Candidate& x) { return x.key >= f; }) >= n) from = f;
     }
     uint64_t up_to = 0;   // the least index with which n are in front of or at (from, index)
     for (int bit = 39; bit >= 0; --bit) {
-      const uint64_t c = up_to | 1ull << bit;
-      if (block_count([&](uint64_t k, uint64_t index) { return k > from || (k == from && index < c); }) < n) up_to = c;
+      const uint64_t f = up_to | 1ull << bit;
+      if (block_count([&](const Candidate& x) { return x.key > from || (x.key == from && x.index < f); }) < n) up_to = f;
     }
     if (threadIdx.x == 0) s_count = 0;
     __syncthreads();
-    gather(from, up_to);
+    each([&](uint32_t k, int i, int list) {
+      if (k < bound) return;
+      const Candidate x = candidate(list, found[i], i < lists);
+      if (x.key > from || (x.key == from && x.index <= up_to)) put_by(x);
+    });
     __syncthreads();
     count = min(s_count, kJoinList);
   }
@@ -303,11 +435,16 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
     a.parents[at] = row0 + b;
     if (a.finished_out) a.finished_out[at] = s_done[b] || t == a.end_token;
   };
+  // in front: a larger score, or an equal one and the lower index
+  if (threadIdx.x < 4) s_list[count + threadIdx.x] = Candidate{0, ~0ull};   // (whole fours are compared)
+  __syncthreads();
   for (int i = threadIdx.x; i < count; i += kJoinThreads) {
-    const uint64_t k = s_key[i], index = s_cand[i];
+    const Candidate x = s_list[i];
     int rank = 0;
-    for (int j = 0; j < count; ++j) rank += s_key[j] > k || (s_key[j] == k && s_cand[j] < index);
-    if (rank < n) put(rank, double_of(k), index);
+    for (int k = 0; k < count; k += 4)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) rank += (int)(s_list[k + u].key > x.key) | ((int)(s_list[k + u].key == x.key) & (int)(s_list[k + u].index < x.index));
+    if (rank < n) put(rank, double_of(x.key), x.index);
   }
   if (count >= n) return;
   // Fewer candidates than asked for: the rest are the lowest indices whose score is -inf, found by looking (one wavefront, 64 indices at a time).
@@ -323,7 +460,7 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
       } else {
         const size_t at = (size_t)(row0 + b) * a.stride + t;
         const float z = is_bf16 ? (float)reinterpret_cast<const bf16_t*>(a.logits)[at] : reinterpret_cast<const float*>(a.logits)[at];
-        const double s = s_base[b] + ((double)z - s_lse[b]);
+        const double s = s_base[b] + ((double)z - s_off[b]);
         none = !(s - s == 0.0);
       }
     }
@@ -360,7 +497,8 @@ __global__ __launch_bounds__(256) void reorder_rows_kernel(RowCopyArgs a, int pi
 template <class T>
 void launch_scan(const BeamArgs& a, hipStream_t st) {
   const dim3 grid(a.chunks, a.groups * a.beams);
-  if (a.threads == 256) beam_scan_kernel<T, 256, 16><<<grid, 256, 0, st>>>(a);
+  if (a.threads == 256 && a.each == 16) beam_scan_kernel<T, 256, 16><<<grid, 256, 0, st>>>(a);
+  else if (a.threads == 256) beam_scan_kernel<T, 256, 32><<<grid, 256, 0, st>>>(a);
   else beam_scan_kernel<T, 1024, 16><<<grid, 1024, 0, st>>>(a);
 }
 
@@ -368,7 +506,8 @@ void launch_scan(const BeamArgs& a, hipStream_t st) {
 
 void beam_plan(BeamArgs& a) {
   a.threads = a.n_out > kBeamFewOut ? 1024 : 256;
-  a.each = 16;
+  // (chunks of twice the size where the others would not run at once)
+  a.each = a.threads == 256 && (int64_t)a.groups * a.beams * ((a.vocab + 4095) / 4096) > kBeamWgs ? 32 : 16;
   a.chunks = (a.vocab + a.threads * a.each - 1) / (a.threads * a.each);
 }
 

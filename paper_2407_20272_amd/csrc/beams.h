@@ -50,6 +50,7 @@ void launch_pages_copy(const PageCopyArgs& a, hipStream_t st);
 // ---- beam.hip ------------------------------------------------------------------------------------------------------
 constexpr int kBeamMost = 128;     // beams of a group, and candidates that come back of one
 constexpr int kBeamFewOut = 32;    // up to so many of a group, the scan's chunks are the smaller ones
+constexpr int kBeamWgs = 1536;     // workgroups of the scan that run at once
 struct BeamArgs {
   const void* logits;        // [rows][stride]
   int64_t stride;
@@ -61,7 +62,7 @@ struct BeamArgs {
   int chunks;                // of a row
   int threads, each;         // workgroup of the scan, and values of a thread
   double2* stats;            // [rows][chunks]: maximum and sum of exponentials relative to it
-  uint64_t* found;           // [rows][chunks][n_out]: key of the logit and complement of its token, falling; 0: none
+  uint64_t* found;           // [groups][n_out][beams][chunks]: key of the logit and complement of its token, falling along n_out; 0: none
 };
 void beam_plan(BeamArgs& a);   // chunks, threads, each
 void launch_beam_select(const BeamArgs& a, int dtype, hipStream_t st);
