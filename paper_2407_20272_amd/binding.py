@@ -640,35 +640,34 @@ def ee_beam_select(logits: torch.Tensor, scores: torch.Tensor, beams: int, token
                    ws: BeamWorkspace, finished: Optional[torch.Tensor] = None, finished_out: Optional[torch.Tensor] = None, end_token: int = -1):
     """logits [groups * beams][vocab] float32 or bfloat16, any row stride; scores [groups * beams] float32; finished [groups * beams] int32; the results
     [groups * n_out] (or [groups][n_out])."""
-    device, (rows, vocab) = _device(), logits.shape
-    assert beams > 0 and rows % beams == 0 and scores.shape == (rows,) and scores.dtype == torch.float32 and scores_out.dtype == torch.float32
-    assert logits.get_device() == device and (logits.stride(1) == 1 or vocab == 1), "rows of consecutive values on the current device"
-    groups = rows // beams
-    total = tokens.numel()
+    device, (rows, vocab), (row_stride, stride) = _device(), logits.shape, logits.stride()
+    groups, total = rows // beams if beams > 0 else 0, tokens.numel()
     n_out = total // groups if groups else 1
-    assert total == groups * n_out and parents.numel() == total and scores_out.numel() == total and tokens.dtype == torch.int32 and parents.dtype == torch.int32
-    assert finished_out is None or finished_out.numel() == total and finished_out.dtype == torch.int32
-    _check(lib().ee_beam_select(logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, _KIND[logits.dtype], _here(scores, device),
-                                None if finished is None else _int32s(finished, (rows,), device), groups, beams, vocab, n_out, end_token,
+    assert beams > 0 and rows == groups * beams == scores.numel() and total == groups * n_out == parents.numel() == scores_out.numel(), "rows of whole groups"
+    assert scores.dtype is scores_out.dtype is torch.float32 and tokens.dtype is parents.dtype is torch.int32
+    assert logits.get_device() == device and (stride == 1 or vocab == 1), "rows of consecutive values on the current device"
+    assert finished is None or finished.numel() == rows and finished.dtype is torch.int32
+    assert finished_out is None or finished_out.numel() == total and finished_out.dtype is torch.int32
+    _check(lib().ee_beam_select(logits.data_ptr(), row_stride if rows > 1 else vocab, _KIND[logits.dtype], _here(scores, device),
+                                None if finished is None else _here(finished, device), groups, beams, vocab, n_out, end_token,
                                 _here(tokens, device), _here(parents, device), _here(scores_out, device),
                                 None if finished_out is None else _here(finished_out, device), _here(ws.buf, device), ws.bytes, _raw_stream(device)))
 
 
 def ee_reorder_rows(x: torch.Tensor, parents: torch.Tensor, out: torch.Tensor):
     """out[m] = x[parents[m]] of any type, rows of consecutive values at any row stride."""
-    device, rows = _device(), parents.shape[0]
-    assert x.dtype == out.dtype and x.shape[1:] == out.shape[1:] and out.shape[0] == rows and parents.dtype == torch.int32
-    size = x.element_size()
-    strides = []
-    for t in (x, out):
-        assert t.get_device() == device, "CUDA tensors of the current device"
-        if t.is_contiguous() or t.shape[0] == 0:
-            strides.append(t.numel() // t.shape[0] * size if t.shape[0] else 0)
-        else:
-            assert t[0].is_contiguous(), "rows of consecutive values"
-            strides.append(t.stride(0) * size)
-    row = out.numel() // rows * size if rows else 0
-    _check(lib().ee_reorder_rows(x.data_ptr(), strides[0], x.shape[0], _here(parents, device), rows, row, out.data_ptr(), strides[1], _raw_stream(device)))
+    device, rows, shape, out_shape = _device(), parents.numel(), x.shape, out.shape
+    assert x.dtype is out.dtype and shape[1:] == out_shape[1:] and out_shape[0] == rows and parents.dtype is torch.int32
+    assert x.get_device() == device and out.get_device() == device, "CUDA tensors of the current device"
+    row = out.nbytes // rows if rows else 0
+    x_stride = out_stride = row
+    if not x.is_contiguous():
+        assert x[0].is_contiguous(), "rows of consecutive values"
+        x_stride = x.stride(0) * x.element_size() if shape[0] > 1 else row
+    if not out.is_contiguous():
+        assert out[0].is_contiguous(), "rows of consecutive values"
+        out_stride = out.stride(0) * out.element_size() if rows > 1 else row
+    _check(lib().ee_reorder_rows(x.data_ptr(), x_stride, shape[0], _here(parents, device), rows, row, out.data_ptr(), out_stride, _raw_stream(device)))
 
 
 def make_prefix_groups(first_row: torch.Tensor, shared_blocks: torch.Tensor, max_shared: int) -> ee_prefix_groups:

@@ -37,15 +37,16 @@ struct PagePlane {
   char* base;
   size_t block_bytes;   // a multiple of 8, of 16 where `base` starts on 16
   int planes;
+  int pieces, wide;     // set by the launch: pieces of one block in all planes; whether they are copied in 16 bytes
 };
 struct PageCopyArgs {
   PagePlane pool[3];
-  int n_pools, num_blocks;
+  int n_pools, num_blocks, pieces;
   const int32_t* moves;   // [n][2]
   const int32_t* count;   // nullptr, or how many of them there are
   int n;
 };
-void launch_pages_copy(const PageCopyArgs& a, hipStream_t st);
+void launch_pages_copy(PageCopyArgs a, hipStream_t st);
 
 // ---- beam.hip ------------------------------------------------------------------------------------------------------
 constexpr int kBeamMost = 128;     // beams of a group, and candidates that come back of one

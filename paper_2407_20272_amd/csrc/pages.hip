@@ -7,6 +7,10 @@ namespace ee {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kCopyWgs = 2048;   // workgroups of a copy that run at once
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 __device__ inline int blocks_of(int len, int max_blocks) { return (min(max(len, 0), max_blocks * 16) + 15) >> 4; }
 
@@ -218,6 +222,112 @@ __global__ __launch_bounds__(kThreads) void pages_give_kernel(int32_t* refs, int
   }
 }
 
+// Both of these for rows and pools that one workgroup looks through: a launch and its waits less.  A thread has a row, a wavefront sixteen times 64 blocks; what it finds
+// free it writes where the blocks before leave it in the list of free ones.
+constexpr int kSmallRows = 1024, kSmallBlocks = 16384;
+__global__ __launch_bounds__(1024) void pages_grow_kernel(int32_t* refs, int num_blocks, PageRows r, const int32_t* new_lens, int32_t* moves, int32_t* missing) {
+  __shared__ int s_free[kSmallBlocks];
+  __shared__ __align__(16) int s_written[kSmallRows];
+  __shared__ int s_first[kSmallRows + 1];
+  __shared__ int s_wave[2][16];
+  const int t = threadIdx.x, wave = t >> 6, lane = t & 63, cap = r.max_blocks * 16;
+  // the wavefront's blocks
+  uint64_t free_bits[16];
+  int n_free = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int b = wave * 1024 + i * 64 + lane;
+    free_bits[i] = __ballot(b < num_blocks && refs[min(b, num_blocks - 1)] <= 0);
+    n_free += __popcll(free_bits[i]);
+  }
+  // this thread's row: the block that it goes on writing, if others refer to it too
+  int len = 0, to = 0, last = -1, count = 0;
+  if (t < r.rows) {
+    len = min(max(r.lens[t], 0), cap);
+    to = max(len, min(new_lens[t], cap));
+    if (to > len && (len & 15)) {
+      last = r.tables[(size_t)t * r.max_blocks + (len >> 4)];
+      if ((unsigned)last >= (unsigned)num_blocks) last = -1;
+      else if ((count = refs[last]) <= 1) last = -1;
+    }
+  }
+  s_written[t] = last;
+  __syncthreads();
+  bool replace = false;
+  if (last >= 0) {   // all of its references are rows of this call, and this is the last of them: it keeps the block
+    int claims = 0, later = 0;
+    for (int m = 0; m < r.rows; m += 4) {
+      const int4 w = *reinterpret_cast<const int4*>(&s_written[m]);   // (rows that there are not: -1)
+      const int same = (w.x == last) + (w.y == last) + (w.z == last) + (w.w == last);
+      claims += same;
+      later |= (w.x == last && m > t) | (w.y == last && m + 1 > t) | (w.z == last && m + 2 > t) | (w.w == last && m + 3 > t);
+    }
+    replace = claims != count || later;
+  }
+  const int want = replace + ((to + 15) >> 4) - ((len + 15) >> 4);   // (0 of threads without a row)
+  // sums of what is wanted before each thread, and of what is free before each wavefront
+  int upto = want;
+#pragma unroll
+  for (int x = 1; x < 64; x <<= 1) {
+    const int o = __shfl_up(upto, x);
+    if (lane >= x) upto += o;
+  }
+  if (lane == 63) {
+    s_wave[0][wave] = upto;
+    s_wave[1][wave] = n_free;
+  }
+  __syncthreads();
+  int first = upto - want, at = 0, wanted = 0, have = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    if (i < wave) {
+      first += s_wave[0][i];
+      at += s_wave[1][i];
+    }
+    wanted += s_wave[0][i];
+    have += s_wave[1][i];
+  }
+  const bool enough = wanted <= have;
+  if (t == 0) *missing = enough ? 0 : wanted - have;
+  s_first[t] = first;
+  if (t == 0) s_first[kSmallRows] = wanted;
+  if (enough) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int k = at + __popcll(free_bits[i] & ((1ull << lane) - 1));
+      if ((free_bits[i] >> lane & 1) && k < wanted) s_free[k] = wave * 1024 + i * 64 + lane;
+      at += __popcll(free_bits[i]);
+    }
+  }
+  __syncthreads();
+  if (t < r.rows) {
+    const int block = enough && replace ? s_free[first] : -1;
+    moves[2 * t] = block >= 0 ? last : -1;
+    moves[2 * t + 1] = block;
+    if (block >= 0) {
+      refs[block] = 1;
+      r.tables[(size_t)t * r.max_blocks + (len >> 4)] = block;
+      atomicSub(&refs[last], 1);
+    }
+    s_written[t] = replace ? ~((len + 15) >> 4) : (len + 15) >> 4;   // where its other blocks go (as the complement: the first has gone)
+  }
+  __syncthreads();
+  if (!enough) return;
+  for (int k = t; k < wanted; k += 1024) {
+    int lo = 0, hi = r.rows - 1;   // the row whose blocks k is among: the last with s_first <= k
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (s_first[mid] <= k) lo = mid;
+      else hi = mid - 1;
+    }
+    const int i = k - s_first[lo], behind = s_written[lo], replaced = behind < 0;
+    if (i < replaced) continue;
+    const int block = s_free[k];
+    refs[block] = 1;
+    r.tables[(size_t)lo * r.max_blocks + (replaced ? ~behind : behind) + i - replaced] = block;
+  }
+}
+
 __global__ __launch_bounds__(kThreads) void pages_taken_kernel(const int32_t* refs, int num_blocks, PageWork w) { taken_chunk(refs, num_blocks, blockIdx.x, w); }
 
 // Packing: with n blocks in use, the i-th of them behind the first n places goes to the i-th free place among these.  Every block finds its place by the
@@ -255,6 +365,71 @@ __global__ __launch_bounds__(kThreads) void pages_pack_kernel(int32_t* refs, int
   }
 }
 
+// The same for pools that one workgroup looks through: the free places among the first n stand in a list.
+__global__ __launch_bounds__(1024) void pages_pack_small_kernel(int32_t* refs, int num_blocks, int32_t* remap, int32_t* moves, int32_t* n_moves) {
+  __shared__ int s_free[kSmallBlocks];
+  __shared__ int s_wave[16];
+  const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
+  uint64_t free_bits[16];
+  int own[16], n_free = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int b = wave * 1024 + i * 64 + lane;
+    own[i] = refs[min(b, num_blocks - 1)];
+    free_bits[i] = __ballot(b < num_blocks && own[i] <= 0);
+    n_free += __popcll(free_bits[i]);
+  }
+  if (lane == 0) s_wave[wave] = n_free;
+  __syncthreads();
+  int before = 0, all = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    if (i < wave) before += s_wave[i];
+    all += s_wave[i];
+  }
+  const int n = num_blocks - all;
+  // free blocks in front of each block; the last one among the first n leaves how many there are
+  int at = before;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int b = wave * 1024 + i * 64 + lane, k = at + __popcll(free_bits[i] & ((1ull << lane) - 1));
+    if (free_bits[i] >> lane & 1) s_free[k] = b;
+    at += __popcll(free_bits[i]);
+  }
+  __syncthreads();
+  int lo = 0, hi = all;            // free places among the first n: those of the list (ascending) below n
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (s_free[mid] < n) lo = mid + 1;
+    else hi = mid;
+  }
+  const int n_go = lo;
+  if (t == 0) *n_moves = n_go;
+  at = before;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int b = wave * 1024 + i * 64 + lane, k = at + __popcll(free_bits[i] & ((1ull << lane) - 1));
+    at += __popcll(free_bits[i]);
+    if (b >= num_blocks) continue;
+    if (b >= n_go) {
+      moves[2 * b] = -1;
+      moves[2 * b + 1] = -1;
+    }
+    if (own[i] <= 0) {
+      remap[b] = -1;
+    } else if (b < n) {
+      remap[b] = b;
+    } else {
+      const int rank = (b - k) - (n - n_go), to = s_free[rank];
+      remap[b] = to;
+      moves[2 * rank] = b;
+      moves[2 * rank + 1] = to;
+      refs[to] = own[i];
+      refs[b] = 0;
+    }
+  }
+}
+
 __global__ __launch_bounds__(kThreads) void pages_remap_kernel(const int32_t* remap, int num_blocks, PageRows r) {
   const int row = blockIdx.x, n = blocks_of(r.lens[row], r.max_blocks);
   for (int e = threadIdx.x; e < n; e += kThreads) {
@@ -280,6 +455,7 @@ __global__ __launch_bounds__(kThreads) void pages_shared_kernel(PageRows r, cons
     if (e < full) {
       const int b = r.tables[(size_t)a * r.max_blocks + e];
       bool differs = false;
+#pragma unroll 8
       for (int m = a + 1; m < z; ++m) differs |= r.tables[(size_t)m * r.max_blocks + e] != b;
       if (differs) same = min(same, e);
     }
@@ -290,52 +466,67 @@ __global__ __launch_bounds__(kThreads) void pages_shared_kernel(PageRows r, cons
   if (threadIdx.x == 0) shared[g] = a < z ? s_least : 0;
 }
 
-// Copies blocks of every pool.  A workgroup takes pieces of 16 KiB: the moves there are of 1024 of the list at a time, gathered in LDS (in their order, the same
-// in every workgroup), times planes and pieces.
+// Copies blocks of every pool, in pieces of 16 KiB: a workgroup takes its pieces of the moves that are its own in turn.  Bound by memory.
 constexpr int kCopyMoves = 1024;
 constexpr int kCopyPiece = 16384;
+
+__device__ inline void copy_piece(const PageCopyArgs& a, int2 move, int piece) {
+  int p = 0;
+  while (p + 1 < a.n_pools && piece >= a.pool[p].pieces) piece -= a.pool[p++].pieces;
+  const PagePlane& pool = a.pool[p];
+  const int each = (int)((pool.block_bytes + kCopyPiece - 1) / kCopyPiece), plane = piece / each, at0 = piece - plane * each;
+  char* base = pool.base + (size_t)plane * a.num_blocks * pool.block_bytes + (size_t)at0 * kCopyPiece;
+  const char* src = base + (size_t)move.x * pool.block_bytes;
+  char* dst = base + (size_t)move.y * pool.block_bytes;
+  const int bytes = (int)min((size_t)kCopyPiece, pool.block_bytes - (size_t)at0 * kCopyPiece);
+  if (pool.wide) {
+    u32x4 v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int at = (u * kThreads + threadIdx.x) * 16;
+      v[u] = u32x4{};
+      if (at < bytes) v[u] = *reinterpret_cast<const u32x4*>(src + at);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (const int at = (u * kThreads + threadIdx.x) * 16; at < bytes) *reinterpret_cast<u32x4*>(dst + at) = v[u];
+  } else {
+    for (int at = threadIdx.x * 8; at < bytes; at += kThreads * 8) *reinterpret_cast<u32x2*>(dst + at) = *reinterpret_cast<const u32x2*>(src + at);
+  }
+}
+
+__device__ inline bool is_move(const PageCopyArgs& a, int2 m) {
+  return (unsigned)m.x < (unsigned)a.num_blocks && (unsigned)m.y < (unsigned)a.num_blocks && m.x != m.y;
+}
+
+// The list has `count` moves, one behind the other (any of them may be none).
 __global__ __launch_bounds__(kThreads) void pages_copy_kernel(PageCopyArgs a) {
+  const int n = min(max(*a.count, 0), a.n);
+  for (int m = blockIdx.y; m < n; m += gridDim.y) {
+    const int2 move = make_int2(a.moves[2 * m], a.moves[2 * m + 1]);
+    if (!is_move(a, move)) continue;
+    for (int piece = blockIdx.x; piece < a.pieces; piece += gridDim.x) copy_piece(a, move, piece);
+  }
+}
+
+// Moves anywhere in the list: those there are of 1024 entries at a time are gathered in LDS, in their order.
+__global__ __launch_bounds__(kThreads) void pages_copy_sparse_kernel(PageCopyArgs a) {
   __shared__ int2 s_move[kCopyMoves];
-  const int n = a.count ? min(max(*a.count, 0), a.n) : a.n;
-  for (int m0 = 0; m0 < n; m0 += kCopyMoves) {
-    __syncthreads();
+  for (int m0 = 0; m0 < a.n; m0 += kCopyMoves) {
     int there = 0;
-    for (int m1 = m0; m1 < min(n, m0 + kCopyMoves); m1 += kThreads) {
+    __syncthreads();
+    for (int m1 = m0; m1 < min(a.n, m0 + kCopyMoves); m1 += kThreads) {
       const int m = m1 + threadIdx.x;
-      const int2 mv = m < n ? make_int2(a.moves[2 * m], a.moves[2 * m + 1]) : make_int2(-1, -1);
-      const bool goes = (unsigned)mv.x < (unsigned)a.num_blocks && (unsigned)mv.y < (unsigned)a.num_blocks && mv.x != mv.y;
+      const int2 move = m < a.n ? make_int2(a.moves[2 * m], a.moves[2 * m + 1]) : make_int2(-1, -1);
+      const bool goes = is_move(a, move);
       int total;
       const int before = scan_before(goes, total);
-      if (goes) s_move[there + before] = mv;
+      if (goes) s_move[there + before] = move;
       there += total;
     }
     __syncthreads();
-    for (int p = 0; p < a.n_pools; ++p) {
-      const PagePlane pool = a.pool[p];
-      const int pieces = (int)((pool.block_bytes + kCopyPiece - 1) / kCopyPiece);
-      const int64_t items = (int64_t)there * pool.planes * pieces;
-      for (int64_t i = blockIdx.x; i < items; i += gridDim.x) {
-        const int piece = (int)(i % pieces);
-        const int64_t rest = i / pieces;
-        const int plane = (int)(rest % pool.planes);
-        const int2 mv = s_move[rest / pool.planes];
-        char* base = pool.base + (size_t)plane * a.num_blocks * pool.block_bytes + (size_t)piece * kCopyPiece;
-        const char* src = base + (size_t)mv.x * pool.block_bytes;
-        char* dst = base + (size_t)mv.y * pool.block_bytes;
-        const int bytes = (int)min((size_t)kCopyPiece, pool.block_bytes - (size_t)piece * kCopyPiece);
-        if (((pool.block_bytes | reinterpret_cast<uintptr_t>(pool.base)) & 15) == 0) {
-          uint4 v[4];
-#pragma unroll
-          for (int u = 0; u < 4; ++u)
-            if (const int at = (u * kThreads + threadIdx.x) * 16; at < bytes) v[u] = *reinterpret_cast<const uint4*>(src + at);
-#pragma unroll
-          for (int u = 0; u < 4; ++u)
-            if (const int at = (u * kThreads + threadIdx.x) * 16; at < bytes) *reinterpret_cast<uint4*>(dst + at) = v[u];
-        } else {
-          for (int at = threadIdx.x * 8; at < bytes; at += kThreads * 8) *reinterpret_cast<uint2*>(dst + at) = *reinterpret_cast<const uint2*>(src + at);
-        }
-      }
-    }
+    for (int m = blockIdx.y; m < there; m += gridDim.y)
+      for (int piece = blockIdx.x; piece < a.pieces; piece += gridDim.x) copy_piece(a, s_move[m], piece);
   }
 }
 
@@ -349,6 +540,10 @@ void launch_pages_release(int32_t* refs, int num_blocks, const PageRows& r, hipS
 
 void launch_pages_grow(int32_t* refs, int num_blocks, const PageRows& r, const int32_t* new_lens, int32_t* moves, int32_t* missing, const PageWork& w,
                        hipStream_t st) {
+  if (r.rows <= kSmallRows && num_blocks <= kSmallBlocks) {
+    pages_grow_kernel<<<1, 1024, 0, st>>>(refs, num_blocks, r, new_lens, moves, missing);
+    return;
+  }
   const int chunks = page_chunks(num_blocks);
   pages_want_kernel<<<chunks + 1, kThreads, 0, st>>>(refs, num_blocks, chunks, r, new_lens, w);
   const int wgs = r.rows < 4096 ? 8 : 64;   // (rows want about one block each; a prompt's thousand are four blocks a thread)
@@ -356,9 +551,13 @@ void launch_pages_grow(int32_t* refs, int num_blocks, const PageRows& r, const i
 }
 
 void launch_pages_compact(int32_t* refs, int num_blocks, const PageRows& r, int32_t* remap, int32_t* moves, int32_t* n_moves, const PageWork& w, hipStream_t st) {
-  const int chunks = page_chunks(num_blocks);
-  pages_taken_kernel<<<chunks, kThreads, 0, st>>>(refs, num_blocks, w);
-  pages_pack_kernel<<<(num_blocks + kThreads - 1) / kThreads, kThreads, chunks * sizeof(int32_t), st>>>(refs, num_blocks, chunks, remap, moves, n_moves, w);
+  if (num_blocks <= kSmallBlocks) {
+    pages_pack_small_kernel<<<1, 1024, 0, st>>>(refs, num_blocks, remap, moves, n_moves);
+  } else {
+    const int chunks = page_chunks(num_blocks);
+    pages_taken_kernel<<<chunks, kThreads, 0, st>>>(refs, num_blocks, w);
+    pages_pack_kernel<<<(num_blocks + kThreads - 1) / kThreads, kThreads, chunks * sizeof(int32_t), st>>>(refs, num_blocks, chunks, remap, moves, n_moves, w);
+  }
   if (r.rows > 0) pages_remap_kernel<<<r.rows, kThreads, 0, st>>>(remap, num_blocks, r);
 }
 
@@ -366,6 +565,20 @@ void launch_pages_shared(const PageRows& r, const int32_t* first_row, int n_grou
   pages_shared_kernel<<<n_groups, kThreads, 0, st>>>(r, first_row, shared);
 }
 
-void launch_pages_copy(const PageCopyArgs& a, hipStream_t st) { pages_copy_kernel<<<2048, kThreads, 0, st>>>(a); }
+void launch_pages_copy(PageCopyArgs a, hipStream_t st) {
+  a.pieces = 0;
+  for (int p = 0; p < a.n_pools; ++p) {
+    PagePlane& pool = a.pool[p];
+    pool.pieces = pool.planes * (int)((pool.block_bytes + kCopyPiece - 1) / kCopyPiece);
+    pool.wide = ((pool.block_bytes | reinterpret_cast<uintptr_t>(pool.base)) & 15) == 0;
+    a.pieces += pool.pieces;
+  }
+  // As many workgroups as run at once, or as the moves have pieces.
+  const int across = a.pieces < kCopyWgs ? a.pieces : kCopyWgs;
+  int down = (kCopyWgs + across - 1) / across;
+  if (down > a.n) down = a.n;
+  if (a.count) pages_copy_kernel<<<dim3(across, down), kThreads, 0, st>>>(a);
+  else pages_copy_sparse_kernel<<<dim3(across, down), kThreads, 0, st>>>(a);
+}
 
 }  // namespace ee

@@ -21,7 +21,7 @@ class Both:
     def __init__(self, num_blocks, rows, wide, seed=0):
         self.r, self.n, self.wide = random.Random(seed), num_blocks, wide
         self.refs = torch.zeros(num_blocks, dtype=torch.int32, device="cuda")
-        self.pool = B.PagePool.of(self.refs, 300)
+        self.pool = B.PagePool.of(self.refs, rows)
         self.sets = []
         for _ in range(2):
             t = torch.full((rows, wide), -7, dtype=torch.int32, device="cuda")
@@ -61,14 +61,15 @@ class Both:
         return old
 
 
-@pytest.mark.parametrize("num_blocks,rows,seed", [(40, 3, 0), (1000, 8, 1), (1024, 33, 2), (2500, 70, 3), (5000, 300, 4)])
+@pytest.mark.parametrize("num_blocks,rows,seed", [(40, 3, 0), (1000, 8, 1), (1024, 33, 2), (2500, 70, 3), (5000, 300, 4), (16384, 40, 5), (16385, 40, 6), (20000, 1024, 7), (40000, 1500, 8),
+                                                  (9000, 1025, 9)])
 def test_a_long_beam_search(num_blocks, rows, seed):
     """Prompts of all lengths, then steps that fork rows at random and grow them, packing on the way; a search that finds no room changes nothing."""
     b = Both(num_blocks, rows, 60, seed)
     room = num_blocks // (2 * rows)
     assert b.grow([b.r.choice([0, 1, 15, 16, 17, b.r.randint(0, 16 * max(1, min(20, room)))]) for _ in range(rows)]) == 0
     at, short = 0, 0
-    for step in range(24):
+    for step in range(24 if rows < 500 else 8):
         parents = [b.r.randrange(rows) if b.r.random() < 0.6 else m for m in range(rows)]
         if step == 7:
             parents[0] = -1
@@ -94,8 +95,15 @@ def test_a_long_beam_search(num_blocks, rows, seed):
     assert b.refs.tolist() == [0] * num_blocks
 
 
-def test_all_or_nothing():
-    b = Both(10, 4, 8)
+@pytest.mark.parametrize("spare", [0, 20000])
+def test_all_or_nothing(spare):
+    """(With a pool beyond what one workgroup looks through, most of it taken.)"""
+    b = Both(10 + spare, 4, 8)
+    if spare:
+        taken = b.r.sample(range(10 + spare), spare)
+        for i in taken:
+            b.o.refs[i] = 1
+        b.refs.copy_(i32(b.o.refs))
     assert b.grow([30, 30, 0, 5]) == 0
     b.fork([0, 0, 1, 3], False)
     assert b.grow([31, 31, 40, 6], 1) == 0       # rows 0 and 1 move (the parents keep theirs), row 2 moves and adds one, row 3 moves
