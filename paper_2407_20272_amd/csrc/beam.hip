@@ -310,36 +310,36 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
     else f = cc >> 32 ? f + float_of((uint32_t)(cc >> 32)) : NAN;
     return f == f ? key_of(fminf(fmaxf(f, -3.4028235e38f), 3.4028235e38f)) : 0u;
   };
-  const int kept = min(all, kJoinKept);
+  // Of the lists' first places, as many as fit, the rough scores are kept; what bound they give is one for all.  Behind them (the lists fall) are candidates only where a
+  // list's last kept place is one.
+  const int kept = min(all, kJoinKept), places = kept / lists;
   uint32_t most = 0;
-  int list_far = list0, list_kept_end = 0;   // (the latter: of the thread's first candidate that is not kept)
-  for (int i0 = threadIdx.x; i0 < all; i0 += 4 * kJoinThreads) {
+  int list_behind = list0;   // the list of the thread's first candidate that is not kept
+  for (int i0 = threadIdx.x; i0 < kept; i0 += 4 * kJoinThreads) {
     uint64_t c[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) c[u] = i0 + u * kJoinThreads < all ? found[i0 + u * kJoinThreads] : 0;
+    for (int u = 0; u < 4; ++u) c[u] = i0 + u * kJoinThreads < kept ? found[i0 + u * kJoinThreads] : 0;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int i = i0 + u * kJoinThreads;
-      if (i == kJoinKept + (int)threadIdx.x) list_kept_end = list_far;
-      if (i < all) {
-        const uint32_t k = rough(list_far, c[u], i < lists);
-        if (i < kJoinKept) s_rough[i] = k;   // (read by the same thread)
+    for (int u = 0; u < 4; ++u)
+      if (const int i = i0 + u * kJoinThreads; i < kept) {
+        const uint32_t k = rough(list_behind, c[u], i < lists);
+        s_rough[i] = k;
         most = max(most, k);
+        list_behind = next_list(list_behind);
       }
-      list_far = next_list(list_far);
-    }
   }
-  // use(rough score, its number, its list) of every candidate of this thread
-  auto each = [&](auto&& use) {
+  // use(rough score, its number, its list) of every kept candidate of this thread, and of those behind that are not below `bound`
+  auto each = [&](uint32_t bound, bool behind, auto&& use) {
     int list = list0;
 #pragma unroll 4
     for (int i = threadIdx.x; i < kept; i += kJoinThreads) {
       use(s_rough[i], i, list);
       list = next_list(list);
     }
-    list = list_kept_end;
-    for (int i = kJoinKept + threadIdx.x; i < all; i += kJoinThreads) {
-      use(rough(list, found[i], i < lists), i, list);
+    if (!behind) return;
+    list = list_behind;
+    for (int i = kept + (int)threadIdx.x; i < all; i += kJoinThreads) {
+      if (places == 0 || s_rough[(places - 1) * lists + list] >= bound) use(rough(list, found[i], i < lists), i, list);
       list = next_list(list);
     }
   };
@@ -376,7 +376,7 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
         middle = bound + (above - bound) / 2;
       }
       int mine = 0;
-      each([&](uint32_t k, int, int) { mine += k >= middle; });
+      each(0, false, [&](uint32_t k, int, int) { mine += k >= middle; });
       const int there = block_sum(mine, turn);
       if (there >= n || turn == 0) bound = middle;
       else above = middle;
@@ -392,7 +392,7 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
     const int at = atomicAdd(&s_count, 1);
     if (at < kJoinList) s_list[at] = x;
   };
-  each([&](uint32_t k, int i, int list) {
+  each(bound, true, [&](uint32_t k, int i, int list) {
     if (k >= bound) put_by(candidate(list, found[i], i < lists));   // (k of none is 0)
   });
   __syncthreads();
@@ -401,7 +401,7 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
     int turn = 0;
     auto block_count = [&](auto&& test) {
       int mine = 0;
-      each([&](uint32_t k, int i, int list) {
+      each(bound, true, [&](uint32_t k, int i, int list) {
         if (k >= bound) mine += test(candidate(list, found[i], i < lists));
       });
       return block_sum(mine, turn++);
@@ -419,7 +419,7 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
     }
     if (threadIdx.x == 0) s_count = 0;
     __syncthreads();
-    each([&](uint32_t k, int i, int list) {
+    each(bound, true, [&](uint32_t k, int i, int list) {
       if (k < bound) return;
       const Candidate x = candidate(list, found[i], i < lists);
       if (x.key > from || (x.key == from && x.index <= up_to)) put_by(x);

@@ -30,7 +30,7 @@ constexpr float kNegBig = -1.0e30f;
 constexpr int kMostColumns = 48;    // of a tile (64 columns' sums and what is multiplied with them are more than 256 registers)
 constexpr int kMostRows = kMostColumns;
 constexpr int kMostWgs = 256;   // workgroups that run at once
-constexpr int kWorthDealing = 64;   // steps of a tile
+constexpr int kWorthDealing = 64;   // steps of a tile of up to 16 KB (half as many of 32)
 constexpr int kDealRows = 1024, kDealGroups = 512, kDealTiles = 512;   // up to so many are dealt out
 
 // The upper halves of two words (two floats truncated to bf16), the first in the low half.
@@ -696,7 +696,7 @@ void shared_attn_plan(SharedAttnArgs& a, int dtype) {
   const int64_t heads = (int64_t)a.kv_heads * a.head_chunks, wgs = a.tiles * heads;
   const int64_t shared = a.max_shared < a.max_context / 16 ? a.max_shared : a.max_context / 16, own = a.max_context - shared * 16;
   const int64_t steps = (shared * 16 + 31) / 32 + (int64_t)(a.rows < a.rows_per_tile ? a.rows : a.rows_per_tile) * ((own + 31) / 32);
-  const bool deal = wgs < kMostWgs ? steps >= kWorthDealing : wgs < 8 * kMostWgs && wgs * steps >= 8 * kWaves * kMostWgs;
+  const bool deal = wgs < kMostWgs ? steps * (dtype == EE_FP32 && a.dh == 128 ? 2 : 1) >= kWorthDealing : wgs < 8 * kMostWgs && wgs * steps >= 8 * kWaves * kMostWgs;
   const bool can = a.rows <= kDealRows && a.n_groups <= kDealGroups && a.tiles <= kDealTiles;
   a.dealt = deal && can ? (heads < kMostWgs ? (int)(kMostWgs / heads) : 1) : 0;
   // Few tiles, each of more steps than wavefronts: fewer rows in each, whose own positions then go side by side (the shared ones are read more often, from cache).

@@ -132,6 +132,17 @@ def test_large_scores():
     check(logits * 1e30, torch.zeros(4), 4, 8)
 
 
+@pytest.mark.parametrize("beams,vocab,n_out", [(57, 105147, 114), (128, 20000, 128), (64, 32000, 128), (20, 9000, 32)])
+@pytest.mark.parametrize("spread", [0.1, 3.0, 200.0])
+def test_unlike_beams(beams, vocab, n_out, spread):
+    """Where few beams have all the best candidates, and more of them than are kept at hand; and where all are alike."""
+    g = gen(beams)
+    logits = torch.randn((beams, vocab), generator=g) * 2
+    check(logits, torch.randn(beams, generator=g) * spread, beams, n_out)
+    finished = torch.rand(beams, generator=g) < 0.3
+    check(logits[:, :vocab - 1].contiguous(), -torch.arange(beams).float() * spread, beams, n_out, finished, 7)
+
+
 def test_a_workspace_of_larger_sizes_and_repeats():
     g = gen(11)
     ws = B.BeamWorkspace(9, 40, 20000, 128)
