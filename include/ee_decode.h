@@ -451,7 +451,7 @@ int ee_reorder_rows(const void* in, int64_t in_stride, int32_t in_rows, const in
 /* Rows whose sequences begin with the same blocks.  Groups are rows first_row[g] .. first_row[g + 1] - 1 of the batch (ascending); the first shared_blocks[g]
  * entries of their block tables are equal.  A group may have one row, or share nothing. */
 typedef struct ee_prefix_groups {
-  int32_t n_groups;             /* 0 .. 65536                                                                */
+  int32_t n_groups;             /* 0 .. 4096                                                                 */
   const int32_t* first_row;     /* dev [n_groups + 1] int32                                               */
   const int32_t* shared_blocks; /* dev [n_groups] int32                                                   */
   int32_t max_shared;           /* host-side upper bound of shared_blocks (more are not shared: read row by row) */
@@ -459,7 +459,7 @@ typedef struct ee_prefix_groups {
 
 /* ee_paged_attention_decode for such rows, n_heads query heads over the desc->n_heads K/V heads of the cache (a multiple; g = n_heads / desc->n_heads):
  *   out[m][h] = softmax_j(q[m][h] . K[j][h / g] / sqrt(head_dim)) . V[j][h / g],   j = 0..context_lens[m] INCLUSIVE,
- * the same result as without groups; shared blocks are read once for up to 64 columns (a row and a query head) instead of once a row.  A row shorter than its group's shared
+ * the same result as without groups; shared blocks are read once for up to 48 columns (a row and a query head; 32 of EE_FP32) instead of once a row.  A row shorter than its group's shared
  * blocks attends its own positions all the same; one with context_lens[m] < 0 attends nothing: its result is 0.  Rows of no group are left as they were.  row_table as in
  * ee_paged_attention_decode (shared blocks are then those of the rows' sequences).
  * q and out dev [rows][n_heads][head_dim] float, 16-byte aligned, not overlapping; pools start on 16 bytes.  Products and sums are float in effect.

@@ -633,7 +633,8 @@ class BeamWorkspace:
         if self.bytes == 0:
             raise EEError(EE_ERR_INVALID_ARG, ee_last_error())
         self.buf = torch.empty(self.bytes, dtype=torch.uint8, device=device)
-        assert self.buf.data_ptr() % 256 == 0
+        self.address, self.device = self.buf.data_ptr(), self.buf.get_device()
+        assert self.address % 256 == 0
 
 
 def ee_beam_select(logits: torch.Tensor, scores: torch.Tensor, beams: int, tokens: torch.Tensor, parents: torch.Tensor, scores_out: torch.Tensor,
@@ -645,13 +646,13 @@ def ee_beam_select(logits: torch.Tensor, scores: torch.Tensor, beams: int, token
     n_out = total // groups if groups else 1
     assert beams > 0 and rows == groups * beams == scores.numel() and total == groups * n_out == parents.numel() == scores_out.numel(), "rows of whole groups"
     assert scores.dtype is scores_out.dtype is torch.float32 and tokens.dtype is parents.dtype is torch.int32
-    assert logits.get_device() == device and (stride == 1 or vocab == 1), "rows of consecutive values on the current device"
+    assert logits.get_device() == device == ws.device and (stride == 1 or vocab == 1), "rows of consecutive values, and a workspace, on the current device"
     assert finished is None or finished.numel() == rows and finished.dtype is torch.int32
     assert finished_out is None or finished_out.numel() == total and finished_out.dtype is torch.int32
     _check(lib().ee_beam_select(logits.data_ptr(), row_stride if rows > 1 else vocab, _KIND[logits.dtype], _here(scores, device),
                                 None if finished is None else _here(finished, device), groups, beams, vocab, n_out, end_token,
                                 _here(tokens, device), _here(parents, device), _here(scores_out, device),
-                                None if finished_out is None else _here(finished_out, device), _here(ws.buf, device), ws.bytes, _raw_stream(device)))
+                                None if finished_out is None else _here(finished_out, device), ws.address, ws.bytes, _raw_stream(device)))
 
 
 def ee_reorder_rows(x: torch.Tensor, parents: torch.Tensor, out: torch.Tensor):
@@ -688,17 +689,18 @@ class SharedWorkspace:
         if self.bytes == 0:
             raise EEError(EE_ERR_INVALID_ARG, ee_last_error())
         self.buf = torch.empty(self.bytes, dtype=torch.uint8, device=device)
-        assert self.buf.data_ptr() % 256 == 0
+        self.address, self.device = self.buf.data_ptr(), self.buf.get_device()
+        assert self.address % 256 == 0
 
 
 def ee_paged_attention_shared(desc: ee_model_desc, cache: PagedKV, layer: int, q: torch.Tensor, batch: ee_batch, groups: ee_prefix_groups,
                               out: torch.Tensor, ws: SharedWorkspace):
     """q, out [rows][n_heads][dh] float32; the cache has desc.n_heads K/V heads."""
     device = _device()
-    assert cache.k.get_device() == device and batch.device == device and groups.device == device, "cache, batch and groups of the current device"
+    assert cache.k.get_device() == device == batch.device and device == groups.device == ws.device, "cache, batch, groups and workspace of the current device"
     rows, heads, dh = q.shape
     assert out.shape == q.shape and rows == batch.batch and dh == desc.head_dim and q.dtype == torch.float32 and out.dtype == torch.float32
-    _check(lib().ee_paged_attention_shared(desc, cache.c, layer, heads, _here(q, device), batch, groups, _here(out, device), _here(ws.buf, device), ws.bytes,
+    _check(lib().ee_paged_attention_shared(desc, cache.c, layer, heads, _here(q, device), batch, groups, _here(out, device), ws.address, ws.bytes,
                                            _raw_stream(device)))
 
 

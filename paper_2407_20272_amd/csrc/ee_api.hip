@@ -1313,6 +1313,7 @@ int ee_kv_quant_evict(const ee_quant_cache* cache, int32_t layer, const ee_batch
 namespace {
 
 constexpr int kMostPageRows = 1 << 20;
+constexpr int kMostGroups = 4096;          // of an attention: every workgroup looks through them
 constexpr int kMostPageBlocks = 1 << 23;   // (the chunks' counts are kept in LDS)
 
 int check_pool(const int32_t* refs, int32_t num_blocks, const char* what) {
@@ -1642,7 +1643,7 @@ int ee_reorder_rows(const void* in, int64_t in_stride, int32_t in_rows, const in
 
 size_t ee_paged_attention_shared_bytes(const ee_model_desc* desc, int32_t n_heads, int32_t max_batch, int32_t max_groups, int32_t max_context) {
   if (check_desc(desc) || check_shared_heads(desc, n_heads)) return 0;
-  if (max_batch < 1 || max_groups < 1 || max_groups > 65536 || max_context < 1 || max_context > kAttnMaxBlocks * 16) {
+  if (max_batch < 1 || max_groups < 1 || max_groups > kMostGroups || max_context < 1 || max_context > kAttnMaxBlocks * 16) {
     set_error("ee_paged_attention_shared_bytes: batch %d, %d groups, context %d", max_batch, max_groups, max_context);
     return 0;
   }
@@ -1666,7 +1667,7 @@ int ee_paged_attention_shared(const ee_model_desc* desc, const ee_kv_cache* cach
   if ((rc = check_desc(desc)) || (rc = check_cache(cache)) || (rc = check_batch(batch, false)) || (rc = check_shared_heads(desc, n_heads))) return rc;
   if (!groups) EE_FAIL(EE_ERR_INVALID_ARG, "ee_paged_attention_shared: groups are NULL");
   if (groups->n_groups < 0 || groups->max_shared < 0) EE_FAIL(EE_ERR_INVALID_ARG, "ee_paged_attention_shared: %d groups, max_shared %d", groups->n_groups, groups->max_shared);
-  if (groups->n_groups > 65536) EE_FAIL(EE_ERR_UNSUPPORTED, "ee_paged_attention_shared: %d groups in one call", groups->n_groups);
+  if (groups->n_groups > kMostGroups) EE_FAIL(EE_ERR_UNSUPPORTED, "ee_paged_attention_shared: %d groups in one call", groups->n_groups);
   if (batch->batch == 0 || groups->n_groups == 0) return EE_OK;
   if (layer < 1 || layer > desc->n_layers) EE_FAIL(EE_ERR_INVALID_ARG, "layer %d outside 1..%d", layer, desc->n_layers);
   if ((rc = check_int32(groups->first_row, "ee_paged_attention_shared")) || (rc = check_int32(groups->shared_blocks, "ee_paged_attention_shared"))) return rc;

@@ -365,8 +365,9 @@ __global__ __launch_bounds__(kThreads) void pages_pack_kernel(int32_t* refs, int
   }
 }
 
-// The same for pools that one workgroup looks through: the free places among the first n stand in a list.
-__global__ __launch_bounds__(1024) void pages_pack_small_kernel(int32_t* refs, int num_blocks, int32_t* remap, int32_t* moves, int32_t* n_moves) {
+// The same for pools that one workgroup looks through: the free places among the first n stand in a list.  `r` has rows where their tables are few enough to follow here.
+constexpr int kSmallEntries = 16384;
+__global__ __launch_bounds__(1024) void pages_pack_small_kernel(int32_t* refs, int num_blocks, PageRows r, int32_t* remap, int32_t* moves, int32_t* n_moves) {
   __shared__ int s_free[kSmallBlocks];
   __shared__ int s_wave[16];
   const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
@@ -427,6 +428,11 @@ __global__ __launch_bounds__(1024) void pages_pack_small_kernel(int32_t* refs, i
       refs[to] = own[i];
       refs[b] = 0;
     }
+  }
+  __syncthreads();   // (what the workgroup has written it may read)
+  for (int i = t; i < r.rows * r.max_blocks; i += 1024) {
+    const int row = i / r.max_blocks, e = i - row * r.max_blocks, b = r.tables[i];
+    if (e < blocks_of(r.lens[row], r.max_blocks) && (unsigned)b < (unsigned)num_blocks) r.tables[i] = remap[b];
   }
 }
 
@@ -552,7 +558,9 @@ void launch_pages_grow(int32_t* refs, int num_blocks, const PageRows& r, const i
 
 void launch_pages_compact(int32_t* refs, int num_blocks, const PageRows& r, int32_t* remap, int32_t* moves, int32_t* n_moves, const PageWork& w, hipStream_t st) {
   if (num_blocks <= kSmallBlocks) {
-    pages_pack_small_kernel<<<1, 1024, 0, st>>>(refs, num_blocks, remap, moves, n_moves);
+    const bool follow = (int64_t)r.rows * r.max_blocks <= kSmallEntries;
+    pages_pack_small_kernel<<<1, 1024, 0, st>>>(refs, num_blocks, follow ? r : PageRows{}, remap, moves, n_moves);
+    if (follow) return;
   } else {
     const int chunks = page_chunks(num_blocks);
     pages_taken_kernel<<<chunks, kThreads, 0, st>>>(refs, num_blocks, w);

@@ -187,7 +187,7 @@ def test_attention_refuses():
     for g in (B.ee_prefix_groups(-1, P, P, 2), B.ee_prefix_groups(1, None, P, 2), B.ee_prefix_groups(1, P, None, 2), B.ee_prefix_groups(1, P + 1, P, 2),
               B.ee_prefix_groups(1, P, P, -1)):
         assert attend(g=g) == INVALID
-    assert attend(g=B.ee_prefix_groups(65537, P, P, 2)) == UNSUPPORTED
+    assert attend(g=B.ee_prefix_groups(4097, P, P, 2)) == UNSUPPORTED
     assert attend(b=batch(rows=70000), heads=128, d=desc(d_model=64, n_heads=1), out=1 << 40) == UNSUPPORTED
     assert attend(b=batch(max_blocks=20000)) == UNSUPPORTED and attend(b=batch(max_context=65)) == SHAPE and attend(b=batch(lens=None)) == INVALID
     # a long context is divided, and says so without a workspace

@@ -19,6 +19,7 @@ class Both:
     """A pool and tables on the device, and the same in lists."""
 
     def __init__(self, num_blocks, rows, wide, seed=0):
+        """(-7 behind a row's blocks: nothing there is read or written)"""
         self.r, self.n, self.wide = random.Random(seed), num_blocks, wide
         self.refs = torch.zeros(num_blocks, dtype=torch.int32, device="cuda")
         self.pool = B.PagePool.of(self.refs, rows)
