@@ -382,7 +382,7 @@ typedef struct ee_page_tables {
   int32_t* block_tables; /* dev [rows][max_blocks]                                                        */
   int32_t* lens;         /* dev [rows]: cached positions (0 .. max_blocks * 16); the first ceil(lens / 16) entries of a row are
                             its blocks, what lies behind is never read                                     */
-  int32_t rows, max_blocks;
+  int32_t rows, max_blocks; /* up to 2^20 and 2^23, together 2^30 entries                                    */
 } ee_page_tables;
 
 /* Scratch bytes of ee_kv_pages_grow and ee_kv_pages_compact for a pool of num_blocks (up to 2^23) and calls of up to max_rows rows.  256-byte
@@ -390,7 +390,7 @@ typedef struct ee_page_tables {
 size_t ee_kv_pages_bytes(int32_t num_blocks, int32_t max_rows);
 
 /* Row m of dst becomes a copy of row parents[m] of src: its blocks (one more reference each) and its length.  parents dev [dst->rows]; where
- * it is no row of src, row m becomes empty.  Entries behind a row's blocks are left as they were.  release = 1: afterwards the rows of src give up theirs, as
+ * it is no row of src, row m becomes empty.  What dst's rows held before is not given up (that is ee_kv_pages_release's).  Entries behind a row's blocks are left as they were.  release = 1: afterwards the rows of src give up theirs, as
  * by ee_kv_pages_release.  dst->max_blocks >= src->max_blocks; the tables must not overlap. */
 int ee_kv_pages_fork(int32_t* refs, int32_t num_blocks, const ee_page_tables* src, const int32_t* parents, const ee_page_tables* dst,
                      int32_t release, void* stream);
@@ -435,7 +435,7 @@ int ee_kv_quant_copy(const ee_quant_cache* cache, const int32_t* moves, int32_t 
  *   logits dev [groups * beams] rows of vocab values of `dtype` (EE_FP32 | EE_BF16), logits_stride (>= vocab) elements apart, any element alignment.
  *   scores dev [groups * beams] float.  finished dev [groups * beams] int32 or NULL (none).  end_token: 0 .. vocab - 1, or -1 (none; not with finished).
  *   tokens, parents (rows of the call), finished_out dev [groups][n_out] int32, scores_out float; finished_out (or NULL) is 1 where the row is finished or the token
- *   is end_token.  Outputs must not overlap scores or finished.
+ *   is end_token.  Results overlap neither each other nor the inputs.
  * beams and n_out are 1 .. 128, n_out <= beams * vocab.  workspace: 256-byte aligned, ee_beam_select_bytes for the call's
  * sizes or larger ones (0: refused sizes), no initialisation, dead between calls. */
 size_t ee_beam_select_bytes(int32_t groups, int32_t beams, int32_t vocab, int32_t n_out);

@@ -697,7 +697,8 @@ def ee_paged_attention_shared(desc: ee_model_desc, cache: PagedKV, layer: int, q
                               out: torch.Tensor, ws: SharedWorkspace):
     """q, out [rows][n_heads][dh] float32; the cache has desc.n_heads K/V heads."""
     device = _device()
-    assert cache.k.get_device() == device == batch.device and device == groups.device == ws.device, "cache, batch, groups and workspace of the current device"
+    assert cache.k.get_device() == device == getattr(batch, "device", device) and device == getattr(groups, "device", device) == ws.device, \
+        "cache, batch, groups and workspace of the current device"
     rows, heads, dh = q.shape
     assert out.shape == q.shape and rows == batch.batch and dh == desc.head_dim and q.dtype == torch.float32 and out.dtype == torch.float32
     _check(lib().ee_paged_attention_shared(desc, cache.c, layer, heads, _here(q, device), batch, groups, _here(out, device), ws.address, ws.bytes,

@@ -5,7 +5,13 @@
 // Two launches.  The scan reads the logits once: a workgroup takes a chunk of a row, keeps its values in registers, and leaves the chunk's maximum, its
 // sum of exponentials and its n best, in order (within a beam the order of the scores is that of the logits, so this needs no sum of the whole row).
 // The join forms the rows' sums from the chunks', the scores of what was found, and the n best of these.
-// What is compared are scores in double: rounded to float many candidates of a beam would be equal, and beams' sums meet there.
+// What is compared are scores in double: rounded to float many candidates of a beam would be equal, and beams' sums meet there.  Exponentials are floats, a thread's sixteen or 32 are added
+// in float and everything behind that in double.
+//
+// Scan + join, kernel times: 4 rows of 2048 floats 4.6 + 4.4 us; 128 rows of 32000 bf16, 8 of 4 back: 7.1 + 7.3; 128 rows of 100003 floats (41 MB are read), 16 of 8 back: 14.8 + 8.5; 64 rows
+// of 32000 floats, 128 of 64 back: 12.6 + 22.  The scan of many rows is bound by memory and by the latency of one chunk (values, maximum, sum, bound, list: 6 us), the join by the latency of its
+// dozen barriers.  Values in chunks of 4096 where all workgroups run at once, else of 8192: the 128 rows of 100003 took 19 us in 4096, more than one round, also with the next chunk's
+// values on their way.
 #include <type_traits>
 
 #include "beams.h"

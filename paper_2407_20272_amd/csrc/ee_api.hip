@@ -1333,6 +1333,8 @@ int check_tables(const ee_page_tables* T, const char* what, PageRows* r) {
   if (T->rows > kMostPageRows) EE_FAIL(EE_ERR_UNSUPPORTED, "%s: %d rows in one call", what, T->rows);
   if (T->max_blocks < 1) EE_FAIL(EE_ERR_INVALID_ARG, "%s: max_blocks must be positive", what);
   if (T->max_blocks > kMostPageBlocks) EE_FAIL(EE_ERR_UNSUPPORTED, "%s: max_blocks %d exceeds %d", what, T->max_blocks, kMostPageBlocks);
+  // (what all rows together may want is counted in 32 bits)
+  if ((int64_t)T->rows * T->max_blocks > 1 << 30) EE_FAIL(EE_ERR_UNSUPPORTED, "%s: %d rows of %d entries in one call", what, T->rows, T->max_blocks);
   return EE_OK;
 }
 
@@ -1585,12 +1587,12 @@ int ee_beam_select(const void* logits, int64_t logits_stride, int32_t dtype, con
       (rc = check_int32(scores_out, "ee_beam_select")))
     return rc;
   if ((reinterpret_cast<uintptr_t>(finished) | reinterpret_cast<uintptr_t>(finished_out)) & 3) EE_FAIL(EE_ERR_INVALID_ARG, "ee_beam_select: misaligned pointer");
-  const size_t in = (size_t)rows * 4, out = (size_t)groups * n_out * 4;
+  const size_t in = (size_t)rows * 4, out = (size_t)groups * n_out * 4, all = ((size_t)(rows - 1) * logits_stride + vocab) * size;
   const void* outs[4] = {tokens, parents, scores_out, finished_out};
   for (int i = 0; i < 4; ++i) {
     if (!outs[i]) continue;
-    if (ranges_meet(outs[i], out, scores, in) || (finished && ranges_meet(outs[i], out, finished, in)))
-      EE_FAIL(EE_ERR_INVALID_ARG, "ee_beam_select: results overlap scores or finished");
+    if (ranges_meet(outs[i], out, scores, in) || (finished && ranges_meet(outs[i], out, finished, in)) || ranges_meet(outs[i], out, logits, all))
+      EE_FAIL(EE_ERR_INVALID_ARG, "ee_beam_select: results overlap logits, scores or finished");
     for (int k = 0; k < i; ++k)
       if (outs[k] && ranges_meet(outs[i], out, outs[k], out)) EE_FAIL(EE_ERR_INVALID_ARG, "ee_beam_select: results overlap each other");
   }

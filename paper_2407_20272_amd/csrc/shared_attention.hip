@@ -3,15 +3,23 @@
 //
 //   out[m][h] = softmax_j(q[m][h] . K[j][h / g] / sqrt(dh)) . V[j][h / g],   j = 0..context_lens[m]
 //
-// A column is a row and one of the g query heads that share a K/V head.  A tile is up to 16 * NT columns of one group.  Its walk is one list of steps
-// of 32 positions: first the shared blocks, multiplied with every column, then each row's own positions, which count for that row's columns alone.  The list
-// is divided into equal parts (a workgroup each), a part's steps go round its wavefronts, and where there is more than one part a second launch joins them.
+// A column is a row and one of the g query heads that share a K/V head.  A tile is 16, 32 or 48 columns of one group, the next that hold a group on average: its walk is one list of
+// steps of 32 positions, first the shared blocks, multiplied with every column, then each row's own positions, which count for that row's columns alone.  A workgroup of eight
+// wavefronts, which take the steps in turn, has a tile, or one of the equal parts of it that its share of all steps is worth (`dealt`: a second launch joins them, by maximum and sum).
 //
 // Both products are transposed, so that no value changes lanes between them:
 //   scores^T [position][column] = K [position][dh] . q^T,      out^T [dh][column] += V^T [dh][position] . p^T
 // A lane ends the first with positions 4j..4j+3 of two blocks (j = lane / 16) of one column, and these are the positions that it contracts over in the second:
-// V's lanes load the same ones, a row's 16 bytes each, and turn eight rows of eight channels around in registers.  Nothing passes through LDS.
-// bf16: q and the probabilities are split into three bf16 parts, 24 bits, multiplied one after the other: float in effect, with a float's range.  fp32: the float matrix instructions.
+// V's lanes load the same ones, a row's 16 bytes each, and turn eight rows of eight channels around in registers.  K and V never pass through LDS; q does where there is more than one
+// tile of 16 columns.  bf16: q and the probabilities are split into three bf16 parts, 24 bits, multiplied one after the other: float in effect, with a float's range (relative error
+// 3.1e-7 on 4 rows behind 96 positions; with the probabilities in two parts 5.1e-6, and the long cases below 4 % faster).  fp32: the float matrix instructions.
+//
+// Bound by what a compute unit takes in (26 GB/s of memory, 28 to 30 with what comes from cache), and for short contexts by the chain in front of it: groups and lengths, block ids, K and V (4 us),
+// and the meeting of the wavefronts (1.5 us).  Kernel times, bf16, dh 128, 32 query heads:
+//   4 rows behind 96 positions, heads of their own: 8.2 us.    8 x 4 rows behind 512 (85 MB): 17.8 us, 12.5 at 6.8 TB/s.
+//   64 rows behind 2000, 100 to 900 of their own, over 8 heads (141 MB): 35.4 + 4.7 us (tiles of 16 columns 50, of 32 37; whole tiles a workgroup 50 in tiles of 16).
+//   12 rows behind 100000 over 8 heads (410 MB): 83 + 4.7 us (16 columns 130, 32 124; whole tiles 932).
+//   Four wavefronts a workgroup were 62 and 220 us where eight were 43 and 156; with tiles that begin in the middle of a workgroup's share of steps the 64 rows took 40.
 #include <type_traits>
 
 #include "beams.h"
@@ -26,11 +34,13 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * 64;
-constexpr float kNegBig = -1.0e30f;
+constexpr float kNegBig = -3.4028235e38f;   // the lowest float: no score that is one is below it
 constexpr int kMostColumns = 48;    // of a tile (64 columns' sums and what is multiplied with them are more than 256 registers)
 constexpr int kMostRows = kMostColumns;
 constexpr int kMostWgs = 256;   // workgroups that run at once
-constexpr int kWorthDealing = 64;   // steps of a tile of up to 16 KB (half as many of 32)
+// Steps of a tile of up to 16 KB (half as many of 32) from which its parts are worth the second launch (5 us and a gap): 39 steps of 35 float rows in 7 groups took 11 to 13 us as whole tiles,
+// 13.3 + 4 dealt out; 31 steps of 32 KB, 45 rows in 15 groups, 28 us whole and 22 dealt out.
+constexpr int kWorthDealing = 64;
 constexpr int kDealRows = 1024, kDealGroups = 512, kDealTiles = 512;   // up to so many are dealt out
 
 // The upper halves of two words (two floats truncated to bf16), the first in the low half.
@@ -699,7 +709,8 @@ void shared_attn_plan(SharedAttnArgs& a, int dtype) {
   const bool deal = wgs < kMostWgs ? steps * (dtype == EE_FP32 && a.dh == 128 ? 2 : 1) >= kWorthDealing : wgs < 8 * kMostWgs && wgs * steps >= 8 * kWaves * kMostWgs;
   const bool can = a.rows <= kDealRows && a.n_groups <= kDealGroups && a.tiles <= kDealTiles;
   a.dealt = deal && can ? (heads < kMostWgs ? (int)(kMostWgs / heads) : 1) : 0;
-  // Few tiles, each of more steps than wavefronts: fewer rows in each, whose own positions then go side by side (the shared ones are read more often, from cache).
+  // Few tiles, each of more steps than wavefronts: fewer rows in each, whose own positions then go side by side (the shared ones are read more often, from cache).  35 float
+  // rows in 7 groups, 12 heads over 4: 15.5 -> 11 us.
   for (int64_t n = steps; !a.dealt && a.head_chunks == 1 && a.rows_per_tile > 1 && n > kWaves && 2 * a.tiles * heads <= kMostWgs;) {
     const int rows = (a.rows_per_tile + 1) / 2;
     n -= (a.rows_per_tile - rows) * ((own + 31) / 32);

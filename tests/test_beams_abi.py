@@ -56,7 +56,7 @@ def test_pools_that_are_refused(call):
 @pytest.mark.parametrize("call,name", [(fork, "src"), (fork, "dst"), (release, "t"), (grow, "t"), (compact, "t"), (shared, "t")])
 def test_tables_that_are_refused(call, name):
     for bad, rc in [(tables(at=None), INVALID), (tables(lens=None), INVALID), (tables(at=P + 1), INVALID), (tables(lens=FAR + 2), INVALID),
-                    (tables(rows=-1), INVALID), (tables(rows=1 << 21), UNSUPPORTED), (tables(blocks=0), INVALID), (tables(blocks=1 << 24), UNSUPPORTED)]:
+                    (tables(rows=-1), INVALID), (tables(rows=1 << 21), UNSUPPORTED), (tables(blocks=0), INVALID), (tables(blocks=1 << 24), UNSUPPORTED), (tables(rows=1 << 12, blocks=(1 << 18) + 1), UNSUPPORTED)]:
         assert call(**{name: bad}) == rc, B.ee_last_error()
     if call is not compact:
         assert call(**{name: None}) == INVALID
@@ -137,6 +137,7 @@ def test_selection_refuses():
     assert select(fin=5 * FAR + 1, end=2) == INVALID and select(fout=5 * FAR + 2) == INVALID
     assert select(tok=FAR + 20) == INVALID and select(out=FAR) == INVALID and select(fin=5 * FAR, end=1, par=5 * FAR + 4) == INVALID
     assert select(par=2 * FAR + 8) == INVALID and select(fout=4 * FAR - 4) == INVALID and "each other" in B.ee_last_error()
+    assert select(tok=P + 2392) == INVALID and select(scores=P + 64, out=P + 2396) == INVALID and "logits" in B.ee_last_error()
     assert select(ws=None) == WORKSPACE and select(ws=P + 16) == WORKSPACE and select(size=64) == WORKSPACE
     assert select(groups=0, z=None) == OK
 

@@ -183,6 +183,34 @@ def test_large_and_small_values():
     c.check()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("score", [1e31, -1e31, 3e37, -3e37])
+def test_scores_far_out(dtype, score):
+    """Scores that are floats, however far out: the softmax of one position is 1, that of equal ones an equal share."""
+    c = Case(dtype, 64, 2, 2, [(1, [17, 33, 50]), (0, [1, 20])], poison=False)
+    c.q = torch.full(c.q.shape, 2.0 ** 40)
+    c.k = torch.full(c.k.shape, score / 2.0 ** 40 / 8).to(c.k.dtype)      # (64 products over sqrt(64): the score)
+    out = c.run()
+    for m, n in enumerate(c.lens):
+        at = torch.arange(n + 1)
+        v = c.v[0, c.tables[m][at // 16].long(), :, at % 16].double().mean(0)
+        assert bool(((out[m].double() - v).abs() <= 2e-5).all())      # (a sum of 50 values below 6, and its 50: 100 roundings of 6 * 2^-24 / 2 are 1.8e-5)
+
+
+@pytest.mark.parametrize("groups,rows", [(64, 2), (65, 1), (70, 3), (513, 1), (600, 2), (4096, 1)])
+def test_many_groups(groups, rows):
+    c = Case("bf16", 64, 2, 2, [(i % 3, [i % 3 * 16 + 1 + (i * 7 + r) % 30 for r in range(rows)]) for i in range(groups)])
+    c.check()
+
+
+@pytest.mark.parametrize("groups,rows,shared,own", [(100, 2, 20, 90), (3, 400, 30, 20), (2, 600, 70, 5), (512, 2, 4, 40)])
+def test_many_rows_dealt_out_or_not(groups, rows, shared, own):
+    """Around the numbers of rows, groups and tiles up to which steps are dealt out."""
+    c = Case("bf16", 64, 2, 1, [(shared - i % 2, [(shared - i % 2) * 16 + 1 + (i + r * 11) % own for r in range(rows)]) for i in range(groups)])
+    a = c.check()
+    assert torch.equal(a, c.run())
+
+
 def test_layers_and_a_larger_workspace():
     c = Case("fp32", 128, 4, 2, [(2, [40, 50]), (0, [300])], layers=3, layer=2)
     ws = B.SharedWorkspace(c.desc, 4, 50, 20, 16000)
