@@ -74,6 +74,12 @@ __device__ inline int wave_total(int v) {
   add(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
   return __builtin_amdgcn_readlane(v, 63);
 }
+// The sum over eight neighbouring lanes: all of them have it.
+__device__ inline int sum_of_8(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xf, 0xf, true);    // quad_perm [1,0,3,2], [2,3,0,1], row_half_mirror
+  v += __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xf, 0xf, true);
+  return v + __builtin_amdgcn_update_dpp(0, v, 0x141, 0xf, 0xf, true);
+}
 __device__ inline double wave_sum(double v) {
   auto add = [&](auto ctrl, auto rows) {
     const uint64_t u = (uint64_t)__double_as_longlong(v);
@@ -99,7 +105,7 @@ constexpr int kScanList = 512;   // candidates of a chunk that are put in order
 template <class T, int THREADS, int EACH>
 __global__ __launch_bounds__(THREADS, EACH > 16 ? 6 : 4) void beam_scan_kernel(BeamArgs a) {
   constexpr int VEC = 16 / sizeof(T), LOADS = EACH / VEC, WAVES = THREADS / 64;
-  __shared__ __align__(16) uint64_t s_list[kScanList + 8];
+  __shared__ __align__(16) uint64_t s_list[kScanList];
   __shared__ uint32_t s_most[256];
   __shared__ double s_sum[WAVES];
   __shared__ uint32_t s_top[WAVES];
@@ -212,15 +218,14 @@ __global__ __launch_bounds__(THREADS, EACH > 16 ? 6 : 4) void beam_scan_kernel(B
   }
   // place k of this list among the group's: [k][beam][chunk]
   uint64_t* found = a.found + (size_t)(row / a.beams) * n * lists + (size_t)(row % a.beams) * a.chunks + chunk;
-  if (threadIdx.x < 8) s_list[count + threadIdx.x] = 0;   // (whole eights are compared)
-  __syncthreads();
-  for (int i = threadIdx.x; i < count; i += THREADS) {
-    const uint64_t c = s_list[i];
+  for (int i0 = 0; i0 < count; i0 += THREADS / 8) {   // eight threads a candidate, each against every eighth
+    const int i = i0 + (int)threadIdx.x / 8;
+    const uint64_t c = i < count ? s_list[i] : 0;
     int rank = 0;
-    for (int j = 0; j < count; j += 8)
-#pragma unroll
-      for (int u = 0; u < 8; ++u) rank += s_list[j + u] > c;
-    if (rank < n) found[(size_t)rank * lists] = c;
+#pragma unroll 4
+    for (int j = threadIdx.x & 7; j < count; j += 8) rank += s_list[j] > c;
+    rank = sum_of_8(rank);
+    if (i < count && rank < n && (threadIdx.x & 7) == 0) found[(size_t)rank * lists] = c;
   }
   for (int i = count + (int)threadIdx.x; i < n; i += THREADS) found[(size_t)i * lists] = 0;
 }
@@ -241,7 +246,7 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
   __shared__ int s_done[kBeamMost];
   __shared__ float s_rough_off[kBeamMost];
   __shared__ uint32_t s_most[kJoinThreads / 4];
-  __shared__ Candidate s_list[kJoinList + 4];
+  __shared__ Candidate s_list[kJoinList];
   __shared__ uint32_t s_rough[kJoinKept];
   __shared__ uint32_t s_bound;
   __shared__ int s_count, s_below[2][WAVES];
@@ -441,16 +446,16 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
     a.parents[at] = row0 + b;
     if (a.finished_out) a.finished_out[at] = s_done[b] || t == a.end_token;
   };
-  // in front: a larger score, or an equal one and the lower index
-  if (threadIdx.x < 4) s_list[count + threadIdx.x] = Candidate{0, ~0ull};   // (whole fours are compared)
-  __syncthreads();
-  for (int i = threadIdx.x; i < count; i += kJoinThreads) {
-    const Candidate x = s_list[i];
+  // in front: a larger score, or an equal one and the lower index (eight threads a candidate, each against every eighth)
+  for (int i0 = 0; i0 < count; i0 += kJoinThreads / 8) {
+    const int i = i0 + (int)threadIdx.x / 8;
+    const Candidate x = s_list[min(i, count - 1)];
     int rank = 0;
-    for (int k = 0; k < count; k += 4)
-#pragma unroll
-      for (int u = 0; u < 4; ++u) rank += (int)(s_list[k + u].key > x.key) | ((int)(s_list[k + u].key == x.key) & (int)(s_list[k + u].index < x.index));
-    if (rank < n) put(rank, double_of(x.key), x.index);
+#pragma unroll 4
+    for (int k = threadIdx.x & 7; k < count; k += 8)
+      rank += (int)(s_list[k].key > x.key) | ((int)(s_list[k].key == x.key) & (int)(s_list[k].index < x.index));
+    rank = sum_of_8(rank);
+    if (i < count && rank < n && (threadIdx.x & 7) == 0) put(rank, double_of(x.key), x.index);
   }
   if (count >= n) return;
   // Fewer candidates than asked for: the rest are the lowest indices whose score is -inf, found by looking (one wavefront, 64 indices at a time).
