@@ -8,8 +8,8 @@
 // What is compared are scores in double: rounded to float many candidates of a beam would be equal, and beams' sums meet there.  Exponentials are floats, a thread's sixteen or 32 are added
 // in float and everything behind that in double.
 //
-// Scan + join, kernel times: 4 rows of 2048 floats 4.6 + 4.4 us; 128 rows of 32000 bf16, 8 of 4 back: 7.1 + 7.3; 128 rows of 100003 floats (41 MB are read), 16 of 8 back: 14.8 + 8.5; 64 rows
-// of 32000 floats, 128 of 64 back: 12.6 + 22.  The scan of many rows is bound by memory and by the latency of one chunk (values, maximum, sum, bound, list: 6 us), the join by the latency of its
+// Scan + join, kernel times: 4 rows of 2048 floats 4.6 + 3.8 us; 128 rows of 32000 bf16, 8 of 4 back: 7.1 + 7.2; 128 rows of 100003 floats (41 MB are read), 16 of 8 back: 14.6 + 7.8; 64 rows
+// of 32000 floats, 128 of 64 back: 9.2 + 15.  The scan of many rows is bound by memory and by the latency of one chunk (values, maximum, sum, bound, list: 6 us), the join by the latency of its
 // dozen barriers.  Values in chunks of 4096 where all workgroups run at once, else of 8192: the 128 rows of 100003 took 19 us in 4096, more than one round, also with the next chunk's
 // values on their way.
 #include <type_traits>
@@ -232,29 +232,37 @@ __global__ __launch_bounds__(THREADS, EACH > 16 ? 6 : 4) void beam_scan_kernel(B
 
 constexpr int kJoinThreads = 1024;
 constexpr int kJoinList = 1024;
-constexpr int kJoinKept = 16384;  // candidates whose rough scores stay in LDS
+constexpr int kJoinKept = 4096;   // candidates that are looked at first
+constexpr int kJoinDeep = 12288;  // and behind these, of the lists that may have more; rough scores of both stay in LDS
 constexpr int kJoinFew = 128;    // so many are put in order without a look at which may count
 
-// A workgroup a group.  The n best of its beams' chunks' are found as in the scan, by the n-th largest of 256 maxima; where beams are so unlike that this lets many
-// more through than n, the bound is moved up by halves until few are left.  Then by counting what is in front.
+// A workgroup a group.  The n best of its beams' chunks' are found as in the scan, by the n-th largest of 256 maxima; where this lets many more through than n, the bound is moved up by halves
+// until few are left.  The lists' first places are looked at, and more of a list only where its last of these is not below the bound (64 rows, 128 back: 16384 candidates looked at 19.5 us,
+// 4096 and some 15; one beam with all the best of 128 over 128256 tokens: 169 and 40, both launches).  Then by counting what is in front.
 __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int is_bf16) {
   constexpr int WAVES = kJoinThreads / 64;
-  struct alignas(16) Candidate {
-    uint64_t key, index;   // of the score in double, 0: none; beam of the group * vocab + token
+  struct Candidate {
+    uint64_t key, index;   // of the score in double, 0: none; beam of the group << 32 | token
   };
   __shared__ double s_off[kBeamMost], s_base[kBeamMost];   // of a beam: the logarithm of its sum; its score
   __shared__ int s_done[kBeamMost];
   __shared__ float s_rough_off[kBeamMost];
   __shared__ uint32_t s_most[kJoinThreads / 4];
-  __shared__ Candidate s_list[kJoinList];
-  __shared__ uint32_t s_rough[kJoinKept];
+  __shared__ uint64_t s_key[kJoinList], s_index[kJoinList];
+  __shared__ uint32_t s_rough[kJoinKept + kJoinDeep];
+  __shared__ uint64_t s_found[kJoinKept];
   __shared__ uint32_t s_bound;
-  __shared__ int s_count, s_below[2][WAVES];
+  __shared__ uint16_t s_deep[kJoinKept];
+  __shared__ int s_count, s_n_deep, s_below[2][WAVES], s_digits[16];
   const int g = blockIdx.x, n = a.n_out, W = a.beams, row0 = g * W;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int lists = W * a.chunks, all = lists * n;
   const uint64_t* found = a.found + (size_t)g * all;   // the lists' first ones, then the second ones, ..
-  if (threadIdx.x == 0) s_count = 0;
+  if (threadIdx.x == 0) s_count = s_n_deep = 0;
+  const int places = min(n, kJoinKept / lists), kept = places ? places * lists : kJoinKept;   // (without whole places the first ones give a bound, and are looked at again)
+  uint64_t first[kJoinKept / kJoinThreads];   // (on their way while the sums are formed)
+#pragma unroll
+  for (int u = 0; u < kJoinKept / kJoinThreads; ++u) first[u] = (int)threadIdx.x + u * kJoinThreads < kept ? found[threadIdx.x + u * kJoinThreads] : 0;
   // The rows' sums: 2^p lanes a row, as many as it has chunks (in a fixed order of additions).
   float far = 0.0f;   // the largest magnitude of what is added to logits
   {
@@ -266,13 +274,13 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
       const int done = a.finished ? a.finished[row] : 0;
       const float base = a.scores[row];
       const double2* stats = a.stats + (size_t)row * a.chunks;
-      double2 first = make_double2(-INFINITY, 0.0);
-      if (c0 < a.chunks && !done) first = stats[c0];
-      float m = (float)first.x;   // (maxima are floats)
+      double2 own = stats[min(c0, a.chunks - 1)];
+      if (c0 >= a.chunks || done) own = make_double2(-INFINITY, 0.0);
+      float m = (float)own.x;   // (maxima are floats)
       if (!done)
         for (int k = c0 + 64; k < a.chunks; k += 64) m = fmaxf(m, (float)stats[k].x);
       for (int o = 1; o < 1 << p; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
-      double sum = first.y != 0.0 ? first.y * exp(first.x - m) : 0.0;   // (NaN stays)
+      double sum = own.y != 0.0 ? own.y * exp(own.x - m) : 0.0;   // (NaN stays)
       if (!done)
         for (int k = c0 + 64; k < a.chunks; k += 64) {
           const double2 s = stats[k];
@@ -290,7 +298,11 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
     }
   }
   __syncthreads();
-  for (int b = 0; b < W; ++b) far = fmaxf(far, fabsf(s_rough_off[b]));
+  {
+    uint32_t most_far = 0;
+    for (int b = lane; b < W; b += 64) most_far = max(most_far, __float_as_uint(fmaxf(fabsf(s_rough_off[b]), 0.0f)));   // (a NaN is 0)
+    far = __uint_as_float(wave_largest(most_far));
+  }
   // A thread's candidates are 1024 apart: the list goes round, the beam is a quotient by a product of 32 bits (exact: lists * chunks is below 2^32).
   const uint32_t by_chunks = a.chunks > 1 ? 0xffffffffu / (uint32_t)a.chunks + 1 : 0;
   auto beam_of = [&](int list) { return a.chunks > 1 ? (int)__umulhi((uint32_t)list, by_chunks) : list; };
@@ -305,10 +317,10 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
     Candidate r;
     if (s_done[b]) {
       s = first && list == b * a.chunks ? s_base[b] : -INFINITY;
-      r.index = (uint64_t)b * a.vocab + a.end_token;
+      r.index = (uint64_t)b << 32 | (uint32_t)a.end_token;
     } else {
       s = cc >> 32 ? s_base[b] + ((double)float_of((uint32_t)(cc >> 32)) - s_off[b]) : -INFINITY;
-      r.index = (uint64_t)b * a.vocab + (0xffffffffu - (uint32_t)cc);
+      r.index = (uint64_t)b << 32 | (0xffffffffu - (uint32_t)cc);
     }
     r.key = s - s == 0.0 ? key_of(s) : 0;   // what is not finite is none
     return r;
@@ -321,39 +333,18 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
     else f = cc >> 32 ? f + float_of((uint32_t)(cc >> 32)) : NAN;
     return f == f ? key_of(fminf(fmaxf(f, -3.4028235e38f), 3.4028235e38f)) : 0u;
   };
-  // Of the lists' first places, as many as fit, the rough scores are kept; what bound they give is one for all.  Behind them (the lists fall) are candidates only where a
-  // list's last kept place is one.
-  const int kept = min(all, kJoinKept), places = kept / lists;
+  // Of the lists' first places, as many as fit, the scores give a bound for all.  Behind them (the lists fall) are candidates only where a list's last place is not below it.
   uint32_t most = 0;
-  int list_behind = list0;   // the list of the thread's first candidate that is not kept
-  for (int i0 = threadIdx.x; i0 < kept; i0 += 4 * kJoinThreads) {
-    uint64_t c[4];
+  int list_of = list0;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) c[u] = i0 + u * kJoinThreads < kept ? found[i0 + u * kJoinThreads] : 0;
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (const int i = i0 + u * kJoinThreads; i < kept) {
-        const uint32_t k = rough(list_behind, c[u], i < lists);
-        s_rough[i] = k;
-        most = max(most, k);
-        list_behind = next_list(list_behind);
-      }
-  }
-  // use(rough score, its number, its list) of every kept candidate of this thread, and of those behind that are not below `bound`
-  auto each = [&](uint32_t bound, bool behind, auto&& use) {
-    int list = list0;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < kept; i += kJoinThreads) {
-      use(s_rough[i], i, list);
-      list = next_list(list);
+  for (int u = 0; u < kJoinKept / kJoinThreads; ++u)
+    if (const int i = (int)threadIdx.x + u * kJoinThreads; i < kept) {
+      const uint32_t k = rough(list_of, first[u], i < lists);
+      s_rough[i] = k;
+      s_found[i] = first[u];
+      most = max(most, k);
+      list_of = next_list(list_of);
     }
-    if (!behind) return;
-    list = list_behind;
-    for (int i = kept + (int)threadIdx.x; i < all; i += kJoinThreads) {
-      if (places == 0 || s_rough[(places - 1) * lists + list] >= bound) use(rough(list, found[i], i < lists), i, list);
-      list = next_list(list);
-    }
-  };
   auto block_sum = [&](int mine, int turn) {   // (two rows of LDS in turn: one barrier a sum)
     mine = wave_total(mine);
     if (lane == 0) s_below[turn & 1][wave] = mine;
@@ -363,7 +354,24 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
     for (int i = 0; i < WAVES; ++i) sum += s_below[turn & 1][i];
     return sum;
   };
-  uint32_t bound = 1;
+  uint32_t bound = 1, above = 0xffffffffu;
+  // The bound moved up by halves until few of these are at it or above (n at least are, or the bound is 1; none from `above` on).
+  auto move_up = [&](int from, int to, uint32_t above) {
+    for (int turn = 0;; ++turn) {
+      uint32_t middle = bound;
+      if (turn) {
+        if (above - bound < 2) break;
+        middle = bound + (above - bound) / 2;
+      }
+      int mine = 0;
+#pragma unroll 4
+      for (int i = from + (int)threadIdx.x; i < to; i += kJoinThreads) mine += s_rough[i] >= middle;
+      const int there = block_sum(mine, turn);
+      if (there >= n || turn == 0) bound = middle;
+      else above = middle;
+      if (there <= max(2 * n, 64) && (there >= n || turn == 0)) break;
+    }
+  };
   if (all > kJoinFew) {
     // four threads' together: quad_perm [1,0,3,2], [2,3,0,1]
     most = max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0xB1, 0xf, 0xf, true));
@@ -377,85 +385,135 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
       const uint32_t b = wave_bound<4, 9>(key, n);
       if (lane == 0) s_bound = b;
     }
-    uint32_t above = wave_largest(max(max(key[0], key[1]), max(key[2], key[3]))) + 1;   // nothing is here or above
+    above = wave_largest(max(max(key[0], key[1]), max(key[2], key[3]))) + 1;   // nothing is here or above
     __syncthreads();
     bound = s_bound;
-    for (int turn = 0;; ++turn) {   // n at least are at the bound or above, fewer from `above` on
-      uint32_t middle = bound;
-      if (turn) {
-        if (above - bound < 2) break;
-        middle = bound + (above - bound) / 2;
+    move_up(0, kept, above);
+  }
+  auto lowered = [&](uint32_t at) -> uint32_t {   // whose score may be at the bound's
+    if (at <= 1) return 1;
+    const float f = float_of(at), least = f - (fabsf(f) + 2.0f * far) * 0x1p-20f;
+    return least > -3.4028235e38f ? key_of(least) : 1;
+  };
+  const int per = n - places;   // candidates of a list behind those kept
+  int deep = 0, held = 0;       // lists that may have some that count; of theirs, those whose rough scores are kept as well, all lists' next places one after the other
+  if (per > 0) {
+    const uint32_t least = lowered(bound);
+    deep = lists;
+    if (places) {
+      for (int l = threadIdx.x; l < lists; l += kJoinThreads)
+        if (s_rough[(places - 1) * lists + l] >= least) s_deep[atomicAdd(&s_n_deep, 1)] = (uint16_t)l;
+      __syncthreads();
+      deep = s_n_deep;
+    }
+    if (deep) {
+      held = min(per, kJoinDeep / deep) * deep;
+#pragma unroll 4
+      for (int q = threadIdx.x; q < held; q += kJoinThreads) {
+        const int to = q / deep, d = q - to * deep, l = places ? s_deep[d] : d;
+        s_rough[kept + q] = rough(l, found[(size_t)(places + to) * lists + l], places + to == 0);
       }
-      int mine = 0;
-      each(0, false, [&](uint32_t k, int, int) { mine += k >= middle; });
-      const int there = block_sum(mine, turn);
-      if (there >= n || turn == 0) bound = middle;
-      else above = middle;
-      if (there <= max(2 * n, 64) && (there >= n || turn == 0)) break;
+      __syncthreads();
+      move_up(places ? 0 : kept, kept + held, places ? above : 0xffffffffu);
     }
   }
-  if (bound > 1) {   // whose score may be at the bound's
-    const float f = float_of(bound), least = f - (fabsf(f) + 2.0f * far) * 0x1p-20f;
-    bound = least > -3.4028235e38f ? key_of(least) : 1;
-  }
+  bound = lowered(bound);
+  const int from_kept = places * lists;
+  // use(candidate) of all that may count (one loop: its code is what has to be fetched)
+  auto each = [&](auto&& use) {
+    int list = list0;
+#pragma unroll 1
+    for (int i = threadIdx.x; i < from_kept + deep * per; i += kJoinThreads) {
+      uint32_t k = 0;
+      uint64_t c = 0;
+      int l = list;
+      bool its_first = i < lists;
+      if (i < from_kept) {
+        k = s_rough[i];
+        c = s_found[i];
+      } else {
+        const int q = i - from_kept, to = q / deep, d = q - to * deep;
+        l = places ? s_deep[d] : d;
+        its_first = places + to == 0;
+        if (q < held) k = s_rough[kept + q];
+        if (q < held ? k >= bound : held == 0 || s_rough[kept + held - deep + d] >= bound) c = found[(size_t)(places + to) * lists + l];
+        if (q >= held) k = rough(l, c, its_first);
+      }
+      if (k >= bound) use(candidate(l, c, its_first));   // (k of none is 0)
+      list = next_list(list);
+    }
+  };
   auto put_by = [&](const Candidate& x) {
     if (!x.key) return;
     const int at = atomicAdd(&s_count, 1);
-    if (at < kJoinList) s_list[at] = x;
+    if (at < kJoinList) {
+      s_key[at] = x.key;
+      s_index[at] = x.index;
+    }
   };
-  each(bound, true, [&](uint32_t k, int i, int list) {
-    if (k >= bound) put_by(candidate(list, found[i], i < lists));   // (k of none is 0)
-  });
+  each(put_by);
   __syncthreads();
   int count = s_count;
-  if (count > kJoinList) {   // as many equal scores: the n-th bit by bit, then its index
-    int turn = 0;
-    auto block_count = [&](auto&& test) {
-      int mine = 0;
-      each(bound, true, [&](uint32_t k, int i, int list) {
-        if (k >= bound) mine += test(candidate(list, found[i], i < lists));
+  if (count > kJoinList) {   // so many (nearly) equal scores: the n-th four bits at a time, then of those like it the last that is needed
+    int need = n;
+    auto digit_of = [&](auto&& test, int shift, bool down) {   // test(x, bits): one that counts, and its bits
+      if (threadIdx.x < 16) s_digits[threadIdx.x] = 0;
+      __syncthreads();
+      int mine[16];
+#pragma unroll
+      for (int d = 0; d < 16; ++d) mine[d] = 0;
+      each([&](const Candidate& x) {
+        uint64_t bits;
+        const bool counts = x.key && test(x, bits);
+#pragma unroll
+        for (int d = 0; d < 16; ++d) mine[d] += counts && (int)(bits >> shift & 15) == d;
       });
-      return block_sum(mine, turn++);
+#pragma unroll
+      for (int d = 0; d < 16; ++d) {
+        const int sum = wave_total(mine[d]);
+        if (lane == 0 && sum) atomicAdd(&s_digits[d], sum);
+      }
+      __syncthreads();
+      int digit = down ? 15 : 0;
+      for (int at; need > (at = s_digits[digit]) && digit != (down ? 0 : 15); digit += down ? -1 : 1) need -= at;
+      __syncthreads();   // (they have been read)
+      return (uint64_t)digit << shift;
     };
-    __syncthreads();   // (the sums' rows may still be read)
-    uint64_t from = 0;
-    for (int bit = 63; bit >= 0; --bit) {
-      const uint64_t f = from | 1ull << bit;
-      if (block_count([&](const Candidate& x) { return x.key >= f; }) >= n) from = f;
-    }
-    uint64_t up_to = 0;   // the least index with which n are in front of or at (from, index)
-    for (int bit = 39; bit >= 0; --bit) {
-      const uint64_t f = up_to | 1ull << bit;
-      if (block_count([&](const Candidate& x) { return x.key > from || (x.key == from && x.index < f); }) < n) up_to = f;
-    }
+    uint64_t from = 0, up_to = 0;
+    for (int shift = 60; shift >= 0; shift -= 4)
+      from |= digit_of([&](const Candidate& x, uint64_t& bits) { bits = x.key; return shift == 60 || x.key >> (shift + 4) == from >> (shift + 4); }, shift, true);
+    for (int shift = 36; shift >= 0; shift -= 4)
+      up_to |= digit_of([&](const Candidate& x, uint64_t& bits) { bits = x.index; return x.key == from && x.index >> (shift + 4) == up_to >> (shift + 4); }, shift, false);
     if (threadIdx.x == 0) s_count = 0;
     __syncthreads();
-    each(bound, true, [&](uint32_t k, int i, int list) {
-      if (k < bound) return;
-      const Candidate x = candidate(list, found[i], i < lists);
+    each([&](const Candidate& x) {
       if (x.key > from || (x.key == from && x.index <= up_to)) put_by(x);
     });
     __syncthreads();
     count = min(s_count, kJoinList);
   }
-  auto put = [&](int rank, double s, uint64_t index) {
-    const int b = (int)(index / a.vocab), t = (int)(index - (uint64_t)b * a.vocab);
+  auto put = [&](int rank, double s, int b, int t) {
     const size_t at = (size_t)g * n + rank;
     a.scores_out[at] = (float)s;
     a.tokens[at] = t;
     a.parents[at] = row0 + b;
     if (a.finished_out) a.finished_out[at] = s_done[b] || t == a.end_token;
   };
-  // in front: a larger score, or an equal one and the lower index (eight threads a candidate, each against every eighth)
+  // in front: a larger score, or an equal one and the lower index (eight threads a candidate, each against every eighth; the indices are looked at only where scores are equal)
   for (int i0 = 0; i0 < count; i0 += kJoinThreads / 8) {
     const int i = i0 + (int)threadIdx.x / 8;
-    const Candidate x = s_list[min(i, count - 1)];
-    int rank = 0;
+    const uint64_t key = s_key[min(i, count - 1)], index = s_index[min(i, count - 1)];
+    int rank = 0, like = 0;
 #pragma unroll 4
-    for (int k = threadIdx.x & 7; k < count; k += 8)
-      rank += (int)(s_list[k].key > x.key) | ((int)(s_list[k].key == x.key) & (int)(s_list[k].index < x.index));
+    for (int k = threadIdx.x & 7; k < count; k += 8) {
+      const uint64_t other = s_key[k];
+      rank += other > key;
+      like += other == key;
+    }
+    if (__any(sum_of_8(like) > 1))
+      for (int k = threadIdx.x & 7; k < count; k += 8) rank += (int)(s_key[k] == key) & (int)(s_index[k] < index);
     rank = sum_of_8(rank);
-    if (i < count && rank < n && (threadIdx.x & 7) == 0) put(rank, double_of(x.key), x.index);
+    if (i < count && rank < n && (threadIdx.x & 7) == 0) put(rank, double_of(key), (int)(index >> 32), (int)(uint32_t)index);
   }
   if (count >= n) return;
   // Fewer candidates than asked for: the rest are the lowest indices whose score is -inf, found by looking (one wavefront, 64 indices at a time).
@@ -463,9 +521,9 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
   int rank = count;
   for (uint64_t i0 = 0; rank < n && i0 < (uint64_t)W * a.vocab; i0 += 64) {
     const uint64_t index = i0 + lane;
-    bool none = index < (uint64_t)W * a.vocab;
+    const int b = (int)(index / a.vocab), t = (int)(index - (uint64_t)b * a.vocab);
+    bool none = b < W;
     if (none) {
-      const int b = (int)(index / a.vocab), t = (int)(index - (uint64_t)b * a.vocab);
       if (s_done[b]) {
         none = t != a.end_token || !(s_base[b] - s_base[b] == 0.0);
       } else {
@@ -477,7 +535,7 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
     }
     const uint64_t bal = __ballot(none);
     const int mine = rank + __popcll(bal & ((1ull << lane) - 1));
-    if (none && mine < n) put(mine, -INFINITY, index);
+    if (none && mine < n) put(mine, -INFINITY, b, t);
     rank += __popcll(bal);
   }
 }

@@ -143,6 +143,25 @@ def test_unlike_beams(beams, vocab, n_out, spread):
     check(logits[:, :vocab - 1].contiguous(), -torch.arange(beams).float() * spread, beams, n_out, finished, 7)
 
 
+@pytest.mark.parametrize("beams,vocab,n_out,dtype", [(128, 270001, 32, F32), (128, 128256, 20, BF), (125, 540001, 40, BF), (128, 794625, 32, BF)])
+@pytest.mark.parametrize("spread", [0.0, 40.0])
+def test_more_lists_than_are_looked_at_first(beams, vocab, n_out, dtype, spread):
+    """Vocabularies whose chunks, over all beams, are up to 12416 lists; of beams that are alike, and of one in front."""
+    g = torch.Generator(device="cuda").manual_seed(vocab)
+    logits = (torch.randn((beams, vocab), generator=g, device="cuda") * 3).to(dtype)
+    logits[:, ::7919] += torch.rand((beams, len(range(0, vocab, 7919))), generator=g, device="cuda").to(dtype)
+    scores = -torch.linspace(0, 1, beams) * spread
+    t, p, s, _ = run(logits, scores, beams, n_out)
+    every = logits.double()
+    every = every - torch.logsumexp(every, 1, keepdim=True) + scores.cuda().double()[:, None]
+    # of equal scores the lower index first: bf16 logits meet within a beam
+    least = torch.topk(every.flatten(), n_out)[0][-1]
+    at = torch.nonzero(every.flatten() >= least).flatten()
+    order = sorted(at.tolist(), key=lambda i: (-float(every.flatten()[i]), i))[:n_out]
+    del every
+    assert [b * vocab + x for b, x in zip(p, t)] == order
+
+
 def test_a_workspace_of_larger_sizes_and_repeats():
     g = gen(11)
     ws = B.BeamWorkspace(9, 40, 20000, 128)
