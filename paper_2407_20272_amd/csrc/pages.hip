@@ -2,9 +2,9 @@
 // counts of the references to every block.  Nothing here waits for the host.
 //
 // All but the copies are bound by latency: a launch and three or four loads that wait for each other.  Kernel times: 4 beams of one prompt forked 2.2 us, grown 5.5, their last blocks copied 4.2,
-// shared blocks found 4.0, released 2.3; 32 beams of 8 prompts 3.0, 7.1, 16 (28 blocks of 2.1 MB, 117 MB read
-// and written, in part from the last-level cache), 5.7, 2.3; a pool of 2700 blocks packed 9.0, and 650 blocks of 0.26 MB copied 74
-// (341 MB, 4.6 TB/s; a large copy makes 4.75).  Growing and packing look through small pools in one workgroup (4 rows grown: 5.5 us, in two launches 5.6 + 3.9).
+// shared blocks found 3.9, released 2.1; 32 beams of 8 prompts 3.4, 7.1, 15 (28 blocks of 2.1 MB, 117 MB read
+// and written, in part from the last-level cache), 5.6, 2.5; a pool of 2700 blocks packed 9.2, and 650 blocks of 0.26 MB copied 70 to 75
+// (341 MB, 4.6 to 4.9 TB/s; a large copy makes 4.75).  Growing and packing look through small pools in one workgroup (4 rows grown: 5.5 us, in two launches 5.6 + 3.9).
 #include "beams.h"
 
 namespace ee {
