@@ -462,7 +462,8 @@ typedef struct ee_prefix_groups {
  * the same result as without groups; shared blocks are read once for up to 48 columns (a row and a query head; 32 of EE_FP32) instead of once a row.  A row shorter than its group's shared
  * blocks attends its own positions all the same; one with context_lens[m] < 0 attends nothing: its result is 0.  Rows of no group are left as they were.  row_table as in
  * ee_paged_attention_decode (shared blocks are then those of the rows' sequences).
- * q and out dev [rows][n_heads][head_dim] float, 16-byte aligned, not overlapping; pools start on 16 bytes.  Products and sums are float in effect.
+ * q and out dev [rows][n_heads][head_dim] float, 16-byte aligned, not overlapping; pools start on 16 bytes.  Products and sums are float in effect; an infinite value
+ * among the q, K or V that a row attends may make its result NaN.
  * workspace: 256-byte aligned, ee_paged_attention_shared_bytes for the call's sizes or larger ones, no initialisation, dead between calls. */
 size_t ee_paged_attention_shared_bytes(const ee_model_desc* desc, int32_t n_heads, int32_t max_batch, int32_t max_groups, int32_t max_context);
 int ee_paged_attention_shared(const ee_model_desc* desc, const ee_kv_cache* cache, int32_t layer, int32_t n_heads, const float* q, const ee_batch* batch,

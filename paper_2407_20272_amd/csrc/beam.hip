@@ -9,7 +9,7 @@
 // in float and everything behind that in double.
 //
 // Scan + join, kernel times: 4 rows of 2048 floats 4.6 + 3.8 us; 128 rows of 32000 bf16, 8 of 4 back: 7.1 + 7.2; 128 rows of 100003 floats (41 MB are read), 16 of 8 back: 14.7 + 8.1; 64 rows
-// of 32000 floats, 128 of 64 back: 9.2 + 15.  The scan of many rows is bound by memory and by the latency of one chunk (values, maximum, sum, bound, list: 6 us), the join by the latency of its
+// of 32000 floats, 128 of 64 back: 9.2 + 11.  The scan of many rows is bound by memory and by the latency of one chunk (values, maximum, sum, bound, list: 6 us), the join by the latency of its
 // dozen barriers.  Values in chunks of 4096 where all workgroups run at once, else of 8192: the 128 rows of 100003 took 19 us in 4096, more than one round, also with the next chunk's
 // values on their way.
 #include <type_traits>
@@ -64,7 +64,7 @@ __device__ inline uint32_t wave_largest(uint32_t v) {
   with(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
   return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
-__device__ inline int wave_total(int v) {
+__device__ inline int wave_upto(int v) {   // over the lanes up to each
   auto add = [&](auto ctrl, auto rows) { v += __builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, decltype(rows)::value, 0xf, false); };
   add(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});
   add(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
@@ -72,8 +72,9 @@ __device__ inline int wave_total(int v) {
   add(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
   add(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});
   add(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
-  return __builtin_amdgcn_readlane(v, 63);
+  return v;
 }
+__device__ inline int wave_total(int v) { return __builtin_amdgcn_readlane(wave_upto(v), 63); }
 // The sum over eight neighbouring lanes: all of them have it.
 __device__ inline int sum_of_8(int v) {
   v += __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xf, 0xf, true);    // quad_perm [1,0,3,2], [2,3,0,1], row_half_mirror
@@ -236,9 +237,9 @@ constexpr int kJoinKept = 4096;   // candidates that are looked at first
 constexpr int kJoinDeep = 12288;  // and behind these, of the lists that may have more; rough scores of both stay in LDS
 constexpr int kJoinFew = 128;    // so many are put in order without a look at which may count
 
-// A workgroup a group.  The n best of its beams' chunks' are found as in the scan, by the n-th largest of 256 maxima; where this lets many more through than n, the bound is moved up by halves
-// until few are left.  The lists' first places are looked at, and more of a list only where its last of these is not below the bound (64 rows, 128 back: 16384 candidates looked at 19.5 us,
-// 4096 and some 15; one beam with all the best of 128 over 128256 tokens: 169 and 40, both launches).  Then by counting what is in front.
+// A workgroup a group.  The n best of its beams' chunks' are found as in the scan, by the n-th largest of 256 maxima; where this lets many more through than n, the bound is moved up by counts
+// of 256 parts until few are left.  The lists' first places are looked at, and more of a list only where its last of these is not below the bound (64 rows, 128 back: 16384 candidates looked at 19.5 us,
+// 4096 and some 11; both launches, one beam with all the best of 128 over 128256 tokens: 169 and 40; 64 beams of 32000 tokens, all but one at -1e9: 36).  Then by counting what is in front.
 __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int is_bf16) {
   constexpr int WAVES = kJoinThreads / 64;
   struct Candidate {
@@ -246,14 +247,16 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
   };
   __shared__ double s_off[kBeamMost], s_base[kBeamMost];   // of a beam: the logarithm of its sum; its score
   __shared__ int s_done[kBeamMost];
-  __shared__ float s_rough_off[kBeamMost];
+  __shared__ float s_rough_off[kBeamMost], s_best[kBeamMost];   // what is added to its logits, and its best score, as floats
   __shared__ uint32_t s_most[kJoinThreads / 4];
   __shared__ uint64_t s_key[kJoinList], s_index[kJoinList];
   __shared__ uint32_t s_rough[kJoinKept + kJoinDeep];
   __shared__ uint64_t s_found[kJoinKept];
   __shared__ uint32_t s_bound;
   __shared__ uint16_t s_deep[kJoinKept];
-  __shared__ int s_count, s_n_deep, s_below[2][WAVES], s_digits[16];
+  __shared__ int s_count, s_n_deep, s_below[WAVES], s_digits[16];
+  __shared__ __align__(16) int s_bins[2][256];
+  __shared__ unsigned long long s_span[2];
   const int g = blockIdx.x, n = a.n_out, W = a.beams, row0 = g * W;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int lists = W * a.chunks, all = lists * n;
@@ -264,7 +267,6 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
 #pragma unroll
   for (int u = 0; u < kJoinKept / kJoinThreads; ++u) first[u] = (int)threadIdx.x + u * kJoinThreads < kept ? found[threadIdx.x + u * kJoinThreads] : 0;
   // The rows' sums: 2^p lanes a row, as many as it has chunks (in a fixed order of additions).
-  float far = 0.0f;   // the largest magnitude of what is added to logits
   {
     int p = 0;
     while (p < 6 && 1 << p < a.chunks) ++p;
@@ -294,10 +296,12 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
         s_done[b] = done != 0;
         // what is not finite stands for rows that have no candidates; what no float is for the largest
         s_rough_off[b] = to - to == 0.0 ? fminf(fmaxf((float)to, -3.4028235e38f), 3.4028235e38f) : NAN;
+        s_best[b] = done ? s_rough_off[b] : fminf(fmaxf((float)(to + m), -3.4028235e38f), 3.4028235e38f);
       }
     }
   }
   __syncthreads();
+  float far = 0.0f;   // the largest magnitude of what is added to logits
   {
     uint32_t most_far = 0;
     for (int b = lane; b < W; b += 64) most_far = max(most_far, __float_as_uint(fmaxf(fabsf(s_rough_off[b]), 0.0f)));   // (a NaN is 0)
@@ -345,31 +349,47 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
       most = max(most, k);
       list_of = next_list(list_of);
     }
-  auto block_sum = [&](int mine, int turn) {   // (two rows of LDS in turn: one barrier a sum)
-    mine = wave_total(mine);
-    if (lane == 0) s_below[turn & 1][wave] = mine;
-    __syncthreads();
-    int sum = 0;
-#pragma unroll
-    for (int i = 0; i < WAVES; ++i) sum += s_below[turn & 1][i];
-    return sum;
-  };
-  uint32_t bound = 1, above = 0xffffffffu;
-  // The bound moved up by halves until few of these are at it or above (n at least are, or the bound is 1; none from `above` on).
+  uint32_t bound = 1, above = 0;
+  // The bound moved up until few of these are at it or above (n at least are, or it stays; none from `above` on): counted, then 256 parts of what is between bound and `above` at a time.
   auto move_up = [&](int from, int to, uint32_t above) {
-    for (int turn = 0;; ++turn) {
-      uint32_t middle = bound;
-      if (turn) {
-        if (above - bound < 2) break;
-        middle = bound + (above - bound) / 2;
-      }
-      int mine = 0;
+    int mine = 0;
 #pragma unroll 4
-      for (int i = from + (int)threadIdx.x; i < to; i += kJoinThreads) mine += s_rough[i] >= middle;
-      const int there = block_sum(mine, turn);
-      if (there >= n || turn == 0) bound = middle;
-      else above = middle;
-      if (there <= max(2 * n, 64) && (there >= n || turn == 0)) break;
+    for (int i = from + (int)threadIdx.x; i < to; i += kJoinThreads) mine += s_rough[i] >= bound;
+    mine = wave_total(mine);
+    if (lane == 0) s_below[wave] = mine;
+    if (threadIdx.x < 512) (&s_bins[0][0])[threadIdx.x] = 0;
+    __syncthreads();
+    int there = 0;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) there += s_below[i];
+    for (int turn = 0; there > max(2 * n, 64) && above - bound > 1; ++turn) {
+      const int shift = max(0, 24 - __builtin_clz(above - 1 - bound));
+      int* bins = s_bins[turn & 1];
+      // (the highest part first; those in the lowest are not counted: n are there or above)
+#pragma unroll 4
+      for (int i = from + (int)threadIdx.x; i < to; i += kJoinThreads) {
+        const uint32_t k = s_rough[i];
+        if (k > bound && (k - bound) >> shift) atomicAdd(&bins[255 - ((k - bound) >> shift)], 1);
+      }
+      __syncthreads();
+      const int4 four = *reinterpret_cast<const int4*>(&bins[lane * 4]);
+      const int upto = wave_upto(four.x + four.y + four.z + four.w);
+      const unsigned long long enough = __ballot(upto >= n);
+      uint32_t part = 0;
+      if (enough) {
+        const int at = __builtin_ctzll(enough);
+        int sum = __builtin_amdgcn_readlane(upto - four.x - four.y - four.z - four.w, at), e = 0;
+        for (; e < 4; ++e) {
+          sum += e == 0 ? __builtin_amdgcn_readlane(four.x, at) : e == 1 ? __builtin_amdgcn_readlane(four.y, at) : e == 2 ? __builtin_amdgcn_readlane(four.z, at) : __builtin_amdgcn_readlane(four.w, at);
+          if (sum >= n) break;
+        }
+        part = 255 - (at * 4 + e);
+        there = sum;
+      }
+      bound += part << shift;
+      if (above - bound > 1u << shift) above = bound + (1u << shift);   // (fewer than n are there)
+      if (threadIdx.x < 256) s_bins[(turn + 1) & 1][threadIdx.x] = 0;   // (read a turn ago)
+      __syncthreads();
     }
   };
   if (all > kJoinFew) {
@@ -390,22 +410,37 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
     bound = s_bound;
     move_up(0, kept, above);
   }
-  auto lowered = [&](uint32_t at) -> uint32_t {   // whose score may be at the bound's
+  // Whose score may be at the bound's: rough scores are off by less than 2^-22 of themselves and of what was added to the logits.  Where that is much, it is looked at of which beams: a search begins
+  // with scores like -1e9 for all beams but one, and a margin for these would let all of the one's candidates through.
+  auto lowered = [&](uint32_t at) -> uint32_t {
     if (at <= 1) return 1;
-    const float f = float_of(at), least = f - (fabsf(f) + 2.0f * far) * 0x1p-20f;
+    const float f = float_of(at);
+    float least = far > 512.0f ? f : f - (fabsf(f) * 0x1p-20f + far * 0x1p-19f);
+    for (int turn = 0; far > 512.0f && turn < 2; ++turn) {   // beams that reach the bound; then those that reach what these leave of it
+      uint32_t most_far = 0;
+      for (int b = lane; b < W; b += 64) {
+        const float off = fabsf(s_rough_off[b]);
+        if (s_best[b] + (fabsf(f) * 0x1p-20f + off * 0x1p-19f) >= least) most_far = max(most_far, __float_as_uint(off));
+      }
+      least = f - (fabsf(f) * 0x1p-20f + __uint_as_float(wave_largest(most_far)) * 0x1p-19f);
+    }
     return least > -3.4028235e38f ? key_of(least) : 1;
   };
+  // Deeper: first the lists whose last place is above the bound, as many of their next places as fit, all lists' one after the other.  Their candidates count for the bound as well; then
+  // the lists that it leaves (those whose last place is like the first bound: of beams far below, floats are alike).
   const int per = n - places;   // candidates of a list behind those kept
-  int deep = 0, held = 0;       // lists that may have some that count; of theirs, those whose rough scores are kept as well, all lists' next places one after the other
+  int deep = 0, held = 0, late = 0;
   if (per > 0) {
-    const uint32_t least = lowered(bound);
-    deep = lists;
-    if (places) {
+    auto gather = [&](auto&& test) {
       for (int l = threadIdx.x; l < lists; l += kJoinThreads)
-        if (s_rough[(places - 1) * lists + l] >= least) s_deep[atomicAdd(&s_n_deep, 1)] = (uint16_t)l;
+        if (test(s_rough[(places - 1) * lists + l])) s_deep[atomicAdd(&s_n_deep, 1)] = (uint16_t)l;
       __syncthreads();
-      deep = s_n_deep;
-    }
+      const int there = s_n_deep;
+      __syncthreads();   // (it has been read)
+      return there;
+    };
+    const uint32_t first_bound = bound;
+    deep = places ? gather([&](uint32_t k) { return k > first_bound; }) : lists;
     if (deep) {
       held = min(per, kJoinDeep / deep) * deep;
 #pragma unroll 4
@@ -414,16 +449,19 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
         s_rough[kept + q] = rough(l, found[(size_t)(places + to) * lists + l], places + to == 0);
       }
       __syncthreads();
-      move_up(places ? 0 : kept, kept + held, places ? above : 0xffffffffu);
+      move_up(places ? 0 : kept, kept + held, places ? above : ~(kLowestKey - 1));   // (of the highest float, and one)
     }
+    bound = lowered(bound);
+    if (places) late = gather([&](uint32_t k) { return k <= first_bound && k >= bound; }) - deep;
+  } else {
+    bound = lowered(bound);
   }
-  bound = lowered(bound);
-  const int from_kept = places * lists;
+  const int from_kept = places * lists, from_deep = from_kept + deep * per;
   // use(candidate) of all that may count (one loop: its code is what has to be fetched)
   auto each = [&](auto&& use) {
     int list = list0;
 #pragma unroll 1
-    for (int i = threadIdx.x; i < from_kept + deep * per; i += kJoinThreads) {
+    for (int i = threadIdx.x; i < from_deep + late * per; i += kJoinThreads) {
       uint32_t k = 0;
       uint64_t c = 0;
       int l = list;
@@ -432,12 +470,14 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
         k = s_rough[i];
         c = s_found[i];
       } else {
-        const int q = i - from_kept, to = q / deep, d = q - to * deep;
-        l = places ? s_deep[d] : d;
+        const bool of_deep = i < from_deep;
+        const int q = of_deep ? i - from_kept : i - from_deep, many = of_deep ? deep : late, to = q / many, d = q - to * many;
+        l = places ? s_deep[of_deep ? d : deep + d] : d;
         its_first = places + to == 0;
-        if (q < held) k = s_rough[kept + q];
-        if (q < held ? k >= bound : held == 0 || s_rough[kept + held - deep + d] >= bound) c = found[(size_t)(places + to) * lists + l];
-        if (q >= held) k = rough(l, c, its_first);
+        const bool kept_here = of_deep && q < held;
+        if (kept_here) k = s_rough[kept + q];
+        if (kept_here ? k >= bound : !of_deep || held == 0 || s_rough[kept + held - deep + d] >= bound) c = found[(size_t)(places + to) * lists + l];
+        if (!kept_here) k = rough(l, c, its_first);
       }
       if (k >= bound) use(candidate(l, c, its_first));   // (k of none is 0)
       list = next_list(list);
@@ -456,34 +496,54 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
   int count = s_count;
   if (count > kJoinList) {   // so many (nearly) equal scores: the n-th four bits at a time, then of those like it the last that is needed
     int need = n;
-    auto digit_of = [&](auto&& test, int shift, bool down) {   // test(x, bits): one that counts, and its bits
-      if (threadIdx.x < 16) s_digits[threadIdx.x] = 0;
-      __syncthreads();
-      int mine[16];
-#pragma unroll
-      for (int d = 0; d < 16; ++d) mine[d] = 0;
-      each([&](const Candidate& x) {
-        uint64_t bits;
-        const bool counts = x.key && test(x, bits);
-#pragma unroll
-        for (int d = 0; d < 16; ++d) mine[d] += counts && (int)(bits >> shift & 15) == d;
-      });
-#pragma unroll
-      for (int d = 0; d < 16; ++d) {
-        const int sum = wave_total(mine[d]);
-        if (lane == 0 && sum) atomicAdd(&s_digits[d], sum);
+    auto nth = [&](auto&& part, bool down) {   // of the part(x, bits) that are asked for, from above or below; what all have in common is seen at once
+      if (threadIdx.x == 0) {
+        s_span[0] = ~0ull;
+        s_span[1] = 0;
       }
       __syncthreads();
-      int digit = down ? 15 : 0;
-      for (int at; need > (at = s_digits[digit]) && digit != (down ? 0 : 15); digit += down ? -1 : 1) need -= at;
-      __syncthreads();   // (they have been read)
-      return (uint64_t)digit << shift;
+      uint64_t lo = ~0ull, hi = 0;
+      each([&](const Candidate& x) {
+        uint64_t bits;
+        if (!x.key || !part(x, bits)) return;
+        lo = min(lo, bits);
+        hi = max(hi, bits);
+      });
+      atomicMin(&s_span[0], (unsigned long long)lo);
+      atomicMax(&s_span[1], (unsigned long long)hi);
+      __syncthreads();
+      lo = s_span[0];
+      hi = s_span[1];
+      int shift = lo == hi ? -4 : (63 - __builtin_clzll(lo ^ hi)) & ~3;
+      uint64_t at = lo == hi ? hi : hi & ~(((1ull << shift) << 4) - 1);
+      for (; shift >= 0; shift -= 4) {
+        if (threadIdx.x < 16) s_digits[threadIdx.x] = 0;
+        __syncthreads();
+        int mine[16];
+#pragma unroll
+        for (int d = 0; d < 16; ++d) mine[d] = 0;
+        each([&](const Candidate& x) {
+          uint64_t bits;
+          const bool counts = x.key && part(x, bits) && bits >> shift >> 4 == at >> shift >> 4;
+#pragma unroll
+          for (int d = 0; d < 16; ++d) mine[d] += counts && (int)(bits >> shift & 15) == d;
+        });
+#pragma unroll
+        for (int d = 0; d < 16; ++d) {
+          const int sum = wave_total(mine[d]);
+          if (lane == 0 && sum) atomicAdd(&s_digits[d], sum);
+        }
+        __syncthreads();
+        int digit = down ? 15 : 0;
+        for (int there; need > (there = s_digits[digit]) && digit != (down ? 0 : 15); digit += down ? -1 : 1) need -= there;
+        at |= (uint64_t)digit << shift;
+        __syncthreads();   // (they have been read)
+      }
+      __syncthreads();
+      return at;
     };
-    uint64_t from = 0, up_to = 0;
-    for (int shift = 60; shift >= 0; shift -= 4)
-      from |= digit_of([&](const Candidate& x, uint64_t& bits) { bits = x.key; return shift == 60 || x.key >> (shift + 4) == from >> (shift + 4); }, shift, true);
-    for (int shift = 36; shift >= 0; shift -= 4)
-      up_to |= digit_of([&](const Candidate& x, uint64_t& bits) { bits = x.index; return x.key == from && x.index >> (shift + 4) == up_to >> (shift + 4); }, shift, false);
+    const uint64_t from = nth([&](const Candidate& x, uint64_t& bits) { bits = x.key; return true; }, true);
+    const uint64_t up_to = nth([&](const Candidate& x, uint64_t& bits) { bits = x.index; return x.key == from; }, false);
     if (threadIdx.x == 0) s_count = 0;
     __syncthreads();
     each([&](const Candidate& x) {

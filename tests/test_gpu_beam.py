@@ -143,6 +143,17 @@ def test_unlike_beams(beams, vocab, n_out, spread):
     check(logits[:, :vocab - 1].contiguous(), -torch.arange(beams).float() * spread, beams, n_out, finished, 7)
 
 
+@pytest.mark.parametrize("beams,vocab,n_out", [(4, 2048, 4), (4, 32000, 8), (64, 32000, 128), (128, 128256, 128)])
+@pytest.mark.parametrize("others", [-1e9, -3e38, -math.inf])
+def test_a_first_step(beams, vocab, n_out, others):
+    """All beams of a group alike, and only the first of them counts."""
+    g = gen(beams + vocab)
+    logits = (torch.randn((1, vocab), generator=g) * 3).expand(beams, vocab).contiguous()
+    scores = torch.full((beams,), others)
+    scores[0] = 0.0
+    check(logits, scores, beams, n_out)
+
+
 @pytest.mark.parametrize("beams,vocab,n_out,dtype", [(128, 270001, 32, F32), (128, 128256, 20, BF), (125, 540001, 40, BF), (128, 794625, 32, BF)])
 @pytest.mark.parametrize("spread", [0.0, 40.0])
 def test_more_lists_than_are_looked_at_first(beams, vocab, n_out, dtype, spread):
