@@ -5,7 +5,7 @@
 // Two launches.  The scan reads the logits once: a workgroup takes a chunk of a row, keeps its values in registers, and leaves the chunk's maximum, its
 // sum of exponentials and its n best, in order (within a beam the order of the scores is that of the logits, so this needs no sum of the whole row).
 // The join forms the rows' sums from the chunks', the scores of what was found, and the n best of these.
-// What is compared are scores in double: rounded to float many candidates of a beam would be equal, and beams' sums meet there.  Exponentials are floats, a thread's sixteen or 32 are added
+// What is compared are scores in double: rounded to float many candidates of a beam would be equal, and beams' sums meet there.  (Where even these are equal, within a beam by logits: it is these that its lists are of.)  Exponentials are floats, a thread's sixteen or 32 are added
 // in float and everything behind that in double.
 //
 // Scan + join, kernel times: 4 rows of 2048 floats 4.6 + 3.8 us; 128 rows of 32000 bf16, 8 of 4 back: 7.1 + 7.2; 128 rows of 100003 floats (41 MB are read), 16 of 8 back: 14.7 + 8.1; 64 rows
@@ -243,7 +243,7 @@ constexpr int kJoinFew = 128;    // so many are put in order without a look at w
 __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int is_bf16) {
   constexpr int WAVES = kJoinThreads / 64;
   struct Candidate {
-    uint64_t key, index;   // of the score in double, 0: none; beam of the group << 32 | token
+    uint64_t key, index;   // of the score in double, 0: none; among equal scores the beam of the group (8 bits), what its logit is below the highest (32), the token (24)
   };
   __shared__ double s_off[kBeamMost], s_base[kBeamMost];   // of a beam: the logarithm of its sum; its score
   __shared__ int s_done[kBeamMost];
@@ -321,10 +321,10 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
     Candidate r;
     if (s_done[b]) {
       s = first && list == b * a.chunks ? s_base[b] : -INFINITY;
-      r.index = (uint64_t)b << 32 | (uint32_t)a.end_token;
+      r.index = (uint64_t)b << 56 | (uint32_t)a.end_token;
     } else {
       s = cc >> 32 ? s_base[b] + ((double)float_of((uint32_t)(cc >> 32)) - s_off[b]) : -INFINITY;
-      r.index = (uint64_t)b << 32 | (0xffffffffu - (uint32_t)cc);
+      r.index = (uint64_t)b << 56 | (~cc >> 32) << 24 | (0xffffffffu - (uint32_t)cc);
     }
     r.key = s - s == 0.0 ? key_of(s) : 0;   // what is not finite is none
     return r;
@@ -573,7 +573,7 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
     if (__any(sum_of_8(like) > 1))
       for (int k = threadIdx.x & 7; k < count; k += 8) rank += (int)(s_key[k] == key) & (int)(s_index[k] < index);
     rank = sum_of_8(rank);
-    if (i < count && rank < n && (threadIdx.x & 7) == 0) put(rank, double_of(key), (int)(index >> 32), (int)(uint32_t)index);
+    if (i < count && rank < n && (threadIdx.x & 7) == 0) put(rank, double_of(key), (int)(index >> 56), (int)(index & 0xffffff));
   }
   if (count >= n) return;
   // Fewer candidates than asked for: the rest are the lowest indices whose score is -inf, found by looking (one wavefront, 64 indices at a time).

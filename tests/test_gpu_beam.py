@@ -154,6 +154,19 @@ def test_a_first_step(beams, vocab, n_out, others):
     check(logits, scores, beams, n_out)
 
 
+@pytest.mark.parametrize("beams,vocab,n_out", [(1, 50, 33), (4, 4096, 128), (5, 40000, 33), (64, 32000, 128)])
+def test_scores_that_hide_the_logits(beams, vocab, n_out):
+    """Scores so large that all of a row's are one double: the order within the row is that of the logits, and the rows' is theirs."""
+    g = gen(vocab)
+    logits = torch.randn((beams, vocab), generator=g)
+    t, p, _, _ = run(logits, torch.full((beams,), -3e38), beams, n_out)
+    assert p == [0] * n_out and t == torch.sort(logits[0], descending=True, stable=True)[1][:n_out].tolist()
+    scores = torch.full((beams,), -1e20)
+    scores[-1] = 1e20
+    t, p, _, _ = run(logits, scores, beams, n_out)
+    assert p == [beams - 1] * n_out and t == torch.sort(logits[-1], descending=True, stable=True)[1][:n_out].tolist()
+
+
 @pytest.mark.parametrize("beams,vocab,n_out,dtype", [(128, 270001, 32, F32), (128, 128256, 20, BF), (125, 540001, 40, BF), (128, 794625, 32, BF)])
 @pytest.mark.parametrize("spread", [0.0, 40.0])
 def test_more_lists_than_are_looked_at_first(beams, vocab, n_out, dtype, spread):
