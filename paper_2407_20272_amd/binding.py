@@ -570,15 +570,17 @@ class PageTables:
         self.c = ee_page_tables(_ptr(block_tables), _ptr(lens), *block_tables.shape)
 
 
-def _pool_device(pool, *tables) -> int:
+def _pool_device(pool, tables, more=None) -> int:
     device = _device()
-    assert all(t is None or t.device == device for t in (pool, *tables)), "a pool and tables of the current device"
+    assert (pool is None or pool.device == device) and (tables is None or tables.device == device) and (more is None or more.device == device), \
+        "a pool and tables of the current device"
     return device
 
 
 def _int32s(t: torch.Tensor, shape, device: int) -> int:
-    assert t.dtype == torch.int32 and t.shape == shape, "int32 of the call's sizes"
-    return _here(t, device)
+    assert t.dtype is torch.int32 and t.shape == shape, "int32 of the call's sizes"
+    assert t.get_device() == device and t.is_contiguous(), "contiguous CUDA tensors of the current device"
+    return t.data_ptr()
 
 
 def ee_kv_pages_fork(pool: PagePool, src: PageTables, parents: torch.Tensor, dst: PageTables, release: bool = False):
@@ -647,18 +649,20 @@ def ee_beam_select(logits: torch.Tensor, scores: torch.Tensor, beams: int, token
     assert beams > 0 and rows == groups * beams == scores.numel() and total == groups * n_out == parents.numel() == scores_out.numel(), "rows of whole groups"
     assert scores.dtype is scores_out.dtype is torch.float32 and tokens.dtype is parents.dtype is torch.int32
     assert logits.get_device() == device == ws.device and (stride == 1 or vocab == 1), "rows of consecutive values, and a workspace, on the current device"
+    assert device == scores.get_device() == tokens.get_device() == parents.get_device() == scores_out.get_device() and scores.is_contiguous() and tokens.is_contiguous() \
+        and parents.is_contiguous() and scores_out.is_contiguous(), "contiguous CUDA tensors of the current device"
     assert finished is None or finished.numel() == rows and finished.dtype is torch.int32
     assert finished_out is None or finished_out.numel() == total and finished_out.dtype is torch.int32
-    _check(lib().ee_beam_select(logits.data_ptr(), row_stride if rows > 1 else vocab, _KIND[logits.dtype], _here(scores, device),
+    _check(lib().ee_beam_select(logits.data_ptr(), row_stride if rows > 1 else vocab, _KIND[logits.dtype], scores.data_ptr(),
                                 None if finished is None else _here(finished, device), groups, beams, vocab, n_out, end_token,
-                                _here(tokens, device), _here(parents, device), _here(scores_out, device),
+                                tokens.data_ptr(), parents.data_ptr(), scores_out.data_ptr(),
                                 None if finished_out is None else _here(finished_out, device), ws.address, ws.bytes, _raw_stream(device)))
 
 
 def ee_reorder_rows(x: torch.Tensor, parents: torch.Tensor, out: torch.Tensor):
     """out[m] = x[parents[m]] of any type, rows of consecutive values at any row stride."""
     device, rows, shape, out_shape = _device(), parents.numel(), x.shape, out.shape
-    assert x.dtype is out.dtype and shape[1:] == out_shape[1:] and out_shape[0] == rows and parents.dtype is torch.int32
+    assert x.dtype is out.dtype and (shape == out_shape or shape[1:] == out_shape[1:]) and out_shape[0] == rows and parents.dtype is torch.int32
     assert x.get_device() == device and out.get_device() == device, "CUDA tensors of the current device"
     row = out.nbytes // rows if rows else 0
     x_stride = out_stride = row
