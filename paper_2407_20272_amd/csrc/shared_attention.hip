@@ -455,14 +455,17 @@ __global__ __launch_bounds__(kThreads) void shared_attn_kernel(SharedAttnArgs a)
         }
       }
     };
+    constexpr bool EARLY = NT < 3;   // all scores first, so that the next K comes while the rest of the step is done; three tiles' do not fit beside it
+    constexpr bool EARLY_V = BF16 && NT == 3;   // the next V as soon as this one is turned: 87 -> 83 us for the 100000 positions above, but 17.6 -> 18.2 for tiles of 16 columns
+    auto next_ids = [&] {   // in front of whichever of the next step's K and V is asked for first (both of this step's have been)
+      if (((k + 1) & 31) == 0) load_ids(k + 1);
+    };
     auto next_k = [&] {
       if (k + 1 < nk) {
-        if (((k + 1) & 31) == 0) load_ids(k + 1);   // (V of this step has been asked for: its blocks' ids are no longer needed)
+        if constexpr (!EARLY_V) next_ids();
         load_k(k + 1);
       }
     };
-    constexpr bool EARLY = NT < 3;   // all scores first, so that the next K comes while the rest of the step is done; three tiles' do not fit beside it
-    constexpr bool EARLY_V = BF16 && NT == 3;   // the next V as soon as this one is turned: 87 -> 83 us for the 100000 positions below, but 17.6 -> 18.2 for tiles of 16 columns
     f32x4 st[EARLY ? NT : 1][2];
     if constexpr (EARLY) {
 #pragma unroll
@@ -497,7 +500,10 @@ __global__ __launch_bounds__(kThreads) void shared_attn_kernel(SharedAttnArgs a)
           vt[u][w] = u & 1 ? high_halves(x, y) : low_halves(x, y);
         }
       if constexpr (EARLY_V) {   // (the registers of V are free)
-        if (k + 1 < nk) load_v(k + 1);
+        if (k + 1 < nk) {
+          next_ids();
+          load_v(k + 1);
+        }
         __builtin_amdgcn_sched_barrier(0);
       }
     }
