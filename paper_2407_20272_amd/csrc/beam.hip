@@ -350,7 +350,7 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
       list_of = next_list(list_of);
     }
   uint32_t bound = 1, above = 0;
-  // The bound moved up until few of these are at it or above (n at least are, or it stays; none from `above` on): counted, then 256 parts of what is between bound and `above` at a time.
+  // The bound moved up until few of these are at it or above (n at least are, or it stays; fewer than n from `above` on): counted, then 256 parts of what is between bound and `above` at a time.
   auto move_up = [&](int from, int to, uint32_t above) {
     int mine = 0;
 #pragma unroll 4
@@ -365,11 +365,11 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
     for (int turn = 0; there > max(2 * n, 64) && above - bound > 1; ++turn) {
       const int shift = max(0, 24 - __builtin_clz(above - 1 - bound));
       int* bins = s_bins[turn & 1];
-      // (the highest part first; those in the lowest are not counted: n are there or above)
+      // (the highest part first, with those that a turn before has left at `above` or over it; those in the lowest are not counted: n are there or above)
 #pragma unroll 4
       for (int i = from + (int)threadIdx.x; i < to; i += kJoinThreads) {
         const uint32_t k = s_rough[i];
-        if (k > bound && (k - bound) >> shift) atomicAdd(&bins[255 - ((k - bound) >> shift)], 1);
+        if (k > bound && (k - bound) >> shift) atomicAdd(&bins[255 - min((k - bound) >> shift, 255u)], 1);
       }
       __syncthreads();
       const int4 four = *reinterpret_cast<const int4*>(&bins[lane * 4]);

@@ -1,0 +1,323 @@
+"""The join of a beam selection without a GPU: the kernel's source is built for the host with stand-ins for the device built-ins (a lane is a coroutine, a cross-lane operation an
+exchange), and LDS as arrays that look at every index.  What the scan leaves is made here, and the result compared with every candidate sorted in float64."""
+import os
+import re
+import subprocess
+
+import numpy as np
+import pytest
+import torch
+
+import beams_oracle as O
+from paper_2407_20272_amd import build
+
+RUNTIME = r"""
+#pragma once
+#include <math.h>
+#include <stddef.h>
+#include <stdint.h>
+#include <stdio.h>
+#include <stdlib.h>
+#include <string.h>
+#define __global__
+#define __device__
+#define __host__
+#define __shared__ static
+#define __forceinline__ inline
+#define __launch_bounds__(...)
+#define __align__(n) __attribute__((aligned(n)))
+#define __syncthreads() emu::meet()
+#define __builtin_amdgcn_readlane(v, l) emu::from(v, l)
+#define __builtin_amdgcn_readfirstlane(v) emu::from(v, 0)
+#define __builtin_amdgcn_update_dpp(old, v, ctrl, rows, banks, bound) emu::dpp(old, v, ctrl, rows, bound)
+#define __builtin_amdgcn_exp2f exp2f
+#define __builtin_amdgcn_sched_barrier(x) ((void)0)
+#define __builtin_nontemporal_load(p) (*(p))
+#define __expf expf
+#define threadIdx (*emu::tid)
+struct dim3 { unsigned x, y, z; };
+struct uint4 { unsigned x, y, z, w; };
+struct __attribute__((aligned(16))) int4 { int x, y, z, w; };
+struct int2 { int x, y; };
+struct float2 { float x, y; };
+struct __attribute__((aligned(16))) float4 { float x, y, z, w; };
+struct __attribute__((aligned(16))) double2 { double x, y; };
+typedef void* hipStream_t;
+typedef int hipError_t;
+inline uint4 make_uint4(unsigned x, unsigned y, unsigned z, unsigned w) { return {x, y, z, w}; }
+inline float2 make_float2(float x, float y) { return {x, y}; }
+inline float4 make_float4(float x, float y, float z, float w) { return {x, y, z, w}; }
+inline double2 make_double2(double x, double y) { return {x, y}; }
+template <class T> inline T min(T a, T b) { return a < b ? a : b; }
+template <class T> inline T max(T a, T b) { return a > b ? a : b; }
+template <class To, class From> inline To as(From x) { To y; static_assert(sizeof x == sizeof y, ""); memcpy(&y, &x, sizeof y); return y; }
+inline int __float_as_int(float x) { return as<int>(x); }
+inline float __int_as_float(int i) { return as<float>(i); }
+inline unsigned __float_as_uint(float x) { return as<unsigned>(x); }
+inline float __uint_as_float(unsigned i) { return as<float>(i); }
+inline long long __double_as_longlong(double x) { return as<long long>(x); }
+inline double __longlong_as_double(long long x) { return as<double>(x); }
+inline unsigned __umulhi(unsigned a, unsigned b) { return (unsigned)((unsigned long long)a * b >> 32); }
+inline int __popcll(unsigned long long x) { return __builtin_popcountll(x); }
+inline float rsqrtf(float x) { return 1 / sqrtf(x); }
+static dim3 blockIdx, gridDim, blockDim = {256, 1, 1};
+namespace emu {
+extern dim3* tid;
+unsigned long long exchange(unsigned long long v, int lane);     // lane's value
+unsigned long long ballot(bool x);
+void meet();
+int lane();
+extern int outside;
+template <class T> T from(T v, int l) { unsigned long long u = 0; memcpy(&u, &v, sizeof v); u = exchange(u, l); memcpy(&v, &u, sizeof v); return v; }
+inline int dpp(int old, int v, int ctrl, int rows, bool bound) {
+  const int l = lane();
+  int src = -1;
+  if (ctrl < 0x100) src = (l & ~3) + (ctrl >> 2 * (l & 3) & 3);
+  else if (ctrl > 0x110 && ctrl < 0x120) src = (l & 15) >= (ctrl & 15) ? l - (ctrl & 15) : -1;
+  else if (ctrl == 0x140) src = l ^ 15;
+  else if (ctrl == 0x141) src = l ^ 7;
+  else if (ctrl == 0x142) src = l >= 16 ? (l & ~15) - 1 : -1;
+  else if (ctrl == 0x143) src = l >= 32 ? 31 : -1;
+  else abort();
+  const int got = from(v, src < 0 ? l : src);
+  return !(rows >> (l >> 4) & 1) ? old : src >= 0 ? got : bound ? 0 : old;
+}
+template <class T, long N> struct Array {                        // LDS
+  T at[N];
+  T& operator[](long i) {
+    static T none;
+    if (i < 0 || i >= N) { if (!outside++) fprintf(stderr, "index %ld of an array of %ld\n", i, N); return none; }
+    return at[i];
+  }
+};
+}
+#define __shfl_xor(v, x) emu::from(v, emu::lane() ^ (x))
+#define __ballot(x) emu::ballot(x)
+#define __any(x) (emu::ballot(x) != 0)
+template <class T> inline T atomicAdd(T* p, T v) { T o = *p; *p += v; return o; }
+template <class T> inline T atomicMin(T* p, T v) { T o = *p; if (v < o) *p = v; return o; }
+template <class T> inline T atomicMax(T* p, T v) { T o = *p; if (v > o) *p = v; return o; }
+"""
+
+PROGRAM = r"""
+#include <ucontext.h>
+#include <vector>
+#include "join_source.h"
+
+constexpr int THREADS = ee::kJoinThreads, WAVES = THREADS / 64;
+namespace emu {
+struct Lane { ucontext_t c; dim3 id; bool at_barrier, over; };
+static Lane lanes[THREADS];
+static ucontext_t here;
+static unsigned long long slots[WAVES][2][64];
+static unsigned turn[THREADS];
+static int cur;
+dim3* tid;
+int outside;
+static ee::BeamArgs args;
+static void leave() { swapcontext(&lanes[cur].c, &here); }
+int lane() { return cur & 63; }
+unsigned long long exchange(unsigned long long v, int l) {       // two sets: a lane may be one exchange ahead of another
+  const int t = cur, wave = t >> 6, set = turn[t]++ & 1;
+  slots[wave][set][t & 63] = v;
+  leave();
+  return slots[wave][set][l];
+}
+unsigned long long ballot(bool x) {
+  const int t = cur, wave = t >> 6, set = turn[t]++ & 1;
+  slots[wave][set][t & 63] = x;
+  leave();
+  unsigned long long bits = 0;
+  for (int l = 0; l < 64; ++l) bits |= slots[wave][set][l] << l;
+  return bits;
+}
+void meet() { lanes[cur].at_barrier = true; leave(); }
+static void body() {
+  ee::beam_join_kernel(args, 0);
+  lanes[cur].over = true;
+  leave();
+}
+static void workgroup() {
+  static std::vector<char> stacks((size_t)THREADS * 65536);
+  for (int t = 0; t < THREADS; ++t) {
+    lanes[t] = Lane{};
+    lanes[t].id = {(unsigned)t, 0, 0};
+    turn[t] = 0;
+    getcontext(&lanes[t].c);
+    lanes[t].c.uc_stack.ss_sp = &stacks[(size_t)t * 65536];
+    lanes[t].c.uc_stack.ss_size = 65536;
+    lanes[t].c.uc_link = nullptr;
+    makecontext(&lanes[t].c, body, 0);
+  }
+  for (;;) {
+    bool any = false;
+    for (int w = 0; w < WAVES; ++w)
+      for (bool again = true; again;) {                          // a step of all 64 lanes, until the wavefront waits or is over
+        again = false;
+        for (int l = 0; l < 64; ++l) {
+          cur = w * 64 + l;
+          if (lanes[cur].at_barrier || lanes[cur].over) continue;
+          tid = &lanes[cur].id;
+          swapcontext(&here, &lanes[cur].c);
+          again = true;
+        }
+      }
+    for (Lane& l : lanes)
+      if (!l.over) l.at_barrier = false, any = true;
+    if (!any) return;
+  }
+}
+}
+
+int main(int argc, char** argv) {                                // file, beams, vocab, n_out, chunks, end
+  const int beams = atoi(argv[2]), vocab = atoi(argv[3]), n = atoi(argv[4]), chunks = atoi(argv[5]), end = atoi(argv[6]);
+  FILE* f = fopen(argv[1], "rb");
+  auto read = [&](auto& v) { if (fread(v.data(), sizeof v[0], v.size(), f) != v.size()) exit(2); };
+  std::vector<float> scores(beams), scores_out(n);
+  std::vector<int32_t> finished(beams), tokens(n), parents(n), finished_out(n);
+  std::vector<double2> stats((size_t)beams * chunks);
+  std::vector<uint64_t> found((size_t)n * beams * chunks);
+  read(scores), read(finished), read(stats), read(found);
+  ee::BeamArgs a{};
+  a.groups = 1, a.beams = beams, a.vocab = vocab, a.n_out = n, a.end_token = end, a.chunks = chunks, a.stride = vocab;
+  a.scores = scores.data(), a.finished = finished.data(), a.stats = stats.data(), a.found = found.data();
+  a.tokens = tokens.data(), a.parents = parents.data(), a.finished_out = finished_out.data(), a.scores_out = scores_out.data();
+  emu::args = a;
+  emu::workgroup();
+  for (int i = 0; i < n; ++i) printf("%d %d %a %d\n", tokens[i], parents[i], scores_out[i], finished_out[i]);
+  fflush(stdout);
+  _Exit(emu::outside ? 3 : 0);
+}
+"""
+
+
+def join_source():
+    """The kernels' source up to the join's end, its LDS in arrays that look at their indices."""
+    with open(os.path.join(build.CSRC, "beam.hip")) as f:
+        source = f.read()
+    end = "// A workgroup copies up to"
+    assert source.count(end) == 1
+    source = source[:source.index(end)]
+
+    def checked(m):
+        out = ""
+        for name, dims in re.findall(r"(\w+)((?:\[[^\]]*\])+)", m.group(2)):
+            t = m.group(1)
+            for d in reversed(re.findall(r"\[([^\]]*)\]", dims)):
+                t = f"emu::Array<{t}, {d}>"
+            out += f"static __align__(16) {t} {name}; "
+        return out + "".join(f"static {m.group(1)} {name}; " for name in re.findall(r"(?:^|, )(\w+)(?=,|$)", m.group(2)))
+
+    source, n = re.subn(r"__shared__ (?:__align__\(16\) )?((?:unsigned long long|\w+)) ([^;]*);", checked, source)
+    assert n >= 12
+    source, n = re.subn(r"int\* bins = ", "auto& bins = ", source)
+    assert n == 1
+    return source + "\n}}\n"
+
+
+@pytest.fixture(scope="module")
+def program(tmp_path_factory):
+    d = tmp_path_factory.mktemp("host_beam_join")
+    (d / "hip").mkdir()
+    (d / "hip" / "hip_runtime.h").write_text(RUNTIME)
+    (d / "join_source.h").write_text(join_source())
+    (d / "program.cpp").write_text(PROGRAM)
+    clang = os.path.join(os.path.dirname(os.path.realpath(build._hipcc())), "..", "llvm", "bin", "clang++")
+    subprocess.run([clang if os.path.exists(clang) else "/opt/rocm/llvm/bin/clang++", "-x", "c++", "-std=c++17", "-O1", "-Wno-everything", "-I" + str(d),
+                    "-I" + os.path.join(build.ROOT, "include"), "-I" + build.CSRC, str(d / "program.cpp"), "-o", str(d / "program")],
+                   check=True, capture_output=True, text=True)
+    return str(d / "program")
+
+
+def scanned(logits, n, size):
+    """What the scan leaves: of every chunk of a row its maximum and sum of exponentials, and its n best as keys with their tokens, in order."""
+    beams, vocab = logits.shape
+    chunks = -(-vocab // size)
+    z = torch.full((beams, chunks * size), -float("inf"))
+    z[:, :vocab] = logits
+    z = z.view(beams, chunks, size)
+    most = z.amax(-1)
+    sums = torch.exp(z - torch.where(torch.isfinite(most), most, 0.0)[..., None]).double().sum(-1)
+    stats = torch.stack([most.double(), sums], -1).numpy()
+    best, at = torch.sort(z, dim=-1, descending=True, stable=True) if vocab < 1 << 16 else torch.topk(z, min(n, size), dim=-1)
+    best, at = (best[..., :n] + 0.0).numpy(), at[..., :n].numpy().astype(np.uint64) + (np.arange(chunks, dtype=np.uint64) * size)[None, :, None]
+    u = best.view(np.uint32)
+    key = np.where(u >> 31, ~u, u | np.uint32(1 << 31)).astype(np.uint64)
+    key[~(best > -np.inf)] = 0
+    cc = key << np.uint64(32) | (np.uint64(0xffffffff) - at)
+    return chunks, stats, np.ascontiguousarray(cc.transpose(2, 0, 1))
+
+
+def check(program, tmp_path, logits, scores, n, finished=None, end=0, size=None):
+    beams, vocab = logits.shape
+    size = size or (16384 if n > 32 else 4096)
+    fin = torch.zeros(beams, dtype=torch.int32) if finished is None else finished.int()
+    chunks, stats, found = scanned(logits, n, size)
+    with open(tmp_path / "in", "wb") as f:
+        for x in (scores.float().numpy(), fin.numpy(), stats, found):
+            f.write(np.ascontiguousarray(x).tobytes())
+    out = subprocess.run([program, str(tmp_path / "in"), *map(str, (beams, vocab, n, chunks, end))], capture_output=True, text=True, timeout=300)
+    assert out.returncode == 0, out.stderr
+    got = [line.split() for line in out.stdout.strip().split("\n")]
+    every = logits.double()
+    score = scores.double()[:, None] + (every - torch.logsumexp(every, 1, keepdim=True))
+    if finished is not None:
+        only = torch.full_like(score, -float("inf"))
+        only[:, end] = scores.double()
+        score = torch.where(finished[:, None] != 0, only, score)
+    least = torch.topk(score.flatten(), n)[0][-1]
+    at = torch.nonzero(score.flatten() >= least).flatten()
+    order = at[torch.sort(score.flatten()[at], descending=True, stable=True)[1]][:n].tolist()
+    assert [(int(g[1]), int(g[0])) for g in got] == [(i // vocab, i % vocab) for i in order]
+
+
+def gen(seed):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return g
+
+
+@pytest.mark.parametrize("beams,vocab,n", [(64, 32000, 128), (16, 9000, 32), (57, 33000, 114), (8, 2000, 100)])
+@pytest.mark.parametrize("wide,spread", [(1.0, 0.1), (3.0, 30.0), (6.0, 0.1), (6.0, 30.0), (20.0, 3.0)])
+def test_logits_far_apart(program, tmp_path, beams, vocab, n, wide, spread):
+    """Where the best few lie well above the others, the bound is moved up by ever narrower parts, and they stay above all of these."""
+    g = gen(int(wide * 7 + spread * 3))
+    check(program, tmp_path, torch.randn((beams, vocab), generator=g) * wide, torch.randn(beams, generator=g) * spread - 20, n)
+
+
+@pytest.mark.parametrize("beams,vocab,n", [(24, 20000, 20), (24, 20000, 33), (64, 32000, 128), (5, 9000, 60)])
+@pytest.mark.parametrize("above", [1, 0.25, 0.9])
+@pytest.mark.parametrize("blob", [0.01, 1e-4])
+def test_a_few_above_many_alike(program, tmp_path, beams, vocab, n, above, blob):
+    """Fewer than are asked for far above all others, and these so near each other that several turns are needed to part them."""
+    g = gen(n)
+    logits = torch.randn((beams, vocab), generator=g) * blob
+    for i in range(1 if above == 1 else int(above * n)):
+        logits[i % beams, 37 * i + 5] = 4.0 + 8.0 * float(torch.rand(1, generator=g))
+    check(program, tmp_path, logits, torch.full((beams,), -3.0), n)
+
+
+@pytest.mark.parametrize("live", [1, 8, 16, 40])
+@pytest.mark.parametrize("others", [-1e9, -1e4])
+def test_some_beams_live(program, tmp_path, live, others):
+    g = gen(live)
+    scores = torch.full((64,), others)
+    scores[torch.randperm(64, generator=g)[:live]] = -torch.rand(live, generator=g) * 30
+    check(program, tmp_path, torch.randn((64, 32000), generator=g) * 3, scores, 128)
+
+
+@pytest.mark.parametrize("n,size", [(20, 4096), (33, 16384), (128, 16384)])
+def test_clusters(program, tmp_path, n, size):
+    """Scores in clusters of all sizes, from a few to more than are asked for, far from each other and close by."""
+    g = gen(n)
+    logits = torch.randn((24, 20000), generator=g) * 0.01 - 12
+    for i, height in enumerate([8.0, 7.9999, 3.0, 2.99, -1.0, -6.0]):
+        at = torch.randint(0, 20000, (24, 1 + 2 * i), generator=g)
+        logits.scatter_(1, at, height + torch.randn(at.shape, generator=g) * 1e-4)
+    finished = (torch.arange(24) % 5 == 3).int()
+    check(program, tmp_path, logits, -torch.rand(24, generator=g).round() * 4 - torch.rand(24, generator=g) * 1e-3, n, finished, 7, size)
+
+
+def test_more_lists_than_are_looked_at_first(program, tmp_path):
+    g = gen(4)
+    check(program, tmp_path, torch.randn((128, 270001), generator=g) * 4, -torch.linspace(0, 9, 128), 32, size=8192)
