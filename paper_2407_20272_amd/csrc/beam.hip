@@ -640,6 +640,14 @@ void beam_plan(BeamArgs& a) {
   a.chunks = (a.vocab + a.threads * a.each - 1) / (a.threads * a.each);
 }
 
+// Fewer rows or tokens may have the smaller chunks: as many of these as run at once.
+int64_t beam_most_chunks(int64_t rows, int vocab, bool few) {
+  auto chunks = [&](int size) { return rows * ((vocab + size - 1) / size); };
+  if (!few) return chunks(16384);
+  const int64_t small = chunks(4096), large = chunks(8192);
+  return small <= kBeamWgs ? small : large > kBeamWgs ? large : kBeamWgs;
+}
+
 void launch_beam_select(const BeamArgs& a, int dtype, hipStream_t st) {
   if (dtype == EE_BF16) launch_scan<bf16_t>(a, st);
   else launch_scan<float>(a, st);

@@ -66,6 +66,7 @@ struct BeamArgs {
   uint64_t* found;           // [groups][n_out][beams][chunks]: key of the logit and complement of its token, falling along n_out; 0: none
 };
 void beam_plan(BeamArgs& a);   // chunks, threads, each
+int64_t beam_most_chunks(int64_t rows, int vocab, bool few);   // of all rows of a call up to these sizes; few: up to kBeamFewOut come back
 void launch_beam_select(const BeamArgs& a, int dtype, hipStream_t st);
 struct RowCopyArgs {
   const char* in;

@@ -1545,30 +1545,25 @@ int check_beams(int32_t groups, int32_t beams, int32_t vocab, int32_t n_out) {
   return EE_OK;
 }
 
+size_t beam_stats_bytes(size_t chunks) { return align256(chunks * sizeof(double2)); }
+size_t beam_bytes(size_t chunks, int n_out) { return beam_stats_bytes(chunks) + align256(chunks * n_out * sizeof(uint64_t)); }
+
 size_t carve_beams(BeamArgs& a, void* ws) {
   beam_plan(a);
-  const size_t pieces = (size_t)a.groups * a.beams * a.chunks, stats = align256(pieces * sizeof(double2));
+  const size_t chunks = (size_t)a.groups * a.beams * a.chunks;
   a.stats = reinterpret_cast<double2*>(ws);
-  a.found = reinterpret_cast<uint64_t*>(reinterpret_cast<char*>(ws) + stats);
-  return stats + align256(pieces * a.n_out * sizeof(uint64_t));
+  a.found = reinterpret_cast<uint64_t*>(reinterpret_cast<char*>(ws) + beam_stats_bytes(chunks));
+  return beam_bytes(chunks, a.n_out);
 }
 
 }  // namespace
 
 size_t ee_beam_select_bytes(int32_t groups, int32_t beams, int32_t vocab, int32_t n_out) {
   if (check_beams(groups, beams, vocab, n_out)) return 0;
-  BeamArgs a{};
-  a.groups = groups < 1 ? 1 : groups;
-  a.beams = beams;
-  a.vocab = vocab;
-  a.n_out = n_out;
-  size_t most = carve_beams(a, nullptr);
-  if (n_out > kBeamFewOut) {   // (fewer come back of smaller chunks)
-    a.n_out = kBeamFewOut;
-    const size_t few = carve_beams(a, nullptr);
-    most = few > most ? few : most;
-  }
-  return most;
+  const int64_t rows = (int64_t)(groups < 1 ? 1 : groups) * beams;
+  const size_t few = beam_bytes(beam_most_chunks(rows, vocab, true), n_out < kBeamFewOut ? n_out : kBeamFewOut);
+  const size_t many = n_out > kBeamFewOut ? beam_bytes(beam_most_chunks(rows, vocab, false), n_out) : 0;
+  return few > many ? few : many;
 }
 
 int ee_beam_select(const void* logits, int64_t logits_stride, int32_t dtype, const float* scores, const int32_t* finished, int32_t groups, int32_t beams,
