@@ -114,7 +114,7 @@ __global__ __launch_bounds__(THREADS, EACH > 16 ? 6 : 4) void beam_scan_kernel(B
   __shared__ int s_count, s_below[WAVES];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int chunk = blockIdx.x, row = blockIdx.y, base = chunk * THREADS * EACH, n = a.n_out, lists = a.beams * a.chunks;
-  const int done = a.finished ? a.finished[row] : 0;   // (looked at when the values have been asked for)
+  if (a.finished && a.finished[row]) return;   // (before any value is asked for: the row's logits may be nowhere)
   const char* z = reinterpret_cast<const char*>(a.logits) + (size_t)row * a.stride * sizeof(T);
   // Values `at(l) + e` for part l; the same places whether the row starts on 16 bytes or not, so that equal rows have equal sums.
   auto at = [&](int l) { return base + (l * THREADS + (int)threadIdx.x) * VEC; };
@@ -127,14 +127,12 @@ __global__ __launch_bounds__(THREADS, EACH > 16 ? 6 : 4) void beam_scan_kernel(B
       raw[l] = u32x4{NONE, NONE, NONE, NONE};
       if (at(l) < a.vocab) raw[l] = *reinterpret_cast<const u32x4*>(z + (uint32_t)at(l) * (uint32_t)sizeof(T));
     }
-    if (done) return;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
       if constexpr (sizeof(T) == 4) x[i] = __uint_as_float(raw[i / 4][i % 4]);
       else x[i] = __uint_as_float(i & 1 ? raw[i / 8][i % 8 / 2] & 0xffff0000u : raw[i / 8][i % 8 / 2] << 16);
     }
   } else {
-    if (done) return;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
       const int t = at(i / VEC) + i % VEC;
