@@ -420,7 +420,7 @@ int ee_kv_pages_compact(int32_t* refs, int32_t num_blocks, const ee_page_tables*
  * (16 positions); 0 for a group without rows.  first_row dev [n_groups + 1] int32, shared_blocks dev [n_groups] int32. */
 int ee_kv_pages_shared(const ee_page_tables* tables, const int32_t* first_row, int32_t n_groups, int32_t* shared_blocks, void* stream);
 
-/* Copies blocks of every layer, K and V (and scales): moves dev [n][2] int32 (from, to); a pair with an entry outside 0 .. num_blocks - 1 is skipped.  count
+/* Copies blocks of every layer, K and V (and scales): moves dev [n][2] int32 (from, to), n up to 2^30; a pair with an entry outside 0 .. num_blocks - 1 is skipped.  count
  * dev [1] int32 or NULL: only the first *count of the n pairs.  No block may be written twice, or both read and written (but a pair of one block with itself
  * does nothing).  Pools start on 16 bytes. */
 int ee_kv_copy(const ee_model_desc* desc, const ee_kv_cache* cache, const int32_t* moves, int32_t n, const int32_t* count, void* stream);

@@ -1370,6 +1370,7 @@ size_t carve_pages(int num_blocks, int rows, void* ws, PageWork* w) {
 
 int copy_pages(PageCopyArgs a, const int32_t* moves, int32_t n, const int32_t* count, const char* what, void* stream) {
   if (n < 0) EE_FAIL(EE_ERR_INVALID_ARG, "%s: %d moves", what, n);
+  if (n > 1 << 30) EE_FAIL(EE_ERR_UNSUPPORTED, "%s: %d moves in one call", what, n);   // (their list is indexed in 32 bits)
   if (n == 0) return EE_OK;
   if (!moves || ((reinterpret_cast<uintptr_t>(moves) | reinterpret_cast<uintptr_t>(count)) & 3)) EE_FAIL(EE_ERR_INVALID_ARG, "%s: moves NULL or misaligned", what);
   for (int p = 0; p < 2; ++p)
