@@ -245,7 +245,7 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
   };
   __shared__ double s_off[kBeamMost], s_base[kBeamMost];   // of a beam: the logarithm of its sum; its score
   __shared__ int s_done[kBeamMost];
-  __shared__ float s_rough_off[kBeamMost], s_best[kBeamMost];   // what is added to its logits, and its best score, as floats
+  __shared__ float s_rough_off[kBeamMost], s_best[kBeamMost];   // half of what is added to its logits (the whole may be twice the largest float), and its best score, as floats
   __shared__ uint32_t s_most[kJoinThreads / 4];
   __shared__ uint64_t s_key[kJoinList], s_index[kJoinList];
   __shared__ uint32_t s_rough[kJoinKept + kJoinDeep];
@@ -292,14 +292,14 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
         s_off[b] = off;
         s_base[b] = base;
         s_done[b] = done != 0;
-        // what is not finite stands for rows that have no candidates; what no float is for the largest
-        s_rough_off[b] = to - to == 0.0 ? fminf(fmaxf((float)to, -3.4028235e38f), 3.4028235e38f) : NAN;
-        s_best[b] = done ? s_rough_off[b] : fminf(fmaxf((float)(to + m), -3.4028235e38f), 3.4028235e38f);
+        // what is not finite stands for rows that have no candidates; a score that no float is for the lowest
+        s_rough_off[b] = to - to == 0.0 ? (float)(0.5 * to) : NAN;
+        s_best[b] = done ? (to - to == 0.0 ? base : NAN) : fminf(fmaxf((float)(to + m), -3.4028235e38f), 3.4028235e38f);
       }
     }
   }
   __syncthreads();
-  float far = 0.0f;   // the largest magnitude of what is added to logits
+  float far = 0.0f;   // the largest magnitude of half of what is added to logits
   {
     uint32_t most_far = 0;
     for (int b = lane; b < W; b += 64) most_far = max(most_far, __float_as_uint(fmaxf(fabsf(s_rough_off[b]), 0.0f)));   // (a NaN is 0)
@@ -330,9 +330,9 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
   // The order of a float near the score, for the first look: the row's part is rounded, and the sum (to less than 2^-22 of the row's part and the score together).  0 for none.
   auto rough = [&](int list, uint64_t cc, bool first) {
     const int b = beam_of(list);
-    float f = s_rough_off[b];
-    if (s_done[b]) f = first && list == b * a.chunks ? f : NAN;
-    else f = cc >> 32 ? f + float_of((uint32_t)(cc >> 32)) : NAN;
+    float f;
+    if (s_done[b]) f = first && list == b * a.chunks ? s_best[b] : NAN;
+    else f = cc >> 32 ? 2.0f * fmaf(0.5f, float_of((uint32_t)(cc >> 32)), s_rough_off[b]) : NAN;
     return f == f ? key_of(fminf(fmaxf(f, -3.4028235e38f), 3.4028235e38f)) : 0u;
   };
   // Of the lists' first places, as many as fit, the scores give a bound for all.  Behind them (the lists fall) are candidates only where a list's last place is not below it.
@@ -413,14 +413,15 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, int
   auto lowered = [&](uint32_t at) -> uint32_t {
     if (at <= 1) return 1;
     const float f = float_of(at);
-    float least = far > 512.0f ? f : f - (fabsf(f) * 0x1p-20f + far * 0x1p-19f);
-    for (int turn = 0; far > 512.0f && turn < 2; ++turn) {   // beams that reach the bound; then those that reach what these leave of it
+    auto margin = [&](float off) { return fabsf(f) * 0x1p-20f + off * 0x1p-18f + 0x1p-140f; };   // (the last of these: halves of the smallest floats)
+    float least = far > 256.0f ? f : f - margin(far);
+    for (int turn = 0; far > 256.0f && turn < 2; ++turn) {   // beams that reach the bound; then those that reach what these leave of it
       uint32_t most_far = 0;
       for (int b = lane; b < W; b += 64) {
         const float off = fabsf(s_rough_off[b]);
-        if (s_best[b] + (fabsf(f) * 0x1p-20f + off * 0x1p-19f) >= least) most_far = max(most_far, __float_as_uint(off));
+        if (s_best[b] + margin(off) >= least) most_far = max(most_far, __float_as_uint(off));
       }
-      least = f - (fabsf(f) * 0x1p-20f + __uint_as_float(wave_largest(most_far)) * 0x1p-19f);
+      least = f - margin(__uint_as_float(wave_largest(most_far)));
     }
     return least > -3.4028235e38f ? key_of(least) : 1;
   };

@@ -248,7 +248,8 @@ def scanned(logits, n, size):
     return chunks, stats, np.ascontiguousarray(cc.transpose(2, 0, 1))
 
 
-def check(program, tmp_path, logits, scores, n, finished=None, end=0, size=None):
+def joined(program, tmp_path, logits, scores, n, finished=None, end=0, size=None):
+    """(row, token) of every result."""
     beams, vocab = logits.shape
     size = size or (16384 if n > 32 else 4096)
     fin = torch.zeros(beams, dtype=torch.int32) if finished is None else finished.int()
@@ -258,7 +259,12 @@ def check(program, tmp_path, logits, scores, n, finished=None, end=0, size=None)
             f.write(np.ascontiguousarray(x).tobytes())
     out = subprocess.run([program, str(tmp_path / "in"), *map(str, (beams, vocab, n, chunks, end))], capture_output=True, text=True, timeout=300)
     assert out.returncode == 0, out.stderr
-    got = [line.split() for line in out.stdout.strip().split("\n")]
+    return [(int(row), int(token)) for token, row, _, _ in (line.split() for line in out.stdout.strip().split("\n"))]
+
+
+def check(program, tmp_path, logits, scores, n, finished=None, end=0, size=None):
+    got = joined(program, tmp_path, logits, scores, n, finished, end, size)
+    vocab = logits.shape[1]
     every = logits.double()
     score = scores.double()[:, None] + (every - torch.logsumexp(every, 1, keepdim=True))
     if finished is not None:
@@ -268,7 +274,27 @@ def check(program, tmp_path, logits, scores, n, finished=None, end=0, size=None)
     least = torch.topk(score.flatten(), n)[0][-1]
     at = torch.nonzero(score.flatten() >= least).flatten()
     order = at[torch.sort(score.flatten()[at], descending=True, stable=True)[1]][:n].tolist()
-    assert [(int(g[1]), int(g[0])) for g in got] == [(i // vocab, i % vocab) for i in order]
+    assert got == [(i // vocab, i % vocab) for i in order]
+
+
+def ordered(logits, scores, n):
+    """The n best of one group where scores hide the logits: of equal ones the lower row, then the larger logit, then the lower token."""
+    z = logits.double()
+    most = z.amax(1, keepdim=True)
+    s = scores.double()[:, None] + (z - (most + torch.log(torch.exp(z - most).sum(1, keepdim=True))))
+    order = sorted(zip((-s).flatten().tolist(), torch.arange(z.shape[0]).repeat_interleave(z.shape[1]).tolist(), (-z).flatten().tolist(),
+                       torch.arange(z.shape[1]).repeat(z.shape[0]).tolist()))
+    return [(b, t) for _, b, _, t in order[:n]]
+
+
+def far_out(large, score):
+    """(logits, scores) of four beams: the first one's logits near `large`, scores around `score`; what a score leaves of a row's sum may be twice the largest float."""
+    g = gen(1)
+    for kind in (0, 1, 2):
+        logits = torch.randn((4, 2048), generator=g)
+        logits[0] = large * (0.9 + 0.1 * torch.rand(2048, generator=g)) if kind == 0 else large if kind == 1 else -large
+        for others in ([1.0, 0.99, 0.99, 0.999], [1.0, 0.333, 0.667, 0.0], [0.1, 1.0, -0.5, 0.9]):
+            yield logits, torch.tensor(others) * score
 
 
 def gen(seed):
@@ -321,3 +347,18 @@ def test_clusters(program, tmp_path, n, size):
 def test_more_lists_than_are_looked_at_first(program, tmp_path):
     g = gen(4)
     check(program, tmp_path, torch.randn((128, 270001), generator=g) * 4, -torch.linspace(0, 9, 128), 32, size=8192)
+
+
+@pytest.mark.parametrize("large", [1e31, 1e37, 1e38, 3e38])
+@pytest.mark.parametrize("score", [1e36, -1e38, 3e38, -3e38])
+def test_logits_and_scores_next_to_the_largest_float(program, tmp_path, large, score):
+    for logits, scores in far_out(large, score):
+        for n in (40, 3):
+            assert joined(program, tmp_path, logits, scores, n) == ordered(logits, scores, n)
+
+
+def test_done_beams_far_out(program, tmp_path):
+    g = gen(2)
+    scores = torch.tensor([-3.4e38, 3.4e38, -1e-42, 1e-44, -3.4028234e38, 0.0] * 10)
+    finished = (torch.arange(60) % 7 < 5).int()
+    check(program, tmp_path, torch.randn((60, 500), generator=g).mul_(0.0), scores, 50, finished, 3)
