@@ -430,7 +430,7 @@ int ee_kv_quant_copy(const ee_quant_cache* cache, const int32_t* moves, int32_t 
  *   scores[row] + (logits[row][t] - log sum_t' exp(logits[row][t'])),
  * a row with finished[row] != 0 only the candidate (row, end_token) with scores[row] (its logits are not read).  A score that is not finite (a token masked by
  * -inf; any of a row with a NaN or +inf among its logits) counts as -inf.  For every group the n_out best, best first; of equal scores the lower
- * row, then the larger logit, then the lower token first, so tokens and rows are given also where all that is left is -inf.  Scores are formed and compared in double, the sum's
+ * row, then the larger logit, then the lower token first.  Tokens and rows are given also where all that is left is -inf: by row and token alone, whatever the logits.  Scores are formed and compared in double, the sum's
  * exponentials in float; among one row's tokens the order is that of the logits.
  *   logits dev [groups * beams] rows of vocab values of `dtype` (EE_FP32 | EE_BF16), logits_stride (>= vocab) elements apart, any element alignment.
  *   scores dev [groups * beams] float.  finished dev [groups * beams] int32 or NULL (none).  end_token: 0 .. vocab - 1, or -1 (none; not with finished).

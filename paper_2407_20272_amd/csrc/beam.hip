@@ -8,8 +8,8 @@
 // What is compared are scores in double: rounded to float many candidates of a beam would be equal, and beams' sums meet there.  (Where even these are equal, within a beam by logits: it is these that its lists are of.)  Exponentials are floats, a thread's sixteen or 32 are added
 // in float and everything behind that in double.
 //
-// Scan + join, kernel times: 4 rows of 2048 floats 4.6 + 3.8 us; 128 rows of 32000 bf16, 8 of 4 back: 7.1 + 7.2; 128 rows of 100003 floats (41 MB are read), 16 of 8 back: 14.7 + 8.1; 64 rows
-// of 32000 floats, 128 of 64 back: 9.2 + 11.  The scan of many rows is bound by memory and by the latency of one chunk (values, maximum, sum, bound, list: 6 us), the join by the latency of its
+// Scan + join, kernel times: 4 rows of 2048 floats 4.5 + 3.7 us; 128 rows of 32000 bf16, 8 of 4 back: 7.1 + 7.1; 128 rows of 100003 floats (51 MB, 41 of them read: a fifth is finished), 16 of 8 back: 13.7 + 8.5;
+// 64 rows of 32000 floats, 128 of 64 back: 9.4 + 11.4.  The scan of many rows is bound by memory and by the latency of one chunk (values, maximum, sum, bound, list: 6 us), the join by the latency of its
 // dozen barriers.  Values in chunks of 4096 where all workgroups run at once, else of 8192: the 128 rows of 100003 took 19 us in 4096, more than one round, also with the next chunk's
 // values on their way.
 #include <type_traits>

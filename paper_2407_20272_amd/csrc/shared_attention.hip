@@ -17,8 +17,9 @@
 // Bound by what a compute unit takes in (26 GB/s of memory, 28 to 30 with what comes from cache), and for short contexts by the chain in front of it: groups and lengths, block ids, K and V (4 us),
 // and the meeting of the wavefronts (1.5 us).  Kernel times, bf16, dh 128, 32 query heads:
 //   4 rows behind 96 positions, heads of their own: 7.4 to 8.2 us.    8 x 4 rows behind 512 (85 MB): 17.8 us, 12.5 at 6.8 TB/s.
-//   64 rows behind 2000, 100 to 900 of their own, over 8 heads (141 MB): 35.6 + 4.7 us, 20.8 at 6.8 TB/s (tiles of 16 columns 50, of 32 37; whole tiles a workgroup 50 in tiles of 16).
-//   12 rows behind 100000 over 8 heads (410 MB): 82 + 4.9 us, 60 at 6.8 TB/s (16 columns 130, 32 124; whole tiles 932).  The counters show no byte read twice.  K through LDS, in whole kilobytes and a step ahead: 39 and 94 us.
+//   64 rows behind 2000, 100 to 900 of their own, over 8 heads (141 MB): 35.2 + 4.7 us, 20.8 at 6.8 TB/s (tiles of 16 columns 50, of 32 37; whole tiles a workgroup 50 in tiles of 16).
+//   48 rows behind 100000, heads of their own (1.7 GB, 52 steps a wavefront): 336 us in all, 5.1 TB/s.
+//   12 rows behind 100000 over 8 heads (410 MB): 82 to 85 + 4.8 us, 60 at 6.8 TB/s (16 columns 130, 32 124; whole tiles 932).  The counters show no byte read twice.  K through LDS, in whole kilobytes and a step ahead: 39 and 94 us.
 //   Four wavefronts a workgroup were 62 and 220 us where eight were 43 and 156; with tiles that begin in the middle of a workgroup's share of steps the 64 rows took 40.
 #include <type_traits>
 
